@@ -381,6 +381,100 @@ int aser_compensated_forward(aser_ctx* ctx, const int8_t* x_codes, const float* 
                              const float* L_A, const float* L_B, int32_t r, int32_t lowrank_split,
                              float* Y, int64_t ldy);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Serving: what lies between the quantized projections of a decoder block (aser_compensated_forward), and the
+ * low-rank adapters of single requests beside such a projection.
+ *
+ * A batch has n_seq requests.  Row t of every token matrix is one new token; request s owns the rows start[s] ..
+ * start[s + 1] - 1, and its new tokens are the last ones of the kv_len[s] tokens that it has in the cache once they are
+ * stored: new token i of n has position kv_len[s] - n + i.  A cache is an array of pages of page_size tokens; position p
+ * of request s lives in slot p % page_size of page pages[s][p / page_size].
+ *
+ * start, kv_len and pages are read on the device only.  What they say is never trusted with an address: start is
+ * clamped to [0, tokens], kv_len to [0, max_kv], and a page number outside [0, n_pages) is a page that is not there
+ * (nothing is stored to it, nothing of it is seen).  Rows that belong to no request are left as they are.  A request's pages
+ * may be shared with others for reading; pages that new tokens are stored to belong to one request. */
+typedef enum aser_kv_dtype {
+    ASER_KV_BF16 = 0,
+    ASER_KV_INT8 = 1    /* per token and head: scale = max_i |u_i| / 127 (1 if zero), code = rint_half_even(u_i / scale)  */
+} aser_kv_dtype;
+
+/* Element (page, head, slot, channel) of k and of v is at page * page_stride + head * head_stride + slot * slot_stride
+ * + channel; strides in elements, multiples of 16, none negative; k and v 16-byte aligned.  Scales are dense,
+ * n_pages x n_kv x page_size fp32, 16-byte aligned; NULL for bf16. */
+typedef struct aser_kv_cache {
+    void* k; void* v;
+    float* k_scale; float* v_scale;
+    int64_t n_pages, page_stride, head_stride, slot_stride;
+    int32_t dtype;      /* aser_kv_dtype                              */
+    int32_t page_size;  /* tokens of a page: 16, 32, 64, 128 or 256   */
+    int32_t n_kv;       /* key/value heads                            */
+    int32_t head_dim;   /* channels of a head: 64, 128 or 256         */
+} aser_kv_cache;
+
+typedef struct aser_kv_batch {
+    const int32_t* start;    /* DEVICE, n_seq + 1, not descending                           */
+    const int32_t* kv_len;   /* DEVICE, n_seq                                               */
+    const int32_t* pages;    /* DEVICE, n_seq x ld_pages; ld_pages * page_size >= max_kv    */
+    int64_t ld_pages;
+    int64_t tokens;          /* rows of the token matrices                                  */
+    int32_t n_seq;
+    int32_t max_new;         /* no request has more new tokens                              */
+    int32_t max_kv;          /* no request has more tokens in the cache                     */
+} aser_kv_batch;
+
+/* What happens to queries and keys before they are used; every part may be absent (NULL).
+ *   norm:      u = x * rsqrt(mean_i x_i^2 + eps) * weight   over a head's channels (head_dim fp32 weights each)
+ *   rotation:  pairs of the first rot_dim channels turn by the token's angles, (a, b) -> (a c - b s, b c + a s) with
+ *              c = rope_cos[p][i], s = rope_sin[p][i] (n_pos x rot_dim / 2 fp32, dense) for pair i of position p; pair i is
+ *              the channels (i, i + rot_dim / 2), or with interleaved != 0 (2 i, 2 i + 1).  The rest passes.
+ *              rot_dim: a multiple of 16, at most head_dim.  n_pos >= max_kv. */
+typedef struct aser_qk_opts {
+    const float* rope_cos; const float* rope_sin;
+    const float* q_norm; const float* k_norm;
+    int64_t n_pos;
+    int32_t rot_dim, interleaved;
+    float eps;
+} aser_qk_opts;
+
+/* Queries, keys and values of the new tokens (bf16 or fp32 alike, x_dtype; rows of n_heads, n_kv and n_kv heads with leading
+ * dimensions ldq, ldk, ldv; slices of one fused projection's output are fine): normalised and rotated as opts says
+ * (NULL: as they are), queries to q_out (bf16, ldqo), keys and values to the cache; values are only stored.  q and q_out
+ * may be NULL together (no queries wanted).  Computed in fp32, rounded once.  A new token whose position is outside
+ * [0, max_kv) or on a page that is not there stores nothing; outside [0, max_kv) its row of q_out is left alone too.
+ * All rows 16-byte aligned (pointers, and leading dimensions in bytes).  n_heads is a multiple of n_kv.  tokens == 0 is
+ * a no-op.  Asynchronous, needs no workspace. */
+int aser_kv_append(aser_ctx* ctx, const void* q, int64_t ldq, int32_t n_heads, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                   int32_t x_dtype, const aser_qk_opts* opts, const aser_kv_cache* cache, const aser_kv_batch* batch,
+                   uint16_t* q_out, int64_t ldqo);
+
+/* Attention of the new tokens over the cache, which already holds their keys and values (aser_kv_append):
+ *     out[t][h] = sum_j p_j v_j,  p_j = exp(scale q.k_j) / sum_j' exp(scale q.k_j')   over the keys j that t sees,
+ * key j of its request when j <= p (p: the token's position) and, with window > 0, j > p - window or j < sinks; query head h
+ * reads key/value head h / (n_heads / n_kv).  A token that sees nothing gets zeros; what the cache holds where nobody looks
+ * (slots past kv_len, pages that are not there) does not matter, NaN included.  Values that some new token of a
+ * request sees and another one does not have to be finite.
+ * q, out: tokens x (n_heads * head_dim) bf16, rows 16-byte aligned; out must not overlap q.  window == 0: no window,
+ * sinks is then not looked at.  Products of bf16 numbers summed in fp32; probabilities are rounded to bf16 for the
+ * second product, their sum is not.  Deterministic.  Asynchronous.
+ * Needs aser_paged_attention_workspace_bytes of workspace (which reads of the structs what is on the host). */
+size_t aser_paged_attention_workspace_bytes(const aser_kv_cache* cache, const aser_kv_batch* batch, int32_t n_heads);
+int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ldq, int32_t n_heads, const aser_kv_cache* cache,
+                         const aser_kv_batch* batch, float scale, int32_t window, int32_t sinks, uint16_t* out, int64_t ldo);
+
+/* Low-rank adapters of single requests beside a projection that all of them share:
+ *     Y[t][o] = Y0[t][o] + scale_a sum_k B_a[o][k] sum_i A_a[k][i] X[t][i],   a = adapter[t],
+ * and Y[t] = Y0[t] where adapter[t] is outside [0, n_adapters) (no adapter).  X: rows x n, bf16 or fp32 (ldx).  adapter:
+ * DEVICE, one int32 per row.  A: n_adapters x r x n and B: n_adapters x m x r, bf16, dense; scale: n_adapters fp32 or
+ * NULL (1).  Y0, Y: rows x m fp32; Y may be Y0 (in place: rows without an adapter are then not touched); Y0 NULL: zeros.
+ * r <= 128 (adapters of smaller rank are padded with zeros), n_adapters <= 4096; any n and m.  The operands are used with
+ * all their bits (fp32 X and the inner products as three bf16 terms), sums are fp32; deterministic.  Asynchronous.
+ * Needs aser_adapter_workspace_bytes of workspace.  rows == 0 is a no-op. */
+size_t aser_adapter_workspace_bytes(int64_t rows, int64_t n, int64_t m, int32_t r);
+int aser_adapter_forward(aser_ctx* ctx, const void* X, int x_dtype, int64_t rows, int64_t n, int64_t ldx, const int32_t* adapter,
+                         const uint16_t* A, const uint16_t* B, const float* scale, int32_t n_adapters, int32_t r, int64_t m,
+                         const float* Y0, int64_t ldy0, float* Y, int64_t ldy);
+
 /* Measurement aid (not a step of the method; bench.py reports it next to the nominal peaks): the rate, in
  * 10^12 operations per second, that a loop of nothing but MFMA instructions reaches on the device, with
  * `workgroups_per_cu` (1 .. 4) workgroups of four wavefronts per compute unit and `iters` rounds of 16

@@ -30,6 +30,8 @@ ASER_PRECISION_FAST = 1
 ASER_PRECISION_EXACT = 2
 ASER_CODES_INT8 = 0
 ASER_CODES_INT4_PACKED = 1
+ASER_KV_BF16 = 0
+ASER_KV_INT8 = 1
 
 EXPORTS = (
     "aser_status_string", "aser_create", "aser_destroy", "aser_last_error", "aser_set_workspace", "aser_set_precision",
@@ -41,6 +43,8 @@ EXPORTS = (
     "aser_forward_workspace_bytes", "aser_compensated_forward", "aser_mfma_rate_probe",
     "aser_error_reconstruct_enqueue", "aser_finish", "aser_calibrate_layers", "aser_pick_concurrent_streams",
     "aser_layer_workspace_bytes", "aser_smoothed_weight", "aser_quant_target",
+    "aser_kv_append", "aser_paged_attention", "aser_paged_attention_workspace_bytes",
+    "aser_adapter_forward", "aser_adapter_workspace_bytes",
 )
 
 
@@ -59,6 +63,25 @@ class aser_layer_desc(ctypes.Structure):
                 ("damp", ctypes.c_float), ("stats_from", _i32), ("S", _vp), ("lds", _i64),
                 ("opts", ctypes.POINTER(aser_svd_opts)), ("L_A", _vp), ("L_B", _vp), ("sigma", _vp),
                 ("err", ctypes.c_double), ("n_iter", _i32), ("status", _i32)]
+
+
+class aser_kv_cache(ctypes.Structure):
+    """Mirror of the C struct of the same name; KvCache fills one from tensors."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("slot_stride", ctypes.c_int64), ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class aser_kv_batch(ctypes.Structure):
+    """Mirror of the C struct of the same name; KvBatch fills one from tensors."""
+    _fields_ = [("start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("pages", ctypes.c_void_p), ("ld_pages", ctypes.c_int64),
+                ("tokens", ctypes.c_int64), ("n_seq", ctypes.c_int32), ("max_new", ctypes.c_int32), ("max_kv", ctypes.c_int32)]
+
+
+class aser_qk_opts(ctypes.Structure):
+    _fields_ = [("rope_cos", ctypes.c_void_p), ("rope_sin", ctypes.c_void_p), ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p),
+                ("n_pos", ctypes.c_int64), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
 class AserError(RuntimeError):
@@ -145,6 +168,17 @@ def load_library() -> ctypes.CDLL:
     lib.aser_compensated_forward.argtypes = [vp, vp, vp, i64, i64, vp, i32, vp, i64, vp, vp, i32, i32, vp, i64]
     lib.aser_quantize_act_rtn.restype = ctypes.c_int
     lib.aser_quantize_act_rtn.argtypes = [vp, vp, ctypes.c_int, i64, i64, i64, vp, i32, vp, vp]
+    cache, batch = ctypes.POINTER(aser_kv_cache), ctypes.POINTER(aser_kv_batch)
+    lib.aser_kv_append.restype = ctypes.c_int
+    lib.aser_kv_append.argtypes = [vp, vp, i64, i32, vp, i64, vp, i64, i32, ctypes.POINTER(aser_qk_opts), cache, batch, vp, i64]
+    lib.aser_paged_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.aser_paged_attention_workspace_bytes.argtypes = [cache, batch, i32]
+    lib.aser_paged_attention.restype = ctypes.c_int
+    lib.aser_paged_attention.argtypes = [vp, vp, i64, i32, cache, batch, f32, i32, i32, vp, i64]
+    lib.aser_adapter_workspace_bytes.restype = ctypes.c_size_t
+    lib.aser_adapter_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.aser_adapter_forward.restype = ctypes.c_int
+    lib.aser_adapter_forward.argtypes = [vp, vp, ctypes.c_int, i64, i64, i64, vp, vp, vp, vp, i32, i32, i64, vp, i64, vp, i64]
     lib.aser_mfma_rate_probe.restype = ctypes.c_int
     lib.aser_mfma_rate_probe.argtypes = [vp, i32, i32, i32, ctypes.POINTER(ctypes.c_double)]
     _lib = lib
@@ -413,6 +447,113 @@ def aser_compensated_forward(ctx: Context, x_codes, x_scales, w_codes, layout: i
     return ctx._lib.aser_compensated_forward(ctx.handle, _ptr(x_codes), _ptr(x_scales), rows, n, _ptr(w_codes), layout,
                                              _ptr(w_scales), m, _ptr(L_A), _ptr(L_B), r, 1 if lowrank_split else 0,
                                              _ptr(Y), _ld(Y, m) if ldy is None else ldy)
+
+
+# ----------------------------------------------------------------------------------- serving
+class KvCache:
+    """A paged cache of keys and values from its tensors: k, v of pages x key/value heads x slots x channels (bfloat16 or
+    int8; any strides that the C struct allows, the same for both), and for int8 the scales, pages x heads x slots fp32."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        import torch
+        if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.dim() != 4 or k.stride(3) != 1:
+            raise ValueError("k and v must be alike, pages x heads x slots x channels with unit channel stride")
+        if k.dtype not in (torch.bfloat16, torch.int8):
+            raise TypeError("a cache holds bfloat16 or int8")
+        if (k.dtype == torch.int8) != (k_scale is not None and v_scale is not None):
+            raise ValueError("an int8 cache has scales, a bfloat16 cache has none")
+        for sc in (k_scale, v_scale):
+            if sc is not None and (sc.dtype != torch.float32 or tuple(sc.shape) != tuple(k.shape[:3]) or not sc.is_contiguous()):
+                raise ValueError("scales must be contiguous float32, pages x heads x slots")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.c = aser_kv_cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), k.shape[0], k.stride(0), k.stride(1), k.stride(2),
+                               ASER_KV_INT8 if k.dtype == torch.int8 else ASER_KV_BF16, k.shape[2], k.shape[1], k.shape[3])
+
+    @classmethod
+    def empty(cls, n_pages: int, n_kv: int, page_size: int, head_dim: int, int8: bool = False, device: int = 0):
+        """A zeroed cache, pages x heads x slots x channels."""
+        import torch
+        dev, shape = "cuda:%d" % device, (n_pages, n_kv, page_size, head_dim)
+        k, v = (torch.zeros(shape, dtype=torch.int8 if int8 else torch.bfloat16, device=dev) for _ in range(2))
+        scales = [torch.zeros(shape[:3], dtype=torch.float32, device=dev) for _ in range(2)] if int8 else [None, None]
+        return cls(k, v, *scales)
+
+
+class KvBatch:
+    """The requests of a batch (C struct aser_kv_batch) from its device tensors: start (n_seq + 1), kv_len (n_seq) and the page
+    table (n_seq x columns), int32.  Their contents may change between calls; tokens, max_new and max_kv bound them."""
+
+    def __init__(self, start, kv_len, pages, *, tokens: int, max_new: int, max_kv: int):
+        import torch
+        n_seq = kv_len.shape[0]
+        if start.shape[0] != n_seq + 1 or pages.dim() != 2 or pages.shape[0] != n_seq:
+            raise ValueError("start has n_seq + 1 entries, kv_len n_seq, pages n_seq rows")
+        if any(t.dtype != torch.int32 for t in (start, kv_len, pages)) or not (start.is_contiguous() and kv_len.is_contiguous()):
+            raise TypeError("start, kv_len and pages must be int32, start and kv_len contiguous")
+        if pages.shape[1] > 1 and pages.stride(1) != 1:
+            raise ValueError("the page table must have unit column stride")
+        self.start, self.kv_len, self.pages = start, kv_len, pages
+        ld = pages.stride(0) if n_seq > 1 else pages.shape[1]
+        self.c = aser_kv_batch(_ptr(start), _ptr(kv_len), _ptr(pages), ld, tokens, n_seq, max_new, max_kv)
+
+
+def aser_kv_append(ctx: Context, q, k, v, cache: KvCache, batch: KvBatch, q_out, *, rope_cos=None, rope_sin=None, interleaved: bool = False,
+                   q_norm=None, k_norm=None, eps: float = 1e-6) -> int:
+    """q, k, v: tokens x (heads * channels), bfloat16 or float32 alike (q and q_out may be None); rope_cos, rope_sin: positions x
+    (rotated channels / 2) float32; q_norm, k_norm: channels of a head, float32."""
+    dt = _dtype_code(k)
+    if _dtype_code(v) != dt or (q is not None and _dtype_code(q) != dt):
+        raise TypeError("q, k and v must have one dtype")
+    opts = None
+    if rope_cos is not None or q_norm is not None or k_norm is not None:
+        if rope_cos is not None and not (rope_cos.is_contiguous() and rope_sin.is_contiguous() and rope_cos.shape == rope_sin.shape):
+            raise ValueError("rope_cos and rope_sin must be contiguous and alike")
+        opts = ctypes.byref(aser_qk_opts(_ptr(rope_cos), _ptr(rope_sin), _ptr(q_norm), _ptr(k_norm), 0 if rope_cos is None else rope_cos.shape[0],
+                                         0 if rope_cos is None else 2 * rope_cos.shape[1], 1 if interleaved else 0, eps))
+    for t in (q, k, v, q_out):
+        if t is not None and t.shape[0] < batch.c.tokens:
+            raise ValueError("q, k, v and q_out need a row for each of the batch's tokens")
+    if q_out is not None and (_dtype_code(q_out) != ASER_DTYPE_BF16 or q_out.shape[1] < q.shape[1]):
+        raise TypeError("q_out must be bfloat16, as wide as q")
+    heads = 0 if q is None else q.shape[1] // cache.c.head_dim
+    return ctx._lib.aser_kv_append(ctx.handle, _ptr(q), 0 if q is None else _ld(q, q.shape[1]), heads, _ptr(k), _ld(k, k.shape[1]), _ptr(v),
+                                   _ld(v, v.shape[1]), dt, opts, ctypes.byref(cache.c), ctypes.byref(batch.c), _ptr(q_out),
+                                   0 if q_out is None else _ld(q_out, q_out.shape[1]))
+
+
+def aser_paged_attention_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads: int) -> int:
+    return int(load_library().aser_paged_attention_workspace_bytes(ctypes.byref(cache.c), ctypes.byref(batch.c), n_heads))
+
+
+def aser_paged_attention(ctx: Context, q, cache: KvCache, batch: KvBatch, out, *, scale: float, window: int = 0, sinks: int = 0) -> int:
+    """q, out: tokens x (heads * channels), bfloat16."""
+    width = q.shape[1]
+    if _dtype_code(q) != ASER_DTYPE_BF16 or _dtype_code(out) != ASER_DTYPE_BF16:
+        raise TypeError("q and out must be bfloat16")
+    if q.shape[0] < batch.c.tokens or out.shape[0] < batch.c.tokens or out.shape[1] < width:
+        raise ValueError("q and out need a row for each of the batch's tokens")
+    return ctx._lib.aser_paged_attention(ctx.handle, _ptr(q), _ld(q, width), width // cache.c.head_dim, ctypes.byref(cache.c), ctypes.byref(batch.c),
+                                         scale, window, sinks, _ptr(out), _ld(out, width))
+
+
+def aser_adapter_workspace_bytes(rows: int, n: int, m: int, r: int) -> int:
+    return int(load_library().aser_adapter_workspace_bytes(rows, n, m, r))
+
+
+def aser_adapter_forward(ctx: Context, X, adapter, A, B, scale, Y0, Y) -> int:
+    """X: rows x n; adapter: rows int32; A: adapters x r x n and B: adapters x m x r, contiguous bfloat16; scale: adapters float32
+    or None; Y0 (None: zeros) and Y: rows x m float32."""
+    n_adapters, r, n = A.shape
+    m = B.shape[1]
+    if not (A.is_contiguous() and B.is_contiguous() and B.shape[0] == n_adapters and B.shape[2] == r and X.shape[1] == n):
+        raise ValueError("A must be adapters x r x n and B adapters x m x r, contiguous")
+    if _dtype_code(A) != ASER_DTYPE_BF16 or _dtype_code(B) != ASER_DTYPE_BF16 or _dtype_code(Y) != ASER_DTYPE_F32:
+        raise TypeError("A and B must be bfloat16, Y float32")
+    rows = X.shape[0]
+    if adapter.shape[0] != rows or adapter.element_size() != 4 or Y.shape[0] < rows or (Y0 is not None and (Y0.shape[0] < rows or Y0.dtype != Y.dtype)):
+        raise ValueError("adapter (int32), Y0 and Y (float32) need an entry for each row of X")
+    return ctx._lib.aser_adapter_forward(ctx.handle, _ptr(X), _dtype_code(X), X.shape[0], n, _ld(X, n), _ptr(adapter), _ptr(A), _ptr(B), _ptr(scale),
+                                         n_adapters, r, m, _ptr(Y0), _ld(Y0, m) if Y0 is not None else m, _ptr(Y), _ld(Y, m))
 
 
 # ----------------------------------------------------------------------------------- one layer, end to end

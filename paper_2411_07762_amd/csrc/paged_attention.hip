@@ -1,0 +1,359 @@
+// Attention of new tokens over a paged cache:
+//     o = sum_j p_j v_j / sum_j p_j,   p_j = exp2(c (q . k_j) - m),   c = scale log2 e,
+// in one pass over the keys with a running maximum m and running sums.  Query heads that share a key/value head are rows of
+// the same tile (row = new token * group + head of the group), so a key is read once for all of them.
+//
+// Few rows (a wavefront per 16 rows, this file).  The products are formed transposed: S^T = K Q^T has a query row per
+// column of the 16 x 16 accumulator, four keys in the registers of a lane; two such tiles are, as they stand, the operand of
+// the next product O^T = V^T P^T (8 keys per lane, in the order 4 g .. 4 g + 3 of the first 16 keys, then of the second 16;
+// g = lane / 16).  The sum over keys does not care for their order, so the values are simply fetched in that order and no
+// probability changes lanes.  V^T wants 8 keys of one channel in a lane where memory has 8 channels of one key: a lane loads
+// D / 16 channels of its 8 keys and a byte permute per pair of keys turns them round.
+// Bound by reading the cache: 4 D bytes per key and head against 64 D / 16 matrix operations of 16 columns.
+#include "bf16_pair.h"
+#include "paged_kv.h"
+
+namespace {
+
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+
+constexpr int kTile = 32;                         // keys of a step
+constexpr float kNone = -1e30f;                   // running maximum before any key
+
+struct AttnArgs {
+    PagedArgs p;
+    const uint16_t* q; int64_t ldq;
+    uint16_t* out; int64_t ldo;
+    float c;                                      // scale * log2(e)
+    int window, sinks;                            // window 0: none
+    int splits, tiles_per_split, row_tiles;
+    float* part_o; float2* part_ml;               // partial results of a split: [pair][split][row][D], [pair][split][row] (maximum, sum)
+};
+
+// Tiles of 32 keys that some row of positions [p_lo, p_hi] may see: [0, sink_tiles) and [main0, main0 + main_tiles).
+struct KeyTiles {
+    int sink_tiles, main0, total;
+    __device__ __forceinline__ KeyTiles(int p_lo, int p_hi, int window, int sinks) {
+        main0 = 0;
+        sink_tiles = 0;
+        if (window > 0) {
+            const int low = p_lo - window + 1;
+            main0 = low > 0 ? low / kTile : 0;
+            const int s = (min(sinks, p_hi + 1) + kTile - 1) / kTile;
+            sink_tiles = min(s, main0);
+        }
+        total = p_hi < 0 ? 0 : sink_tiles + p_hi / kTile - main0 + 1;
+    }
+    __device__ __forceinline__ int first_key(int i) const { return (i < sink_tiles ? i : main0 + i - sink_tiles) * kTile; }
+};
+
+// Two codes of 8 bits, sign-extended, as two bf16 values in a word.
+template <int B>
+__device__ __forceinline__ uint32_t codes_pair(uint32_t w) {
+    return upper_halves((float)(int8_t)(w >> (8 * B)), (float)(int8_t)(w >> (8 * B + 8)));
+}
+
+template <int D, bool I8>
+__global__ __launch_bounds__(256) void attn_few_kernel(AttnArgs g) {
+    constexpr int KS = D / 32;                    // steps of 32 channels in K Q^T
+    constexpr int NB = D / 16;                    // channels of a lane in V^T, and accumulators of O^T
+    __shared__ float sm_o[4][16][D + 4];
+    __shared__ float sm_m[4][16], sm_l[4][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, grp = lane >> 4;
+    const int kvh = blockIdx.x % g.p.n_kv, tile = blockIdx.x / g.p.n_kv, split = blockIdx.y, s = tile / g.row_tiles, rt = tile % g.row_tiles;
+    int64_t row0;
+    const int count = (int)request_rows(g.p, s, &row0), kv = request_kv_len(g.p, s);
+    const int rows = count * g.p.group - rt * 16;                            // rows of this tile, if positive
+    if (rows <= 0) return;
+    const int my_row = min(rt * 16 + n, count * g.p.group - 1), my_tok = my_row / g.p.group, my_head = my_row % g.p.group;
+    const int my_pos = kv - count + my_tok;
+    const int last_row = min(rt * 16 + 15, count * g.p.group - 1);
+    const int p_lo = max(kv - count + rt * 16 / g.p.group, 0), p_hi = kv - count + last_row / g.p.group;
+    const KeyTiles kt(p_lo, p_hi, g.window, g.sinks);
+    const int t0 = split * g.tiles_per_split, t1 = min(t0 + g.tiles_per_split, kt.total);
+    if (t0 >= t1 && split > 0) return;
+    const int low_all = g.window > 0 ? kv - count + rt * 16 / g.p.group - g.window + 1 : 0;   // the same for the tile's first row
+    const int my_low = g.window > 0 ? my_pos - g.window + 1 : 0;             // keys below are seen up to sinks only
+
+    // the row's query: B operand of K Q^T, channels 32 step + 8 grp ..
+    bf16x8_t q[KS];
+    const int64_t q_at = (row0 + my_tok) * g.ldq + (int64_t)(kvh * g.p.group + my_head) * D;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) q[k] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(g.q + q_at + 32 * k + 8 * grp));
+
+    f32x4_t o[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) o[b] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    float m = kNone, l = 0.f;
+    const int* table = g.p.pages + s * g.p.ld_pages;
+    const int64_t head_at = kvh * g.p.head_stride;
+    const int page_mask = (1 << g.p.page_shift) - 1;
+
+    for (int i = t0 + wave; i < t1; i += 4) {
+        const int key0 = kt.first_key(i);
+        int64_t at[2], sc_at[2];
+        bool there[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k0 = key0 + 16 * h;
+            int page = k0 < kv ? table[k0 >> g.p.page_shift] : -1;           // the table has columns for kv tokens only
+            there[h] = (uint32_t)page < (uint32_t)g.p.n_pages;
+            if (!there[h]) page = 0;
+            at[h] = (int64_t)page * g.p.page_stride + head_at + (int64_t)(k0 & page_mask) * g.p.slot_stride;
+            sc_at[h] = (((int64_t)page * g.p.n_kv + kvh) << g.p.page_shift) + (k0 & page_mask);
+        }
+        // keys: A operand, row n, channels 32 step + 8 grp ..
+        uint4 kw[2][KS];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const int64_t e = at[h] + n * g.p.slot_stride + 32 * k + 8 * grp;
+                if (I8) {
+                    const uint2 w = *(const uint2*)((const int8_t*)g.p.k + e);
+                    kw[h][k] = make_uint4(w.x, w.y, 0u, 0u);
+                } else {
+                    kw[h][k] = *(const uint4*)((const uint16_t*)g.p.k + e);
+                }
+            }
+        // values: NB channels from NB n of keys 4 grp + e of both halves
+        constexpr int VW = I8 ? NB / 4 : NB / 2;                             // words
+        uint32_t vw[8][VW];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t a = at[h] + (4 * grp + e) * g.p.slot_stride + NB * n;
+                const uint32_t* src = I8 ? (const uint32_t*)((const int8_t*)g.p.v + a) : (const uint32_t*)((const uint16_t*)g.p.v + a);
+                if constexpr (VW == 1) vw[4 * h + e][0] = src[0];
+                else if constexpr (VW == 2) { const uint2 w = *(const uint2*)src; vw[4 * h + e][0] = w.x; vw[4 * h + e][1] = w.y; }
+                else {
+#pragma unroll
+                    for (int x = 0; x < VW; x += 4) {
+                        const uint4 w = *(const uint4*)(src + x);
+                        vw[4 * h + e][x] = w.x; vw[4 * h + e][x + 1] = w.y; vw[4 * h + e][x + 2] = w.z; vw[4 * h + e][x + 3] = w.w;
+                    }
+                }
+            }
+        float ks[8], vs[8];
+        if (I8) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float4 a = *(const float4*)(g.p.k_scale + sc_at[h] + 4 * grp), b = *(const float4*)(g.p.v_scale + sc_at[h] + 4 * grp);
+                ks[4 * h] = a.x; ks[4 * h + 1] = a.y; ks[4 * h + 2] = a.z; ks[4 * h + 3] = a.w;
+                vs[4 * h] = b.x; vs[4 * h + 1] = b.y; vs[4 * h + 2] = b.z; vs[4 * h + 3] = b.w;
+            }
+        }
+        f32x4_t st[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            st[h] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                uint4 w = kw[h][k];
+                if (I8) w = make_uint4(codes_pair<0>(w.x), codes_pair<2>(w.x), codes_pair<0>(w.y), codes_pair<2>(w.y));
+                st[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w), q[k], st[h], 0, 0, 0);
+            }
+        }
+        // logits in units of log2, masked to -inf
+        float x[8];
+        const bool plain = key0 + kTile <= p_lo + 1 && there[0] && there[1] && (g.window <= 0 || key0 >= p_hi - g.window + 1 || key0 + kTile <= g.sinks);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = st[e >> 2][e & 3] * (I8 ? g.c * ks[e] : g.c);
+        if (!plain) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int h = e >> 2, key = key0 + 16 * h + 4 * grp + (e & 3);
+                // one comparison after the other, no branches: this compiler has lost the first of several masked values in branches
+                const bool seen = there[h] & (key <= my_pos) & ((key >= my_low) | (key < g.sinks));
+                x[e] = seen ? x[e] : -INFINITY;
+                // what nobody of this tile sees does not count, whatever the slot holds
+                const bool used = there[h] & (key <= p_hi) & ((key >= low_all) | (key < g.sinks));
+                if (I8) vs[e] = used ? vs[e] : 0.f;
+#pragma unroll
+                for (int w = 0; w < VW; ++w) vw[e][w] = used ? vw[e][w] : 0u;
+            }
+        }
+        float top = x[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
+        // The maximum moves only when a logit is 8 above it: until then p <= 2^8, which neither fp32 sums nor bf16 mind.
+        if (__ballot(top > m + 8.f)) {
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float m_new = fmaxf(m, top), r = __builtin_amdgcn_exp2f(m - m_new);
+            m = m_new;
+            l *= r;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) o[b] *= r;
+        }
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(x[e] - m);
+            l += p[e];
+            if (I8) p[e] *= vs[e];
+        }
+        const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, make_uint4(bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3]), bf16_pair(p[4], p[5]), bf16_pair(p[6], p[7])));
+#pragma unroll
+        for (int w = 0; w < NB / 2; ++w) {                                    // channels 2 w and 2 w + 1 of the lane
+            uint32_t v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = I8 ? ((w & 1) ? codes_pair<2>(vw[e][w / 2]) : codes_pair<0>(vw[e][w / 2])) : vw[e][w];
+            uint4 even, odd;
+            even = make_uint4(__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u),
+                              __builtin_amdgcn_perm(v[5], v[4], 0x05040100u), __builtin_amdgcn_perm(v[7], v[6], 0x05040100u));
+            odd = make_uint4(__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u),
+                             __builtin_amdgcn_perm(v[5], v[4], 0x07060302u), __builtin_amdgcn_perm(v[7], v[6], 0x07060302u));
+            o[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, even), pb, o[2 * w], 0, 0, 0);
+            o[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, odd), pb, o[2 * w + 1], 0, 0, 0);
+        }
+    }
+
+    // the four wavefronts' results meet: row n, channels NB (4 grp + e) + b
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (lane < 16) { sm_m[wave][n] = m; sm_l[wave][n] = l; }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int b = 0; b < NB; b += 4)
+            *(f32x4_t*)&sm_o[wave][n][NB * (4 * grp + e) + b] = (f32x4_t){o[b][e], o[b + 1][e], o[b + 2][e], o[b + 3][e]};
+    __syncthreads();
+    constexpr int PER = D / 16;                                              // channels of a thread: 16 threads per row
+    const int r = tid >> 4, ch = (tid & 15) * PER;
+    if (r >= rows) return;
+    float mm = sm_m[0][r];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) mm = fmaxf(mm, sm_m[w][r]);
+    float ll = 0.f, acc[PER];
+#pragma unroll
+    for (int c = 0; c < PER; ++c) acc[c] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(sm_m[w][r] - mm);
+        ll += sm_l[w][r] * f;
+#pragma unroll
+        for (int c = 0; c < PER; ++c) acc[c] += sm_o[w][r][ch + c] * f;
+    }
+    const int used = (kt.total + g.tiles_per_split - 1) / g.tiles_per_split;  // splits that have keys
+    if (used <= 1) {
+        const float inv = ll > 0.f ? 1.f / ll : 0.f;
+        const int row = rt * 16 + r;
+        uint16_t* dst = g.out + (row0 + row / g.p.group) * g.ldo + (int64_t)(kvh * g.p.group + row % g.p.group) * D + ch;
+#pragma unroll
+        for (int c = 0; c < PER; c += 4) *(uint2*)(dst + c) = make_uint2(bf16_pair(acc[c] * inv, acc[c + 1] * inv), bf16_pair(acc[c + 2] * inv, acc[c + 3] * inv));
+    } else {
+        const int64_t pr = ((int64_t)blockIdx.x * g.splits + split) * 16 + r;
+        if ((tid & 15) == 0) g.part_ml[pr] = make_float2(mm, ll);
+#pragma unroll
+        for (int c = 0; c < PER; c += 4) *(f32x4_t*)(g.part_o + pr * D + ch + c) = (f32x4_t){acc[c], acc[c + 1], acc[c + 2], acc[c + 3]};
+    }
+}
+
+// Joins the splits of one row: o = sum_s w_s o_s / sum_s w_s l_s, w_s = exp2(m_s - max m).
+template <int D>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs g) {
+    constexpr int CL = D / 4, SL = 256 / CL;      // lanes over channels (4 each), splits side by side
+    __shared__ f32x4_t sm[SL][CL];
+    __shared__ float sm_l[SL];
+    const int tid = threadIdx.x, cl = tid % CL, sl = tid / CL, r = blockIdx.y;
+    const int kvh = blockIdx.x % g.p.n_kv, tile = blockIdx.x / g.p.n_kv, s = tile / g.row_tiles, rt = tile % g.row_tiles;
+    int64_t row0;
+    const int count = (int)request_rows(g.p, s, &row0), kv = request_kv_len(g.p, s), row = rt * 16 + r;
+    if (row >= count * g.p.group) return;
+    const int last_row = min(rt * 16 + 15, count * g.p.group - 1);
+    const KeyTiles kt(max(kv - count + rt * 16 / g.p.group, 0), kv - count + last_row / g.p.group, g.window, g.sinks);
+    const int used = (kt.total + g.tiles_per_split - 1) / g.tiles_per_split;
+    if (used <= 1) return;
+    const int64_t pr = (int64_t)blockIdx.x * g.splits * 16 + r;
+    float mm = kNone;
+    for (int i = 0; i < used; ++i) mm = fmaxf(mm, g.part_ml[pr + (int64_t)i * 16].x);
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    float ll = 0.f;
+    for (int i = sl; i < used; i += SL) {
+        const int64_t at = pr + (int64_t)i * 16;
+        const float2 ml = g.part_ml[at];
+        const float f = __builtin_amdgcn_exp2f(ml.x - mm);
+        ll += ml.y * f;
+        acc += *(const f32x4_t*)(g.part_o + at * D + 4 * cl) * f;
+    }
+    sm[sl][cl] = acc;
+    if (cl == 0) sm_l[sl] = ll;
+    __syncthreads();
+    if (sl) return;
+    for (int i = 1; i < SL; ++i) { acc += sm[i][cl]; ll += sm_l[i]; }
+    const float inv = ll > 0.f ? 1.f / ll : 0.f;
+    uint16_t* dst = g.out + (row0 + row / g.p.group) * g.ldo + (int64_t)(kvh * g.p.group + row % g.p.group) * D + 4 * cl;
+    *(uint2*)dst = make_uint2(bf16_pair(acc[0] * inv, acc[1] * inv), bf16_pair(acc[2] * inv, acc[3] * inv));
+}
+
+struct Plan { int splits, tiles_per_split, row_tiles; };
+
+// Splits of the key axis, so that about `want` workgroups are there; a split has at least 8 tiles, two for each wavefront.
+Plan plan_few(int64_t n_seq, int64_t n_kv, int64_t group, int64_t max_new, int64_t max_kv) {
+    Plan p;
+    p.row_tiles = (int)ceil_div64(max_new * group, 16);
+    const int64_t tiles = max_kv / kTile + 2, pairs = n_seq * n_kv * p.row_tiles, want = 1024;
+    int64_t splits = ceil_div64(want, pairs), most = tiles / 8;
+    if (splits > most) splits = most;
+    if (splits < 1) splits = 1;
+    p.tiles_per_split = (int)ceil_div64(tiles, splits);
+    p.splits = (int)ceil_div64(tiles, p.tiles_per_split);
+    return p;
+}
+
+template <int D>
+int run_few(aser_ctx* ctx, const AttnArgs& g) {
+    const dim3 grid((unsigned)((int64_t)g.p.n_seq * g.row_tiles * g.p.n_kv), (unsigned)g.splits);
+    if (g.p.k_scale) attn_few_kernel<D, true><<<grid, 256, 0, ctx->stream>>>(g);
+    else attn_few_kernel<D, false><<<grid, 256, 0, ctx->stream>>>(g);
+    ASER_TRY(aser_check_launch(ctx, "attn_few_kernel"));
+    if (g.splits > 1) {
+        attn_join_kernel<D><<<dim3(grid.x, 16), 256, 0, ctx->stream>>>(g);
+        return aser_check_launch(ctx, "attn_join_kernel");
+    }
+    return ASER_OK;
+}
+
+}  // namespace
+
+extern "C" size_t aser_paged_attention_workspace_bytes(const aser_kv_cache* c, const aser_kv_batch* b, int32_t n_heads) {
+    if (!c || !b || c->n_kv <= 0 || n_heads < c->n_kv || b->n_seq <= 0 || b->max_new <= 0 || b->max_kv <= 0 || c->head_dim <= 0) return kAserWsTail;
+    const Plan p = plan_few(b->n_seq, c->n_kv, n_heads / c->n_kv, b->max_new, b->max_kv);
+    if (p.splits <= 1) return kAserWsTail;
+    const size_t rows = (size_t)b->n_seq * p.row_tiles * c->n_kv * p.splits * 16;
+    return align_up(rows * c->head_dim * 4, 256) + align_up(rows * 8, 256) + kAserWsTail;
+}
+
+extern "C" int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ldq, int32_t n_heads, const aser_kv_cache* cache,
+                                    const aser_kv_batch* batch, float scale, int32_t window, int32_t sinks, uint16_t* out, int64_t ldo) {
+    if (!ctx) return ASER_ERR_INVALID_ARG;
+    if (!q || !out) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "paged_attention: null pointer");
+    AttnArgs g{};
+    ASER_TRY(aser_paged_args(ctx, "paged_attention", cache, batch, n_heads, &g.p));
+    const int64_t width = (int64_t)n_heads * cache->head_dim;
+    if (ldq < width || ldo < width) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: leading dimension below the heads' channels");
+    if (!aser_rows_aligned(q, ldq, 2) || !aser_rows_aligned(out, ldo, 2)) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "paged_attention: rows must be 16-byte aligned");
+    if (window < 0 || sinks < 0) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: negative window or sinks");
+    if (!(scale - scale == 0.f)) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "paged_attention: scale is not finite");
+    if (batch->tokens == 0 || batch->max_new == 0) return ASER_OK;
+    const Plan plan = plan_few(g.p.n_seq, g.p.n_kv, g.p.group, batch->max_new, batch->max_kv);
+    g.q = q; g.ldq = ldq; g.out = out; g.ldo = ldo;
+    g.c = scale * 1.4426950408889634f;
+    g.window = window;
+    g.sinks = window > 0 ? sinks : 0;
+    g.splits = plan.splits; g.tiles_per_split = plan.tiles_per_split; g.row_tiles = plan.row_tiles;
+    if (g.splits > 1) {
+        const size_t rows = (size_t)g.p.n_seq * g.row_tiles * g.p.n_kv * g.splits * 16, o_bytes = align_up(rows * cache->head_dim * 4, 256);
+        if (!ctx->ws || ctx->ws_bytes < o_bytes + align_up(rows * 8, 256) + kAserWsTail) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "paged_attention: workspace too small");
+        g.part_o = (float*)ctx->ws;
+        g.part_ml = (float2*)((char*)ctx->ws + o_bytes);
+    }
+    if ((int64_t)g.p.n_seq * g.row_tiles * g.p.n_kv > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: too many requests times rows");
+    ASER_TRY(aser_prepare_device(ctx));
+    if (cache->head_dim == 64) return run_few<64>(ctx, g);
+    if (cache->head_dim == 128) return run_few<128>(ctx, g);
+    return run_few<256>(ctx, g);
+}
