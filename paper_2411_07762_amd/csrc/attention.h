@@ -1,0 +1,48 @@
+// What the attention kernels for few rows and for prompts share.
+#pragma once
+#include "bf16_pair.h"
+#include "paged_kv.h"
+
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+
+constexpr float kNone = -1e30f;                   // running maximum before any key
+
+struct AttnArgs {
+    PagedArgs p;
+    const uint16_t* q; int64_t ldq;
+    uint16_t* out; int64_t ldo;
+    float c;                                      // scale * log2(e)
+    int window, sinks;                            // window 0: none
+    int few_rows;                                 // requests of up to so many rows (tokens * group) take the kernel for few rows, -1: none does
+    int splits, tiles_per_split, row_tiles;
+    float* part_o; float2* part_ml;               // partial results of a split: [pair][split][row][D], [pair][split][row] (maximum, sum)
+};
+
+// Tiles of TILE keys that some row of positions [p_lo, p_hi] may see: [0, sink_tiles) and [main0, main0 + main_tiles).
+template <int TILE>
+struct KeyTiles {
+    int sink_tiles, main0, total;
+    __device__ __forceinline__ KeyTiles(int p_lo, int p_hi, int window, int sinks) {
+        main0 = 0;
+        sink_tiles = 0;
+        if (window > 0) {
+            const int low = p_lo - window + 1;
+            main0 = low > 0 ? low / TILE : 0;
+            const int s = (min(sinks, p_hi + 1) + TILE - 1) / TILE;
+            sink_tiles = min(s, main0);
+        }
+        total = p_hi < 0 ? 0 : sink_tiles + p_hi / TILE - main0 + 1;
+    }
+    __device__ __forceinline__ int first_key(int i) const { return (i < sink_tiles ? i : main0 + i - sink_tiles) * TILE; }
+};
+
+// Two codes of 8 bits, sign-extended, as two bf16 values in a word.
+template <int B>
+__device__ __forceinline__ uint32_t codes_pair(uint32_t w) {
+    return upper_halves((float)(int8_t)(w >> (8 * B)), (float)(int8_t)(w >> (8 * B + 8)));
+}
+
+// prompt_attention.hip: requests of more than few_rows rows.
+int aser_attention_prompt(aser_ctx* ctx, AttnArgs g, int head_dim, int64_t max_rows, float* part, size_t part_bytes);

@@ -10,52 +10,14 @@
 // probability changes lanes.  V^T wants 8 keys of one channel in a lane where memory has 8 channels of one key: a lane loads
 // D / 16 channels of its 8 keys and a byte permute per pair of keys turns them round.
 // Bound by reading the cache: 4 D bytes per key and head against 64 D / 16 matrix operations of 16 columns.
-#include "bf16_pair.h"
-#include "paged_kv.h"
+#include "attention.h"
 
 namespace {
 
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-
 constexpr int kTile = 32;                         // keys of a step
-constexpr float kNone = -1e30f;                   // running maximum before any key
-
-struct AttnArgs {
-    PagedArgs p;
-    const uint16_t* q; int64_t ldq;
-    uint16_t* out; int64_t ldo;
-    float c;                                      // scale * log2(e)
-    int window, sinks;                            // window 0: none
-    int splits, tiles_per_split, row_tiles;
-    float* part_o; float2* part_ml;               // partial results of a split: [pair][split][row][D], [pair][split][row] (maximum, sum)
-};
-
-// Tiles of 32 keys that some row of positions [p_lo, p_hi] may see: [0, sink_tiles) and [main0, main0 + main_tiles).
-struct KeyTiles {
-    int sink_tiles, main0, total;
-    __device__ __forceinline__ KeyTiles(int p_lo, int p_hi, int window, int sinks) {
-        main0 = 0;
-        sink_tiles = 0;
-        if (window > 0) {
-            const int low = p_lo - window + 1;
-            main0 = low > 0 ? low / kTile : 0;
-            const int s = (min(sinks, p_hi + 1) + kTile - 1) / kTile;
-            sink_tiles = min(s, main0);
-        }
-        total = p_hi < 0 ? 0 : sink_tiles + p_hi / kTile - main0 + 1;
-    }
-    __device__ __forceinline__ int first_key(int i) const { return (i < sink_tiles ? i : main0 + i - sink_tiles) * kTile; }
-};
-
-// Two codes of 8 bits, sign-extended, as two bf16 values in a word.
-template <int B>
-__device__ __forceinline__ uint32_t codes_pair(uint32_t w) {
-    return upper_halves((float)(int8_t)(w >> (8 * B)), (float)(int8_t)(w >> (8 * B + 8)));
-}
 
 template <int D, bool I8>
-__global__ __launch_bounds__(256) void attn_few_kernel(AttnArgs g) {
+__global__ __launch_bounds__(256, 2) void attn_few_kernel(AttnArgs g) {
     constexpr int KS = D / 32;                    // steps of 32 channels in K Q^T
     constexpr int NB = D / 16;                    // channels of a lane in V^T, and accumulators of O^T
     __shared__ float sm_o[4][16][D + 4];
@@ -65,12 +27,12 @@ __global__ __launch_bounds__(256) void attn_few_kernel(AttnArgs g) {
     int64_t row0;
     const int count = (int)request_rows(g.p, s, &row0), kv = request_kv_len(g.p, s);
     const int rows = count * g.p.group - rt * 16;                            // rows of this tile, if positive
-    if (rows <= 0) return;
+    if (rows <= 0 || count * g.p.group > g.few_rows) return;
     const int my_row = min(rt * 16 + n, count * g.p.group - 1), my_tok = my_row / g.p.group, my_head = my_row % g.p.group;
     const int my_pos = kv - count + my_tok;
     const int last_row = min(rt * 16 + 15, count * g.p.group - 1);
     const int p_lo = max(kv - count + rt * 16 / g.p.group, 0), p_hi = kv - count + last_row / g.p.group;
-    const KeyTiles kt(p_lo, p_hi, g.window, g.sinks);
+    const KeyTiles<kTile> kt(p_lo, p_hi, g.window, g.sinks);
     const int t0 = split * g.tiles_per_split, t1 = min(t0 + g.tiles_per_split, kt.total);
     if (t0 >= t1 && split > 0) return;
     const int low_all = g.window > 0 ? kv - count + rt * 16 / g.p.group - g.window + 1 : 0;   // the same for the tile's first row
@@ -262,9 +224,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs g) {
     const int kvh = blockIdx.x % g.p.n_kv, tile = blockIdx.x / g.p.n_kv, s = tile / g.row_tiles, rt = tile % g.row_tiles;
     int64_t row0;
     const int count = (int)request_rows(g.p, s, &row0), kv = request_kv_len(g.p, s), row = rt * 16 + r;
-    if (row >= count * g.p.group) return;
+    if (row >= count * g.p.group || count * g.p.group > g.few_rows) return;
     const int last_row = min(rt * 16 + 15, count * g.p.group - 1);
-    const KeyTiles kt(max(kv - count + rt * 16 / g.p.group, 0), kv - count + last_row / g.p.group, g.window, g.sinks);
+    const KeyTiles<kTile> kt(max(kv - count + rt * 16 / g.p.group, 0), kv - count + last_row / g.p.group, g.window, g.sinks);
     const int used = (kt.total + g.tiles_per_split - 1) / g.tiles_per_split;
     if (used <= 1) return;
     const int64_t pr = (int64_t)blockIdx.x * g.splits * 16 + r;
@@ -289,12 +251,15 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs g) {
     *(uint2*)dst = make_uint2(bf16_pair(acc[0] * inv, acc[1] * inv), bf16_pair(acc[2] * inv, acc[3] * inv));
 }
 
+constexpr int kFewRows = 64;                      // requests of more rows take the kernel for prompts
+
 struct Plan { int splits, tiles_per_split, row_tiles; };
 
 // Splits of the key axis, so that about `want` workgroups are there; a split has at least 8 tiles, two for each wavefront.
 Plan plan_few(int64_t n_seq, int64_t n_kv, int64_t group, int64_t max_new, int64_t max_kv) {
     Plan p;
-    p.row_tiles = (int)ceil_div64(max_new * group, 16);
+    const int64_t rows = max_new * group < kFewRows ? max_new * group : kFewRows;
+    p.row_tiles = (int)ceil_div64(rows, 16);
     const int64_t tiles = max_kv / kTile + 2, pairs = n_seq * n_kv * p.row_tiles, want = 1024;
     int64_t splits = ceil_div64(want, pairs), most = tiles / 8;
     if (splits > most) splits = most;
@@ -344,6 +309,7 @@ extern "C" int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ld
     g.c = scale * 1.4426950408889634f;
     g.window = window;
     g.sinks = window > 0 ? sinks : 0;
+    g.few_rows = kFewRows;
     g.splits = plan.splits; g.tiles_per_split = plan.tiles_per_split; g.row_tiles = plan.row_tiles;
     if (g.splits > 1) {
         const size_t rows = (size_t)g.p.n_seq * g.row_tiles * g.p.n_kv * g.splits * 16, o_bytes = align_up(rows * cache->head_dim * 4, 256);
@@ -353,6 +319,11 @@ extern "C" int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ld
     }
     if ((int64_t)g.p.n_seq * g.row_tiles * g.p.n_kv > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: too many requests times rows");
     ASER_TRY(aser_prepare_device(ctx));
+    const int64_t max_rows = (int64_t)batch->max_new * g.p.group;
+    if (max_rows > kFewRows) {
+        // a single request that has every row needs the other kernel only when it has few, which the host cannot see
+        ASER_TRY(aser_attention_prompt(ctx, g, cache->head_dim, max_rows, nullptr, 0));
+    }
     if (cache->head_dim == 64) return run_few<64>(ctx, g);
     if (cache->head_dim == 128) return run_few<128>(ctx, g);
     return run_few<256>(ctx, g);
