@@ -209,13 +209,17 @@ def _ld(t, cols: int) -> int:
     return t.stride(0)
 
 
+_DTYPE_CODES = {}
+
+
 def _dtype_code(t) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
-        return ASER_DTYPE_BF16
-    if t.dtype == torch.float32:
-        return ASER_DTYPE_F32
-    raise TypeError("activations must be bfloat16 or float32")
+    if not _DTYPE_CODES:
+        import torch
+        _DTYPE_CODES.update({torch.bfloat16: ASER_DTYPE_BF16, torch.float32: ASER_DTYPE_F32})
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
+        raise TypeError("activations must be bfloat16 or float32")
+    return code
 
 
 class Context:
@@ -468,6 +472,7 @@ class KvCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.c = aser_kv_cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), k.shape[0], k.stride(0), k.stride(1), k.stride(2),
                                ASER_KV_INT8 if k.dtype == torch.int8 else ASER_KV_BF16, k.shape[2], k.shape[1], k.shape[3])
+        self.ref, self.head_dim = ctypes.byref(self.c), k.shape[3]
 
     @classmethod
     def empty(cls, n_pages: int, n_kv: int, page_size: int, head_dim: int, int8: bool = False, device: int = 0):
@@ -495,45 +500,56 @@ class KvBatch:
         self.start, self.kv_len, self.pages = start, kv_len, pages
         ld = pages.stride(0) if n_seq > 1 else pages.shape[1]
         self.c = aser_kv_batch(_ptr(start), _ptr(kv_len), _ptr(pages), ld, tokens, n_seq, max_new, max_kv)
+        self.ref, self.tokens = ctypes.byref(self.c), tokens
+
+
+def _token_rows(t, tokens: int):
+    """(address, leading dimension, columns) of a matrix with a row for each token of a batch."""
+    rows, cols = t.shape
+    ld, unit = t.stride()
+    if rows < tokens or unit != 1:
+        raise ValueError("token matrices need a row for each of the batch's tokens and unit column stride")
+    return t.data_ptr(), ld, cols
 
 
 def aser_kv_append(ctx: Context, q, k, v, cache: KvCache, batch: KvBatch, q_out, *, rope_cos=None, rope_sin=None, interleaved: bool = False,
                    q_norm=None, k_norm=None, eps: float = 1e-6) -> int:
     """q, k, v: tokens x (heads * channels), bfloat16 or float32 alike (q and q_out may be None); rope_cos, rope_sin: positions x
     (rotated channels / 2) float32; q_norm, k_norm: channels of a head, float32."""
-    dt = _dtype_code(k)
-    if _dtype_code(v) != dt or (q is not None and _dtype_code(q) != dt):
+    dt, tokens, opts = _dtype_code(k), batch.tokens, None
+    if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
         raise TypeError("q, k and v must have one dtype")
-    opts = None
     if rope_cos is not None or q_norm is not None or k_norm is not None:
-        if rope_cos is not None and not (rope_cos.is_contiguous() and rope_sin.is_contiguous() and rope_cos.shape == rope_sin.shape):
-            raise ValueError("rope_cos and rope_sin must be contiguous and alike")
-        opts = ctypes.byref(aser_qk_opts(_ptr(rope_cos), _ptr(rope_sin), _ptr(q_norm), _ptr(k_norm), 0 if rope_cos is None else rope_cos.shape[0],
-                                         0 if rope_cos is None else 2 * rope_cos.shape[1], 1 if interleaved else 0, eps))
-    for t in (q, k, v, q_out):
-        if t is not None and t.shape[0] < batch.c.tokens:
-            raise ValueError("q, k, v and q_out need a row for each of the batch's tokens")
-    if q_out is not None and (_dtype_code(q_out) != ASER_DTYPE_BF16 or q_out.shape[1] < q.shape[1]):
-        raise TypeError("q_out must be bfloat16, as wide as q")
-    heads = 0 if q is None else q.shape[1] // cache.c.head_dim
-    return ctx._lib.aser_kv_append(ctx.handle, _ptr(q), 0 if q is None else _ld(q, q.shape[1]), heads, _ptr(k), _ld(k, k.shape[1]), _ptr(v),
-                                   _ld(v, v.shape[1]), dt, opts, ctypes.byref(cache.c), ctypes.byref(batch.c), _ptr(q_out),
-                                   0 if q_out is None else _ld(q_out, q_out.shape[1]))
+        n_pos = half = 0
+        if rope_cos is not None:
+            n_pos, half = rope_cos.shape
+            if not (rope_cos.is_contiguous() and rope_sin.is_contiguous() and rope_sin.shape == rope_cos.shape):
+                raise ValueError("rope_cos and rope_sin must be contiguous and alike")
+        opts = ctypes.byref(aser_qk_opts(_ptr(rope_cos), _ptr(rope_sin), _ptr(q_norm), _ptr(k_norm), n_pos, 2 * half, 1 if interleaved else 0, eps))
+    kp, ldk, _ = _token_rows(k, tokens)
+    vp, ldv, _ = _token_rows(v, tokens)
+    qp = op = None
+    ldq = ldo = heads = 0
+    if q is not None:
+        qp, ldq, width = _token_rows(q, tokens)
+        op, ldo, out_width = _token_rows(q_out, tokens)
+        if _dtype_code(q_out) != ASER_DTYPE_BF16 or out_width < width:
+            raise TypeError("q_out must be bfloat16, as wide as q")
+        heads = width // cache.head_dim
+    return ctx._lib.aser_kv_append(ctx.handle, qp, ldq, heads, kp, ldk, vp, ldv, dt, opts, cache.ref, batch.ref, op, ldo)
 
 
 def aser_paged_attention_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads: int) -> int:
-    return int(load_library().aser_paged_attention_workspace_bytes(ctypes.byref(cache.c), ctypes.byref(batch.c), n_heads))
+    return int(load_library().aser_paged_attention_workspace_bytes(cache.ref, batch.ref, n_heads))
 
 
 def aser_paged_attention(ctx: Context, q, cache: KvCache, batch: KvBatch, out, *, scale: float, window: int = 0, sinks: int = 0) -> int:
     """q, out: tokens x (heads * channels), bfloat16."""
-    width = q.shape[1]
-    if _dtype_code(q) != ASER_DTYPE_BF16 or _dtype_code(out) != ASER_DTYPE_BF16:
-        raise TypeError("q and out must be bfloat16")
-    if q.shape[0] < batch.c.tokens or out.shape[0] < batch.c.tokens or out.shape[1] < width:
-        raise ValueError("q and out need a row for each of the batch's tokens")
-    return ctx._lib.aser_paged_attention(ctx.handle, _ptr(q), _ld(q, width), width // cache.c.head_dim, ctypes.byref(cache.c), ctypes.byref(batch.c),
-                                         scale, window, sinks, _ptr(out), _ld(out, width))
+    qp, ldq, width = _token_rows(q, batch.tokens)
+    op, ldo, out_width = _token_rows(out, batch.tokens)
+    if _dtype_code(q) != ASER_DTYPE_BF16 or out.dtype != q.dtype or out_width < width:
+        raise TypeError("q and out must be bfloat16, out as wide as q")
+    return ctx._lib.aser_paged_attention(ctx.handle, qp, ldq, width // cache.head_dim, cache.ref, batch.ref, scale, window, sinks, op, ldo)
 
 
 def aser_adapter_workspace_bytes(rows: int, n: int, m: int, r: int) -> int:
@@ -544,16 +560,21 @@ def aser_adapter_forward(ctx: Context, X, adapter, A, B, scale, Y0, Y) -> int:
     """X: rows x n; adapter: rows int32; A: adapters x r x n and B: adapters x m x r, contiguous bfloat16; scale: adapters float32
     or None; Y0 (None: zeros) and Y: rows x m float32."""
     n_adapters, r, n = A.shape
+    rows, cols = X.shape
     m = B.shape[1]
-    if not (A.is_contiguous() and B.is_contiguous() and B.shape[0] == n_adapters and B.shape[2] == r and X.shape[1] == n):
+    if cols != n or tuple(B.shape) != (n_adapters, m, r) or not (A.is_contiguous() and B.is_contiguous()):
         raise ValueError("A must be adapters x r x n and B adapters x m x r, contiguous")
-    if _dtype_code(A) != ASER_DTYPE_BF16 or _dtype_code(B) != ASER_DTYPE_BF16 or _dtype_code(Y) != ASER_DTYPE_F32:
-        raise TypeError("A and B must be bfloat16, Y float32")
-    rows = X.shape[0]
-    if adapter.shape[0] != rows or adapter.element_size() != 4 or Y.shape[0] < rows or (Y0 is not None and (Y0.shape[0] < rows or Y0.dtype != Y.dtype)):
-        raise ValueError("adapter (int32), Y0 and Y (float32) need an entry for each row of X")
-    return ctx._lib.aser_adapter_forward(ctx.handle, _ptr(X), _dtype_code(X), X.shape[0], n, _ld(X, n), _ptr(adapter), _ptr(A), _ptr(B), _ptr(scale),
-                                         n_adapters, r, m, _ptr(Y0), _ld(Y0, m) if Y0 is not None else m, _ptr(Y), _ld(Y, m))
+    if _dtype_code(A) != ASER_DTYPE_BF16 or B.dtype != A.dtype or _dtype_code(Y) != ASER_DTYPE_F32 or (Y0 is not None and Y0.dtype != Y.dtype):
+        raise TypeError("A and B must be bfloat16, Y0 and Y float32")
+    if adapter.shape[0] != rows or adapter.element_size() != 4 or (scale is not None and scale.shape[0] < n_adapters):
+        raise ValueError("adapter has an int32 for each row of X, scale a float32 for each adapter")
+    xp, ldx, _ = _token_rows(X, rows)
+    yp, ldy, width = _token_rows(Y, rows)
+    y0p, ldy0, width0 = (None, m, m) if Y0 is None else _token_rows(Y0, rows)
+    if width < m or width0 < m:
+        raise ValueError("Y0 and Y must be as wide as B is high")
+    return ctx._lib.aser_adapter_forward(ctx.handle, xp, _dtype_code(X), rows, n, ldx, adapter.data_ptr(), A.data_ptr(), B.data_ptr(),
+                                         _ptr(scale), n_adapters, r, m, y0p, ldy0, yp, ldy)
 
 
 # ----------------------------------------------------------------------------------- one layer, end to end

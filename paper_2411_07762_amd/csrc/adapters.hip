@@ -1,7 +1,7 @@
 // Low-rank adapters of many requests beside a projection that they share:
 //     Y[t] = Y0[t] + s_a (x_t A_a^T) B_a^T,   a the adapter of row t.
-// Rows with the same adapter are taken 16 at a time, so that an adapter is read once for 16 of its rows, wherever they are in
-// the batch: the sum is the same for a row whatever its neighbours.  Two launches, P = x A^T in parts of the channel axis
+// Rows with the same adapter are taken 16 or 32 at a time, so that an adapter is read once for so many of its rows, wherever they
+// are in the batch: the sum is the same for a row whatever its neighbours.  Two launches, P = x A^T in parts of the channel axis
 // and Y = Y0 + s P B^T, which adds the parts in their order; a third in front sorts the rows by adapter when there are
 // more than 64 of them (up to 64 the groups are formed by a ballot in every wavefront).  A few operations per byte of A, B,
 // X and Y: bound by memory, or by the launches when few rows come.
@@ -17,8 +17,9 @@ namespace {
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
-constexpr int kTok = 16;            // rows of a tile
-constexpr int kFewRows = 64;        // up to here groups are formed by ballot
+constexpr int kFewRows = 64;        // up to here groups are formed by ballot, in tiles of 16 rows
+constexpr int kManyTiles = 2;       // beyond, a tile has so many times 16 rows
+constexpr int kLoop = 4;            // and a wavefront takes so many times 64 outputs, with P in registers
 constexpr int kMaxAdapters = 4096;
 
 struct AdArgs {
@@ -33,71 +34,89 @@ struct AdArgs {
 };
 
 // Sorts the rows by adapter (rows without one last) and cuts the result into tiles.  One workgroup: counts per adapter, their
-// running sums, places.
-__global__ __launch_bounds__(1024) void adapter_sort_kernel(AdArgs g, int max_tiles) {
-    __shared__ int cnt[kMaxAdapters + 1], tile_at[1024], row_at[1024];
-    const int tid = threadIdx.x, na = g.n_adapters;
+// running sums, places.  The rows of a prompt have one adapter: a wavefront whose rows agree counts them in one step.
+__global__ __launch_bounds__(1024) void adapter_sort_kernel(AdArgs g, int tok, int max_tiles) {
+    __shared__ int cnt[kMaxAdapters + 1], wave_rows[16], wave_tiles[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, na = g.n_adapters;
+    auto take = [&](int64_t base, bool place) {        // 64 rows from base on
+        const bool in = base + lane < g.rows;
+        int a = in ? g.id[base + lane] : 0;
+        if ((uint32_t)a >= (uint32_t)na) a = na;
+        const int a0 = __builtin_amdgcn_readfirstlane(a);
+        const uint64_t here = __ballot(in);
+        int at;
+        if (__ballot(in & (a == a0)) == here) {
+            int first = 0;
+            if (lane == 0) first = atomicAdd(&cnt[a0], __popcll(here));
+            at = __builtin_amdgcn_readfirstlane(first) + lane;
+        } else {
+            at = in ? atomicAdd(&cnt[a], 1) : 0;
+        }
+        if (place && in) g.order[at] = (int32_t)(base + lane);
+    };
     for (int i = tid; i <= na; i += 1024) cnt[i] = 0;
     __syncthreads();
-    for (int64_t t = tid; t < g.rows; t += 1024) {
-        const int a = g.id[t];
-        atomicAdd(&cnt[(uint32_t)a < (uint32_t)na ? a : na], 1);
-    }
+    for (int64_t base = 64 * wave; base < g.rows; base += 1024) take(base, false);
     __syncthreads();
     // thread i owns `per` consecutive adapters
     const int per = (na + 1 + 1023) / 1024, lo = min(tid * per, na + 1), hi = min(lo + per, na + 1);
     int nr = 0, nt = 0;
-    for (int i = lo; i < hi; ++i) { nr += cnt[i]; nt += (cnt[i] + kTok - 1) / kTok; }
-    row_at[tid] = nr;
-    tile_at[tid] = nt;
-    __syncthreads();
-    for (int o = 1; o < 1024; o <<= 1) {
-        const int a = tid >= o ? row_at[tid - o] : 0, b = tid >= o ? tile_at[tid - o] : 0;
-        __syncthreads();
-        row_at[tid] += a;
-        tile_at[tid] += b;
-        __syncthreads();
+    for (int i = lo; i < hi; ++i) { nr += cnt[i]; nt += (cnt[i] + tok - 1) / tok; }
+    int r0 = nr, t0 = nt;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int x = __shfl_up(r0, o), y = __shfl_up(t0, o);
+        r0 += lane >= o ? x : 0;
+        t0 += lane >= o ? y : 0;
     }
-    const int total = tile_at[1023];
-    int r0 = row_at[tid] - nr, t0 = tile_at[tid] - nt;
+    if (lane == 63) { wave_rows[wave] = r0; wave_tiles[wave] = t0; }
+    __syncthreads();
+    int total = 0;
+    r0 -= nr;
+    t0 -= nt;
+    for (int w = 0; w < 16; ++w) {
+        r0 += w < wave ? wave_rows[w] : 0;
+        t0 += w < wave ? wave_tiles[w] : 0;
+        total += wave_tiles[w];
+    }
     for (int i = lo; i < hi; ++i) {
         const int c = cnt[i];
-        for (int x = 0; x < c; x += kTok) g.tiles[t0++] = make_int4(i < na ? i : -1, r0 + x, min(kTok, c - x), 0);
+        for (int x = 0; x < c; x += tok) g.tiles[t0++] = make_int4(i < na ? i : -1, r0 + x, min(tok, c - x), 0);
         cnt[i] = r0;                                   // from here on: the next free place
         r0 += c;
     }
     for (int i = total + tid; i < max_tiles; i += 1024) g.tiles[i] = make_int4(-2, 0, 0, 0);
     __syncthreads();
-    for (int64_t t = tid; t < g.rows; t += 1024) {
-        const int a = g.id[t];
-        g.order[atomicAdd(&cnt[(uint32_t)a < (uint32_t)na ? a : na], 1)] = (int32_t)t;
-    }
+    for (int64_t base = 64 * wave; base < g.rows; base += 1024) take(base, true);
 }
 
-// The rows of a workgroup's tile: adapter (-1: rows without one, -2: no such tile) and the row in column `col`, -1 past the last.
+// The rows of a workgroup's tile: adapter (-1: rows without one, -2: no such tile) and the rows in columns `col` (+ 16 ..), -1 past the last.
+template <int NT>
 struct TileRows {
-    int adapter, row;
+    int adapter, row[NT];
     __device__ __forceinline__ TileRows(const AdArgs& g, int tile, int lane) {
         const int col = lane & 15;
-        if (g.tiles) {
+        if constexpr (NT > 1) {
             const int4 t = g.tiles[tile];
             adapter = t.x;
-            row = col < t.z ? g.order[t.y + col] : -1;
-            return;
-        }
-        // tile = slots j + q: the rows whose adapter is row j's, if no earlier row has it; 16 q .. of them
-        const int slots = (int)((g.rows + kTok - 1) / kTok), j = tile / slots, skip = tile % slots * kTok;
-        int a = lane < g.rows ? g.id[lane] : -2;
-        if (lane < g.rows && (uint32_t)a >= (uint32_t)g.n_adapters) a = -1;
-        const int mine = __shfl(a, j);
-        const uint64_t same = __ballot(a == mine && lane < g.rows);
-        adapter = (int)(__ffsll((unsigned long long)same) - 1) == j && __popcll(same) > skip ? mine : -2;
-        row = -1;
-        uint64_t left = same;
-        for (int i = 0, k = __popcll(same); i < k; ++i) {
-            const int at = __ffsll((unsigned long long)left) - 1;
-            left &= left - 1;
-            if (i == skip + col) row = at;
+#pragma unroll
+            for (int x = 0; x < NT; ++x) row[x] = 16 * x + col < t.z ? g.order[t.y + 16 * x + col] : -1;
+        } else {
+            // tile = slots j + q: the rows whose adapter is row j's, if no earlier row has it; 16 q .. of them
+            const int slots = (int)((g.rows + 15) / 16), j = tile / slots, skip = tile % slots * 16;
+            int a = lane < g.rows ? g.id[lane] : -2;
+            if (lane < g.rows && (uint32_t)a >= (uint32_t)g.n_adapters) a = -1;
+            const int mine = __builtin_amdgcn_readlane(a, j);
+            const uint64_t same = __ballot(a == mine && lane < g.rows);
+            adapter = (int)(__ffsll((unsigned long long)same) - 1) == j && __popcll(same) > skip ? mine : -2;
+            row[0] = -1;
+            if (adapter == -2) return;
+            uint64_t left = same;
+            for (int i = 0, k = __popcll(same); i < k; ++i) {
+                const int at = __ffsll((unsigned long long)left) - 1;
+                left &= left - 1;
+                if (i == skip + col) row[0] = at;
+            }
         }
     }
 };
@@ -148,115 +167,167 @@ __device__ __forceinline__ void row8_f32(const float* row, int64_t c, int64_t n,
 }
 
 // P[part][row][.] = x A^T over the part's channels; the four wavefronts take every fourth step of 32 channels.
-template <int RT, bool F32, bool VEC>
+template <int RT, bool F32, bool VEC, int NT>
 __global__ __launch_bounds__(256) void adapter_down_kernel(AdArgs g) {
-    __shared__ f32x4_t sm[3][RT][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
-    const TileRows tr(g, blockIdx.x, lane);
+    __shared__ f32x4_t sm[3][NT][RT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
+    const TileRows<NT> tr(g, blockIdx.x, lane);
     if (tr.adapter < 0) return;
-    const bool live = tr.row >= 0;
-    const int64_t row = live ? tr.row : 0;
     const int64_t c0 = blockIdx.y * g.part_n, c1 = c0 + g.part_n < g.n ? c0 + g.part_n : g.n;
     const uint16_t* a_row = g.A + (int64_t)tr.adapter * g.r * g.n;
-    f32x4_t acc[RT];
+    f32x4_t acc[NT][RT];
 #pragma unroll
-    for (int i = 0; i < RT; ++i) acc[i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    for (int x = 0; x < NT; ++x)
+#pragma unroll
+        for (int i = 0; i < RT; ++i) acc[x][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
     for (int64_t c = c0 + 32 * wave; c < c1; c += 128) {
         const int64_t at = c + 8 * grp;
-        bf16x8_t x[3], a[RT];
-        float xf[8];
-        if (F32) row8_f32<VEC>((const float*)g.X + row * g.ldx, at, g.n, live, xf);
-        else x[0] = row8<VEC>((const uint16_t*)g.X + row * g.ldx, at, g.n, live);
+        bf16x8_t a[RT];
+        float xf[NT][8];
+        bf16x8_t xb[NT];
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            const int64_t row = max(tr.row[x], 0);
+            if (F32) row8_f32<VEC>((const float*)g.X + row * g.ldx, at, g.n, tr.row[x] >= 0, xf[x]);
+            else xb[x] = row8<VEC>((const uint16_t*)g.X + row * g.ldx, at, g.n, tr.row[x] >= 0);
+        }
 #pragma unroll
         for (int i = 0; i < RT; ++i) a[i] = row8<VEC>(a_row + (16 * i + col) * g.n, at, g.n, 16 * i + col < g.r);
-        if (F32) three_terms(xf, x);
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
+        for (int x = 0; x < NT; ++x) {
+            bf16x8_t t[3];
+            if (F32) three_terms(xf[x], t);
+            else t[0] = xb[x];
 #pragma unroll
-            for (int k = F32 ? 2 : 0; k >= 0; --k) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], x[k], acc[i], 0, 0, 0);
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int k = F32 ? 2 : 0; k >= 0; --k) acc[x][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], t[k], acc[x][i], 0, 0, 0);
+        }
     }
     if (wave)
 #pragma unroll
-        for (int i = 0; i < RT; ++i) sm[wave - 1][i][lane] = acc[i];
+        for (int x = 0; x < NT; ++x)
+#pragma unroll
+            for (int i = 0; i < RT; ++i) sm[wave - 1][x][i][lane] = acc[x][i];
     __syncthreads();
-    if (wave || !live) return;
-    float* dst = g.P + ((int64_t)blockIdx.y * g.rows + row) * g.rp;
+    if (wave) return;
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        f32x4_t v = acc[i];
+    for (int x = 0; x < NT; ++x) {
+        if (tr.row[x] < 0) continue;
+        float* dst = g.P + ((int64_t)blockIdx.y * g.rows + tr.row[x]) * g.rp;
 #pragma unroll
-        for (int w = 0; w < 3; ++w) v += sm[w][i][lane];
-        if (16 * i < g.rp) *(f32x4_t*)(dst + 16 * i + 4 * grp) = v;
+        for (int i = 0; i < RT; ++i) {
+            f32x4_t v = acc[x][i];
+#pragma unroll
+            for (int w = 0; w < 3; ++w) v += sm[w][x][i][lane];
+            if (16 * i < g.rp) *(f32x4_t*)(dst + 16 * i + 4 * grp) = v;
+        }
     }
 }
 
-// Y = Y0 + s P B^T: a wavefront has 64 outputs, a workgroup 256.  ALIGNED: four outputs of a row at a time.
-template <int KS, bool VEC>
+// Y = Y0 + s P B^T: a wavefront has LOOP times 64 outputs, four times that far apart from each other.  aligned: four outputs at a time.
+template <int KS, bool VEC, int NT, int LOOP>
 __global__ __launch_bounds__(256) void adapter_up_kernel(AdArgs g, bool aligned) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
-    const TileRows tr(g, blockIdx.x, lane);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
+    const TileRows<NT> tr(g, blockIdx.x, lane);
     if (tr.adapter == -2 || (tr.adapter == -1 && g.Y0 == g.Y)) return;
-    const bool live = tr.row >= 0;
-    const int64_t row = live ? tr.row : 0, o0 = (int64_t)blockIdx.y * 256 + wave * 64;
-    if (o0 >= g.m) return;
-    f32x4_t acc[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-    if (tr.adapter >= 0) {
+    const bool some = tr.adapter >= 0;
+    bf16x8_t t[NT][KS][3];
+    const uint16_t* b = g.B;
+    if (some) {
         const float s = g.scale ? g.scale[tr.adapter] : 1.f;
-        const uint16_t* b = g.B + (int64_t)tr.adapter * g.m * g.r;
+        b += (int64_t)tr.adapter * g.m * g.r;
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            const int at = 32 * k + 8 * grp;
-            float p[8];
+        for (int x = 0; x < NT; ++x)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] = 0.f;
-            if (live && at < g.rp)
-                for (int part = 0; part < g.parts; ++part) {
-                    const float* src = g.P + ((int64_t)part * g.rows + row) * g.rp + at;
-                    const float4 u = *(const float4*)src, v = *(const float4*)(src + 4);
-                    p[0] += u.x; p[1] += u.y; p[2] += u.z; p[3] += u.w;
-                    p[4] += v.x; p[5] += v.y; p[6] += v.z; p[7] += v.w;
+            for (int k = 0; k < KS; ++k) {
+                const int at = 32 * k + 8 * grp;
+                float p[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) p[j] = 0.f;
+                if (tr.row[x] >= 0 && at < g.rp) {
+                    const float* src = g.P + (int64_t)tr.row[x] * g.rp + at;
+#pragma unroll 4
+                    for (int part = 0; part < g.parts; ++part, src += g.rows * g.rp) {
+                        const float4 u = *(const float4*)src, v = *(const float4*)(src + 4);
+                        p[0] += u.x; p[1] += u.y; p[2] += u.z; p[3] += u.w;
+                        p[4] += v.x; p[5] += v.y; p[6] += v.z; p[7] += v.w;
+                    }
                 }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] *= s;
-            bf16x8_t t[3];
-            three_terms(p, t);
+                for (int j = 0; j < 8; ++j) p[j] *= s;
+                three_terms(p, t[x][k]);
+            }
+    }
+    for (int loop = 0; loop < LOOP; ++loop) {
+        const int64_t o0 = ((int64_t)blockIdx.y * LOOP + loop) * 256 + wave * 64;
+        if (o0 >= g.m) return;
+        f32x4_t acc[NT][4];
+#pragma unroll
+        for (int x = 0; x < NT; ++x)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int64_t o = o0 + 16 * i + col;
-                const bf16x8_t w = row8<VEC>(b + o * g.r, at, g.r, o < g.m);
+                acc[x][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+                const int64_t o = o0 + 16 * i + 4 * grp;
+                if (g.Y0 && tr.row[x] >= 0) {
+                    const float* y0 = g.Y0 + (int64_t)tr.row[x] * g.ldy0 + o;
+                    if (aligned && o + 4 <= g.m) acc[x][i] = *(const f32x4_t*)y0;
+                    else {
 #pragma unroll
-                for (int x = 2; x >= 0; --x) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, t[x], acc[i], 0, 0, 0);
+                        for (int e = 0; e < 4; ++e)
+                            if (o + e < g.m) acc[x][i][e] = y0[e];
+                    }
+                }
+            }
+        if (some) {
+            f32x4_t sum[NT][4];
+#pragma unroll
+            for (int x = 0; x < NT; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[x][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t o = o0 + 16 * i + col;
+                    const bf16x8_t w = row8<VEC>(b + o * g.r, 32 * k + 8 * grp, g.r, o < g.m);
+#pragma unroll
+                    for (int x = 0; x < NT; ++x)
+#pragma unroll
+                        for (int e = 2; e >= 0; --e) sum[x][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, t[x][k][e], sum[x][i], 0, 0, 0);
+                }
+#pragma unroll
+            for (int x = 0; x < NT; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[x][i] += sum[x][i];
+        }
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            if (tr.row[x] < 0) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t o = o0 + 16 * i + 4 * grp;
+                float* y = g.Y + (int64_t)tr.row[x] * g.ldy + o;
+                if (aligned && o + 4 <= g.m) *(f32x4_t*)y = acc[x][i];
+                else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (o + e < g.m) y[e] = acc[x][i][e];
+                }
             }
         }
     }
-    if (!live) return;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t o = o0 + 16 * i + 4 * grp;
-        float* y = g.Y + row * g.ldy + o;
-        const float* y0 = g.Y0 ? g.Y0 + row * g.ldy0 + o : nullptr;
-        if (aligned && o + 4 <= g.m) {
-            f32x4_t v = acc[i];
-            if (y0) v += *(const f32x4_t*)y0;
-            *(f32x4_t*)y = v;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (o + e < g.m) y[e] = acc[i][e] + (y0 ? y0[e] : 0.f);
-        }
-    }
 }
 
-struct AdPlan { int tiles, parts; int64_t part_n; size_t p_bytes, order_bytes, tile_bytes; };
+struct AdPlan { int tok, tiles, parts; int64_t part_n; size_t p_bytes, order_bytes, tile_bytes; };
 
 AdPlan plan_adapters(int64_t rows, int64_t n, int r) {
     AdPlan p;
     const bool few = rows <= kFewRows;
-    p.tiles = (int)(few ? ceil_div64(rows, kTok) * rows : ceil_div64(rows, kTok) + kMaxAdapters + 1);
+    p.tok = few ? 16 : 16 * kManyTiles;
+    p.tiles = (int)(few ? ceil_div64(rows, p.tok) * rows : ceil_div64(rows, p.tok) + kMaxAdapters + 1);
     // parts of the channel axis: about 512 workgroups, at least 256 channels each
-    const int64_t groups = few ? rows : ceil_div64(rows, kTok);
+    const int64_t groups = few ? rows : ceil_div64(rows, p.tok);
     int64_t parts = ceil_div64(512, groups);
     if (parts > ceil_div64(n, 256)) parts = ceil_div64(n, 256);
     if (parts > 16) parts = 16;
@@ -268,20 +339,34 @@ AdPlan plan_adapters(int64_t rows, int64_t n, int r) {
     return p;
 }
 
-template <int RT>
+template <int RT, int NT>
 void launch_down(const AdArgs& g, bool f32, bool vec, dim3 grid, hipStream_t st) {
     if (f32) {
-        if (vec) adapter_down_kernel<RT, true, true><<<grid, 256, 0, st>>>(g);
-        else adapter_down_kernel<RT, true, false><<<grid, 256, 0, st>>>(g);
+        if (vec) adapter_down_kernel<RT, true, true, NT><<<grid, 256, 0, st>>>(g);
+        else adapter_down_kernel<RT, true, false, NT><<<grid, 256, 0, st>>>(g);
     } else {
-        if (vec) adapter_down_kernel<RT, false, true><<<grid, 256, 0, st>>>(g);
-        else adapter_down_kernel<RT, false, false><<<grid, 256, 0, st>>>(g);
+        if (vec) adapter_down_kernel<RT, false, true, NT><<<grid, 256, 0, st>>>(g);
+        else adapter_down_kernel<RT, false, false, NT><<<grid, 256, 0, st>>>(g);
     }
 }
-template <int KS>
+template <int NT>
+void launch_downs(const AdArgs& g, bool f32, bool vec, dim3 grid, hipStream_t st) {
+    if (g.r <= 16) launch_down<1, NT>(g, f32, vec, grid, st);
+    else if (g.r <= 32) launch_down<2, NT>(g, f32, vec, grid, st);
+    else if (g.r <= 64) launch_down<4, NT>(g, f32, vec, grid, st);
+    else launch_down<8, NT>(g, f32, vec, grid, st);
+}
+template <int KS, int NT, int LOOP>
 void launch_up(const AdArgs& g, bool vec, bool aligned, dim3 grid, hipStream_t st) {
-    if (vec) adapter_up_kernel<KS, true><<<grid, 256, 0, st>>>(g, aligned);
-    else adapter_up_kernel<KS, false><<<grid, 256, 0, st>>>(g, aligned);
+    if (vec) adapter_up_kernel<KS, true, NT, LOOP><<<grid, 256, 0, st>>>(g, aligned);
+    else adapter_up_kernel<KS, false, NT, LOOP><<<grid, 256, 0, st>>>(g, aligned);
+}
+template <int NT, int LOOP>
+void launch_ups(const AdArgs& g, bool vec, bool aligned, unsigned tiles, hipStream_t st) {
+    const dim3 grid(tiles, (unsigned)ceil_div64(g.m, 256 * LOOP));
+    if (g.r <= 32) launch_up<1, NT, LOOP>(g, vec, aligned, grid, st);
+    else if (g.r <= 64) launch_up<2, NT, LOOP>(g, vec, aligned, grid, st);
+    else launch_up<4, NT, LOOP>(g, vec, aligned, grid, st);
 }
 
 }  // namespace
@@ -313,23 +398,20 @@ extern "C" int aser_adapter_forward(aser_ctx* ctx, const void* X, int x_dtype, i
         g.order = (int32_t*)((char*)ctx->ws + p.p_bytes);
         g.tiles = (int4*)((char*)ctx->ws + p.p_bytes + p.order_bytes);
         // no more tiles than full ones and one for each adapter, and for the rows without one, that is there
-        const int64_t most = ceil_div64(rows, kTok) + (n_adapters + 1 < rows ? n_adapters + 1 : rows);
+        const int64_t most = ceil_div64(rows, p.tok) + (n_adapters + 1 < rows ? n_adapters + 1 : rows);
         tiles = (int)(most < p.tiles ? most : p.tiles);
-        adapter_sort_kernel<<<1, 1024, 0, ctx->stream>>>(g, tiles);
+        adapter_sort_kernel<<<1, 1024, 0, ctx->stream>>>(g, p.tok, tiles);
         ASER_TRY(aser_check_launch(ctx, "adapter_sort_kernel"));
     }
     const int xw = f32 ? 3 : 7;                          // elements of 16 bytes, less one
     const bool vec_a = n % 8 == 0 && ((uintptr_t)A & 15) == 0 && ((uintptr_t)X & 15) == 0 && (ldx & xw) == 0;
     const bool vec_b = r % 8 == 0 && ((uintptr_t)B & 15) == 0;
     const bool aligned = (ldy & 3) == 0 && ((uintptr_t)Y & 15) == 0 && (!Y0 || ((ldy0 & 3) == 0 && ((uintptr_t)Y0 & 15) == 0));
-    const dim3 down((unsigned)tiles, (unsigned)p.parts), up((unsigned)tiles, (unsigned)ceil_div64(m, 256));
-    if (r <= 16) launch_down<1>(g, f32, vec_a, down, ctx->stream);
-    else if (r <= 32) launch_down<2>(g, f32, vec_a, down, ctx->stream);
-    else if (r <= 64) launch_down<4>(g, f32, vec_a, down, ctx->stream);
-    else launch_down<8>(g, f32, vec_a, down, ctx->stream);
+    const dim3 down((unsigned)tiles, (unsigned)p.parts);
+    if (rows > kFewRows) launch_downs<kManyTiles>(g, f32, vec_a, down, ctx->stream);
+    else launch_downs<1>(g, f32, vec_a, down, ctx->stream);
     ASER_TRY(aser_check_launch(ctx, "adapter_down_kernel"));
-    if (r <= 32) launch_up<1>(g, vec_b, aligned, up, ctx->stream);
-    else if (r <= 64) launch_up<2>(g, vec_b, aligned, up, ctx->stream);
-    else launch_up<4>(g, vec_b, aligned, up, ctx->stream);
+    if (rows > kFewRows) launch_ups<kManyTiles, kLoop>(g, vec_b, aligned, (unsigned)tiles, ctx->stream);
+    else launch_ups<1, 1>(g, vec_b, aligned, (unsigned)tiles, ctx->stream);
     return aser_check_launch(ctx, "adapter_up_kernel");
 }

@@ -16,8 +16,8 @@ struct AttnArgs {
     float c;                                      // scale * log2(e)
     int window, sinks;                            // window 0: none
     int few_rows;                                 // requests of up to so many rows (tokens * group) take the kernel for few rows, -1: none does
-    int splits, tiles_per_split, row_tiles;
-    float* part_o; float2* part_ml;               // partial results of a split: [pair][split][row][D], [pair][split][row] (maximum, sum)
+    int splits, tiles_per_split, row_tiles;       // the kernel for few rows: parts of the key axis, their steps, most row tiles of a request
+    float* part_o; float2* part_ml;               // results of splits: [row tile and head][split][row][D], [..][split][row] (maximum, sum)
 };
 
 // Tiles of TILE keys that some row of positions [p_lo, p_hi] may see: [0, sink_tiles) and [main0, main0 + main_tiles).
