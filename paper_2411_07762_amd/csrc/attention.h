@@ -35,8 +35,18 @@ struct KeyTiles {
         }
         total = p_hi < 0 ? 0 : sink_tiles + p_hi / TILE - main0 + 1;
     }
+    // Tiles, counted from the first, that begin at or before key `p`.
+    __device__ __forceinline__ int count_up_to(int p) const {
+        const int t = p < 0 ? 0 : p / TILE + 1;
+        return t <= main0 ? min(t, sink_tiles) : sink_tiles + t - main0;
+    }
     __device__ __forceinline__ int first_key(int i) const { return (i < sink_tiles ? i : main0 + i - sink_tiles) * TILE; }
 };
+
+// Words that no kernel of this call writes, through the scalar cache: beside copies into LDS the compiler takes vector loads for them, and
+// waits for those together with every copy in flight.
+typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
+__device__ __forceinline__ ScalarInts scalar_ints(const int32_t* p) { return (ScalarInts)(uintptr_t)p; }
 
 // Two codes of 8 bits, sign-extended, as two bf16 values in a word.
 template <int B>
@@ -44,5 +54,6 @@ __device__ __forceinline__ uint32_t codes_pair(uint32_t w) {
     return upper_halves((float)(int8_t)(w >> (8 * B)), (float)(int8_t)(w >> (8 * B + 8)));
 }
 
-// prompt_attention.hip: requests of more than few_rows rows.
-int aser_attention_prompt(aser_ctx* ctx, AttnArgs g, int head_dim, int64_t max_rows, float* part, size_t part_bytes);
+// prompt_attention.hip: requests of more than few_rows rows; keys: the most that a row sees.  Its workspace is at the start of ctx's.
+size_t aser_attention_prompt_workspace(int64_t tokens, int64_t n_seq, int64_t n_kv, int64_t group, int head_dim, int64_t keys);
+int aser_attention_prompt(aser_ctx* ctx, AttnArgs g, int head_dim, int64_t keys);

@@ -60,7 +60,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void attn_few_kernel(AttnArg
 #pragma unroll
     for (int b = 0; b < NB; ++b) o[b] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
     float m = kNone, l = 0.f;
-    const int* table = g.p.pages + s * g.p.ld_pages;
+    const ScalarInts table = scalar_ints(g.p.pages + s * g.p.ld_pages);
     const int page_mask = (1 << g.p.page_shift) - 1;
     // a lane's offsets in bytes inside 16 slots; everything else of an address is the same for the wavefront
     constexpr int ES = I8 ? 1 : 2, KW = I8 ? 2 : 4, VW = I8 ? NB / 4 : NB / 2;         // bytes of an element; words of a load
@@ -348,9 +348,14 @@ size_t few_workspace(const Plan& p, int64_t n_seq, int64_t n_kv, int head_dim, s
 }  // namespace
 
 extern "C" size_t aser_paged_attention_workspace_bytes(const aser_kv_cache* c, const aser_kv_batch* b, int32_t n_heads) {
-    if (!c || !b || c->n_kv <= 0 || n_heads < c->n_kv || b->n_seq <= 0 || b->max_new <= 0 || b->max_kv <= 0 || c->head_dim <= 0) return kAserWsTail;
-    size_t o_bytes;
-    return few_workspace(plan_few(b->n_seq, c->n_kv, n_heads / c->n_kv, b->max_new, b->max_kv), b->n_seq, c->n_kv, c->head_dim, &o_bytes) + kAserWsTail;
+    if (!c || !b || c->n_kv <= 0 || n_heads < c->n_kv || b->n_seq <= 0 || b->tokens <= 0 || b->max_new <= 0 || b->max_kv <= 0 || c->head_dim <= 0) return kAserWsTail;
+    const int64_t group = n_heads / c->n_kv;
+    size_t o_bytes, need = few_workspace(plan_few(b->n_seq, c->n_kv, group, b->max_new, b->max_kv), b->n_seq, c->n_kv, c->head_dim, &o_bytes);
+    if (b->max_new * group > kFewRows) {
+        const size_t prompt = aser_attention_prompt_workspace(b->tokens, b->n_seq, c->n_kv, group, c->head_dim, b->max_kv);
+        if (prompt > need) need = prompt;
+    }
+    return need + kAserWsTail;
 }
 
 extern "C" int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ldq, int32_t n_heads, const aser_kv_cache* cache,
@@ -365,25 +370,29 @@ extern "C" int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ld
     if (window < 0 || sinks < 0) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: negative window or sinks");
     if (!(scale - scale == 0.f)) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "paged_attention: scale is not finite");
     if (batch->tokens == 0 || batch->max_new == 0) return ASER_OK;
-    const Plan plan = plan_few(g.p.n_seq, g.p.n_kv, g.p.group, batch->max_new, keys_seen(batch->max_kv, batch->max_new, window, window > 0 ? sinks : 0));
+    const int64_t keys = keys_seen(batch->max_kv, batch->max_new, window, window > 0 ? sinks : 0), max_rows = (int64_t)batch->max_new * g.p.group;
+    const Plan plan = plan_few(g.p.n_seq, g.p.n_kv, g.p.group, batch->max_new, keys);
     g.q = q; g.ldq = ldq; g.out = out; g.ldo = ldo;
     g.c = scale * 1.4426950408889634f;
     g.window = window;
     g.sinks = window > 0 ? sinks : 0;
     g.few_rows = kFewRows;
     g.splits = plan.splits; g.tiles_per_split = plan.tiles_per_split; g.row_tiles = plan.row_tiles;
-    if ((int64_t)g.p.n_seq * g.row_tiles * g.p.n_kv > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: too many requests times rows");
-    size_t o_bytes;
-    const size_t need = few_workspace(plan, g.p.n_seq, g.p.n_kv, cache->head_dim, &o_bytes);
-    if (need > 0 && (!ctx->ws || ctx->ws_bytes < need + kAserWsTail)) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "paged_attention: workspace too small");
-    g.part_o = (float*)ctx->ws;
-    g.part_ml = (float2*)((char*)ctx->ws + o_bytes);
-    ASER_TRY(aser_prepare_device(ctx));
-    const int64_t max_rows = (int64_t)batch->max_new * g.p.group;
+    if ((int64_t)g.p.n_seq * g.row_tiles * g.p.n_kv > INT32_MAX || batch->tokens * g.p.group > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: too many requests times rows");
+    size_t o_bytes, need = few_workspace(plan, g.p.n_seq, g.p.n_kv, cache->head_dim, &o_bytes);
     if (max_rows > kFewRows) {
-        // a single request that has every row needs the other kernel only when it has few, which the host cannot see
-        ASER_TRY(aser_attention_prompt(ctx, g, cache->head_dim, max_rows, nullptr, 0));
+        const size_t prompt = aser_attention_prompt_workspace(g.p.tokens, g.p.n_seq, g.p.n_kv, g.p.group, cache->head_dim, keys);
+        if (prompt > need) need = prompt;
     }
+    if (need > 0 && (!ctx->ws || ctx->ws_bytes < need + kAserWsTail)) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "paged_attention: workspace too small");
+    ASER_TRY(aser_prepare_device(ctx));
+    if (max_rows > kFewRows) {
+        if (g.p.n_seq == 1) g.few_rows = -1;      // one request: the kernel for prompts takes it whatever it is
+        ASER_TRY(aser_attention_prompt(ctx, g, cache->head_dim, keys));
+        if (g.p.n_seq == 1) return ASER_OK;
+    }
+    g.part_o = (float*)ctx->ws;                   // the same memory: the launches follow each other
+    g.part_ml = (float2*)((char*)ctx->ws + o_bytes);
     if (cache->head_dim == 64) return run_few<64>(ctx, g, max_rows);
     if (cache->head_dim == 128) return run_few<128>(ctx, g, max_rows);
     return run_few<256>(ctx, g, max_rows);

@@ -30,16 +30,19 @@ __device__ __forceinline__ bf16x8_t lds_tr(const char* lo, const char* hi) {
 struct RowTile {
     int seq, tile;
     __device__ __forceinline__ RowTile(const AttnArgs& g, int u, int bm, int lane) {
-        int total = 0;
+        int total = 0, nt = 0;
         for (int pass = 0; pass < 2; ++pass) {
             int before = 0;
             seq = -1;
             for (int base = 0; base < g.p.n_seq; base += 64) {
-                int nt = 0;
-                if (base + lane < g.p.n_seq) {
+                if (pass == 1 && g.p.n_seq <= 64) {
+                    // up to 64 requests: the first pass has left them
+                } else if (base + lane < g.p.n_seq) {
                     int64_t first;
                     const int64_t rows = request_rows(g.p, base + lane, &first) * g.p.group;
                     nt = rows > g.few_rows ? (int)((rows + bm - 1) / bm) : 0;
+                } else {
+                    nt = 0;
                 }
                 int upto = nt;
 #pragma unroll
@@ -65,17 +68,20 @@ struct RowTile {
     }
 };
 
+// Stages of each of `splits` parts of a row tile's list.
+__device__ __forceinline__ int stages_per_split(int total, int splits) { return max((total + splits - 1) / splits, 1); }
+
 template <int D, bool I8, int RB, int W>
-__global__ __launch_bounds__(64 * W, W / 4) void attn_prompt_kernel(AttnArgs g) {
+__global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(AttnArgs g) {
     constexpr int KEYS = D == 256 ? 32 : 64, SUB = KEYS / 32, CH = D / 8, KS = D / 16, DB = D / 32;
-    constexpr int PITCH = 2 * D, HALF = KEYS * PITCH, STAGE = 2 * HALF, NST = 4, BM = 32 * RB * W;
+    constexpr int PITCH = 2 * D, HALF = KEYS * PITCH, STAGE = 2 * HALF, NST = 4, NSC = 8, BM = 32 * RB * W;
     constexpr int GR = KEYS / W;                  // keys that a wavefront stages, all on one page
     constexpr int LOADS = GR * CH / 64;           // 16-byte loads of a lane for them, of K and of V each
     static_assert(LOADS >= 1, "a wavefront stages at least one load");
     extern __shared__ __align__(16) char smem[];
-    int* sm_there = (int*)(smem + NST * STAGE);   // [stage][wave]: the page of its keys is there
-    float* sm_ks = (float*)(sm_there + NST * W);  // int8: [stage][key] scales of K, then of V
-    float* sm_vs = sm_ks + NST * KEYS;
+    int* sm_missing = (int*)(smem + NST * STAGE); // some page of these keys is not there
+    float* sm_ks = (float*)(sm_missing + 4);      // int8: [stage % NSC][key] scales of K, then of V
+    float* sm_vs = sm_ks + NSC * KEYS;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
     const int kvh = blockIdx.x % g.p.n_kv;
     const RowTile rt(g, blockIdx.x / g.p.n_kv, BM, lane);
@@ -86,7 +92,11 @@ __global__ __launch_bounds__(64 * W, W / 4) void attn_prompt_kernel(AttnArgs g) 
     const int first = __builtin_amdgcn_readfirstlane(rt.tile) * BM, base_pos = kv - count;
     const int p_lo = max(base_pos + first / group, 0), p_hi = base_pos + min(first + BM - 1, rows - 1) / group;
     const int low_all = g.window > 0 ? base_pos + first / group - g.window + 1 : 0;
+    // stages of the tile, and this workgroup's: t0 .. t0 + t1 - 1, numbered from 0 below
     const KeyTiles<KEYS> kt(p_lo, p_hi, g.window, g.sinks);
+    const int per_split = stages_per_split(kt.total, g.splits), t0 = blockIdx.y * per_split, t1 = min(kt.total - t0, per_split);
+    if (t1 <= 0 && blockIdx.y > 0) return;
+    auto first_key = [&](int i) -> int { return kt.first_key(t0 + i); };
 
     // rows of this wavefront
     const int wfirst = first + wave * 32 * RB;
@@ -121,69 +131,87 @@ __global__ __launch_bounds__(64 * W, W / 4) void attn_prompt_kernel(AttnArgs g) 
     }
 
     // staging: wavefront w has keys GR w .. of a stage; lane: row lane / CH (+ 64 / CH per load), slot lane % CH
-    const int* table = g.p.pages + s * g.p.ld_pages;
+    const ScalarInts table = scalar_ints(g.p.pages + s * g.p.ld_pages);
     const int page_mask = (1 << g.p.page_shift) - 1;
     const int64_t head_at = kvh * g.p.head_stride;
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * GR * PITCH;
     auto k_swizzle = [](int r) { return D == 64 ? (r >> 1) & 7 : r & 15; };
     auto v_swizzle = [](int r) { return D == 64 ? 4 * ((r >> 1) & 1) : 4 * (r & 3); };
+    // Where this wavefront's keys of a stage are, the same for all lanes; page_of(i) is asked for a step before it is needed.
+    struct Place { int64_t at; int key; bool there, all; };   // elements from the head's first; first key; all: the tile sees every one
     auto page_of = [&](int i) -> int {
-        const int key = kt.first_key(i) + GR * wave;
-        return i < kt.total && key < kv ? table[key >> g.p.page_shift] : -1;
+        const int key = first_key(i) + GR * wave;
+        return i < t1 && key < kv ? table[key >> g.p.page_shift] : -1;
     };
-    uint4 held[I8 ? LOADS : 1];                    // int8: codes on their way (one 16-byte load is two chunks of a row)
-    float held_scale = 0.f;
-    auto issue = [&](int i, int page) {            // stage i of the list into slot i % NST
-        const int st = i & (NST - 1), key0 = kt.first_key(i) + GR * wave;
-        const bool there = (uint32_t)page < (uint32_t)g.p.n_pages;
-        const int64_t at = (int64_t)(there ? page : 0) * g.p.page_stride + head_at + (int64_t)(key0 & page_mask) * g.p.slot_stride;
-        if (lane == 0) sm_there[st * W + wave] = there ? 1 : 0;
-        if constexpr (!I8) {
+    auto place_of = [&](int i, int page) -> Place {
+        Place x;
+        x.key = first_key(i) + GR * wave;
+        x.there = (uint32_t)page < (uint32_t)g.p.n_pages;
+        x.at = (int64_t)(x.there ? page : 0) * g.p.page_stride + (int64_t)((x.key & page_mask) * (uint32_t)g.p.slot_stride);
+        x.all = x.there && x.key + GR - 1 <= p_hi && (x.key >= low_all || x.key + GR <= g.sinks);
+        return x;
+    };
+    // what nobody of this tile sees is not looked at
+    auto wanted = [&](const Place& x, int r) -> bool { return x.there & (x.key + r <= p_hi) & ((x.key + r >= low_all) | (x.key + r < g.sinks)); };
+    uint32_t lane_off[2][LOADS];                   // bytes from a wavefront's first slot to the chunk that a lane copies
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+    for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int t = 0; t < LOADS; ++t) {
-                    const int r = t * (64 / CH) + lane / CH, slot = lane % CH, rr = GR * wave + r, key = key0 + r;
-                    const int chunk = slot ^ (half ? v_swizzle(rr) : k_swizzle(rr));
-                    const bool used = there & (key <= p_hi) & ((key >= low_all) | (key < g.sinks));
-                    const char* src = (const char*)((half ? (const uint16_t*)g.p.v : (const uint16_t*)g.p.k) + at + r * g.p.slot_stride + 8 * chunk);
-                    if (!used) src = (const char*)&g_zeros;
-                    const uint32_t dst = ring + st * STAGE + half * HALF + t * 1024;
-                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(dst), "v"(src) : "memory", "m0");
-                }
+        for (int t = 0; t < LOADS; ++t) {
+            const int r = t * (64 / CH) + lane / CH, rr = GR * wave + r;
+            lane_off[half][t] = 2 * (r * (uint32_t)g.p.slot_stride + 8 * ((lane % CH) ^ (half ? v_swizzle(rr) : k_swizzle(rr))));
+        }
+    const char* k_head = (const char*)((const uint16_t*)g.p.k + head_at);
+    const char* v_head = (const char*)((const uint16_t*)g.p.v + head_at);
+    // bf16: this wavefront's part of the keys (half 0) or values (half 1) of stage i, on its way into slot i % NST
+    auto copy = [&](int i, const Place& x, int half) {
+        const char* base = (half ? v_head : k_head) + 2 * x.at;
+        const uint32_t slot = ring + (i & (NST - 1)) * STAGE + half * HALF;
+        if (x.all) {
+#pragma unroll
+            for (int t = 0; t < LOADS; ++t)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                             : : "s"(slot + t * 1024), "v"(lane_off[half][t]), "s"(base) : "memory", "m0");
         } else {
-            // a lane takes 16 codes (two chunks) of row lane / (CH / 2): first the loads of K, then of V
 #pragma unroll
             for (int t = 0; t < LOADS; ++t) {
-                const int x = t * 64 + lane, half = x / (GR * CH / 2), y = x % (GR * CH / 2), r = y / (CH / 2), key = key0 + r;
-                const bool used = there & (key <= p_hi) & ((key >= low_all) | (key < g.sinks));
-                const int8_t* src = (half ? (const int8_t*)g.p.v : (const int8_t*)g.p.k) + at + r * g.p.slot_stride + 16 * (y % (CH / 2));
-                held[t] = make_uint4(0u, 0u, 0u, 0u);
-                if (used) held[t] = *(const uint4*)src;
-            }
-            if (lane < 2 * GR) {
-                const int r = lane % GR, key = key0 + r;
-                const bool used = there & (key <= p_hi) & ((key >= low_all) | (key < g.sinks));
-                const float* src = (lane < GR ? g.p.k_scale : g.p.v_scale) + (((int64_t)(there ? page : 0) * g.p.n_kv + kvh) << g.p.page_shift) + (key0 & page_mask) + r;
-                held_scale = used ? *src : 0.f;
+                const char* src = base + lane_off[half][t];
+                if (!wanted(x, t * (64 / CH) + lane / CH)) src = (const char*)&g_zeros;
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(slot + t * 1024), "v"(src) : "memory", "m0");
             }
         }
     };
-    auto land = [&](int i) {                       // int8: what issue(i) has fetched goes to LDS, widened
-        if constexpr (I8) {
-            const int st = i & (NST - 1);
-            char* dst = smem + st * STAGE + wave * GR * PITCH;
+    // int8: codes and scales of stage i into registers, and from there, widened, to LDS
+    uint4 held[I8 ? LOADS : 1];
+    float held_scale = 0.f;
+    auto fetch = [&](int i, int page) {
+        const Place x = place_of(i, page);
+        // a load is 16 codes (two chunks) of a row: first those of K, then those of V
 #pragma unroll
-            for (int t = 0; t < LOADS; ++t) {
-                const int x = t * 64 + lane, half = x / (GR * CH / 2), y = x % (GR * CH / 2), r = y / (CH / 2), ch = 2 * (y % (CH / 2)), rr = GR * wave + r;
-                const int sw = half ? v_swizzle(rr) : k_swizzle(rr);
-                char* row = dst + half * HALF + r * PITCH;
-                const uint4 w = held[t];
-                *(uint4*)(row + ((ch ^ sw) << 4)) = make_uint4(codes_pair<0>(w.x), codes_pair<2>(w.x), codes_pair<0>(w.y), codes_pair<2>(w.y));
-                *(uint4*)(row + (((ch + 1) ^ sw) << 4)) = make_uint4(codes_pair<0>(w.z), codes_pair<2>(w.z), codes_pair<0>(w.w), codes_pair<2>(w.w));
-            }
-            if (lane < 2 * GR) (lane < GR ? sm_ks : sm_vs)[st * KEYS + GR * wave + lane % GR] = held_scale;
+        for (int t = 0; t < LOADS; ++t) {
+            const int y = t * 64 + lane, half = y / (GR * CH / 2), z = y % (GR * CH / 2), r = z / (CH / 2);
+            const int8_t* src = (half ? (const int8_t*)g.p.v : (const int8_t*)g.p.k) + head_at + x.at + (int64_t)r * g.p.slot_stride + 16 * (z % (CH / 2));
+            held[t] = make_uint4(0u, 0u, 0u, 0u);
+            if (wanted(x, r)) held[t] = *(const uint4*)src;
         }
+        if (lane < 2 * GR) {
+            const int r = lane % GR;
+            const float* src = (lane < GR ? g.p.k_scale : g.p.v_scale) + (((int64_t)(x.there ? page : 0) * g.p.n_kv + kvh) << g.p.page_shift) + (x.key & page_mask) + r;
+            held_scale = wanted(x, r) ? *src : 0.f;
+        }
+    };
+    auto land = [&](int i) {
+        char* dst = smem + (i & (NST - 1)) * STAGE + wave * GR * PITCH;
+#pragma unroll
+        for (int t = 0; t < LOADS; ++t) {
+            const int x = t * 64 + lane, half = x / (GR * CH / 2), y = x % (GR * CH / 2), r = y / (CH / 2), ch = 2 * (y % (CH / 2)), rr = GR * wave + r;
+            const int sw = half ? v_swizzle(rr) : k_swizzle(rr);
+            char* row = dst + half * HALF + r * PITCH;
+            const uint4 w = held[t];
+            *(uint4*)(row + ((ch ^ sw) << 4)) = make_uint4(codes_pair<0>(w.x), codes_pair<2>(w.x), codes_pair<0>(w.y), codes_pair<2>(w.y));
+            *(uint4*)(row + (((ch + 1) ^ sw) << 4)) = make_uint4(codes_pair<0>(w.z), codes_pair<2>(w.z), codes_pair<0>(w.w), codes_pair<2>(w.w));
+        }
+        if (lane < 2 * GR) (lane < GR ? sm_ks : sm_vs)[(i & (NSC - 1)) * KEYS + GR * wave + lane % GR] = held_scale;
     };
 
     // operand offsets inside a stage
@@ -196,122 +224,118 @@ __global__ __launch_bounds__(64 * W, W / 4) void attn_prompt_kernel(AttnArgs g) 
         for (int d = 0; d < DB; ++d) v_off[d] = HALF + r * PITCH + (((4 * d + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) ^ v_swizzle(r)) << 4) + 8 * (i & 1);
     }
 
-    const int t0 = 0, t1 = kt.total;
-    int page_next = -1;
-    if constexpr (!I8) {
-#pragma unroll
-        for (int i = 0; i < NST - 1; ++i) {
-            const int page = page_of(t0 + i);
-            if (t0 + i < t1) issue(t0 + i, page);
-        }
-        page_next = page_of(t0 + NST - 1);
-    } else {
-        if (t0 < t1) { issue(t0, page_of(t0)); land(t0); }
-        if (t0 + 1 < t1) issue(t0 + 1, page_of(t0 + 1));
-        page_next = page_of(t0 + 2);
-    }
-    for (int i = t0; i < t1; ++i) {
-        if constexpr (!I8) {
-            // stages i + 1 and i + 2 may still be on their way
-            const int behind = min(t1 - 1 - i, NST - 2);
-            if (behind == 2) __builtin_amdgcn_s_waitcnt(0x0070 | (4 * LOADS & 15) | ((4 * LOADS >> 4) << 14));
-            else if (behind == 1) __builtin_amdgcn_s_waitcnt(0x0070 | (2 * LOADS & 15) | ((2 * LOADS >> 4) << 14));
-            else __builtin_amdgcn_s_waitcnt(0x0070);
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            if (i + NST - 1 < t1) {
-                issue(i + NST - 1, page_next);
-                page_next = page_of(i + NST);
-            }
-        } else {
-            __syncthreads();
-            if (i + 1 < t1) land(i + 1);
-            if (i + 2 < t1) {
-                issue(i + 2, page_next);
-                page_next = page_of(i + 3);
-            }
-        }
+    const int mine = idle ? 0 : max(min(kt.count_up_to(wp_hi) - t0, t1), 0);     // stages that this wavefront works on: those behind lie past its rows
+    bool missing = false;                          // some page that the tile may look at is not there
+    f32x16_t sc[SUB][RB];                          // logits of a stage, rows and keys as S^T has them
+    bf16x8_t pb[SUB][RB][2];                       // its probabilities
+    auto logits = [&](int i) {
         const char* stage = smem + (i & (NST - 1)) * STAGE;
-        const int st = i & (NST - 1);
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
-            const int key0 = kt.first_key(i) + 32 * u;
-            const int wlow = g.window > 0 ? wp_lo - g.window + 1 : 0;
-            if (idle || key0 > wp_hi || (key0 + 31 < wlow && key0 >= g.sinks)) continue;
-            f32x16_t st_acc[RB];
+            bf16x8_t kf[KS];
+#pragma unroll
+            for (int k = 0; k < KS; ++k) kf[k] = *(const bf16x8_t*)(stage + k_off[k] + u * 32 * PITCH);
 #pragma unroll
             for (int b = 0; b < RB; ++b)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) st_acc[b][e] = 0.f;
+                for (int e = 0; e < 16; ++e) sc[u][b][e] = 0.f;
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                const bf16x8_t kf = *(const bf16x8_t*)(stage + k_off[k] + u * 32 * PITCH);
+            for (int k = 0; k < KS; ++k)
 #pragma unroll
-                for (int b = 0; b < RB; ++b) st_acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[b][k], st_acc[b], 0, 0, 0);
-            }
-            if constexpr (I8) {
+                for (int b = 0; b < RB; ++b) sc[u][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], q[b][k], sc[u][b], 0, 0, 0);
+        }
+    };
+    auto softmax = [&](int i) {
+        const int key0 = first_key(i), fl = i & (NSC - 1);
+        if constexpr (I8) {
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
 #pragma unroll
                 for (int e4 = 0; e4 < 4; ++e4) {
-                    const f32x4_t ks = *(const f32x4_t*)(sm_ks + st * KEYS + 32 * u + 8 * e4 + 4 * h);
+                    const f32x4_t ks = *(const f32x4_t*)(sm_ks + fl * KEYS + 32 * u + 8 * e4 + 4 * h);
 #pragma unroll
                     for (int b = 0; b < RB; ++b)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) st_acc[b][4 * e4 + e] *= ks[e];
+                        for (int e = 0; e < 4; ++e) sc[u][b][4 * e4 + e] *= ks[e];
                 }
+        }
+        const bool plain = !missing && key0 + KEYS - 1 <= wp_lo && (g.window <= 0 || key0 >= wp_hi - g.window + 1 || key0 + KEYS <= g.sinks);
+        if (!plain) {
+            uint64_t pages_there = ~0ull;          // bit x: the page of key0 + x is there
+            if (missing) {
+                const int key = min(key0 + lane, kv - 1);
+                pages_there = __ballot((uint32_t)g.p.pages[s * g.p.ld_pages + (key >> g.p.page_shift)] < (uint32_t)g.p.n_pages);
             }
-            int there = 1;
+            int first = key0 + 4 * h;
+            asm volatile("" : "+v"(first));        // nothing of this rare piece is worth registers outside of it
 #pragma unroll
-            for (int x = 0; x < 32 / GR; ++x) there &= sm_there[st * W + u * (32 / GR) + x];
-            there = __builtin_amdgcn_readfirstlane(there);
-            const bool plain = there && key0 + 31 <= wp_lo && (g.window <= 0 || key0 >= wp_hi - g.window + 1 || key0 + 32 <= g.sinks);
-            if (!plain) {
+            for (int u = 0; u < SUB; ++u) {
+                const uint32_t there = (uint32_t)(pages_there >> (32 * u)) >> (4 * h);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int off = 8 * (e >> 2) + 4 * h + (e & 3), key = key0 + off;
-                    const bool page_there = sm_there[st * W + (32 * u + off) / GR] != 0;
+                    const int off = 8 * (e >> 2) + (e & 3), key = first + 32 * u + off;
 #pragma unroll
                     for (int b = 0; b < RB; ++b) {
-                        const bool seen = page_there & (key <= pos[b]) & ((key >= pos[b] - g.window + 1) | (key < g.sinks) | (g.window <= 0));
-                        st_acc[b][e] = seen ? st_acc[b][e] : -INFINITY;
+                        const bool seen = ((there >> off & 1) != 0) & (key <= pos[b]) & ((key >= pos[b] - g.window + 1) | (key < g.sinks) | (g.window <= 0));
+                        sc[u][b][e] = seen ? sc[u][b][e] : -INFINITY;
                     }
                 }
             }
-            bf16x8_t pb[RB][2];
+        }
+        bool higher = false;
+        float top[RB];
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            top[b] = sc[0][b][0];
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top[b] = fmaxf(top[b], sc[u][b][e]);
+            top[b] *= c;
+            higher |= top[b] > m[b] + 8.f;
+        }
+        // the maximum moves only when a logit is 8 above it: until then p <= 2^8, which neither fp32 sums nor bf16 mind
+        if (__ballot(higher)) {
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
-                float top = st_acc[b][0];
+                const float m_new = fmaxf(m[b], fmaxf(top[b], __shfl_xor(top[b], 32))), r = __builtin_amdgcn_exp2f(m[b] - m_new);
+                m[b] = m_new;
+                l[b] *= r;
 #pragma unroll
-                for (int e = 1; e < 16; ++e) top = fmaxf(top, st_acc[b][e]);
-                top *= c;
-                // the maximum moves only when a logit is 8 above it: until then p <= 2^8, which neither fp32 sums nor bf16 mind
-                if (__ballot(top > m[b] + 8.f)) {
-                    top = fmaxf(top, __shfl_xor(top, 32));
-                    const float m_new = fmaxf(m[b], top), r = __builtin_amdgcn_exp2f(m[b] - m_new);
-                    m[b] = m_new;
-                    l[b] *= r;
+                for (int d = 0; d < DB; ++d) o[b][d] *= r;
+            }
+        }
 #pragma unroll
-                    for (int d = 0; d < DB; ++d) o[b][d] *= r;
-                }
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
                 float p[16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    p[e] = __builtin_amdgcn_exp2f(fmaf(st_acc[b][e], c, -m[b]));
-                    l[b] += p[e];
-                }
+                for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sc[u][b][e], c, -m[b]));
+                uint32_t w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = bf16_pair(p[2 * e], p[2 * e + 1]);
+                float sum[2] = {0.f, 0.f};
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum[e & 1] += p[e];
+                l[b] += sum[0] + sum[1];
                 if constexpr (I8) {
 #pragma unroll
                     for (int e4 = 0; e4 < 4; ++e4) {
-                        const f32x4_t vs = *(const f32x4_t*)(sm_vs + st * KEYS + 32 * u + 8 * e4 + 4 * h);
+                        const f32x4_t vs = *(const f32x4_t*)(sm_vs + fl * KEYS + 32 * u + 8 * e4 + 4 * h);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) p[4 * e4 + e] *= vs[e];
+                        for (int e = 0; e < 4; e += 2) w[2 * e4 + e / 2] = bf16_pair(p[4 * e4 + e] * vs[e], p[4 * e4 + e + 1] * vs[e + 1]);
                     }
                 }
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    pb[b][x] = __builtin_bit_cast(bf16x8_t, make_uint4(bf16_pair(p[8 * x], p[8 * x + 1]), bf16_pair(p[8 * x + 2], p[8 * x + 3]),
-                                                                       bf16_pair(p[8 * x + 4], p[8 * x + 5]), bf16_pair(p[8 * x + 6], p[8 * x + 7])));
+                for (int x = 0; x < 2; ++x) pb[u][b][x] = __builtin_bit_cast(bf16x8_t, make_uint4(w[4 * x], w[4 * x + 1], w[4 * x + 2], w[4 * x + 3]));
             }
+        __builtin_amdgcn_sched_barrier(0);         // all of it in this phase
+    };
+    auto outputs = [&](int i) {
+        const char* stage = smem + (i & (NST - 1)) * STAGE;
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -319,43 +343,246 @@ __global__ __launch_bounds__(64 * W, W / 4) void attn_prompt_kernel(AttnArgs g) 
                     const char* v = stage + v_off[d] + (32 * u + 16 * x) * PITCH;
                     const bf16x8_t vf = lds_tr(v, v + 8 * PITCH);
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) o[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[b][x], o[b][d], 0, 0, 0);
+                    for (int b = 0; b < RB; ++b) o[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[u][b][x], o[b][d], 0, 0, 0);
                 }
+    };
+    // outputs(i) and logits(i + 1) in one piece.  Nothing but the order of instructions hides the latency of the LDS reads here, so it is
+    // laid down: four instructions at a time, the operands of those two groups further on asked for before them.
+    auto products = [&](int i) {
+        const char* stage = smem + (i & (NST - 1)) * STAGE;
+        const char* next = smem + ((i + 1) & (NST - 1)) * STAGE;
+        constexpr int PV = 2 * SUB * DB, ALL = PV + KS * SUB;
+        static_assert(PV % 4 == 0 && ALL % 4 == 0, "groups of four");
+        bf16x8_t fr[3][4];
+        auto ask = [&](int n, bf16x8_t& f) {
+            if (n < PV) {
+                const char* v = stage + v_off[n % DB] + 16 * (n / DB) * PITCH;
+                f = lds_tr(v, v + 8 * PITCH);
+            } else {
+                f = *(const bf16x8_t*)(next + k_off[(n - PV) / SUB] + (n - PV) % SUB * 32 * PITCH);
+            }
+        };
+        auto multiply = [&](int n, const bf16x8_t& f) {
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                if (n < PV) {
+                    o[b][n % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pb[n / DB / 2][b][n / DB % 2], o[b][n % DB], 0, 0, 0);
+                } else {
+                    const int k = (n - PV) / SUB, u = (n - PV) % SUB;
+                    f32x16_t zero = {};
+                    sc[u][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[b][k], k ? sc[u][b] : zero, 0, 0, 0);
+                }
+            }
+        };
+#pragma unroll
+        for (int n = 0; n < 8; ++n) ask(n, fr[n / 4][n % 4]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < ALL / 4; ++j) {
+#pragma unroll
+            for (int n = 4 * (j + 2); n < 4 * (j + 3) && n < ALL; ++n) ask(n, fr[(j + 2) % 3][n % 4]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = 4 * j; n < 4 * j + 4; ++n) multiply(n, fr[j % 3][n % 4]);
+            __builtin_amdgcn_sched_barrier(0);
         }
+    };
+    // Waits for this wavefront's LDS accesses and all its copies but those of the last step, then for the others.  `more`: those have all theirs.
+    auto meet = [&](bool copies, bool more) {
+        if (I8 || !copies) __builtin_amdgcn_s_waitcnt(0xC07F);                                                     // lgkmcnt(0)
+        else if (more) __builtin_amdgcn_s_waitcnt(0x0070 | (2 * LOADS & 15) | ((2 * LOADS >> 4) << 14));
+        else __builtin_amdgcn_s_waitcnt(0x0070);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    // Step i: copies of the keys of stage i + 3 and the values of stage i + 2 begun, into slots that were read last in step i - 1; softmax of stage
+    // i; products P V of stage i and K Q of stage i + 1; copies begun in step i - 1 waited for; barrier.  int8: stage i + 2 lands and
+    // i + 3 is fetched with the products.  LAG: the two halves of a workgroup, one wavefront of each on a SIMD, work half a step apart, with
+    // a barrier after the softmax too, so that one is at the vector unit while the other is at the matrix unit (128 channels: 549 -> 518 us; with
+    // 64 channels the vector unit has more to do than the matrix unit and the second barrier costs more than it gives: 110 -> 133).
+    constexpr bool LAG = W == 8 && D == 128;
+    const bool behind = LAG && wave >= 4;
+    int page_k;
+    Place place_v;
+    if constexpr (!I8) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            const Place x = place_of(i, page_of(i));
+            if (i < t1) copy(i, x, 0);
+            if (i > 0 && i - 1 < t1) copy(i - 1, place_v, 1);
+            place_v = x;
+        }
+    } else {
+        if (t1 > 0) { fetch(0, page_of(0)); land(0); }
+        if (t1 > 1) { fetch(1, page_of(1)); land(1); }
+        if (t1 > 2) fetch(2, page_of(2));
     }
+    page_k = page_of(3);
+    {
+        const int shift = g.p.page_shift, sink_pages = g.window > 0 ? (min(g.sinks, p_hi + 1) + page_mask) >> shift : 0;
+        const int last = p_hi < 0 ? -1 : min(p_hi, kv - 1) >> shift;
+        for (int x = tid; x <= last; x += 64 * W)
+            if (x < sink_pages || x >= max(low_all, 0) >> shift) missing |= (uint32_t)g.p.pages[s * g.p.ld_pages + x] >= (uint32_t)g.p.n_pages;
+        if (tid == 0) *sm_missing = 0;
+        __syncthreads();
+        if (missing) *sm_missing = 1;
+        if constexpr (!I8) meet(true, t1 > 2);
+        else meet(false, false);
+        missing = __builtin_amdgcn_readfirstlane(*sm_missing) != 0;
+    }
+    if (mine > 0) logits(0);
+    if (behind) meet(false, false);
+    auto begin = [&](int i) {
+        if constexpr (!I8) {
+            const Place x = place_of(i + 3, page_k);
+            if (i + 3 < t1) copy(i + 3, x, 0);
+            if (i + 2 < t1) copy(i + 2, place_v, 1);
+            place_v = x;
+            page_k = page_of(i + 4);
+        }
+    };
+    auto between = [&](int i) {
+        if constexpr (LAG) meet(false, false);
+        if constexpr (I8) {
+            if (i + 2 < t1) land(i + 2);
+            if (i + 3 < t1) fetch(i + 3, page_k);
+            page_k = page_of(i + 4);
+        }
+    };
+    int i = 0;
+    for (; i < mine - 1; ++i) {
+        begin(i);
+        softmax(i);
+        between(i);
+        __builtin_amdgcn_s_setprio(1);
+        products(i);
+        __builtin_amdgcn_s_setprio(0);
+        meet(true, i + 3 < t1);
+    }
+    if (i < mine) {
+        begin(i);
+        softmax(i);
+        between(i);
+        outputs(i);
+        meet(true, i + 3 < t1);
+        ++i;
+    }
+    for (; i < t1; ++i) {
+        begin(i);
+        between(i);
+        meet(true, i + 3 < t1);
+    }
+    if (LAG && !behind) meet(false, false);
+    const bool whole = per_split >= kt.total;
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
         const int r = wfirst + 32 * b + col;
         l[b] += __shfl_xor(l[b], 32);
         if (r >= rows) continue;
-        const float inv = l[b] > 0.f ? 1.f / l[b] : 0.f;
-        uint16_t* dst = g.out + (row0 + r / group) * g.ldo + (int64_t)(kvh * group + r % group) * D + 4 * h;
+        if (whole) {
+            const float inv = l[b] > 0.f ? 1.f / l[b] : 0.f;
+            uint16_t* dst = g.out + (row0 + r / group) * g.ldo + (int64_t)(kvh * group + r % group) * D + 4 * h;
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+            for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int e = 0; e < 16; e += 4)
-                *(uint2*)(dst + 32 * d + 2 * e) = make_uint2(bf16_pair(o[b][d][e] * inv, o[b][d][e + 1] * inv), bf16_pair(o[b][d][e + 2] * inv, o[b][d][e + 3] * inv));
+                for (int e = 0; e < 16; e += 4)
+                    *(uint2*)(dst + 32 * d + 2 * e) = make_uint2(bf16_pair(o[b][d][e] * inv, o[b][d][e + 1] * inv), bf16_pair(o[b][d][e + 2] * inv, o[b][d][e + 3] * inv));
+        } else {
+            const int64_t pr = ((int64_t)blockIdx.x * g.splits + blockIdx.y) * BM + (r - first);
+            if (h == 0) g.part_ml[pr] = make_float2(m[b], l[b]);
+            float* dst = g.part_o + pr * D + 4 * h;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) *(f32x4_t*)(dst + 32 * d + 2 * e) = (f32x4_t){o[b][d][e], o[b][d][e + 1], o[b][d][e + 2], o[b][d][e + 3]};
+        }
     }
 }
 
-template <int D, bool I8, int RB, int W>
-int launch_prompt(aser_ctx* ctx, const AttnArgs& g) {
-    constexpr int KEYS = D == 256 ? 32 : 64, BM = 32 * RB * W;
-    constexpr size_t lds = 4 * (2 * KEYS * 2 * D) + 4 * W * 4 + (I8 ? 4 * KEYS * 8 : 0);
-    const int64_t tiles = ceil_div64(g.p.tokens * g.p.group, BM) + g.p.n_seq;
-    if (tiles * g.p.n_kv > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: too many rows");
-    auto kernel = attn_prompt_kernel<D, I8, RB, W>;
+// Joins the splits of a row tile: o = sum_s w_s o_s / sum_s w_s l_s, w_s = exp2(m_s - max m); four channels of a row per thread.
+template <int D, int BM, int KEYS>
+__global__ __launch_bounds__(256) void attn_prompt_join_kernel(AttnArgs g) {
+    constexpr int CL = D / 4, R = 256 / CL;
+    const int tid = threadIdx.x, c = tid % CL * 4, in_tile = blockIdx.y * R + tid / CL;
+    const int kvh = blockIdx.x % g.p.n_kv;
+    const RowTile rt(g, blockIdx.x / g.p.n_kv, BM, tid & 63);
+    const int s = __builtin_amdgcn_readfirstlane(rt.seq);
+    if (s < 0) return;
+    int64_t row0;
+    const int count = (int)request_rows(g.p, s, &row0), kv = request_kv_len(g.p, s), rows = count * g.p.group, group = g.p.group;
+    const int first = __builtin_amdgcn_readfirstlane(rt.tile) * BM, base_pos = kv - count, r = first + in_tile;
+    const KeyTiles<KEYS> kt(max(base_pos + first / group, 0), base_pos + min(first + BM - 1, rows - 1) / group, g.window, g.sinks);
+    const int per = stages_per_split(kt.total, g.splits);
+    if (per >= kt.total || r >= rows) return;
+    const int used = (kt.total + per - 1) / per;
+    const int64_t pr = (int64_t)blockIdx.x * g.splits * BM + in_tile;
+    float top = kNone;
+    for (int i = 0; i < used; ++i) top = fmaxf(top, g.part_ml[pr + (int64_t)i * BM].x);
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < used; ++i) {
+        const float2 ml = g.part_ml[pr + (int64_t)i * BM];
+        const float w = __builtin_amdgcn_exp2f(ml.x - top);
+        l += w * ml.y;
+        acc += *(const f32x4_t*)(g.part_o + (pr + (int64_t)i * BM) * D + c) * w;
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    uint16_t* dst = g.out + (row0 + r / group) * g.ldo + (int64_t)(kvh * group + r % group) * D + c;
+    *(uint2*)dst = make_uint2(bf16_pair(acc[0] * inv, acc[1] * inv), bf16_pair(acc[2] * inv, acc[3] * inv));
+}
+
+// Sizes of a launch.  A workgroup per compute unit (two with 64 channels) is what the device holds; when the row tiles are fewer than half of that, the
+// keys are split, 6 stages at least to a workgroup, and the parts joined by a second launch.
+struct PromptPlan { int64_t tiles; int splits, bm; size_t o_bytes, bytes; };
+
+PromptPlan plan_prompt(int64_t tokens, int64_t n_seq, int64_t n_kv, int64_t group, int head_dim, int64_t keys) {
+    PromptPlan p;
+    p.bm = head_dim == 128 ? 256 : 128;
+    p.tiles = ceil_div64(tokens * group, p.bm) + n_seq;
+    const int64_t stages = keys / (head_dim == 256 ? 32 : 64) + 2, full = head_dim == 64 ? 512 : 256;
+    int64_t splits = full / (p.tiles * n_kv);
+    if (splits > stages / 6) splits = stages / 6;
+    if (splits < 1) splits = 1;
+    p.splits = (int)splits;
+    const size_t rows = splits > 1 ? (size_t)(p.tiles * n_kv) * p.splits * p.bm : 0;
+    p.o_bytes = align_up(rows * head_dim * 4, 256);
+    p.bytes = p.o_bytes + align_up(rows * 8, 256);
+    return p;
+}
+
+template <int D, bool I8, int W>
+int launch_prompt(aser_ctx* ctx, const AttnArgs& g, const PromptPlan& p) {
+    constexpr int KEYS = D == 256 ? 32 : 64, BM = 32 * W, CL = D / 4;
+    constexpr size_t lds = 4 * (2 * KEYS * 2 * D) + 16 + (I8 ? 8 * KEYS * 8 : 0);
+    if (p.tiles * g.p.n_kv > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: too many rows");
+    const unsigned blocks = (unsigned)(p.tiles * g.p.n_kv);
+    auto kernel = attn_prompt_kernel<D, I8, 1, W>;
     ASER_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    kernel<<<dim3((unsigned)(tiles * g.p.n_kv)), 64 * W, lds, ctx->stream>>>(g);
-    return aser_check_launch(ctx, "attn_prompt_kernel");
+    kernel<<<dim3(blocks, (unsigned)p.splits), 64 * W, lds, ctx->stream>>>(g);
+    ASER_TRY(aser_check_launch(ctx, "attn_prompt_kernel"));
+    if (p.splits > 1) {
+        attn_prompt_join_kernel<D, BM, KEYS><<<dim3(blocks, BM / (256 / CL)), 256, 0, ctx->stream>>>(g);
+        return aser_check_launch(ctx, "attn_prompt_join_kernel");
+    }
+    return ASER_OK;
 }
 
 }  // namespace
 
-int aser_attention_prompt(aser_ctx* ctx, AttnArgs g, int head_dim, int64_t max_rows, float* part, size_t part_bytes) {
+size_t aser_attention_prompt_workspace(int64_t tokens, int64_t n_seq, int64_t n_kv, int64_t group, int head_dim, int64_t keys) {
+    return plan_prompt(tokens, n_seq, n_kv, group, head_dim, keys).bytes;
+}
+
+int aser_attention_prompt(aser_ctx* ctx, AttnArgs g, int head_dim, int64_t keys) {
     const bool i8 = g.p.k_scale != nullptr;
-    (void)max_rows; (void)part; (void)part_bytes;
-    if (head_dim == 64) return i8 ? launch_prompt<64, true, 1, 8>(ctx, g) : launch_prompt<64, false, 1, 8>(ctx, g);
-    if (head_dim == 128) return i8 ? launch_prompt<128, true, 1, 8>(ctx, g) : launch_prompt<128, false, 1, 8>(ctx, g);
-    return i8 ? launch_prompt<256, true, 1, 4>(ctx, g) : launch_prompt<256, false, 1, 4>(ctx, g);
+    const PromptPlan p = plan_prompt(g.p.tokens, g.p.n_seq, g.p.n_kv, g.p.group, head_dim, keys);
+    g.splits = p.splits;
+    g.part_o = (float*)ctx->ws;
+    g.part_ml = (float2*)((char*)ctx->ws + p.o_bytes);
+    if (head_dim == 64) return i8 ? launch_prompt<64, true, 4>(ctx, g, p) : launch_prompt<64, false, 4>(ctx, g, p);
+    if (head_dim == 128) return i8 ? launch_prompt<128, true, 8>(ctx, g, p) : launch_prompt<128, false, 8>(ctx, g, p);
+    return i8 ? launch_prompt<256, true, 4>(ctx, g, p) : launch_prompt<256, false, 4>(ctx, g, p);
 }
