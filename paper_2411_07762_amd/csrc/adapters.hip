@@ -171,9 +171,10 @@ template <int RT, bool F32, bool VEC, int NT>
 __global__ __launch_bounds__(256) void adapter_down_kernel(AdArgs g) {
     __shared__ f32x4_t sm[3][NT][RT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
-    const TileRows<NT> tr(g, blockIdx.x, lane);
+    const int part = blockIdx.x % g.parts;
+    const TileRows<NT> tr(g, blockIdx.x / g.parts, lane);
     if (tr.adapter < 0) return;
-    const int64_t c0 = blockIdx.y * g.part_n, c1 = c0 + g.part_n < g.n ? c0 + g.part_n : g.n;
+    const int64_t c0 = part * g.part_n, c1 = c0 + g.part_n < g.n ? c0 + g.part_n : g.n;
     const uint16_t* a_row = g.A + (int64_t)tr.adapter * g.r * g.n;
     f32x4_t acc[NT][RT];
 #pragma unroll
@@ -214,7 +215,7 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdArgs g) {
 #pragma unroll
     for (int x = 0; x < NT; ++x) {
         if (tr.row[x] < 0) continue;
-        float* dst = g.P + ((int64_t)blockIdx.y * g.rows + tr.row[x]) * g.rp;
+        float* dst = g.P + ((int64_t)part * g.rows + tr.row[x]) * g.rp;
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             f32x4_t v = acc[x][i];
@@ -225,11 +226,16 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdArgs g) {
     }
 }
 
-// Y = Y0 + s P B^T: a wavefront has LOOP times 64 outputs, four times that far apart from each other.  aligned: four outputs at a time.
+// Y = Y0 + s P B^T: a wavefront has LOOP times 64 outputs, four times that far apart from each other.  The accumulators go through LDS, so
+// that Y0 and Y are read and written 256 bytes of a row at a time.  aligned: rows of both start on 16-byte boundaries.
 template <int KS, bool VEC, int NT, int LOOP>
-__global__ __launch_bounds__(256) void adapter_up_kernel(AdArgs g, bool aligned) {
+__global__ __launch_bounds__(256, NT > 1 ? 3 : 4) void adapter_up_kernel(AdArgs g, bool aligned) {
+    constexpr int ROWS = 16 * NT, PITCH = 68;      // floats of a row in LDS
+    constexpr int SUMS = 4 * NT * KS * 2 * 64 * 4, TURN = 4 * ROWS * PITCH;
+    __shared__ __align__(16) float sm[SUMS > TURN ? SUMS : TURN];
+    const int blocks = (int)((g.m + 256 * LOOP - 1) / (256 * LOOP)), block = blockIdx.x % blocks;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
-    const TileRows<NT> tr(g, blockIdx.x, lane);
+    const TileRows<NT> tr(g, blockIdx.x / blocks, lane);
     if (tr.adapter == -2 || (tr.adapter == -1 && g.Y0 == g.Y)) return;
     const bool some = tr.adapter >= 0;
     bf16x8_t t[NT][KS][3];
@@ -237,83 +243,100 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdArgs g, bool aligned)
     if (some) {
         const float s = g.scale ? g.scale[tr.adapter] : 1.f;
         b += (int64_t)tr.adapter * g.m * g.r;
+        f32x4_t* sums = (f32x4_t*)sm;              // [wave][NT][KS][2][lane]
+        // a wavefront adds every fourth part, the four sums meet
 #pragma unroll
         for (int x = 0; x < NT; ++x)
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 const int at = 32 * k + 8 * grp;
-                float p[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) p[j] = 0.f;
+                f32x4_t u = {0.f, 0.f, 0.f, 0.f}, v = u;
                 if (tr.row[x] >= 0 && at < g.rp) {
-                    const float* src = g.P + (int64_t)tr.row[x] * g.rp + at;
 #pragma unroll 4
-                    for (int part = 0; part < g.parts; ++part, src += g.rows * g.rp) {
-                        const float4 u = *(const float4*)src, v = *(const float4*)(src + 4);
-                        p[0] += u.x; p[1] += u.y; p[2] += u.z; p[3] += u.w;
-                        p[4] += v.x; p[5] += v.y; p[6] += v.z; p[7] += v.w;
+                    for (int part = wave; part < g.parts; part += 4) {
+                        const float* src = g.P + ((int64_t)part * g.rows + tr.row[x]) * g.rp + at;
+                        u += *(const f32x4_t*)src;
+                        v += *(const f32x4_t*)(src + 4);
                     }
                 }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) p[j] *= s;
-                three_terms(p, t[x][k]);
+                sums[(((wave * NT + x) * KS + k) * 2) * 64 + lane] = u;
+                sums[(((wave * NT + x) * KS + k) * 2 + 1) * 64 + lane] = v;
             }
-    }
-    for (int loop = 0; loop < LOOP; ++loop) {
-        const int64_t o0 = ((int64_t)blockIdx.y * LOOP + loop) * 256 + wave * 64;
-        if (o0 >= g.m) return;
-        f32x4_t acc[NT][4];
+        __syncthreads();
 #pragma unroll
         for (int x = 0; x < NT; ++x)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                acc[x][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-                const int64_t o = o0 + 16 * i + 4 * grp;
-                if (g.Y0 && tr.row[x] >= 0) {
-                    const float* y0 = g.Y0 + (int64_t)tr.row[x] * g.ldy0 + o;
-                    if (aligned && o + 4 <= g.m) acc[x][i] = *(const f32x4_t*)y0;
-                    else {
+            for (int k = 0; k < KS; ++k) {
+                f32x4_t w[2];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (o + e < g.m) acc[x][i][e] = y0[e];
-                    }
+                for (int j = 0; j < 2; ++j) {
+                    const f32x4_t* at = sums + ((x * KS + k) * 2 + j) * 64 + lane;
+                    constexpr int NEXT = NT * KS * 2 * 64;
+                    w[j] = (at[0] + at[NEXT]) + (at[2 * NEXT] + at[3 * NEXT]);
                 }
+                float p[8] = {w[0][0] * s, w[0][1] * s, w[0][2] * s, w[0][3] * s, w[1][0] * s, w[1][1] * s, w[1][2] * s, w[1][3] * s};
+                three_terms(p, t[x][k]);
             }
-        if (some) {
-            f32x4_t sum[NT][4];
+        __syncthreads();                           // before the turns below overwrite the sums
+    }
+    // this lane's rows and outputs at the turn: rows 4 j + grp, four outputs from 4 col on
+    int out_row[4 * NT];
 #pragma unroll
-            for (int x = 0; x < NT; ++x)
+    for (int j = 0; j < 4 * NT; ++j) out_row[j] = __shfl(tr.row[j / 4], 4 * (j % 4) + grp);
+    float* turn = sm + wave * ROWS * PITCH;
+    for (int loop = 0; loop < LOOP; ++loop) {
+        const int64_t o0 = ((int64_t)block * LOOP + loop) * 256 + wave * 64;
+        if (o0 >= g.m) return;
+        const int64_t o = o0 + 4 * col;
+        const bool four = aligned && o + 4 <= g.m;
+        f32x4_t y[4 * NT];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[x][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < KS; ++k)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int64_t o = o0 + 16 * i + col;
-                    const bf16x8_t w = row8<VEC>(b + o * g.r, 32 * k + 8 * grp, g.r, o < g.m);
-#pragma unroll
-                    for (int x = 0; x < NT; ++x)
-#pragma unroll
-                        for (int e = 2; e >= 0; --e) sum[x][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, t[x][k][e], sum[x][i], 0, 0, 0);
-                }
-#pragma unroll
-            for (int x = 0; x < NT; ++x)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[x][i] += sum[x][i];
-        }
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            if (tr.row[x] < 0) continue;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t o = o0 + 16 * i + 4 * grp;
-                float* y = g.Y + (int64_t)tr.row[x] * g.ldy + o;
-                if (aligned && o + 4 <= g.m) *(f32x4_t*)y = acc[x][i];
+        for (int j = 0; j < 4 * NT; ++j) {
+            y[j] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+            if (g.Y0 && out_row[j] >= 0) {
+                const float* y0 = g.Y0 + (int64_t)out_row[j] * g.ldy0 + o;
+                if (four) y[j] = __builtin_nontemporal_load((const f32x4_t*)y0);
                 else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (o + e < g.m) y[e] = acc[x][i][e];
+                        if (o + e < g.m) y[j][e] = y0[e];
                 }
+            }
+        }
+        if (some) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                f32x4_t acc[NT];
+#pragma unroll
+                for (int x = 0; x < NT; ++x) acc[x] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+                const int64_t row = o0 + 16 * i + col;
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    const bf16x8_t w = row8<VEC>(b + row * g.r, 32 * k + 8 * grp, g.r, row < g.m);
+#pragma unroll
+                    for (int x = 0; x < NT; ++x)
+#pragma unroll
+                        for (int e = 2; e >= 0; --e) acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, t[x][k][e], acc[x], 0, 0, 0);
+                }
+#pragma unroll
+                for (int x = 0; x < NT; ++x) *(f32x4_t*)(turn + (16 * x + col) * PITCH + 16 * i + 4 * grp) = acc[x];
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int j = 0; j < 4 * NT; ++j) y[j] += *(const f32x4_t*)(turn + (4 * j + grp) * PITCH + 4 * col);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+#pragma unroll
+        for (int j = 0; j < 4 * NT; ++j) {
+            if (out_row[j] < 0) continue;
+            float* dst = g.Y + (int64_t)out_row[j] * g.ldy + o;
+            if (four) *(f32x4_t*)dst = y[j];
+            else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (o + e < g.m) dst[e] = y[j][e];
             }
         }
     }
@@ -362,8 +385,8 @@ void launch_up(const AdArgs& g, bool vec, bool aligned, dim3 grid, hipStream_t s
     else adapter_up_kernel<KS, false, NT, LOOP><<<grid, 256, 0, st>>>(g, aligned);
 }
 template <int NT, int LOOP>
-void launch_ups(const AdArgs& g, bool vec, bool aligned, unsigned tiles, hipStream_t st) {
-    const dim3 grid(tiles, (unsigned)ceil_div64(g.m, 256 * LOOP));
+void launch_ups(const AdArgs& g, bool vec, bool aligned, int64_t tiles, hipStream_t st) {
+    const dim3 grid((unsigned)(tiles * ceil_div64(g.m, 256 * LOOP)));
     if (g.r <= 32) launch_up<1, NT, LOOP>(g, vec, aligned, grid, st);
     else if (g.r <= 64) launch_up<2, NT, LOOP>(g, vec, aligned, grid, st);
     else launch_up<4, NT, LOOP>(g, vec, aligned, grid, st);
@@ -407,11 +430,12 @@ extern "C" int aser_adapter_forward(aser_ctx* ctx, const void* X, int x_dtype, i
     const bool vec_a = n % 8 == 0 && ((uintptr_t)A & 15) == 0 && ((uintptr_t)X & 15) == 0 && (ldx & xw) == 0;
     const bool vec_b = r % 8 == 0 && ((uintptr_t)B & 15) == 0;
     const bool aligned = (ldy & 3) == 0 && ((uintptr_t)Y & 15) == 0 && (!Y0 || ((ldy0 & 3) == 0 && ((uintptr_t)Y0 & 15) == 0));
-    const dim3 down((unsigned)tiles, (unsigned)p.parts);
+    if (tiles * ceil_div64(m, 256) > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "adapter_forward: too many rows times outputs");
+    const dim3 down((unsigned)(tiles * (int64_t)p.parts));       // neighbours read the same rows: consecutive memory, whatever the rows' distance
     if (rows > kFewRows) launch_downs<kManyTiles>(g, f32, vec_a, down, ctx->stream);
     else launch_downs<1>(g, f32, vec_a, down, ctx->stream);
     ASER_TRY(aser_check_launch(ctx, "adapter_down_kernel"));
-    if (rows > kFewRows) launch_ups<kManyTiles, kLoop>(g, vec_b, aligned, (unsigned)tiles, ctx->stream);
-    else launch_ups<1, 1>(g, vec_b, aligned, (unsigned)tiles, ctx->stream);
+    if (rows > kFewRows) launch_ups<kManyTiles, kLoop>(g, vec_b, aligned, tiles, ctx->stream);
+    else launch_ups<1, 1>(g, vec_b, aligned, tiles, ctx->stream);
     return aser_check_launch(ctx, "adapter_up_kernel");
 }

@@ -50,11 +50,11 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void attn_few_kernel(AttnArg
     const int low_all = g.window > 0 ? kv - count + rt * 16 / g.p.group - g.window + 1 : 0;   // the same for the tile's first row
     const int my_low = g.window > 0 ? my_pos - g.window + 1 : 0;             // keys below are seen up to sinks only
 
-    // the row's query: B operand of K Q^T, channels 32 step + 8 grp ..
+    // the row's query: B operand of K Q^T, channels 32 step + 8 grp ..; int8: 64 (step / 2) + 16 grp + 8 (step % 2) .., so that a load is 16 codes
     bf16x8_t q[KS];
     const int64_t q_at = (row0 + my_tok) * g.ldq + (int64_t)(kvh * g.p.group + my_head) * D;
 #pragma unroll
-    for (int k = 0; k < KS; ++k) q[k] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(g.q + q_at + 32 * k + 8 * grp));
+    for (int k = 0; k < KS; ++k) q[k] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(g.q + q_at + (I8 ? 64 * (k / 2) + 16 * grp + 8 * (k % 2) : 32 * k + 8 * grp)));
 
     f32x4_t o[NB];
 #pragma unroll
@@ -63,9 +63,12 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void attn_few_kernel(AttnArg
     const ScalarInts table = scalar_ints(g.p.pages + s * g.p.ld_pages);
     const int page_mask = (1 << g.p.page_shift) - 1;
     // a lane's offsets in bytes inside 16 slots; everything else of an address is the same for the wavefront
-    constexpr int ES = I8 ? 1 : 2, KW = I8 ? 2 : 4, VW = I8 ? NB / 4 : NB / 2;         // bytes of an element; words of a load
+    constexpr int ES = I8 ? 1 : 2, KL = I8 ? D / 64 : KS;                    // bytes of an element; 16-byte loads of K for 16 keys
+    constexpr int VW = I8 ? NB / 4 : NB / 2;                                 // words of a lane's channels of a key
+    constexpr int VK = I8 && D < 256 ? 256 / D : 1;                          // int8: keys that 16 lanes cover with 16-byte loads of V
     const uint32_t pitch = (uint32_t)g.p.slot_stride * ES;
-    const uint32_t k_off = n * pitch + 8 * grp * ES, v_off = 4 * grp * pitch + NB * n * ES;
+    const uint32_t k_off = n * pitch + 16 * grp;
+    const uint32_t v_off = VK > 1 ? (4 * grp + n / (16 / VK)) * pitch + 16 * (n % (16 / VK)) : 4 * grp * pitch + NB * n * ES;
     const int64_t page_bytes = g.p.page_stride * ES;
     const char* k_head = (const char*)g.p.k + kvh * g.p.head_stride * ES;
     const char* v_head = (const char*)g.p.v + kvh * g.p.head_stride * ES;
@@ -73,7 +76,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void attn_few_kernel(AttnArg
     // A step's keys and values.  Enough of them are on their way because 16 wavefronts of a compute unit do this; fetching a step ahead instead
     // takes the registers of half of those and was slower (int8, 64 channels: 80 -> 97 us).
     struct Step {
-        uint32_t kw[2][KS][KW], vw[8][VW];
+        uint32_t kw[2][KL][4], vw[8 * VW];            // of key e (0 .. 3 of the first 16, then of the second): vw[VW e ..]
         float ks[I8 ? 8 : 1], vs[I8 ? 8 : 1];
         int key0;
         bool there[2];
@@ -94,16 +97,20 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void attn_few_kernel(AttnArg
             // in scalar registers as they stand: the loads then add the lane's offset themselves
             const char *k_at = k_head + at, *v_at = v_head + at, *v_next;
             asm volatile("" : "+s"(k_at), "+s"(v_at));
-            // keys: A operand, row n, channels 32 step + 8 grp ..
+            // keys: A operand, row n
 #pragma unroll
-            for (int k = 0; k < KS; ++k) load_words<KW, ONCE>(k_at + k_off + 32 * k * ES, f.kw[h][k]);
-            // values: NB channels from NB n of keys 4 grp + e
+            for (int k = 0; k < KL; ++k) load_words<4, ONCE>(k_at + k_off + 64 * k, f.kw[h][k]);
+            // values: the lane's channels of keys 4 grp + e; int8 of fewer than 256 channels: 16 codes of every VK-th key, see regroup()
 #pragma unroll
-            for (int e = 0; e < 4; ++e, v_at = v_next) {
-                v_next = v_at + pitch;
+            for (int e = 0; e < 4; e += VK, v_at = v_next) {
+                v_next = v_at + VK * pitch;
                 asm volatile("" : "+s"(v_next));
+                if constexpr (VK > 1) {
+                    load_words<4, ONCE>(v_at + v_off, f.vw + (4 * h + e) * VW);
+                } else {
 #pragma unroll
-                for (int x = 0; x < VW; x += 4) load_words<(VW < 4 ? VW : 4), ONCE>(v_at + v_off + 4 * x, f.vw[4 * h + e] + x);
+                    for (int x = 0; x < VW; x += 4) load_words<(VW < 4 ? VW : 4), ONCE>(v_at + v_off + 4 * x, f.vw + (4 * h + e) * VW + x);
+                }
             }
             if constexpr (I8) {
                 const int64_t sc = (((int64_t)page * g.p.n_kv + kvh) << g.p.page_shift) + (k0 & page_mask) + 4 * grp;
@@ -115,7 +122,35 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void attn_few_kernel(AttnArg
         page_next[0] = page_at(i + 4, 0);
         page_next[1] = page_at(i + 4, 1);
     };
+    // int8 of 64 or 128 channels: 16 lanes have loaded VK keys together, lane n 16 codes of key n / (16 / VK).  The VK lanes with the same codes'
+    // places turn that round, so that each has 16 / VK of the codes of all VK keys: its own keys' words stay in order.
+    auto regroup = [&](Step& f) {
+        if constexpr (VK > 1) {
+#pragma unroll
+            for (int x = 0; x < 8; x += VK) {
+                uint32_t* v = f.vw + x * VW;
+                const uint32_t w0 = v[0], w1 = v[1], w2 = v[2], w3 = v[3];
+                const bool odd = n & 4, high = n & 8;
+                if constexpr (VK == 4) {           // a 4 x 4 transpose over lanes n, n ^ 4, n ^ 8, n ^ 12
+                    const uint32_t a0 = __builtin_amdgcn_ds_swizzle(odd ? w0 : w1, 0x101F), a1 = __builtin_amdgcn_ds_swizzle(odd ? w2 : w3, 0x101F);
+                    const uint32_t b0 = odd ? a0 : w0, b1 = odd ? w1 : a0, b2 = odd ? a1 : w2, b3 = odd ? w3 : a1;
+                    const uint32_t c0 = __builtin_amdgcn_ds_swizzle(high ? b0 : b2, 0x201F), c1 = __builtin_amdgcn_ds_swizzle(high ? b1 : b3, 0x201F);
+                    v[0] = high ? c0 : b0;
+                    v[1] = high ? c1 : b1;
+                    v[2] = high ? b2 : c0;
+                    v[3] = high ? b3 : c1;
+                } else {                           // pairs of words between lanes n and n ^ 8
+                    const uint32_t a0 = __builtin_amdgcn_ds_swizzle(high ? w0 : w2, 0x201F), a1 = __builtin_amdgcn_ds_swizzle(high ? w1 : w3, 0x201F);
+                    v[0] = high ? a0 : w0;
+                    v[1] = high ? a1 : w1;
+                    v[2] = high ? w2 : a0;
+                    v[3] = high ? w3 : a1;
+                }
+            }
+        }
+    };
     auto use = [&](Step& f) {
+        regroup(f);
         const int key0 = f.key0;
         f32x4_t st[2];
 #pragma unroll
@@ -123,7 +158,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void attn_few_kernel(AttnArg
             st[h] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                const uint32_t* x = f.kw[h][k];
+                const uint32_t* x = I8 ? f.kw[h][k / 2] + 2 * (k % 2) : f.kw[h][k];
                 uint4 w;
                 if constexpr (I8) w = make_uint4(codes_pair<0>(x[0]), codes_pair<2>(x[0]), codes_pair<0>(x[1]), codes_pair<2>(x[1]));
                 else w = make_uint4(x[0], x[1], x[2], x[3]);
@@ -146,7 +181,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void attn_few_kernel(AttnArg
                 const bool used = f.there[h] & (key <= p_hi) & ((key >= low_all) | (key < g.sinks));
                 if (I8) f.vs[e] = used ? f.vs[e] : 0.f;
 #pragma unroll
-                for (int w = 0; w < VW; ++w) f.vw[e][w] = used ? f.vw[e][w] : 0u;
+                for (int w = 0; w < VW; ++w) f.vw[e * VW + w] = used ? f.vw[e * VW + w] : 0u;
             }
         }
         float top = x[0];
@@ -180,7 +215,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void attn_few_kernel(AttnArg
         for (int w = 0; w < NB / 2; ++w) {                                    // channels 2 w and 2 w + 1 of the lane
             uint32_t v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = I8 ? ((w & 1) ? codes_pair<2>(f.vw[e][w / 2]) : codes_pair<0>(f.vw[e][w / 2])) : f.vw[e][w];
+            for (int e = 0; e < 8; ++e) v[e] = I8 ? ((w & 1) ? codes_pair<2>(f.vw[e * VW + w / 2]) : codes_pair<0>(f.vw[e * VW + w / 2])) : f.vw[e * VW + w];
             uint4 even, odd;
             even = make_uint4(__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u),
                               __builtin_amdgcn_perm(v[5], v[4], 0x05040100u), __builtin_amdgcn_perm(v[7], v[6], 0x05040100u));
@@ -203,7 +238,8 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void attn_few_kernel(AttnArg
         }
     }
 
-    // the four wavefronts' results meet: row n, channels NB (4 grp + e) + b
+    // the four wavefronts' results meet: row n, of lane x = 4 grp + e of V^T the channels from first(x) on
+    auto first = [](int x) { return VK > 1 ? 16 * (x % (16 / VK)) + NB * (x / (16 / VK)) : NB * x; };
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     if (lane < 16) { sm_m[wave][n] = m; sm_l[wave][n] = l; }
@@ -211,7 +247,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void attn_few_kernel(AttnArg
     for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int b = 0; b < NB; b += 4)
-            *(f32x4_t*)&sm_o[wave][n][NB * (4 * grp + e) + b] = (f32x4_t){o[b][e], o[b + 1][e], o[b + 2][e], o[b + 3][e]};
+            *(f32x4_t*)&sm_o[wave][n][first(4 * grp + e) + b] = (f32x4_t){o[b][e], o[b + 1][e], o[b + 2][e], o[b + 3][e]};
     __syncthreads();
     constexpr int PER = D / 16;                                              // channels of a thread: 16 threads per row
     const int r = tid >> 4, ch = (tid & 15) * PER;
@@ -321,15 +357,19 @@ int64_t keys_seen(int64_t max_kv, int64_t max_new, int64_t window, int64_t sinks
     return window > 0 && seen < max_kv ? seen : max_kv;
 }
 
-// One row tile reads its keys once.  Then the hint that a line is not wanted again pays where every load takes whole sectors: 64 requests of up
-// to 8192 tokens, 128 bf16 channels, 242 -> 223 us; not for the short loads of int8 (149 -> 179) nor where several row tiles share
-// the keys (142 -> 195 with four).
+// One row tile reads its keys once.  Then the hint that a line is not wanted again pays: 64 requests of up to 8192 tokens, 128 channels, bf16 242 -> 223 us,
+// int8 138 -> 131; not where several row tiles share the keys (142 -> 195 with four).
 template <int D>
 int run_few(aser_ctx* ctx, const AttnArgs& g, int64_t max_rows) {
     const dim3 grid((unsigned)((int64_t)g.p.n_seq * g.row_tiles * g.p.n_kv), (unsigned)g.splits);
-    if (g.p.k_scale) attn_few_kernel<D, true, false><<<grid, 256, 0, ctx->stream>>>(g);
-    else if (g.row_tiles == 1) attn_few_kernel<D, false, true><<<grid, 256, 0, ctx->stream>>>(g);
-    else attn_few_kernel<D, false, false><<<grid, 256, 0, ctx->stream>>>(g);
+    const bool once = g.row_tiles == 1;
+    if (g.p.k_scale) {
+        if (once) attn_few_kernel<D, true, true><<<grid, 256, 0, ctx->stream>>>(g);
+        else attn_few_kernel<D, true, false><<<grid, 256, 0, ctx->stream>>>(g);
+    } else {
+        if (once) attn_few_kernel<D, false, true><<<grid, 256, 0, ctx->stream>>>(g);
+        else attn_few_kernel<D, false, false><<<grid, 256, 0, ctx->stream>>>(g);
+    }
     ASER_TRY(aser_check_launch(ctx, "attn_few_kernel"));
     if (g.splits > 1) {
         const int64_t rows = max_rows < 16 ? max_rows : 16;
