@@ -19,7 +19,6 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kFewRows = 64;        // up to here groups are formed by ballot, in tiles of 16 rows
 constexpr int kManyTiles = 2;       // beyond, a tile has so many times 16 rows
-constexpr int kLoop = 4;            // and a wavefront takes so many times 64 outputs, with P in registers
 constexpr int kMaxAdapters = 4096;
 
 struct AdArgs {
@@ -226,14 +225,14 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdArgs g) {
     }
 }
 
-// Y = Y0 + s P B^T: a wavefront has LOOP times 64 outputs, four times that far apart from each other.  The accumulators go through LDS, so
-// that Y0 and Y are read and written 256 bytes of a row at a time.  aligned: rows of both start on 16-byte boundaries.
-template <int KS, bool VEC, int NT, int LOOP>
+// Y = Y0 + s P B^T: a wavefront has 64 outputs, a workgroup 256 (several times as many for each wavefront, with P kept, were slower: 300 rows, 4096 outputs:
+// 15.4 us, 22.8 with four).  The accumulators go through LDS, so that Y0 and Y are read and written 256 bytes of a row at a time.  aligned: rows of both start on 16-byte boundaries.
+template <int KS, bool VEC, int NT>
 __global__ __launch_bounds__(256, NT > 1 ? 3 : 4) void adapter_up_kernel(AdArgs g, bool aligned) {
     constexpr int ROWS = 16 * NT, PITCH = 68;      // floats of a row in LDS
     constexpr int SUMS = 4 * NT * KS * 2 * 64 * 4, TURN = 4 * ROWS * PITCH;
     __shared__ __align__(16) float sm[SUMS > TURN ? SUMS : TURN];
-    const int blocks = (int)((g.m + 256 * LOOP - 1) / (256 * LOOP)), block = blockIdx.x % blocks;
+    const int blocks = (int)((g.m + 255) / 256), block = blockIdx.x % blocks;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
     const TileRows<NT> tr(g, blockIdx.x / blocks, lane);
     if (tr.adapter == -2 || (tr.adapter == -1 && g.Y0 == g.Y)) return;
@@ -284,60 +283,56 @@ __global__ __launch_bounds__(256, NT > 1 ? 3 : 4) void adapter_up_kernel(AdArgs 
 #pragma unroll
     for (int j = 0; j < 4 * NT; ++j) out_row[j] = __shfl(tr.row[j / 4], 4 * (j % 4) + grp);
     float* turn = sm + wave * ROWS * PITCH;
-    for (int loop = 0; loop < LOOP; ++loop) {
-        const int64_t o0 = ((int64_t)block * LOOP + loop) * 256 + wave * 64;
-        if (o0 >= g.m) return;
-        const int64_t o = o0 + 4 * col;
-        const bool four = aligned && o + 4 <= g.m;
-        f32x4_t y[4 * NT];
+    const int64_t o0 = (int64_t)block * 256 + wave * 64;
+    if (o0 >= g.m) return;
+    const int64_t o = o0 + 4 * col;
+    const bool four = aligned && o + 4 <= g.m;
+    f32x4_t y[4 * NT];
 #pragma unroll
-        for (int j = 0; j < 4 * NT; ++j) {
-            y[j] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-            if (g.Y0 && out_row[j] >= 0) {
-                const float* y0 = g.Y0 + (int64_t)out_row[j] * g.ldy0 + o;
-                if (four) y[j] = __builtin_nontemporal_load((const f32x4_t*)y0);
-                else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (o + e < g.m) y[j][e] = y0[e];
-                }
-            }
-        }
-        if (some) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                f32x4_t acc[NT];
-#pragma unroll
-                for (int x = 0; x < NT; ++x) acc[x] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-                const int64_t row = o0 + 16 * i + col;
-#pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    const bf16x8_t w = row8<VEC>(b + row * g.r, 32 * k + 8 * grp, g.r, row < g.m);
-#pragma unroll
-                    for (int x = 0; x < NT; ++x)
-#pragma unroll
-                        for (int e = 2; e >= 0; --e) acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, t[x][k][e], acc[x], 0, 0, 0);
-                }
-#pragma unroll
-                for (int x = 0; x < NT; ++x) *(f32x4_t*)(turn + (16 * x + col) * PITCH + 16 * i + 4 * grp) = acc[x];
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int j = 0; j < 4 * NT; ++j) y[j] += *(const f32x4_t*)(turn + (4 * j + grp) * PITCH + 4 * col);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-        }
-#pragma unroll
-        for (int j = 0; j < 4 * NT; ++j) {
-            if (out_row[j] < 0) continue;
-            float* dst = g.Y + (int64_t)out_row[j] * g.ldy + o;
-            if (four) *(f32x4_t*)dst = y[j];
+    for (int j = 0; j < 4 * NT; ++j) {
+        y[j] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+        if (g.Y0 && out_row[j] >= 0) {
+            const float* y0 = g.Y0 + (int64_t)out_row[j] * g.ldy0 + o;
+            if (four) y[j] = __builtin_nontemporal_load((const f32x4_t*)y0);
             else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (o + e < g.m) dst[e] = y[j][e];
+                    if (o + e < g.m) y[j][e] = y0[e];
             }
+        }
+    }
+    if (some) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f32x4_t acc[NT];
+#pragma unroll
+            for (int x = 0; x < NT; ++x) acc[x] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+            const int64_t row = o0 + 16 * i + col;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const bf16x8_t w = row8<VEC>(b + row * g.r, 32 * k + 8 * grp, g.r, row < g.m);
+#pragma unroll
+                for (int x = 0; x < NT; ++x)
+#pragma unroll
+                    for (int e = 2; e >= 0; --e) acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, t[x][k][e], acc[x], 0, 0, 0);
+            }
+#pragma unroll
+            for (int x = 0; x < NT; ++x) *(f32x4_t*)(turn + (16 * x + col) * PITCH + 16 * i + 4 * grp) = acc[x];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < 4 * NT; ++j) y[j] += *(const f32x4_t*)(turn + (4 * j + grp) * PITCH + 4 * col);
+    }
+#pragma unroll
+    for (int j = 0; j < 4 * NT; ++j) {
+        if (out_row[j] < 0) continue;
+        float* dst = g.Y + (int64_t)out_row[j] * g.ldy + o;
+        if (four) *(f32x4_t*)dst = y[j];
+        else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (o + e < g.m) dst[e] = y[j][e];
         }
     }
 }
@@ -379,17 +374,17 @@ void launch_downs(const AdArgs& g, bool f32, bool vec, dim3 grid, hipStream_t st
     else if (g.r <= 64) launch_down<4, NT>(g, f32, vec, grid, st);
     else launch_down<8, NT>(g, f32, vec, grid, st);
 }
-template <int KS, int NT, int LOOP>
+template <int KS, int NT>
 void launch_up(const AdArgs& g, bool vec, bool aligned, dim3 grid, hipStream_t st) {
-    if (vec) adapter_up_kernel<KS, true, NT, LOOP><<<grid, 256, 0, st>>>(g, aligned);
-    else adapter_up_kernel<KS, false, NT, LOOP><<<grid, 256, 0, st>>>(g, aligned);
+    if (vec) adapter_up_kernel<KS, true, NT><<<grid, 256, 0, st>>>(g, aligned);
+    else adapter_up_kernel<KS, false, NT><<<grid, 256, 0, st>>>(g, aligned);
 }
-template <int NT, int LOOP>
+template <int NT>
 void launch_ups(const AdArgs& g, bool vec, bool aligned, int64_t tiles, hipStream_t st) {
-    const dim3 grid((unsigned)(tiles * ceil_div64(g.m, 256 * LOOP)));
-    if (g.r <= 32) launch_up<1, NT, LOOP>(g, vec, aligned, grid, st);
-    else if (g.r <= 64) launch_up<2, NT, LOOP>(g, vec, aligned, grid, st);
-    else launch_up<4, NT, LOOP>(g, vec, aligned, grid, st);
+    const dim3 grid((unsigned)(tiles * ceil_div64(g.m, 256)));
+    if (g.r <= 32) launch_up<1, NT>(g, vec, aligned, grid, st);
+    else if (g.r <= 64) launch_up<2, NT>(g, vec, aligned, grid, st);
+    else launch_up<4, NT>(g, vec, aligned, grid, st);
 }
 
 }  // namespace
@@ -435,7 +430,7 @@ extern "C" int aser_adapter_forward(aser_ctx* ctx, const void* X, int x_dtype, i
     if (rows > kFewRows) launch_downs<kManyTiles>(g, f32, vec_a, down, ctx->stream);
     else launch_downs<1>(g, f32, vec_a, down, ctx->stream);
     ASER_TRY(aser_check_launch(ctx, "adapter_down_kernel"));
-    if (rows > kFewRows) launch_ups<kManyTiles, kLoop>(g, vec_b, aligned, tiles, ctx->stream);
-    else launch_ups<1, 1>(g, vec_b, aligned, tiles, ctx->stream);
+    if (rows > kFewRows) launch_ups<kManyTiles>(g, vec_b, aligned, tiles, ctx->stream);
+    else launch_ups<1>(g, vec_b, aligned, tiles, ctx->stream);
     return aser_check_launch(ctx, "adapter_up_kernel");
 }

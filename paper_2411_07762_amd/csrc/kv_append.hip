@@ -52,7 +52,7 @@ __device__ __forceinline__ void load8(const void* base, int64_t i, float x[8]) {
 
 template <int D, bool F32, bool I8>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs g) {
-    constexpr int L = D / 8, R = 64 / L, U = 2;
+    constexpr int L = D / 8, R = 64 / L, U = 4;
     const int lane = threadIdx.x & 63;
     const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int64_t t = wave / g.waves_per_token;
