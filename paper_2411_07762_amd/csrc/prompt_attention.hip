@@ -68,13 +68,16 @@ struct RowTile {
     }
 };
 
+// Slots for stages in LDS: two workgroups of up to 128 channels fit a compute unit, of 256 one does.
+constexpr int slots_of(int d) { return d == 128 ? 2 : 4; }
+
 // Stages of each of `splits` parts of a row tile's list.
 __device__ __forceinline__ int stages_per_split(int total, int splits) { return max((total + splits - 1) / splits, 1); }
 
 template <int D, bool I8, int RB, int W>
 __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(AttnArgs g) {
     constexpr int KEYS = D == 256 ? 32 : 64, SUB = KEYS / 32, CH = D / 8, KS = D / 16, DB = D / 32;
-    constexpr int PITCH = 2 * D, HALF = KEYS * PITCH, STAGE = 2 * HALF, NST = 4, NSC = 8, BM = 32 * RB * W;
+    constexpr int PITCH = 2 * D, HALF = KEYS * PITCH, STAGE = 2 * HALF, NST = slots_of(D), AHEAD = NST == 4 || I8 ? 3 : 2, NSC = 8, BM = 32 * RB * W;
     constexpr int GR = KEYS / W;                  // keys that a wavefront stages, all on one page
     constexpr int LOADS = GR * CH / 64;           // 16-byte loads of a lane for them, of K and of V each
     static_assert(LOADS >= 1, "a wavefront stages at least one load");
@@ -138,7 +141,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
     auto k_swizzle = [](int r) { return D == 64 ? (r >> 1) & 7 : r & 15; };
     auto v_swizzle = [](int r) { return D == 64 ? 4 * ((r >> 1) & 1) : 4 * (r & 3); };
     // Where this wavefront's keys of a stage are, the same for all lanes; page_of(i) is asked for a step before it is needed.
-    struct Place { int64_t at; int key; bool there, all; };   // elements from the head's first; first key; all: the tile sees every one
+    struct Place { int64_t at; int key, page; bool there, all; };   // elements from the head's first; first key; all: the tile sees every one
     auto page_of = [&](int i) -> int {
         const int key = first_key(i) + GR * wave;
         return i < t1 && key < kv ? table[key >> g.p.page_shift] : -1;
@@ -146,6 +149,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
     auto place_of = [&](int i, int page) -> Place {
         Place x;
         x.key = first_key(i) + GR * wave;
+        x.page = page;
         x.there = (uint32_t)page < (uint32_t)g.p.n_pages;
         x.at = (int64_t)(x.there ? page : 0) * g.p.page_stride + (int64_t)((x.key & page_mask) * (uint32_t)g.p.slot_stride);
         x.all = x.there && x.key + GR - 1 <= p_hi && (x.key >= low_all || x.key + GR <= g.sinks);
@@ -181,37 +185,33 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
             }
         }
     };
-    // int8: codes and scales of stage i into registers, and from there, widened, to LDS
-    uint4 held[I8 ? LOADS : 1];
-    float held_scale = 0.f;
-    auto fetch = [&](int i, int page) {
-        const Place x = place_of(i, page);
-        // a load is 16 codes (two chunks) of a row: first those of K, then those of V
+    // int8: codes and scales of the keys of stage i (half 0) or its values (half 1) into registers, and from there, widened, to LDS.  A load is 16
+    // codes (two chunks) of a row.
+    uint4 held[2][I8 ? LOADS / 2 : 1];
+    float held_scale[2] = {0.f, 0.f};
+    auto fetch = [&](const Place& x, int half) {
 #pragma unroll
-        for (int t = 0; t < LOADS; ++t) {
-            const int y = t * 64 + lane, half = y / (GR * CH / 2), z = y % (GR * CH / 2), r = z / (CH / 2);
+        for (int t = 0; t < LOADS / 2; ++t) {
+            const int z = t * 64 + lane, r = z / (CH / 2);
             const int8_t* src = (half ? (const int8_t*)g.p.v : (const int8_t*)g.p.k) + head_at + x.at + (int64_t)r * g.p.slot_stride + 16 * (z % (CH / 2));
-            held[t] = make_uint4(0u, 0u, 0u, 0u);
-            if (wanted(x, r)) held[t] = *(const uint4*)src;
+            held[half][t] = make_uint4(0u, 0u, 0u, 0u);
+            if (wanted(x, r)) held[half][t] = *(const uint4*)src;
         }
-        if (lane < 2 * GR) {
-            const int r = lane % GR;
-            const float* src = (lane < GR ? g.p.k_scale : g.p.v_scale) + (((int64_t)(x.there ? page : 0) * g.p.n_kv + kvh) << g.p.page_shift) + (x.key & page_mask) + r;
-            held_scale = wanted(x, r) ? *src : 0.f;
+        if (lane < GR) {
+            const float* src = (half ? g.p.v_scale : g.p.k_scale) + (((int64_t)(x.there ? x.page : 0) * g.p.n_kv + kvh) << g.p.page_shift) + (x.key & page_mask) + lane;
+            held_scale[half] = wanted(x, lane) ? *src : 0.f;
         }
     };
-    auto land = [&](int i) {
-        char* dst = smem + (i & (NST - 1)) * STAGE + wave * GR * PITCH;
+    auto land = [&](int i, int half) {
+        char* dst = smem + (i & (NST - 1)) * STAGE + half * HALF + wave * GR * PITCH;
 #pragma unroll
-        for (int t = 0; t < LOADS; ++t) {
-            const int x = t * 64 + lane, half = x / (GR * CH / 2), y = x % (GR * CH / 2), r = y / (CH / 2), ch = 2 * (y % (CH / 2)), rr = GR * wave + r;
-            const int sw = half ? v_swizzle(rr) : k_swizzle(rr);
-            char* row = dst + half * HALF + r * PITCH;
-            const uint4 w = held[t];
-            *(uint4*)(row + ((ch ^ sw) << 4)) = make_uint4(codes_pair<0>(w.x), codes_pair<2>(w.x), codes_pair<0>(w.y), codes_pair<2>(w.y));
-            *(uint4*)(row + (((ch + 1) ^ sw) << 4)) = make_uint4(codes_pair<0>(w.z), codes_pair<2>(w.z), codes_pair<0>(w.w), codes_pair<2>(w.w));
+        for (int t = 0; t < LOADS / 2; ++t) {
+            const int z = t * 64 + lane, r = z / (CH / 2), ch = 2 * (z % (CH / 2)), rr = GR * wave + r, sw = half ? v_swizzle(rr) : k_swizzle(rr);
+            const uint4 w = held[half][t];
+            *(uint4*)(dst + r * PITCH + ((ch ^ sw) << 4)) = make_uint4(codes_pair<0>(w.x), codes_pair<2>(w.x), codes_pair<0>(w.y), codes_pair<2>(w.y));
+            *(uint4*)(dst + r * PITCH + (((ch + 1) ^ sw) << 4)) = make_uint4(codes_pair<0>(w.z), codes_pair<2>(w.z), codes_pair<0>(w.w), codes_pair<2>(w.w));
         }
-        if (lane < 2 * GR) (lane < GR ? sm_ks : sm_vs)[(i & (NSC - 1)) * KEYS + GR * wave + lane % GR] = held_scale;
+        if (lane < GR) (half ? sm_vs : sm_ks)[(i & (NSC - 1)) * KEYS + GR * wave + lane] = held_scale[half];
     };
 
     // operand offsets inside a stage
@@ -387,39 +387,43 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // Waits for this wavefront's LDS accesses and all its copies but those of the last step, then for the others.  `more`: those have all theirs.
-    auto meet = [&](bool copies, bool more) {
-        if (I8 || !copies) __builtin_amdgcn_s_waitcnt(0xC07F);                                                     // lgkmcnt(0)
-        else if (more) __builtin_amdgcn_s_waitcnt(0x0070 | (2 * LOADS & 15) | ((2 * LOADS >> 4) << 14));
+    // Ends a step: waits for this wavefront's LDS accesses and its copies, all or (`more`, four slots) all but those begun in this step, then for the others.
+    auto meet = [&](bool more) {
+        if (I8) __builtin_amdgcn_s_waitcnt(0xC07F);                                                     // lgkmcnt(0)
+        else if (more && NST == 4) __builtin_amdgcn_s_waitcnt(0x0070 | (2 * LOADS & 15) | ((2 * LOADS >> 4) << 14));
         else __builtin_amdgcn_s_waitcnt(0x0070);
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
 
-    // Step i: copies of the keys of stage i + 3 and the values of stage i + 2 begun, into slots that were read last in step i - 1; softmax of stage
-    // i; products P V of stage i and K Q of stage i + 1; copies begun in step i - 1 waited for; barrier.  int8: stage i + 2 lands and
-    // i + 3 is fetched with the products.  LAG: the two halves of a workgroup, one wavefront of each on a SIMD, work half a step apart, with
-    // a barrier after the softmax too, so that one is at the vector unit while the other is at the matrix unit (128 channels: 549 -> 518 us; with
-    // 64 channels the vector unit has more to do than the matrix unit and the second barrier costs more than it gives: 110 -> 133).
-    constexpr bool LAG = W == 8 && D == 128;
-    const bool behind = LAG && wave >= 4;
+    // Step i: copies of the keys of stage i + AHEAD and the values of the stage before it begun, into slots that were read last in step i - 1;
+    // softmax of stage i; products P V of stage i and K Q of stage i + 1; what step i + 1 needs waited for; barrier.  int8: the keys of stage i + 2 and
+    // the values of stage i + 1 land, the next ones are fetched.  While one workgroup of the compute unit is at its softmax (vector unit), the other
+    // one may be at its products (matrix unit): two of four wavefronts each were as fast as one of eight whose halves a second barrier kept
+    // half a step apart (530 and 523 us for 8192 tokens; without it 571), and faster where there are few rows (3 x 200 tokens behind 1500: 46 -> 37).
     int page_k;
     Place place_v;
     if constexpr (!I8) {
 #pragma unroll
-        for (int i = 0; i < 3; ++i) {
+        for (int i = 0; i < AHEAD; ++i) {
             const Place x = place_of(i, page_of(i));
             if (i < t1) copy(i, x, 0);
             if (i > 0 && i - 1 < t1) copy(i - 1, place_v, 1);
             place_v = x;
         }
     } else {
-        if (t1 > 0) { fetch(0, page_of(0)); land(0); }
-        if (t1 > 1) { fetch(1, page_of(1)); land(1); }
-        if (t1 > 2) fetch(2, page_of(2));
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {          // stages past the last come as zeros
+            const Place x = place_of(i, page_of(i));
+            fetch(x, 0);
+            if (i > 0) fetch(place_v, 1);
+            if (i < 2) land(i, 0);
+            if (i == 1) land(0, 1);
+            place_v = x;
+        }
     }
-    page_k = page_of(3);
+    page_k = page_of(AHEAD);
     {
         const int shift = g.p.page_shift, sink_pages = g.window > 0 ? (min(g.sinks, p_hi + 1) + page_mask) >> shift : 0;
         const int last = p_hi < 0 ? -1 : min(p_hi, kv - 1) >> shift;
@@ -428,53 +432,54 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
         if (tid == 0) *sm_missing = 0;
         __syncthreads();
         if (missing) *sm_missing = 1;
-        if constexpr (!I8) meet(true, t1 > 2);
-        else meet(false, false);
+        meet(t1 >= AHEAD);
         missing = __builtin_amdgcn_readfirstlane(*sm_missing) != 0;
     }
     if (mine > 0) logits(0);
-    if (behind) meet(false, false);
-    auto begin = [&](int i) {
+    auto begin = [&](int i) {                      // of a step, before its softmax: copies on their way
         if constexpr (!I8) {
-            const Place x = place_of(i + 3, page_k);
-            if (i + 3 < t1) copy(i + 3, x, 0);
-            if (i + 2 < t1) copy(i + 2, place_v, 1);
+            const Place x = place_of(i + AHEAD, page_k);
+            if (i + AHEAD < t1) copy(i + AHEAD, x, 0);
+            if (i + AHEAD - 1 < t1) copy(i + AHEAD - 1, place_v, 1);
             place_v = x;
-            page_k = page_of(i + 4);
+            page_k = page_of(i + AHEAD + 1);
         }
     };
-    auto between = [&](int i) {
-        if constexpr (LAG) meet(false, false);
+    auto refill = [&](int i) {                     // behind the softmax, which has hidden the loads' latency
         if constexpr (I8) {
-            if (i + 2 < t1) land(i + 2);
-            if (i + 3 < t1) fetch(i + 3, page_k);
-            page_k = page_of(i + 4);
+            const Place x = place_of(i + AHEAD, page_k);
+            land(i + 2, 0);
+            land(i + 1, 1);
+            fetch(x, 0);
+            fetch(place_v, 1);
+            place_v = x;
+            page_k = page_of(i + AHEAD + 1);
         }
     };
+    // The last step by itself: where paths meet the compiler moves all accumulators from one set of registers to another.
     int i = 0;
     for (; i < mine - 1; ++i) {
         begin(i);
         softmax(i);
-        between(i);
+        refill(i);
         __builtin_amdgcn_s_setprio(1);
         products(i);
         __builtin_amdgcn_s_setprio(0);
-        meet(true, i + 3 < t1);
+        meet(i + AHEAD < t1);
     }
     if (i < mine) {
         begin(i);
         softmax(i);
-        between(i);
+        refill(i);
         outputs(i);
-        meet(true, i + 3 < t1);
+        meet(i + AHEAD < t1);
         ++i;
     }
     for (; i < t1; ++i) {
         begin(i);
-        between(i);
-        meet(true, i + 3 < t1);
+        refill(i);
+        meet(i + AHEAD < t1);
     }
-    if (LAG && !behind) meet(false, false);
     const bool whole = per_split >= kt.total;
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
@@ -540,9 +545,9 @@ struct PromptPlan { int64_t tiles; int splits, bm; size_t o_bytes, bytes; };
 
 PromptPlan plan_prompt(int64_t tokens, int64_t n_seq, int64_t n_kv, int64_t group, int head_dim, int64_t keys) {
     PromptPlan p;
-    p.bm = head_dim == 128 ? 256 : 128;
+    p.bm = 128;
     p.tiles = ceil_div64(tokens * group, p.bm) + n_seq;
-    const int64_t stages = keys / (head_dim == 256 ? 32 : 64) + 2, full = head_dim == 64 ? 512 : 256;
+    const int64_t stages = keys / (head_dim == 256 ? 32 : 64) + 2, full = head_dim == 256 ? 256 : 512;
     int64_t splits = full / (p.tiles * n_kv);
     if (splits > stages / 6) splits = stages / 6;
     if (splits < 1) splits = 1;
@@ -556,7 +561,7 @@ PromptPlan plan_prompt(int64_t tokens, int64_t n_seq, int64_t n_kv, int64_t grou
 template <int D, bool I8, int W>
 int launch_prompt(aser_ctx* ctx, const AttnArgs& g, const PromptPlan& p) {
     constexpr int KEYS = D == 256 ? 32 : 64, BM = 32 * W, CL = D / 4;
-    constexpr size_t lds = 4 * (2 * KEYS * 2 * D) + 16 + (I8 ? 8 * KEYS * 8 : 0);
+    constexpr size_t lds = slots_of(D) * (2 * KEYS * 2 * D) + 16 + (I8 ? 8 * KEYS * 8 : 0);
     if (p.tiles * g.p.n_kv > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: too many rows");
     const unsigned blocks = (unsigned)(p.tiles * g.p.n_kv);
     auto kernel = attn_prompt_kernel<D, I8, 1, W>;
@@ -583,6 +588,6 @@ int aser_attention_prompt(aser_ctx* ctx, AttnArgs g, int head_dim, int64_t keys)
     g.part_o = (float*)ctx->ws;
     g.part_ml = (float2*)((char*)ctx->ws + p.o_bytes);
     if (head_dim == 64) return i8 ? launch_prompt<64, true, 4>(ctx, g, p) : launch_prompt<64, false, 4>(ctx, g, p);
-    if (head_dim == 128) return i8 ? launch_prompt<128, true, 8>(ctx, g, p) : launch_prompt<128, false, 8>(ctx, g, p);
+    if (head_dim == 128) return i8 ? launch_prompt<128, true, 4>(ctx, g, p) : launch_prompt<128, false, 4>(ctx, g, p);
     return i8 ? launch_prompt<256, true, 4>(ctx, g, p) : launch_prompt<256, false, 4>(ctx, g, p);
 }
