@@ -9,8 +9,22 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr float kNone = -1e30f;                   // running maximum before any key
 
+// n / d for 0 <= n < 2^31 as (n m) >> (31 + s): with 2^s >= d and m = floor(2^(31 + s) / d) + 1 the product is above n 2^(31 + s) / d by less than
+// 2^(31 + s) / d.  A division by a number that is not known to the compiler takes some 150 cycles.
+struct Divider {
+    uint32_t m; int s;
+    __host__ static Divider by(uint32_t d) {
+        Divider x{0u, 31};
+        while (((uint64_t)1 << (x.s - 31)) < d) ++x.s;
+        x.m = (uint32_t)(((uint64_t)1 << x.s) / d + 1);
+        return x;
+    }
+    __device__ __forceinline__ int operator()(int n) const { return (int)((uint64_t)(uint32_t)n * m >> s); }
+};
+
 struct AttnArgs {
     PagedArgs p;
+    Divider by_group, by_kv;                      // divisions by p.group and p.n_kv
     const uint16_t* q; int64_t ldq;
     uint16_t* out; int64_t ldo;
     float c;                                      // scale * log2(e)

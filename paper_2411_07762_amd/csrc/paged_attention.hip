@@ -413,6 +413,8 @@ extern "C" int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ld
     const int64_t keys = keys_seen(batch->max_kv, batch->max_new, window, window > 0 ? sinks : 0), max_rows = (int64_t)batch->max_new * g.p.group;
     const Plan plan = plan_few(g.p.n_seq, g.p.n_kv, g.p.group, batch->max_new, keys);
     g.q = q; g.ldq = ldq; g.out = out; g.ldo = ldo;
+    g.by_group = Divider::by(g.p.group);
+    g.by_kv = Divider::by(g.p.n_kv);
     g.c = scale * 1.4426950408889634f;
     g.window = window;
     g.sinks = window > 0 ? sinks : 0;

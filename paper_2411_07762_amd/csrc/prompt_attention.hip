@@ -17,8 +17,6 @@ namespace {
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
 
-__device__ const uint4 g_zeros = {0u, 0u, 0u, 0u};
-
 __device__ __forceinline__ bf16x8_t lds_tr(const char* lo, const char* hi) {
     typedef s16x4_t __attribute__((address_space(3))) * lds_s4p;
     const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4p)lo);
@@ -26,50 +24,56 @@ __device__ __forceinline__ bf16x8_t lds_tr(const char* lo, const char* hi) {
     return __builtin_bit_cast(bf16x8_t, (s16x8_t)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// The u-th row tile of BM rows, counted from the last request's last one (later rows see more keys: long tiles start first).
+// The u-th row tile of `bm` rows, counted from the last request's last one (later rows see more keys: long tiles start first), and its request: rows
+// row0 .. row0 + count - 1, kv keys.  Every lane looks at one request, up to 64 of them once.
 struct RowTile {
-    int seq, tile;
+    int seq = -1, tile = 0, row0 = 0, count = 0, kv = 0;
     __device__ __forceinline__ RowTile(const AttnArgs& g, int u, int bm, int lane) {
-        int total = 0, nt = 0;
-        for (int pass = 0; pass < 2; ++pass) {
-            int before = 0;
-            seq = -1;
-            for (int base = 0; base < g.p.n_seq; base += 64) {
-                if (pass == 1 && g.p.n_seq <= 64) {
-                    // up to 64 requests: the first pass has left them
-                } else if (base + lane < g.p.n_seq) {
-                    int64_t first;
-                    const int64_t rows = request_rows(g.p, base + lane, &first) * g.p.group;
-                    nt = rows > g.few_rows ? (int)((rows + bm - 1) / bm) : 0;
-                } else {
-                    nt = 0;
-                }
-                int upto = nt;
-#pragma unroll
-                for (int o = 1; o < 64; o <<= 1) {
-                    const int x = __shfl_up(upto, o);
-                    upto += lane >= o ? x : 0;
-                }
-                if (pass == 1) {
-                    const int t = total - 1 - u;
-                    const uint64_t mine = __ballot((before + upto > t) & (before + upto - nt <= t));
-                    if (mine) {
-                        const int l = __ffsll((unsigned long long)mine) - 1;
-                        seq = base + l;
-                        tile = t - (before + __shfl(upto - nt, l));
-                        return;
-                    }
-                }
-                before += __shfl(upto, 63);
+        int my_row0, my_count, my_kv, tiles, upto, in_all = 0;
+        auto look = [&](int base) {
+            my_row0 = my_count = my_kv = tiles = 0;
+            if (base + lane < g.p.n_seq) {
+                int64_t at;
+                my_count = (int)request_rows(g.p, base + lane, &at);
+                my_row0 = (int)at;
+                my_kv = request_kv_len(g.p, base + lane);
+                const int64_t rows = (int64_t)my_count * g.p.group;
+                tiles = rows > g.few_rows ? (int)((rows + bm - 1) / bm) : 0;
             }
-            total = before;
-            if (u >= total) return;
+            const int n = min(g.p.n_seq - base, 64);
+            upto = tiles;
+            for (int o = 1; o < n; o <<= 1) {
+                const int x = __shfl_up(upto, o);
+                upto += lane >= o ? x : 0;
+            }
+            in_all = __builtin_amdgcn_readlane(upto, n - 1);
+        };
+        auto pick = [&](int base, int t) {         // tile t of these requests
+            const int l = __ffsll((unsigned long long)__ballot((upto > t) & (upto - tiles <= t))) - 1;
+            seq = base + l;
+            tile = t - __builtin_amdgcn_readlane(upto - tiles, l);
+            row0 = __builtin_amdgcn_readlane(my_row0, l);
+            count = __builtin_amdgcn_readlane(my_count, l);
+            kv = __builtin_amdgcn_readlane(my_kv, l);
+        };
+        if (g.p.n_seq <= 64) {
+            look(0);
+            if (u < in_all) pick(0, in_all - 1 - u);
+            return;
+        }
+        int total = 0;
+        for (int base = 0; base < g.p.n_seq; base += 64) { look(base); total += in_all; }
+        int t = total - 1 - u;
+        for (int base = 0; t >= 0 && base < g.p.n_seq; base += 64) {
+            look(base);
+            if (t < in_all) { pick(base, t); return; }
+            t -= in_all;
         }
     }
 };
 
 // Slots for stages in LDS: two workgroups of up to 128 channels fit a compute unit, of 256 one does.
-constexpr int slots_of(int d) { return d == 128 ? 2 : 4; }
+constexpr int slots_of(int d) { return d == 256 ? 4 : 2; }
 
 // Stages of each of `splits` parts of a row tile's list.
 __device__ __forceinline__ int stages_per_split(int total, int splits) { return max((total + splits - 1) / splits, 1); }
@@ -86,15 +90,14 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
     float* sm_ks = (float*)(sm_missing + 4);      // int8: [stage % NSC][key] scales of K, then of V
     float* sm_vs = sm_ks + NSC * KEYS;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
-    const int kvh = blockIdx.x % g.p.n_kv;
-    const RowTile rt(g, blockIdx.x / g.p.n_kv, BM, lane);
-    const int s = __builtin_amdgcn_readfirstlane(rt.seq);
-    if (s < 0) return;
-    int64_t row0;
-    const int count = (int)request_rows(g.p, s, &row0), kv = request_kv_len(g.p, s), rows = count * g.p.group, group = g.p.group;
-    const int first = __builtin_amdgcn_readfirstlane(rt.tile) * BM, base_pos = kv - count;
-    const int p_lo = max(base_pos + first / group, 0), p_hi = base_pos + min(first + BM - 1, rows - 1) / group;
-    const int low_all = g.window > 0 ? base_pos + first / group - g.window + 1 : 0;
+    const int u = g.by_kv(blockIdx.x), kvh = blockIdx.x - u * g.p.n_kv;
+    const RowTile rt(g, u, BM, lane);
+    if (rt.seq < 0) return;
+    const int s = rt.seq, count = rt.count, kv = rt.kv, rows = count * g.p.group, group = g.p.group;
+    const int64_t row0 = rt.row0;
+    const int first = rt.tile * BM, base_pos = kv - count;
+    const int p_lo = max(base_pos + g.by_group(first), 0), p_hi = base_pos + g.by_group(min(first + BM - 1, rows - 1));
+    const int low_all = g.window > 0 ? base_pos + g.by_group(first) - g.window + 1 : 0;
     // stages of the tile, and this workgroup's: t0 .. t0 + t1 - 1, numbered from 0 below
     const KeyTiles<KEYS> kt(p_lo, p_hi, g.window, g.sinks);
     const int per_split = stages_per_split(kt.total, g.splits), t0 = blockIdx.y * per_split, t1 = min(kt.total - t0, per_split);
@@ -104,7 +107,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
     // rows of this wavefront
     const int wfirst = first + wave * 32 * RB;
     const bool idle = wfirst >= rows;
-    const int wp_lo = base_pos + min(wfirst, rows - 1) / group, wp_hi = base_pos + min(wfirst + 32 * RB - 1, rows - 1) / group;
+    const int wp_lo = base_pos + g.by_group(min(wfirst, rows - 1)), wp_hi = base_pos + g.by_group(min(wfirst + 32 * RB - 1, rows - 1));
     int pos[RB];
     bf16x8_t q[RB][KS];
     const uint32_t flip = g.c < 0.f ? 0x80008000u : 0u;                      // a negative scale turns the queries round
@@ -112,8 +115,9 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
         const int r = min(wfirst + 32 * b + col, rows - 1);
-        pos[b] = base_pos + r / group;
-        const uint16_t* src = g.q + (row0 + r / group) * g.ldq + (int64_t)(kvh * group + r % group) * D + 8 * h;
+        const int token = g.by_group(r);
+        pos[b] = base_pos + token;
+        const uint16_t* src = g.q + (row0 + token) * g.ldq + (int64_t)(kvh * group + r - token * group) * D + 8 * h;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             uint4 w = *(const uint4*)(src + 16 * k);
@@ -143,8 +147,8 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
     // Where this wavefront's keys of a stage are, the same for all lanes; page_of(i) is asked for a step before it is needed.
     struct Place { int64_t at; int key, page; bool there, all; };   // elements from the head's first; first key; all: the tile sees every one
     auto page_of = [&](int i) -> int {
-        const int key = first_key(i) + GR * wave;
-        return i < t1 && key < kv ? table[key >> g.p.page_shift] : -1;
+        const int key = first_key(i) + GR * wave, page = table[min(key, kv - 1) >> g.p.page_shift];   // kv > 0 where there are stages
+        return (i < t1) & (key < kv) ? page : -1;
     };
     auto place_of = [&](int i, int page) -> Place {
         Place x;
@@ -167,40 +171,51 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
         }
     const char* k_head = (const char*)((const uint16_t*)g.p.k + head_at);
     const char* v_head = (const char*)((const uint16_t*)g.p.v + head_at);
-    // bf16: this wavefront's part of the keys (half 0) or values (half 1) of stage i, on its way into slot i % NST
-    auto copy = [&](int i, const Place& x, int half) {
-        const char* base = (half ? v_head : k_head) + 2 * x.at;
-        const uint32_t slot = ring + (i & (NST - 1)) * STAGE + half * HALF;
-        if (x.all) {
+    // bf16: the n-th of 2 LOADS copies of a step, of this wavefront's part of the keys (first LOADS) or values, on its way into slot i % NST.  Lanes
+    // whose key nobody of the tile sees copy nothing: what is in LDS there has a probability of 0, and is finite, as values seen before are, or the zeros
+    // of the beginning.
+    struct Part { int64_t at; uint64_t lanes[LOADS]; bool whole; };            // whole: no copy is without lanes
+    auto part_of = [&](const Place& x) -> Part {
+        Part y;
+        y.at = 2 * x.at;
+        y.whole = true;
 #pragma unroll
-            for (int t = 0; t < LOADS; ++t)
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                             : : "s"(slot + t * 1024), "v"(lane_off[half][t]), "s"(base) : "memory", "m0");
-        } else {
+        for (int t = 0; t < LOADS; ++t) y.lanes[t] = ~0ull;
+        if (!x.all) {
 #pragma unroll
             for (int t = 0; t < LOADS; ++t) {
-                const char* src = base + lane_off[half][t];
-                if (!wanted(x, t * (64 / CH) + lane / CH)) src = (const char*)&g_zeros;
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(slot + t * 1024), "v"(src) : "memory", "m0");
+                y.lanes[t] = __ballot(wanted(x, t * (64 / CH) + lane / CH));
+                y.whole &= y.lanes[t] != 0;
             }
         }
+        return y;
+    };
+    auto copy = [&](int i, const Part& y, int n) {
+        const int half = n >= LOADS, t = n % LOADS;
+        const char* base = (half ? v_head : k_head) + y.at;
+        const uint32_t slot = ring + (i & (NST - 1)) * STAGE + half * HALF + t * 1024;
+        asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
+                     : : "s"(slot), "v"(lane_off[half][t]), "s"(base), "s"(y.lanes[t]) : "memory", "m0");
     };
     // int8: codes and scales of the keys of stage i (half 0) or its values (half 1) into registers, and from there, widened, to LDS.  A load is 16
     // codes (two chunks) of a row.
     uint4 held[2][I8 ? LOADS / 2 : 1];
     float held_scale[2] = {0.f, 0.f};
-    auto fetch = [&](const Place& x, int half) {
+    bool held_there[2] = {false, false};
+    uint32_t code_off[I8 ? LOADS / 2 : 1];
 #pragma unroll
-        for (int t = 0; t < LOADS / 2; ++t) {
-            const int z = t * 64 + lane, r = z / (CH / 2);
-            const int8_t* src = (half ? (const int8_t*)g.p.v : (const int8_t*)g.p.k) + head_at + x.at + (int64_t)r * g.p.slot_stride + 16 * (z % (CH / 2));
-            held[half][t] = make_uint4(0u, 0u, 0u, 0u);
-            if (wanted(x, r)) held[half][t] = *(const uint4*)src;
-        }
-        if (lane < GR) {
-            const float* src = (half ? g.p.v_scale : g.p.k_scale) + (((int64_t)(x.there ? x.page : 0) * g.p.n_kv + kvh) << g.p.page_shift) + (x.key & page_mask) + lane;
-            held_scale[half] = wanted(x, lane) ? *src : 0.f;
-        }
+    for (int t = 0; t < LOADS / 2; ++t) {
+        const int z = t * 64 + lane;
+        code_off[t] = z / (CH / 2) * (uint32_t)g.p.slot_stride + 16 * (z % (CH / 2));
+    }
+    auto fetch = [&](const Place& x, int half) {
+        // any code is finite: those of keys that nobody sees need no care beside a scale of 0
+        const int8_t* src = (half ? (const int8_t*)g.p.v : (const int8_t*)g.p.k) + head_at + x.at;
+#pragma unroll
+        for (int t = 0; t < LOADS / 2; ++t) held[half][t] = *(const uint4*)(src + code_off[t]);
+        const float* scale = (half ? g.p.v_scale : g.p.k_scale) + (((int64_t)(x.there ? x.page : 0) * g.p.n_kv + kvh) << g.p.page_shift) + (x.key & page_mask);
+        held_scale[half] = scale[lane & (GR - 1)];
+        held_there[half] = wanted(x, lane & (GR - 1));
     };
     auto land = [&](int i, int half) {
         char* dst = smem + (i & (NST - 1)) * STAGE + half * HALF + wave * GR * PITCH;
@@ -211,7 +226,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
             *(uint4*)(dst + r * PITCH + ((ch ^ sw) << 4)) = make_uint4(codes_pair<0>(w.x), codes_pair<2>(w.x), codes_pair<0>(w.y), codes_pair<2>(w.y));
             *(uint4*)(dst + r * PITCH + (((ch + 1) ^ sw) << 4)) = make_uint4(codes_pair<0>(w.z), codes_pair<2>(w.z), codes_pair<0>(w.w), codes_pair<2>(w.w));
         }
-        if (lane < GR) (half ? sm_vs : sm_ks)[(i & (NSC - 1)) * KEYS + GR * wave + lane] = held_scale[half];
+        if (lane < GR) (half ? sm_vs : sm_ks)[(i & (NSC - 1)) * KEYS + GR * wave + lane] = held_there[half] ? held_scale[half] : 0.f;
     };
 
     // operand offsets inside a stage
@@ -305,31 +320,32 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
                 for (int d = 0; d < DB; ++d) o[b][d] *= r;
             }
         }
+        float sum[RB][2] = {};
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
-                float p[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sc[u][b][e], c, -m[b]));
                 uint32_t w[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = bf16_pair(p[2 * e], p[2 * e + 1]);
-                float sum[2] = {0.f, 0.f};
+                for (int e4 = 0; e4 < 4; ++e4) {
+                    float p[4];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sum[e & 1] += p[e];
-                l[b] += sum[0] + sum[1];
-                if constexpr (I8) {
+                    for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sc[u][b][4 * e4 + e], c, -m[b]));
 #pragma unroll
-                    for (int e4 = 0; e4 < 4; ++e4) {
+                    for (int e = 0; e < 4; ++e) sum[b][e & 1] += p[e];
+                    if constexpr (I8) {
                         const f32x4_t vs = *(const f32x4_t*)(sm_vs + fl * KEYS + 32 * u + 8 * e4 + 4 * h);
 #pragma unroll
-                        for (int e = 0; e < 4; e += 2) w[2 * e4 + e / 2] = bf16_pair(p[4 * e4 + e] * vs[e], p[4 * e4 + e + 1] * vs[e + 1]);
+                        for (int e = 0; e < 4; ++e) p[e] *= vs[e];
                     }
+                    w[2 * e4] = bf16_pair(p[0], p[1]);
+                    w[2 * e4 + 1] = bf16_pair(p[2], p[3]);
                 }
 #pragma unroll
                 for (int x = 0; x < 2; ++x) pb[u][b][x] = __builtin_bit_cast(bf16x8_t, make_uint4(w[4 * x], w[4 * x + 1], w[4 * x + 2], w[4 * x + 3]));
             }
+#pragma unroll
+        for (int b = 0; b < RB; ++b) l[b] += sum[b][0] + sum[b][1];
         __builtin_amdgcn_sched_barrier(0);         // all of it in this phase
     };
     auto outputs = [&](int i) {
@@ -347,13 +363,12 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
                 }
     };
     // outputs(i) and logits(i + 1) in one piece.  Nothing but the order of instructions hides the latency of the LDS reads here, so it is
-    // laid down: four instructions at a time, the operands of those two groups further on asked for before them.
+    // laid down: behind each instruction the operand of the one four further on is asked for, into the registers that it has read.
     auto products = [&](int i) {
         const char* stage = smem + (i & (NST - 1)) * STAGE;
         const char* next = smem + ((i + 1) & (NST - 1)) * STAGE;
         constexpr int PV = 2 * SUB * DB, ALL = PV + KS * SUB;
-        static_assert(PV % 4 == 0 && ALL % 4 == 0, "groups of four");
-        bf16x8_t fr[3][4];
+        bf16x8_t fr[4];
         auto ask = [&](int n, bf16x8_t& f) {
             if (n < PV) {
                 const char* v = stage + v_off[n % DB] + 16 * (n / DB) * PITCH;
@@ -375,22 +390,20 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
             }
         };
 #pragma unroll
-        for (int n = 0; n < 8; ++n) ask(n, fr[n / 4][n % 4]);
+        for (int n = 0; n < 4; ++n) ask(n, fr[n]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j < ALL / 4; ++j) {
-#pragma unroll
-            for (int n = 4 * (j + 2); n < 4 * (j + 3) && n < ALL; ++n) ask(n, fr[(j + 2) % 3][n % 4]);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int n = 4 * j; n < 4 * j + 4; ++n) multiply(n, fr[j % 3][n % 4]);
+        for (int n = 0; n < ALL; ++n) {
+            multiply(n, fr[n % 4]);
+            if (n + 4 < ALL) ask(n + 4, fr[n % 4]);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // Ends a step: waits for this wavefront's LDS accesses and its copies, all or (`more`, four slots) all but those begun in this step, then for the others.
-    auto meet = [&](bool more) {
+    // Ends a step: waits for this wavefront's LDS accesses and its copies, all or (four slots, `later`) all but those begun in this step, then for the others.
+    // later: every copy of this step has lanes, so that the counter has it.
+    auto meet = [&](bool later) {
         if (I8) __builtin_amdgcn_s_waitcnt(0xC07F);                                                     // lgkmcnt(0)
-        else if (more && NST == 4) __builtin_amdgcn_s_waitcnt(0x0070 | (2 * LOADS & 15) | ((2 * LOADS >> 4) << 14));
+        else if (NST == 4 && later) __builtin_amdgcn_s_waitcnt(0x0070 | (2 * LOADS & 15) | ((2 * LOADS >> 4) << 14));
         else __builtin_amdgcn_s_waitcnt(0x0070);
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -402,20 +415,43 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
     // the values of stage i + 1 land, the next ones are fetched.  While one workgroup of the compute unit is at its softmax (vector unit), the other
     // one may be at its products (matrix unit): two of four wavefronts each were as fast as one of eight whose halves a second barrier kept
     // half a step apart (530 and 523 us for 8192 tokens; without it 571), and faster where there are few rows (3 x 200 tokens behind 1500: 46 -> 37).
-    int page_k;
-    Place place_v;
+    // What the first steps need from the page table is asked for at once, and whether all pages of the keys that the tile may see are there: those of
+    // the sinks, then those from the window's first.
+    int pages[AHEAD + 1];
+#pragma unroll
+    for (int i = 0; i <= AHEAD; ++i) pages[i] = t1 > 0 ? page_of(i) : -1;
+    const int last_page = p_hi < 0 ? -1 : min(p_hi, kv - 1) >> g.p.page_shift;
+    const int sink_pages = g.window > 0 ? min((min(g.sinks, p_hi + 1) + page_mask) >> g.p.page_shift, last_page + 1) : 0;
+    const int skipped = max((max(low_all, 0) >> g.p.page_shift) - sink_pages, 0);
+    auto is_missing = [&](int x) -> bool {
+        x += x < sink_pages ? 0 : skipped;
+        return x <= last_page && (uint32_t)g.p.pages[s * g.p.ld_pages + x] >= (uint32_t)g.p.n_pages;
+    };
+    missing = is_missing(tid);
+    int page_k = pages[AHEAD];
+    Place place_v;                                 // int8
+    Part part_k, part_v;                           // bf16: copied in this step, of stages i + AHEAD and i + AHEAD - 1
     if constexpr (!I8) {
 #pragma unroll
+        for (int x = 0; x < NST; ++x)
+#pragma unroll
+            for (int t = 0; t < LOADS; ++t) *(uint4*)(smem + x * STAGE + HALF + wave * GR * PITCH + t * 1024 + lane * 16) = make_uint4(0u, 0u, 0u, 0u);
+        __builtin_amdgcn_s_waitcnt(0xC07F);        // lgkmcnt(0)
+#pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const Place x = place_of(i, page_of(i));
-            if (i < t1) copy(i, x, 0);
-            if (i > 0 && i - 1 < t1) copy(i - 1, place_v, 1);
-            place_v = x;
+            part_k = part_of(place_of(i, pages[i]));
+#pragma unroll
+            for (int n = 0; n < LOADS; ++n) copy(i, part_k, n);
+            if (i > 0) {
+#pragma unroll
+                for (int n = LOADS; n < 2 * LOADS; ++n) copy(i - 1, part_v, n);
+            }
+            part_v = part_k;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {          // stages past the last come as zeros
-            const Place x = place_of(i, page_of(i));
+        for (int i = 0; i < AHEAD; ++i) {          // stages past the last come with scales of 0
+            const Place x = place_of(i, pages[i]);
             fetch(x, 0);
             if (i > 0) fetch(place_v, 1);
             if (i < 2) land(i, 0);
@@ -423,30 +459,29 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
             place_v = x;
         }
     }
-    page_k = page_of(AHEAD);
     {
-        const int shift = g.p.page_shift, sink_pages = g.window > 0 ? (min(g.sinks, p_hi + 1) + page_mask) >> shift : 0;
-        const int last = p_hi < 0 ? -1 : min(p_hi, kv - 1) >> shift;
-        for (int x = tid; x <= last; x += 64 * W)
-            if (x < sink_pages || x >= max(low_all, 0) >> shift) missing |= (uint32_t)g.p.pages[s * g.p.ld_pages + x] >= (uint32_t)g.p.n_pages;
+        for (int x = tid + 64 * W; x <= last_page - skipped; x += 64 * W) missing |= is_missing(x);
         if (tid == 0) *sm_missing = 0;
         __syncthreads();
         if (missing) *sm_missing = 1;
-        meet(t1 >= AHEAD);
+        meet(false);
         missing = __builtin_amdgcn_readfirstlane(*sm_missing) != 0;
     }
     if (mine > 0) logits(0);
     auto begin = [&](int i) {                      // of a step, before its softmax: copies on their way
         if constexpr (!I8) {
-            const Place x = place_of(i + AHEAD, page_k);
-            if (i + AHEAD < t1) copy(i + AHEAD, x, 0);
-            if (i + AHEAD - 1 < t1) copy(i + AHEAD - 1, place_v, 1);
-            place_v = x;
+            part_k = part_of(place_of(i + AHEAD, page_k));
+#pragma unroll
+            for (int n = 0; n < 2 * LOADS; ++n) copy(n < LOADS ? i + AHEAD : i + AHEAD - 1, n < LOADS ? part_k : part_v, n);
             page_k = page_of(i + AHEAD + 1);
         }
     };
-    auto refill = [&](int i) {                     // behind the softmax, which has hidden the loads' latency
-        if constexpr (I8) {
+    auto refill = [&](int i) -> bool {
+        if constexpr (!I8) {
+            const bool later = part_k.whole && part_v.whole;
+            part_v = part_k;
+            return later;
+        } else {                                   // behind the softmax, which has hidden the loads' latency
             const Place x = place_of(i + AHEAD, page_k);
             land(i + 2, 0);
             land(i + 1, 1);
@@ -454,6 +489,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
             fetch(place_v, 1);
             place_v = x;
             page_k = page_of(i + AHEAD + 1);
+            return false;
         }
     };
     // The last step by itself: where paths meet the compiler moves all accumulators from one set of registers to another.
@@ -461,24 +497,24 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
     for (; i < mine - 1; ++i) {
         begin(i);
         softmax(i);
-        refill(i);
+        const bool later = refill(i);
         __builtin_amdgcn_s_setprio(1);
         products(i);
         __builtin_amdgcn_s_setprio(0);
-        meet(i + AHEAD < t1);
+        meet(later);
     }
     if (i < mine) {
         begin(i);
         softmax(i);
-        refill(i);
+        const bool later = refill(i);
         outputs(i);
-        meet(i + AHEAD < t1);
+        meet(later);
         ++i;
     }
     for (; i < t1; ++i) {
         begin(i);
-        refill(i);
-        meet(i + AHEAD < t1);
+        const bool later = refill(i);
+        meet(later);
     }
     const bool whole = per_split >= kt.total;
 #pragma unroll
@@ -488,7 +524,8 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
         if (r >= rows) continue;
         if (whole) {
             const float inv = l[b] > 0.f ? 1.f / l[b] : 0.f;
-            uint16_t* dst = g.out + (row0 + r / group) * g.ldo + (int64_t)(kvh * group + r % group) * D + 4 * h;
+            const int token = g.by_group(r);
+            uint16_t* dst = g.out + (row0 + token) * g.ldo + (int64_t)(kvh * group + r - token * group) * D + 4 * h;
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -511,14 +548,12 @@ template <int D, int BM, int KEYS>
 __global__ __launch_bounds__(256) void attn_prompt_join_kernel(AttnArgs g) {
     constexpr int CL = D / 4, R = 256 / CL;
     const int tid = threadIdx.x, c = tid % CL * 4, in_tile = blockIdx.y * R + tid / CL;
-    const int kvh = blockIdx.x % g.p.n_kv;
-    const RowTile rt(g, blockIdx.x / g.p.n_kv, BM, tid & 63);
-    const int s = __builtin_amdgcn_readfirstlane(rt.seq);
-    if (s < 0) return;
-    int64_t row0;
-    const int count = (int)request_rows(g.p, s, &row0), kv = request_kv_len(g.p, s), rows = count * g.p.group, group = g.p.group;
-    const int first = __builtin_amdgcn_readfirstlane(rt.tile) * BM, base_pos = kv - count, r = first + in_tile;
-    const KeyTiles<KEYS> kt(max(base_pos + first / group, 0), base_pos + min(first + BM - 1, rows - 1) / group, g.window, g.sinks);
+    const int u = g.by_kv(blockIdx.x), kvh = blockIdx.x - u * g.p.n_kv;
+    const RowTile rt(g, u, BM, tid & 63);
+    if (rt.seq < 0) return;
+    const int rows = rt.count * g.p.group, group = g.p.group;
+    const int first = rt.tile * BM, base_pos = rt.kv - rt.count, r = first + in_tile;
+    const KeyTiles<KEYS> kt(max(base_pos + g.by_group(first), 0), base_pos + g.by_group(min(first + BM - 1, rows - 1)), g.window, g.sinks);
     const int per = stages_per_split(kt.total, g.splits);
     if (per >= kt.total || r >= rows) return;
     const int used = (kt.total + per - 1) / per;
@@ -535,7 +570,8 @@ __global__ __launch_bounds__(256) void attn_prompt_join_kernel(AttnArgs g) {
         acc += *(const f32x4_t*)(g.part_o + (pr + (int64_t)i * BM) * D + c) * w;
     }
     const float inv = l > 0.f ? 1.f / l : 0.f;
-    uint16_t* dst = g.out + (row0 + r / group) * g.ldo + (int64_t)(kvh * group + r % group) * D + c;
+    const int token = g.by_group(r);
+    uint16_t* dst = g.out + (rt.row0 + (int64_t)token) * g.ldo + (int64_t)(kvh * group + r - token * group) * D + c;
     *(uint2*)dst = make_uint2(bf16_pair(acc[0] * inv, acc[1] * inv), bf16_pair(acc[2] * inv, acc[3] * inv));
 }
 
