@@ -79,7 +79,7 @@ constexpr int slots_of(int d) { return d == 256 ? 4 : 2; }
 __device__ __forceinline__ int stages_per_split(int total, int splits) { return max((total + splits - 1) / splits, 1); }
 
 template <int D, bool I8, int RB, int W>
-__global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(AttnArgs g) {
+__global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_prompt_kernel(AttnArgs g) {
     constexpr int KEYS = D == 256 ? 32 : 64, SUB = KEYS / 32, CH = D / 8, KS = D / 16, DB = D / 32;
     constexpr int PITCH = 2 * D, HALF = KEYS * PITCH, STAGE = 2 * HALF, NST = slots_of(D), AHEAD = NST == 4 || I8 ? 3 : 2, NSC = 8, BM = 32 * RB * W;
     constexpr int GR = KEYS / W;                  // keys that a wavefront stages, all on one page
@@ -147,14 +147,13 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
     // Where this wavefront's keys of a stage are, the same for all lanes; page_of(i) is asked for a step before it is needed.
     struct Place { int64_t at; int key, page; bool there, all; };   // elements from the head's first; first key; all: the tile sees every one
     auto page_of = [&](int i) -> int {
-        const int key = first_key(i) + GR * wave, page = table[min(key, kv - 1) >> g.p.page_shift];   // kv > 0 where there are stages
-        return (i < t1) & (key < kv) ? page : -1;
+        return table[min(first_key(i) + GR * wave, kv - 1) >> g.p.page_shift];                         // kv > 0 where there are stages
     };
     auto place_of = [&](int i, int page) -> Place {
         Place x;
         x.key = first_key(i) + GR * wave;
         x.page = page;
-        x.there = (uint32_t)page < (uint32_t)g.p.n_pages;
+        x.there = (i < t1) & (x.key < kv) & ((uint32_t)page < (uint32_t)g.p.n_pages);
         x.at = (int64_t)(x.there ? page : 0) * g.p.page_stride + (int64_t)((x.key & page_mask) * (uint32_t)g.p.slot_stride);
         x.all = x.there && x.key + GR - 1 <= p_hi && (x.key >= low_all || x.key + GR <= g.sinks);
         return x;
@@ -276,25 +275,32 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
         }
         const bool plain = !missing && key0 + KEYS - 1 <= wp_lo && (g.window <= 0 || key0 >= wp_hi - g.window + 1 || key0 + KEYS <= g.sinks);
         if (!plain) {
-            uint64_t pages_there = ~0ull;          // bit x: the page of key0 + x is there
-            if (missing) {
-                const int key = min(key0 + lane, kv - 1);
-                pages_there = __ballot((uint32_t)g.p.pages[s * g.p.ld_pages + (key >> g.p.page_shift)] < (uint32_t)g.p.n_pages);
-            }
-            int first = key0 + 4 * h;
-            asm volatile("" : "+v"(first));        // nothing of this rare piece is worth registers outside of it
+            // a row sees the keys from `low` to `high`, and those below `sink`, counted from this lane's first
+            const int first = key0 + 4 * h, sink = g.window > 0 ? g.sinks - first : 0;
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) {
-                const uint32_t there = (uint32_t)(pages_there >> (32 * u)) >> (4 * h);
+            for (int b = 0; b < RB; ++b) {
+                int high = pos[b] - first, low = g.window > 0 ? high - g.window + 1 : INT32_MIN;
+                asm volatile("" : "+v"(high), "+v"(low));   // nothing of this rare piece is worth registers outside of it
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int off = 8 * (e >> 2) + (e & 3), key = first + 32 * u + off;
+                for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) {
-                        const bool seen = ((there >> off & 1) != 0) & (key <= pos[b]) & ((key >= pos[b] - g.window + 1) | (key < g.sinks) | (g.window <= 0));
+                    for (int e = 0; e < 16; ++e) {
+                        const int off = 32 * u + 8 * (e >> 2) + (e & 3);
+                        const bool seen = (off <= high) & ((off >= low) | (off < sink));
                         sc[u][b][e] = seen ? sc[u][b][e] : -INFINITY;
                     }
-                }
+            }
+            if (missing) {
+                const int key = min(key0 + lane, kv - 1);
+                const uint64_t there = __ballot((uint32_t)g.p.pages[s * g.p.ld_pages + (key >> g.p.page_shift)] < (uint32_t)g.p.n_pages) >> (4 * h);
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const bool seen = (there >> (32 * u + 8 * (e >> 2) + (e & 3)) & 1) != 0;
+#pragma unroll
+                        for (int b = 0; b < RB; ++b) sc[u][b][e] = seen ? sc[u][b][e] : -INFINITY;
+                    }
             }
         }
         bool higher = false;
@@ -483,12 +489,12 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attn_prompt_kernel(A
             return later;
         } else {                                   // behind the softmax, which has hidden the loads' latency
             const Place x = place_of(i + AHEAD, page_k);
+            page_k = page_of(i + AHEAD + 1);
             land(i + 2, 0);
             land(i + 1, 1);
             fetch(x, 0);
             fetch(place_v, 1);
             place_v = x;
-            page_k = page_of(i + AHEAD + 1);
             return false;
         }
     };
