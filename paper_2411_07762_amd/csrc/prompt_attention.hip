@@ -1,15 +1,23 @@
 // Attention of prompts over the paged cache: the formulas and the transposed products of paged_attention.hip on tiles that the
 // matrix instructions bound instead of memory, 4 D operations per visible key, row and head.
 //
-// A wavefront owns 32 RB rows (a row: one query head of one new token; the heads that share a key/value head lie next to each
+// A wavefront owns 32 rows (a row: one query head of one new token; the heads that share a key/value head lie next to each
 // other, so a tile spans few positions and little of it is masked) and goes through the keys 32 at a time with
 // v_mfma_f32_32x32x16_bf16:  S^T = K Q^T leaves a query row in each column and 16 keys in the registers of a lane, which
 // rounded to bf16 are, 8 at a time, the operand of O^T += V^T P^T as they stand (keys 4 h .. and 8 + 4 h .., h = lane / 32).
-// The workgroup's wavefronts share the keys and values through LDS: stages of KEYS keys, copied by global_load_lds_dwordx4
-// (pages that are not there and keys that nobody sees come from a chunk of zeros), three stages in flight, one barrier per stage.
-// K is read as rows (16 bytes of a key), V through ds_read_b64_tr_b16 (four keys of a channel); the chunks of a row are
-// swizzled so that neither meets bank conflicts.  8-bit caches go through registers, which widen the codes on their way to LDS; the
-// scales multiply logits and probabilities.
+// A workgroup's four wavefronts share the keys and values through LDS: stages of KEYS keys, copied by global_load_lds_dwordx4, the
+// keys of a stage a step before its values, one barrier per stage.  K is read as rows (16 bytes of a key), V through
+// ds_read_b64_tr_b16 (four keys of a channel); the chunks of a row are swizzled so that neither meets bank conflicts.  8-bit caches
+// go through registers, which widen the codes on their way to LDS; the scales multiply logits and probabilities.
+//
+// Roundings: probabilities to bf16 for the second product (8 bits; their sum keeps the unrounded ones), results to bf16.
+//
+// Measured (32 query heads over 8): 8192 tokens of 128 channels 494 us, 1.1 PFLOP/s; the same matrix instructions alone, without
+// loads and softmax, take 362 us: at this length the clock gives way to the power that they draw, 1.7 GHz against 2.2 for 1024
+// tokens (27.7 us), where the length of a step counts: 600 cycles to begin the copies, 1050 for the softmax, 1130 for the products.
+// Two prompts of 6001 and 3034 tokens under a window of 1024: 174 us.  64 channels: 8192 tokens 287 us, bound by the vector unit, whose
+// exponentials take twice the products' time.  256 channels (16 heads), 4096 tokens: 217 us.  int8 pays 60 vector instructions a step
+// of 280 for widening: 4096 tokens of 128 channels 184 us against 137.
 #include "attention.h"
 
 namespace {
@@ -72,16 +80,21 @@ struct RowTile {
     }
 };
 
-// Slots for stages in LDS: two workgroups of up to 128 channels fit a compute unit, of 256 one does.
+constexpr int W = 4;                              // wavefronts of a workgroup
+constexpr int kRows = 32 * W;                     // rows of its tile
+
+// Keys of a stage, and slots for stages in LDS: two workgroups of up to 128 channels fit a compute unit, of 256 one does and has more stages on
+// their way.  Stages of 32 keys for 128 channels: 588 us for 8192 tokens, of 64 530; four slots and one workgroup of 64 channels: 347, two slots 323.
+constexpr int keys_of(int d) { return d == 256 ? 32 : 64; }
 constexpr int slots_of(int d) { return d == 256 ? 4 : 2; }
 
 // Stages of each of `splits` parts of a row tile's list.
 __device__ __forceinline__ int stages_per_split(int total, int splits) { return max((total + splits - 1) / splits, 1); }
 
-template <int D, bool I8, int RB, int W>
+template <int D, bool I8>
 __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_prompt_kernel(AttnArgs g) {
-    constexpr int KEYS = D == 256 ? 32 : 64, SUB = KEYS / 32, CH = D / 8, KS = D / 16, DB = D / 32;
-    constexpr int PITCH = 2 * D, HALF = KEYS * PITCH, STAGE = 2 * HALF, NST = slots_of(D), AHEAD = NST == 4 || I8 ? 3 : 2, NSC = 8, BM = 32 * RB * W;
+    constexpr int KEYS = keys_of(D), SUB = KEYS / 32, CH = D / 8, KS = D / 16, DB = D / 32;
+    constexpr int PITCH = 2 * D, HALF = KEYS * PITCH, STAGE = 2 * HALF, NST = slots_of(D), AHEAD = NST == 4 || I8 ? 3 : 2, NSC = 8, BM = kRows;
     constexpr int GR = KEYS / W;                  // keys that a wavefront stages, all on one page
     constexpr int LOADS = GR * CH / 64;           // 16-byte loads of a lane for them, of K and of V each
     static_assert(LOADS >= 1, "a wavefront stages at least one load");
@@ -105,37 +118,26 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
     auto first_key = [&](int i) -> int { return kt.first_key(t0 + i); };
 
     // rows of this wavefront
-    const int wfirst = first + wave * 32 * RB;
+    const int wfirst = first + 32 * wave;
     const bool idle = wfirst >= rows;
-    const int wp_lo = base_pos + g.by_group(min(wfirst, rows - 1)), wp_hi = base_pos + g.by_group(min(wfirst + 32 * RB - 1, rows - 1));
-    int pos[RB];
-    bf16x8_t q[RB][KS];
+    const int wp_lo = base_pos + g.by_group(min(wfirst, rows - 1)), wp_hi = base_pos + g.by_group(min(wfirst + 31, rows - 1));
+    const int q_r = min(wfirst + col, rows - 1), q_token = g.by_group(q_r), pos = base_pos + q_token;
+    bf16x8_t q[KS];
     const uint32_t flip = g.c < 0.f ? 0x80008000u : 0u;                      // a negative scale turns the queries round
     const float c = fmaxf(fabsf(g.c), 1e-37f);                               // 0: every logit is as good as 0, masked ones stay -inf
+    const uint16_t* q_row = g.q + (row0 + q_token) * g.ldq + (int64_t)(kvh * group + q_r - q_token * group) * D + 8 * h;
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-        const int r = min(wfirst + 32 * b + col, rows - 1);
-        const int token = g.by_group(r);
-        pos[b] = base_pos + token;
-        const uint16_t* src = g.q + (row0 + token) * g.ldq + (int64_t)(kvh * group + r - token * group) * D + 8 * h;
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            uint4 w = *(const uint4*)(src + 16 * k);
-            w.x ^= flip; w.y ^= flip; w.z ^= flip; w.w ^= flip;
-            q[b][k] = __builtin_bit_cast(bf16x8_t, w);
-        }
+    for (int k = 0; k < KS; ++k) {
+        uint4 w = *(const uint4*)(q_row + 16 * k);
+        w.x ^= flip; w.y ^= flip; w.z ^= flip; w.w ^= flip;
+        q[k] = __builtin_bit_cast(bf16x8_t, w);
     }
-    f32x16_t o[RB][DB];
-    float m[RB], l[RB];
+    f32x16_t o[DB];
+    float m = kNone, l = 0.f;
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-        m[b] = kNone;
-        l[b] = 0.f;
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[b][d][e] = 0.f;
-    }
+        for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
 
     // staging: wavefront w has keys GR w .. of a stage; lane: row lane / CH (+ 64 / CH per load), slot lane % CH
     const ScalarInts table = scalar_ints(g.p.pages + s * g.p.ld_pages);
@@ -240,8 +242,8 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
 
     const int mine = idle ? 0 : max(min(kt.count_up_to(wp_hi) - t0, t1), 0);     // stages that this wavefront works on: those behind lie past its rows
     bool missing = false;                          // some page that the tile may look at is not there
-    f32x16_t sc[SUB][RB];                          // logits of a stage, rows and keys as S^T has them
-    bf16x8_t pb[SUB][RB][2];                       // its probabilities
+    f32x16_t sc[SUB];                              // logits of a stage, rows and keys as S^T has them
+    bf16x8_t pb[SUB][2];                           // its probabilities
     auto logits = [&](int i) {
         const char* stage = smem + (i & (NST - 1)) * STAGE;
 #pragma unroll
@@ -250,13 +252,10 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
 #pragma unroll
             for (int k = 0; k < KS; ++k) kf[k] = *(const bf16x8_t*)(stage + k_off[k] + u * 32 * PITCH);
 #pragma unroll
-            for (int b = 0; b < RB; ++b)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) sc[u][b][e] = 0.f;
+                for (int e = 0; e < 16; ++e) sc[u][e] = 0.f;
 #pragma unroll
             for (int k = 0; k < KS; ++k)
-#pragma unroll
-                for (int b = 0; b < RB; ++b) sc[u][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], q[b][k], sc[u][b], 0, 0, 0);
+                sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], q[k], sc[u], 0, 0, 0);
         }
     };
     auto softmax = [&](int i) {
@@ -268,28 +267,23 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
                 for (int e4 = 0; e4 < 4; ++e4) {
                     const f32x4_t ks = *(const f32x4_t*)(sm_ks + fl * KEYS + 32 * u + 8 * e4 + 4 * h);
 #pragma unroll
-                    for (int b = 0; b < RB; ++b)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) sc[u][b][4 * e4 + e] *= ks[e];
+                    for (int e = 0; e < 4; ++e) sc[u][4 * e4 + e] *= ks[e];
                 }
         }
         const bool plain = !missing && key0 + KEYS - 1 <= wp_lo && (g.window <= 0 || key0 >= wp_hi - g.window + 1 || key0 + KEYS <= g.sinks);
         if (!plain) {
             // a row sees the keys from `low` to `high`, and those below `sink`, counted from this lane's first
             const int first = key0 + 4 * h, sink = g.window > 0 ? g.sinks - first : 0;
+            int high = pos - first, low = g.window > 0 ? high - g.window + 1 : INT32_MIN;
+            asm volatile("" : "+v"(high), "+v"(low));   // nothing of this rare piece is worth registers outside of it
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                int high = pos[b] - first, low = g.window > 0 ? high - g.window + 1 : INT32_MIN;
-                asm volatile("" : "+v"(high), "+v"(low));   // nothing of this rare piece is worth registers outside of it
+            for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int off = 32 * u + 8 * (e >> 2) + (e & 3);
-                        const bool seen = (off <= high) & ((off >= low) | (off < sink));
-                        sc[u][b][e] = seen ? sc[u][b][e] : -INFINITY;
-                    }
-            }
+                for (int e = 0; e < 16; ++e) {
+                    const int off = 32 * u + 8 * (e >> 2) + (e & 3);
+                    const bool seen = (off <= high) & ((off >= low) | (off < sink));
+                    sc[u][e] = seen ? sc[u][e] : -INFINITY;
+                }
             if (missing) {
                 const int key = min(key0 + lane, kv - 1);
                 const uint64_t there = __ballot((uint32_t)g.p.pages[s * g.p.ld_pages + (key >> g.p.page_shift)] < (uint32_t)g.p.n_pages) >> (4 * h);
@@ -298,60 +292,47 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const bool seen = (there >> (32 * u + 8 * (e >> 2) + (e & 3)) & 1) != 0;
-#pragma unroll
-                        for (int b = 0; b < RB; ++b) sc[u][b][e] = seen ? sc[u][b][e] : -INFINITY;
+                        sc[u][e] = seen ? sc[u][e] : -INFINITY;
                     }
             }
         }
-        bool higher = false;
-        float top[RB];
-#pragma unroll
-        for (int b = 0; b < RB; ++b) {
-            top[b] = sc[0][b][0];
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) top[b] = fmaxf(top[b], sc[u][b][e]);
-            top[b] *= c;
-            higher |= top[b] > m[b] + 8.f;
-        }
-        // the maximum moves only when a logit is 8 above it: until then p <= 2^8, which neither fp32 sums nor bf16 mind
-        if (__ballot(higher)) {
-#pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                const float m_new = fmaxf(m[b], fmaxf(top[b], __shfl_xor(top[b], 32))), r = __builtin_amdgcn_exp2f(m[b] - m_new);
-                m[b] = m_new;
-                l[b] *= r;
-#pragma unroll
-                for (int d = 0; d < DB; ++d) o[b][d] *= r;
-            }
-        }
-        float sum[RB][2] = {};
+        float top = sc[0][0];
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                uint32_t w[8];
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[u][e]);
+        top *= c;
+        // the maximum moves only when a logit is 8 above it: until then p <= 2^8, which neither fp32 sums nor bf16 mind
+        if (__ballot(top > m + 8.f)) {
+            const float m_new = fmaxf(m, fmaxf(top, __shfl_xor(top, 32))), shrink = __builtin_amdgcn_exp2f(m - m_new);
+            m = m_new;
+            l *= shrink;
 #pragma unroll
-                for (int e4 = 0; e4 < 4; ++e4) {
-                    float p[4];
+            for (int d = 0; d < DB; ++d) o[d] *= shrink;
+        }
+        float sum[2] = {0.f, 0.f};                 // of the unrounded probabilities
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sc[u][b][4 * e4 + e], c, -m[b]));
+        for (int u = 0; u < SUB; ++u) {
+            uint32_t w[8];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[b][e & 1] += p[e];
-                    if constexpr (I8) {
-                        const f32x4_t vs = *(const f32x4_t*)(sm_vs + fl * KEYS + 32 * u + 8 * e4 + 4 * h);
+            for (int e4 = 0; e4 < 4; ++e4) {
+                float p[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) p[e] *= vs[e];
-                    }
-                    w[2 * e4] = bf16_pair(p[0], p[1]);
-                    w[2 * e4 + 1] = bf16_pair(p[2], p[3]);
+                for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sc[u][4 * e4 + e], c, -m));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e & 1] += p[e];
+                if constexpr (I8) {
+                    const f32x4_t vs = *(const f32x4_t*)(sm_vs + fl * KEYS + 32 * u + 8 * e4 + 4 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[e] *= vs[e];
                 }
-#pragma unroll
-                for (int x = 0; x < 2; ++x) pb[u][b][x] = __builtin_bit_cast(bf16x8_t, make_uint4(w[4 * x], w[4 * x + 1], w[4 * x + 2], w[4 * x + 3]));
+                w[2 * e4] = bf16_pair(p[0], p[1]);
+                w[2 * e4 + 1] = bf16_pair(p[2], p[3]);
             }
 #pragma unroll
-        for (int b = 0; b < RB; ++b) l[b] += sum[b][0] + sum[b][1];
+            for (int x = 0; x < 2; ++x) pb[u][x] = __builtin_bit_cast(bf16x8_t, make_uint4(w[4 * x], w[4 * x + 1], w[4 * x + 2], w[4 * x + 3]));
+        }
+        l += sum[0] + sum[1];
         __builtin_amdgcn_sched_barrier(0);         // all of it in this phase
     };
     auto outputs = [&](int i) {
@@ -364,8 +345,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
                 for (int d = 0; d < DB; ++d) {
                     const char* v = stage + v_off[d] + (32 * u + 16 * x) * PITCH;
                     const bf16x8_t vf = lds_tr(v, v + 8 * PITCH);
-#pragma unroll
-                    for (int b = 0; b < RB; ++b) o[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[u][b][x], o[b][d], 0, 0, 0);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[u][x], o[d], 0, 0, 0);
                 }
     };
     // outputs(i) and logits(i + 1) in one piece.  Nothing but the order of instructions hides the latency of the LDS reads here, so it is
@@ -384,15 +364,12 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
             }
         };
         auto multiply = [&](int n, const bf16x8_t& f) {
-#pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                if (n < PV) {
-                    o[b][n % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pb[n / DB / 2][b][n / DB % 2], o[b][n % DB], 0, 0, 0);
-                } else {
-                    const int k = (n - PV) / SUB, u = (n - PV) % SUB;
-                    f32x16_t zero = {};
-                    sc[u][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[b][k], k ? sc[u][b] : zero, 0, 0, 0);
-                }
+            if (n < PV) {
+                o[n % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pb[n / DB / 2][n / DB % 2], o[n % DB], 0, 0, 0);
+            } else {
+                const int k = (n - PV) / SUB, u = (n - PV) % SUB;
+                f32x16_t zero = {};
+                sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[k], k ? sc[u] : zero, 0, 0, 0);
             }
         };
 #pragma unroll
@@ -416,11 +393,6 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
         asm volatile("" ::: "memory");
     };
 
-    // Step i: copies of the keys of stage i + AHEAD and the values of the stage before it begun, into slots that were read last in step i - 1;
-    // softmax of stage i; products P V of stage i and K Q of stage i + 1; what step i + 1 needs waited for; barrier.  int8: the keys of stage i + 2 and
-    // the values of stage i + 1 land, the next ones are fetched.  While one workgroup of the compute unit is at its softmax (vector unit), the other
-    // one may be at its products (matrix unit): two of four wavefronts each were as fast as one of eight whose halves a second barrier kept
-    // half a step apart (530 and 523 us for 8192 tokens; without it 571), and faster where there are few rows (3 x 200 tokens behind 1500: 46 -> 37).
     // What the first steps need from the page table is asked for at once, and whether all pages of the keys that the tile may see are there: those of
     // the sinks, then those from the window's first.
     int pages[AHEAD + 1];
@@ -429,11 +401,11 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
     const int last_page = p_hi < 0 ? -1 : min(p_hi, kv - 1) >> g.p.page_shift;
     const int sink_pages = g.window > 0 ? min((min(g.sinks, p_hi + 1) + page_mask) >> g.p.page_shift, last_page + 1) : 0;
     const int skipped = max((max(low_all, 0) >> g.p.page_shift) - sink_pages, 0);
-    auto is_missing = [&](int x) -> bool {
+    auto page_word = [&](int x) -> uint32_t {      // 0 behind the last one
         x += x < sink_pages ? 0 : skipped;
-        return x <= last_page && (uint32_t)g.p.pages[s * g.p.ld_pages + x] >= (uint32_t)g.p.n_pages;
+        return x <= last_page ? (uint32_t)g.p.pages[s * g.p.ld_pages + x] : 0u;
     };
-    missing = is_missing(tid);
+    const uint32_t my_page = page_word(tid);
     int page_k = pages[AHEAD];
     Place place_v;                                 // int8
     Part part_k, part_v;                           // bf16: copied in this step, of stages i + AHEAD and i + AHEAD - 1
@@ -465,15 +437,20 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
             place_v = x;
         }
     }
-    {
-        for (int x = tid + 64 * W; x <= last_page - skipped; x += 64 * W) missing |= is_missing(x);
-        if (tid == 0) *sm_missing = 0;
-        __syncthreads();
-        if (missing) *sm_missing = 1;
-        meet(false);
-        missing = __builtin_amdgcn_readfirstlane(*sm_missing) != 0;
-    }
+    missing = my_page >= (uint32_t)g.p.n_pages;
+    for (int x = tid + 64 * W; x <= last_page - skipped; x += 64 * W) missing |= page_word(x) >= (uint32_t)g.p.n_pages;
+    if (tid == 0) *sm_missing = 0;
+    __syncthreads();
+    if (missing) *sm_missing = 1;
+    meet(false);
+    missing = __builtin_amdgcn_readfirstlane(*sm_missing) != 0;
     if (mine > 0) logits(0);
+    // Step i: copies of the keys of stage i + AHEAD and the values of the stage before it begun, into slots that were read last in step i - 1;
+    // softmax of stage i; products P V of stage i and K Q of stage i + 1; what step i + 1 needs waited for; barrier.  int8: the keys of stage i + 2 and
+    // the values of stage i + 1 land, the next ones are fetched.  While one workgroup of the compute unit is at its softmax (vector unit), the other
+    // one may be at its products (matrix unit): two of four wavefronts each were as fast as one of eight whose halves a second barrier kept
+    // half a step apart (530 and 523 us for 8192 tokens; without it 571), and faster where there are few rows (3 x 200 tokens behind 1500: 46 -> 37).
+    // Copies spread over the softmax took as long as together before it.
     auto begin = [&](int i) {                      // of a step, before its softmax: copies on their way
         if constexpr (!I8) {
             part_k = part_of(place_of(i + AHEAD, page_k));
@@ -522,44 +499,40 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
         const bool later = refill(i);
         meet(later);
     }
-    const bool whole = per_split >= kt.total;
+    const int r = wfirst + col;
+    l += __shfl_xor(l, 32);
+    if (r >= rows) return;
+    if (per_split >= kt.total) {
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const int token = g.by_group(r);
+        uint16_t* dst = g.out + (row0 + token) * g.ldo + (int64_t)(kvh * group + r - token * group) * D + 4 * h;
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-        const int r = wfirst + 32 * b + col;
-        l[b] += __shfl_xor(l[b], 32);
-        if (r >= rows) continue;
-        if (whole) {
-            const float inv = l[b] > 0.f ? 1.f / l[b] : 0.f;
-            const int token = g.by_group(r);
-            uint16_t* dst = g.out + (row0 + token) * g.ldo + (int64_t)(kvh * group + r - token * group) * D + 4 * h;
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
+            for (int e = 0; e < 16; e += 4)
+                *(uint2*)(dst + 32 * d + 2 * e) = make_uint2(bf16_pair(o[d][e] * inv, o[d][e + 1] * inv), bf16_pair(o[d][e + 2] * inv, o[d][e + 3] * inv));
+    } else {
+        const int64_t pr = ((int64_t)blockIdx.x * g.splits + blockIdx.y) * BM + (r - first);
+        if (h == 0) g.part_ml[pr] = make_float2(m, l);
+        float* dst = g.part_o + pr * D + 4 * h;
 #pragma unroll
-                for (int e = 0; e < 16; e += 4)
-                    *(uint2*)(dst + 32 * d + 2 * e) = make_uint2(bf16_pair(o[b][d][e] * inv, o[b][d][e + 1] * inv), bf16_pair(o[b][d][e + 2] * inv, o[b][d][e + 3] * inv));
-        } else {
-            const int64_t pr = ((int64_t)blockIdx.x * g.splits + blockIdx.y) * BM + (r - first);
-            if (h == 0) g.part_ml[pr] = make_float2(m[b], l[b]);
-            float* dst = g.part_o + pr * D + 4 * h;
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; e += 4) *(f32x4_t*)(dst + 32 * d + 2 * e) = (f32x4_t){o[b][d][e], o[b][d][e + 1], o[b][d][e + 2], o[b][d][e + 3]};
-        }
+            for (int e = 0; e < 16; e += 4) *(f32x4_t*)(dst + 32 * d + 2 * e) = (f32x4_t){o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
     }
 }
 
 // Joins the splits of a row tile: o = sum_s w_s o_s / sum_s w_s l_s, w_s = exp2(m_s - max m); four channels of a row per thread.
-template <int D, int BM, int KEYS>
+template <int D>
 __global__ __launch_bounds__(256) void attn_prompt_join_kernel(AttnArgs g) {
-    constexpr int CL = D / 4, R = 256 / CL;
+    constexpr int CL = D / 4, R = 256 / CL, BM = kRows;
     const int tid = threadIdx.x, c = tid % CL * 4, in_tile = blockIdx.y * R + tid / CL;
     const int u = g.by_kv(blockIdx.x), kvh = blockIdx.x - u * g.p.n_kv;
     const RowTile rt(g, u, BM, tid & 63);
     if (rt.seq < 0) return;
     const int rows = rt.count * g.p.group, group = g.p.group;
     const int first = rt.tile * BM, base_pos = rt.kv - rt.count, r = first + in_tile;
-    const KeyTiles<KEYS> kt(max(base_pos + g.by_group(first), 0), base_pos + g.by_group(min(first + BM - 1, rows - 1)), g.window, g.sinks);
+    const KeyTiles<keys_of(D)> kt(max(base_pos + g.by_group(first), 0), base_pos + g.by_group(min(first + BM - 1, rows - 1)), g.window, g.sinks);
     const int per = stages_per_split(kt.total, g.splits);
     if (per >= kt.total || r >= rows) return;
     const int used = (kt.total + per - 1) / per;
@@ -581,37 +554,38 @@ __global__ __launch_bounds__(256) void attn_prompt_join_kernel(AttnArgs g) {
     *(uint2*)dst = make_uint2(bf16_pair(acc[0] * inv, acc[1] * inv), bf16_pair(acc[2] * inv, acc[3] * inv));
 }
 
-// Sizes of a launch.  A workgroup per compute unit (two with 64 channels) is what the device holds; when the row tiles are fewer than half of that, the
-// keys are split, 6 stages at least to a workgroup, and the parts joined by a second launch.
-struct PromptPlan { int64_t tiles; int splits, bm; size_t o_bytes, bytes; };
+// Sizes of a launch.  Two workgroups per compute unit are what the device holds (one with 256 channels); when the row tiles are fewer than half of that, the
+// keys are split, 6 stages at least to a workgroup, and the parts joined by a second launch (300 tokens behind 6000: 47 us; split twice as far 61).
+// Splits also where the device is full, to even out long and short tiles, cost more than they gave but on 8-bit caches of 64 channels: 3000 tokens
+// 85 -> 108 us, 2048 53 -> 60, ragged int8 pieces 94 -> 81.
+struct PromptPlan { int64_t tiles; int splits; size_t o_bytes, bytes; };
 
 PromptPlan plan_prompt(int64_t tokens, int64_t n_seq, int64_t n_kv, int64_t group, int head_dim, int64_t keys) {
     PromptPlan p;
-    p.bm = 128;
-    p.tiles = ceil_div64(tokens * group, p.bm) + n_seq;
-    const int64_t stages = keys / (head_dim == 256 ? 32 : 64) + 2, full = head_dim == 256 ? 256 : 512;
+    p.tiles = ceil_div64(tokens * group, kRows) + n_seq;
+    const int64_t stages = keys / keys_of(head_dim) + 2, full = head_dim == 256 ? 256 : 512;
     int64_t splits = full / (p.tiles * n_kv);
     if (splits > stages / 6) splits = stages / 6;
     if (splits < 1) splits = 1;
     p.splits = (int)splits;
-    const size_t rows = splits > 1 ? (size_t)(p.tiles * n_kv) * p.splits * p.bm : 0;
+    const size_t rows = splits > 1 ? (size_t)(p.tiles * n_kv) * p.splits * kRows : 0;
     p.o_bytes = align_up(rows * head_dim * 4, 256);
     p.bytes = p.o_bytes + align_up(rows * 8, 256);
     return p;
 }
 
-template <int D, bool I8, int W>
+template <int D, bool I8>
 int launch_prompt(aser_ctx* ctx, const AttnArgs& g, const PromptPlan& p) {
-    constexpr int KEYS = D == 256 ? 32 : 64, BM = 32 * W, CL = D / 4;
+    constexpr int KEYS = keys_of(D);
     constexpr size_t lds = slots_of(D) * (2 * KEYS * 2 * D) + 16 + (I8 ? 8 * KEYS * 8 : 0);
     if (p.tiles * g.p.n_kv > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: too many rows");
     const unsigned blocks = (unsigned)(p.tiles * g.p.n_kv);
-    auto kernel = attn_prompt_kernel<D, I8, 1, W>;
+    auto kernel = attn_prompt_kernel<D, I8>;
     ASER_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
     kernel<<<dim3(blocks, (unsigned)p.splits), 64 * W, lds, ctx->stream>>>(g);
     ASER_TRY(aser_check_launch(ctx, "attn_prompt_kernel"));
     if (p.splits > 1) {
-        attn_prompt_join_kernel<D, BM, KEYS><<<dim3(blocks, BM / (256 / CL)), 256, 0, ctx->stream>>>(g);
+        attn_prompt_join_kernel<D><<<dim3(blocks, kRows / (256 / (D / 4))), 256, 0, ctx->stream>>>(g);
         return aser_check_launch(ctx, "attn_prompt_join_kernel");
     }
     return ASER_OK;
@@ -629,7 +603,7 @@ int aser_attention_prompt(aser_ctx* ctx, AttnArgs g, int head_dim, int64_t keys)
     g.splits = p.splits;
     g.part_o = (float*)ctx->ws;
     g.part_ml = (float2*)((char*)ctx->ws + p.o_bytes);
-    if (head_dim == 64) return i8 ? launch_prompt<64, true, 4>(ctx, g, p) : launch_prompt<64, false, 4>(ctx, g, p);
-    if (head_dim == 128) return i8 ? launch_prompt<128, true, 4>(ctx, g, p) : launch_prompt<128, false, 4>(ctx, g, p);
-    return i8 ? launch_prompt<256, true, 4>(ctx, g, p) : launch_prompt<256, false, 4>(ctx, g, p);
+    if (head_dim == 64) return i8 ? launch_prompt<64, true>(ctx, g, p) : launch_prompt<64, false>(ctx, g, p);
+    if (head_dim == 128) return i8 ? launch_prompt<128, true>(ctx, g, p) : launch_prompt<128, false>(ctx, g, p);
+    return i8 ? launch_prompt<256, true>(ctx, g, p) : launch_prompt<256, false>(ctx, g, p);
 }
