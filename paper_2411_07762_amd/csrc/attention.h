@@ -24,7 +24,7 @@ struct Divider {
 
 struct AttnArgs {
     PagedArgs p;
-    Divider by_group, by_kv;                      // divisions by p.group and p.n_kv
+    Divider by_group, by_kv, by_tiles, by_split;  // divisions by p.group, p.n_kv, row_tiles and tiles_per_split
     const uint16_t* q; int64_t ldq;
     uint16_t* out; int64_t ldo;
     float c;                                      // scale * log2(e)

@@ -35,19 +35,19 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void attn_few_kernel(AttnArg
     __shared__ float sm_o[4][16][D + 4];
     __shared__ float sm_m[4][16], sm_l[4][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, grp = lane >> 4;
-    const int kvh = blockIdx.x % g.p.n_kv, tile = blockIdx.x / g.p.n_kv, split = blockIdx.y, s = tile / g.row_tiles, rt = tile % g.row_tiles;
+    const int tile = g.by_kv(blockIdx.x), kvh = blockIdx.x - tile * g.p.n_kv, split = blockIdx.y, s = g.by_tiles(tile), rt = tile - s * g.row_tiles;
     int64_t row0;
     const int count = (int)request_rows(g.p, s, &row0), kv = request_kv_len(g.p, s);
     const int rows = count * g.p.group - rt * 16;                            // rows of this tile, if positive
     if (rows <= 0 || count * g.p.group > g.few_rows) return;
-    const int my_row = min(rt * 16 + n, count * g.p.group - 1), my_tok = my_row / g.p.group, my_head = my_row % g.p.group;
+    const int my_row = min(rt * 16 + n, count * g.p.group - 1), my_tok = g.by_group(my_row), my_head = my_row - my_tok * g.p.group;
     const int my_pos = kv - count + my_tok;
     const int last_row = min(rt * 16 + 15, count * g.p.group - 1);
-    const int p_lo = max(kv - count + rt * 16 / g.p.group, 0), p_hi = kv - count + last_row / g.p.group;
+    const int p_lo = max(kv - count + g.by_group(rt * 16), 0), p_hi = kv - count + g.by_group(last_row);
     const KeyTiles<kTile> kt(p_lo, p_hi, g.window, g.sinks);
     const int t0 = split * g.tiles_per_split, t1 = min(t0 + g.tiles_per_split, kt.total);
     if (t0 >= t1 && split > 0) return;
-    const int low_all = g.window > 0 ? kv - count + rt * 16 / g.p.group - g.window + 1 : 0;   // the same for the tile's first row
+    const int low_all = g.window > 0 ? kv - count + g.by_group(rt * 16) - g.window + 1 : 0;   // the same for the tile's first row
     const int my_low = g.window > 0 ? my_pos - g.window + 1 : 0;             // keys below are seen up to sinks only
 
     // the row's query: B operand of K Q^T, channels 32 step + 8 grp ..; int8: 64 (step / 2) + 16 grp + 8 (step % 2) .., so that a load is 16 codes
@@ -265,11 +265,12 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void attn_few_kernel(AttnArg
 #pragma unroll
         for (int c = 0; c < PER; ++c) acc[c] += sm_o[w][r][ch + c] * f;
     }
-    const int used = (kt.total + g.tiles_per_split - 1) / g.tiles_per_split;  // splits that have keys
+    const int used = g.by_split(kt.total + g.tiles_per_split - 1);  // splits that have keys
     if (used <= 1) {
         const float inv = ll > 0.f ? 1.f / ll : 0.f;
         const int row = rt * 16 + r;
-        uint16_t* dst = g.out + (row0 + row / g.p.group) * g.ldo + (int64_t)(kvh * g.p.group + row % g.p.group) * D + ch;
+        const int token = g.by_group(row);
+        uint16_t* dst = g.out + (row0 + token) * g.ldo + (int64_t)(kvh * g.p.group + row - token * g.p.group) * D + ch;
 #pragma unroll
         for (int c = 0; c < PER; c += 4) *(uint2*)(dst + c) = make_uint2(bf16_pair(acc[c] * inv, acc[c + 1] * inv), bf16_pair(acc[c + 2] * inv, acc[c + 3] * inv));
     } else {
@@ -288,15 +289,15 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs g) {
     __shared__ f32x4_t sm[SL][CL];
     __shared__ float sm_w[kMaxSplits], sm_m[4], sm_l[4];
     const int tid = threadIdx.x, cl = tid % CL, sl = tid / CL, r = blockIdx.y;
-    const int kvh = blockIdx.x % g.p.n_kv, tile = blockIdx.x / g.p.n_kv, s = tile / g.row_tiles, rt = tile % g.row_tiles;
+    const int tile = g.by_kv(blockIdx.x), kvh = blockIdx.x - tile * g.p.n_kv, s = g.by_tiles(tile), rt = tile - s * g.row_tiles;
     const int64_t pr = (int64_t)blockIdx.x * g.splits * 16 + r;
     float2 ml = g.part_ml[pr + (int64_t)min(tid, g.splits - 1) * 16];
     int64_t row0;
     const int count = (int)request_rows(g.p, s, &row0), kv = request_kv_len(g.p, s), row = rt * 16 + r;
     if (row >= count * g.p.group || count * g.p.group > g.few_rows) return;
     const int last_row = min(rt * 16 + 15, count * g.p.group - 1);
-    const KeyTiles<kTile> kt(max(kv - count + rt * 16 / g.p.group, 0), kv - count + last_row / g.p.group, g.window, g.sinks);
-    const int used = (kt.total + g.tiles_per_split - 1) / g.tiles_per_split;
+    const KeyTiles<kTile> kt(max(kv - count + g.by_group(rt * 16), 0), kv - count + g.by_group(last_row), g.window, g.sinks);
+    const int used = g.by_split(kt.total + g.tiles_per_split - 1);
     if (used <= 1) return;
     if (tid >= used) ml = make_float2(kNone, 0.f);
     float top = ml.x;
@@ -322,7 +323,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs g) {
     for (int i = 1; i < SL; ++i) acc += sm[i][cl];
     ll = (sm_l[0] + sm_l[1]) + (sm_l[2] + sm_l[3]);
     const float inv = ll > 0.f ? 1.f / ll : 0.f;
-    uint16_t* dst = g.out + (row0 + row / g.p.group) * g.ldo + (int64_t)(kvh * g.p.group + row % g.p.group) * D + 4 * cl;
+    const int token = g.by_group(row);
+    uint16_t* dst = g.out + (row0 + token) * g.ldo + (int64_t)(kvh * g.p.group + row - token * g.p.group) * D + 4 * cl;
     *(uint2*)dst = make_uint2(bf16_pair(acc[0] * inv, acc[1] * inv), bf16_pair(acc[2] * inv, acc[3] * inv));
 }
 
@@ -420,6 +422,8 @@ extern "C" int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ld
     g.sinks = window > 0 ? sinks : 0;
     g.few_rows = kFewRows;
     g.splits = plan.splits; g.tiles_per_split = plan.tiles_per_split; g.row_tiles = plan.row_tiles;
+    g.by_tiles = Divider::by(g.row_tiles);
+    g.by_split = Divider::by(g.tiles_per_split);
     if ((int64_t)g.p.n_seq * g.row_tiles * g.p.n_kv > INT32_MAX || batch->tokens * g.p.group > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: too many requests times rows");
     size_t o_bytes, need = few_workspace(plan, g.p.n_seq, g.p.n_kv, cache->head_dim, &o_bytes);
     if (max_rows > kFewRows) {
