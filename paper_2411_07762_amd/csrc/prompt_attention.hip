@@ -173,11 +173,11 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
     const char* k_head = (const char*)((const uint16_t*)g.p.k + head_at);
     const char* v_head = (const char*)((const uint16_t*)g.p.v + head_at);
     // bf16: the n-th of 2 LOADS copies of a step, of this wavefront's part of the keys (first LOADS) or values, on its way into slot i % NST.  Lanes
-    // whose key nobody of the tile sees copy nothing: what is in LDS there has a probability of 0, and is finite, as values seen before are, or the zeros
-    // of the beginning.
-    struct Part { int64_t at; uint64_t lanes[LOADS]; bool whole; };            // whole: no copy is without lanes
-    auto part_of = [&](const Place& x) -> Part {
+    // whose key nobody of the tile sees copy nothing: such a key's logit does not matter, and its value, whose probability is 0, is set to 0 before.
+    struct Part { int64_t at; uint64_t lanes[LOADS]; bool whole, clear; };     // whole: no copy is without lanes; clear: values are to be set to 0
+    auto part_of = [&](int i, const Place& x) -> Part {
         Part y;
+        y.clear = !x.all && i < t1;
         y.at = 2 * x.at;
         y.whole = true;
 #pragma unroll
@@ -197,6 +197,14 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
         const uint32_t slot = ring + (i & (NST - 1)) * STAGE + half * HALF + t * 1024;
         asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
                      : : "s"(slot), "v"(lane_off[half][t]), "s"(base), "s"(y.lanes[t]) : "memory", "m0");
+    };
+    auto clear_values = [&](int i) {
+#pragma unroll
+        for (int t = 0; t < LOADS; ++t)
+            *(uint4*)(smem + (i & (NST - 1)) * STAGE + HALF + wave * GR * PITCH + t * 1024 + lane * 16) = make_uint4(0u, 0u, 0u, 0u);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0xC07F);        // lgkmcnt(0): before the copies
+        asm volatile("" ::: "memory");
     };
     // int8: codes and scales of the keys of stage i (half 0) or its values (half 1) into registers, and from there, widened, to LDS.  A load is 16
     // codes (two chunks) of a row.
@@ -411,16 +419,12 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
     Part part_k, part_v;                           // bf16: copied in this step, of stages i + AHEAD and i + AHEAD - 1
     if constexpr (!I8) {
 #pragma unroll
-        for (int x = 0; x < NST; ++x)
-#pragma unroll
-            for (int t = 0; t < LOADS; ++t) *(uint4*)(smem + x * STAGE + HALF + wave * GR * PITCH + t * 1024 + lane * 16) = make_uint4(0u, 0u, 0u, 0u);
-        __builtin_amdgcn_s_waitcnt(0xC07F);        // lgkmcnt(0)
-#pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            part_k = part_of(place_of(i, pages[i]));
+            part_k = part_of(i, place_of(i, pages[i]));
 #pragma unroll
             for (int n = 0; n < LOADS; ++n) copy(i, part_k, n);
             if (i > 0) {
+                if (part_v.clear) clear_values(i - 1);
 #pragma unroll
                 for (int n = LOADS; n < 2 * LOADS; ++n) copy(i - 1, part_v, n);
             }
@@ -445,6 +449,13 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
     meet(false);
     missing = __builtin_amdgcn_readfirstlane(*sm_missing) != 0;
     if (mine > 0) logits(0);
+    // Where two slots are all, step 0 writes keys to the slot that this has read: nobody may before everybody has.
+    if constexpr (NST == 2) {
+        __builtin_amdgcn_s_waitcnt(0xC07F);        // lgkmcnt(0)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    }
     // Step i: copies of the keys of stage i + AHEAD and the values of the stage before it begun, into slots that were read last in step i - 1;
     // softmax of stage i; products P V of stage i and K Q of stage i + 1; what step i + 1 needs waited for; barrier.  int8: the keys of stage i + 2 and
     // the values of stage i + 1 land, the next ones are fetched.  While one workgroup of the compute unit is at its softmax (vector unit), the other
@@ -453,7 +464,8 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
     // Copies spread over the softmax took as long as together before it.
     auto begin = [&](int i) {                      // of a step, before its softmax: copies on their way
         if constexpr (!I8) {
-            part_k = part_of(place_of(i + AHEAD, page_k));
+            part_k = part_of(i + AHEAD, place_of(i + AHEAD, page_k));
+            if (part_v.clear) clear_values(i + AHEAD - 1);
 #pragma unroll
             for (int n = 0; n < 2 * LOADS; ++n) copy(n < LOADS ? i + AHEAD : i + AHEAD - 1, n < LOADS ? part_k : part_v, n);
             page_k = page_of(i + AHEAD + 1);

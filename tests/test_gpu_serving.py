@@ -286,6 +286,38 @@ def test_attention_repeats_and_follows_its_stream():
             assert torch.equal(out, first)
 
 
+
+@pytest.mark.parametrize("int8", [False, True], ids=["bf16", "int8"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_attention_of_more_rows_than_the_device_holds_at_once(d, int8):
+    """40 requests that are one and the same: each has the first one's result to the bit, however their workgroups follow one another."""
+    new, kv, heads, kv_heads, copies = 260, 330, 32, 8, 40
+    req = Requests([new], [kv], 32)
+    cache = make_cache(req, kv_heads, d, int8, 11)
+    q, out = attend(req, cache, heads)
+    check_attention("one of %d, %d channels%s" % (copies, d, ", int8" if int8 else ""), req, cache, heads, q, out)
+    many = Requests([new], [kv], 32)
+    many.new, many.kv = [new] * copies, [kv] * copies
+    many.pages = np.repeat(req.pages, copies, axis=0)
+    many.start = (new * np.arange(copies + 1)).astype(np.int32)
+    many.kv_len = np.full(copies, kv, np.int32)
+    many.tokens = new * copies
+    all_q = q.repeat(copies, 1)
+    ctx, batch = new_ctx(), many.batch()
+    ctx.ensure_workspace(aser.aser_paged_attention_workspace_bytes(cache, batch, heads))
+    got = torch.empty(many.tokens, heads * d, dtype=torch.bfloat16, device=DEV)
+    for _ in range(3):
+        got.fill_(7.0)
+        ctx.check(aser.aser_paged_attention(ctx, all_q, cache, batch, got, scale=d ** -0.5))
+        torch.cuda.synchronize()
+        views = got.view(copies, new, heads * d)
+        wrong = [s for s in range(copies) if not torch.equal(views[s], views[0])]
+        assert not wrong, "requests %s differ from the first" % wrong
+        assert torch.equal(views[0], views[copies - 1])
+        bar = BF16 * out.float().abs().max().item()
+        assert (views[0].float() - out.float()).abs().max().item() <= 2 * bar
+
+
 # ------------------------------------------------------------------------------------------------ append
 APPEND = [
     # new, kv, heads, kv_heads, d, page, x, int8, norm, style, rot
