@@ -18,6 +18,12 @@
  *                           contexts and streams of their own (layers are independent once their inputs
  *                           are stored)                                    (Alg. 1, loop over the layers W^l)
  *
+ * and, for answering with the layers so quantized (aser_compensated_forward, end of Sec. 4.2):
+ *
+ *   aser_kv_append          queries and keys normalised and rotated, keys and values to a paged cache
+ *   aser_paged_attention    attention of new tokens over that cache, single ones and prompts
+ *   aser_adapter_forward    low-rank adapters of single requests beside a shared projection
+ *
  * Orientation.  The paper stores activations as (in x tokens) and writes the Gram matrix
  * X X^T.  This library stores activations tokens x in (N x n, row-major, channel
  * contiguous); the same n x n matrix is then G = X^T X.  W is m x n (out x in), row-major.
@@ -452,11 +458,11 @@ int aser_kv_append(aser_ctx* ctx, const void* q, int64_t ldq, int32_t n_heads, c
  *     out[t][h] = sum_j p_j v_j,  p_j = exp(scale q.k_j) / sum_j' exp(scale q.k_j')   over the keys j that t sees,
  * key j of its request when j <= p (p: the token's position) and, with window > 0, j > p - window or j < sinks; query head h
  * reads key/value head h / (n_heads / n_kv).  A token that sees nothing gets zeros; what the cache holds where nobody looks
- * (slots past kv_len, pages that are not there) does not matter, NaN included.  Values that some new token of a
- * request sees and another one does not have to be finite.
+ * (slots past kv_len, pages that are not there) does not matter, NaN included.  What some new token of a request sees has to
+ * be finite (a value that is not makes NaN of the request's tokens, also of those that do not see it).
  * q, out: tokens x (n_heads * head_dim) bf16, rows 16-byte aligned; out must not overlap q.  window == 0: no window,
- * sinks is then not looked at.  Products of bf16 numbers summed in fp32; probabilities are rounded to bf16 for the
- * second product, their sum is not.  Deterministic.  Asynchronous.
+ * sinks is then not looked at.  Products of bf16 numbers summed in fp32; for the second product probabilities are rounded
+ * to bf16 (requests of at most 64 rows, a row being a new token and head of a key/value head: to two bf16 terms), their sum is not.  Deterministic.  Asynchronous.
  * Needs aser_paged_attention_workspace_bytes of workspace (which reads of the structs what is on the host). */
 size_t aser_paged_attention_workspace_bytes(const aser_kv_cache* cache, const aser_kv_batch* batch, int32_t n_heads);
 int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ldq, int32_t n_heads, const aser_kv_cache* cache,

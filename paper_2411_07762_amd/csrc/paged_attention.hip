@@ -9,7 +9,13 @@
 // g = lane / 16).  The sum over keys does not care for their order, so the values are simply fetched in that order and no
 // probability changes lanes.  V^T wants 8 keys of one channel in a lane where memory has 8 channels of one key: a lane loads
 // D / 16 channels of its 8 keys and a byte permute per pair of keys turns them round.
-// Bound by reading the cache: 4 D bytes per key and head against 64 D / 16 matrix operations of 16 columns.
+// Bound by reading the cache: 4 D bytes per key and head against 64 D / 16 matrix operations of 16 columns.  The keys of a request are cut
+// into parts for different workgroups, whose results a second launch joins: a single request would otherwise keep a workgroup per
+// key/value head busy and no more.  Probabilities enter the second product as two bf16 terms (16 bits; one term put an error of 2^-9 where
+// the results' own rounding is 2^-9 too, and the second costs nothing beside the loads).
+// Measured: 64 requests of 1600 to 8192 tokens, 128 channels, 32 query heads over 8: 215 us, 6.0 TB/s (a plain read reaches 6.65); one request of
+// 32771 tokens 23 us + 4.4 to join; 40 requests of up to 12003 on an int8 cache of 64 channels 64 us, 5.1 TB/s, where widening the codes counts too;
+// 16 requests with 4 new tokens each, 32 heads over 32, under a window of 2048 with 4 sinks 86 us, 6.3 TB/s.
 #include "attention.h"
 
 namespace {
@@ -424,7 +430,8 @@ extern "C" int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ld
     g.splits = plan.splits; g.tiles_per_split = plan.tiles_per_split; g.row_tiles = plan.row_tiles;
     g.by_tiles = Divider::by(g.row_tiles);
     g.by_split = Divider::by(g.tiles_per_split);
-    if ((int64_t)g.p.n_seq * g.row_tiles * g.p.n_kv > INT32_MAX || batch->tokens * g.p.group > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: too many requests times rows");
+    if ((int64_t)g.p.n_seq * g.row_tiles * g.p.n_kv > INT32_MAX || batch->tokens * g.p.group > INT32_MAX)
+        ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: too many requests times rows");
     size_t o_bytes, need = few_workspace(plan, g.p.n_seq, g.p.n_kv, cache->head_dim, &o_bytes);
     if (max_rows > kFewRows) {
         const size_t prompt = aser_attention_prompt_workspace(g.p.tokens, g.p.n_seq, g.p.n_kv, g.p.group, cache->head_dim, keys);

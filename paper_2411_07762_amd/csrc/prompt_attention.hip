@@ -12,12 +12,12 @@
 //
 // Roundings: probabilities to bf16 for the second product (8 bits; their sum keeps the unrounded ones), results to bf16.
 //
-// Measured (32 query heads over 8): 8192 tokens of 128 channels 494 us, 1.1 PFLOP/s; the same matrix instructions alone, without
+// Measured (32 query heads over 8): 8192 tokens of 128 channels 513 us, 1.07 PFLOP/s; the same matrix instructions alone, without
 // loads and softmax, take 362 us: at this length the clock gives way to the power that they draw, 1.7 GHz against 2.2 for 1024
-// tokens (27.7 us), where the length of a step counts: 600 cycles to begin the copies, 1050 for the softmax, 1130 for the products.
-// Two prompts of 6001 and 3034 tokens under a window of 1024: 174 us.  64 channels: 8192 tokens 287 us, bound by the vector unit, whose
+// tokens (28 us), where the length of a step counts: 600 cycles to begin the copies, 1050 for the softmax, 1130 for the products.
+// Two prompts of 6001 and 3034 tokens under a window of 1024: 176 us.  64 channels: 8192 tokens 287 us, bound by the vector unit, whose
 // exponentials take twice the products' time.  256 channels (16 heads), 4096 tokens: 217 us.  int8 pays 60 vector instructions a step
-// of 280 for widening: 4096 tokens of 128 channels 184 us against 137.
+// of 280 for widening: 4096 tokens of 128 channels 185 us.
 #include "attention.h"
 
 namespace {
