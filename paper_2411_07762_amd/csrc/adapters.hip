@@ -142,7 +142,8 @@ __device__ __forceinline__ void three_terms(float x[8], bf16x8_t t[3]) {
 
 // Eight consecutive values of a row of n, from column c on; zeros past its end.  Rows start where they like: the loads take 16 bytes from any
 // element on.  last (the same for all lanes): the row may end inside or before these eight; then the row's last eight are loaded and moved down.
-// Before, rows of other than a multiple of 8 values were read one by one: 315 rows of 258 inputs, 675 outputs, rank 128 33.6 us, now 26.1; 1962 rows of 5035 outputs 51.5, now 39.4.
+// Before, rows of other than a multiple of 8 values were read one by one: 315 rows of 258 inputs, 675 outputs, rank 128 33.6 us, with these loads 26.1;
+// 1962 rows of 5035 outputs 51.5 and 39.4.
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -262,6 +263,29 @@ __global__ __launch_bounds__(256, NT > 1 ? 3 : 4) void adapter_up_kernel(AdArgs 
     const TileRows<NT> tr(g, blockIdx.x / blocks, lane);
     if (tr.adapter == -2 || (tr.adapter == -1 && g.Y0 == g.Y)) return;
     const bool some = tr.adapter >= 0;
+    // this lane's rows and outputs at the turn: rows 4 j + grp, four outputs from 4 col on.  Y0 is asked for first of all: 1962 rows of 5035 outputs
+    // 39.4 -> 36.6 us.
+    int out_row[4 * NT];
+#pragma unroll
+    for (int j = 0; j < 4 * NT; ++j) out_row[j] = __shfl(tr.row[j / 4], 4 * (j % 4) + grp);
+    float* turn = sm + wave * ROWS * PITCH;
+    const int64_t o0 = (int64_t)block * 256 + wave * 64;
+    const int64_t o = o0 + 4 * col;
+    const bool four = o + 4 <= g.m;
+    f32x4_t y[4 * NT];
+#pragma unroll
+    for (int j = 0; j < 4 * NT; ++j) {
+        y[j] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+        if (g.Y0 && out_row[j] >= 0 && o < g.m) {
+            const float* y0 = g.Y0 + (int64_t)out_row[j] * g.ldy0 + o;
+            if (four) y[j] = __builtin_nontemporal_load((const f32x4_any*)y0);
+            else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (o + e < g.m) y[j][e] = y0[e];
+            }
+        }
+    }
     bf16x8_t t[NT][KS][3];
     const uint16_t* b = g.B;
     if (some) {
@@ -303,29 +327,7 @@ __global__ __launch_bounds__(256, NT > 1 ? 3 : 4) void adapter_up_kernel(AdArgs 
             }
         __syncthreads();                           // before the turns below overwrite the sums
     }
-    // this lane's rows and outputs at the turn: rows 4 j + grp, four outputs from 4 col on
-    int out_row[4 * NT];
-#pragma unroll
-    for (int j = 0; j < 4 * NT; ++j) out_row[j] = __shfl(tr.row[j / 4], 4 * (j % 4) + grp);
-    float* turn = sm + wave * ROWS * PITCH;
-    const int64_t o0 = (int64_t)block * 256 + wave * 64;
     if (o0 >= g.m) return;
-    const int64_t o = o0 + 4 * col;
-    const bool four = o + 4 <= g.m;
-    f32x4_t y[4 * NT];
-#pragma unroll
-    for (int j = 0; j < 4 * NT; ++j) {
-        y[j] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-        if (g.Y0 && out_row[j] >= 0) {
-            const float* y0 = g.Y0 + (int64_t)out_row[j] * g.ldy0 + o;
-            if (four) y[j] = __builtin_nontemporal_load((const f32x4_any*)y0);
-            else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (o + e < g.m) y[j][e] = y0[e];
-            }
-        }
-    }
     if (some) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {

@@ -18,7 +18,7 @@
 // Two prompts of 6001 and 3034 tokens under a window of 1024: 176 us.  64 channels: 8192 tokens 287 us, bound by the vector unit, whose
 // exponentials take twice the products' time.  256 channels (16 heads), 4096 tokens: 217 us.  int8 pays 60 vector instructions a step
 // of 280 for widening: 4096 tokens of 128 channels 185 us.
-#include "attention.h"
+#include "few_rows.h"
 
 namespace {
 
@@ -103,7 +103,12 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
     float* sm_ks = (float*)(sm_missing + 4);      // int8: [stage % NSC][key] scales of K, then of V
     float* sm_vs = sm_ks + NSC * KEYS;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
-    const int u = g.by_kv(blockIdx.x), kvh = blockIdx.x - u * g.p.n_kv;
+    if ((int)blockIdx.x >= g.prompt_all) {         // behind the prompts: the rows of requests that have few
+        const int b = blockIdx.x - g.prompt_all, split = g.by_pairs(b);
+        few_rows<D, I8, false>(g, b - split * (g.p.n_seq * g.row_tiles * g.p.n_kv), split, *(FewShared<D>*)smem);
+        return;
+    }
+    const int part = g.by_blocks(blockIdx.x), block = blockIdx.x - part * g.prompt_blocks, u = g.by_kv(block), kvh = block - u * g.p.n_kv;
     const RowTile rt(g, u, BM, lane);
     if (rt.seq < 0) return;
     const int s = rt.seq, count = rt.count, kv = rt.kv, rows = count * g.p.group, group = g.p.group;
@@ -113,8 +118,8 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
     const int low_all = g.window > 0 ? base_pos + g.by_group(first) - g.window + 1 : 0;
     // stages of the tile, and this workgroup's: t0 .. t0 + t1 - 1, numbered from 0 below
     const KeyTiles<KEYS> kt(p_lo, p_hi, g.window, g.sinks);
-    const int per_split = stages_per_split(kt.total, g.splits), t0 = blockIdx.y * per_split, t1 = min(kt.total - t0, per_split);
-    if (t1 <= 0 && blockIdx.y > 0) return;
+    const int per_split = stages_per_split(kt.total, g.prompt_splits), t0 = part * per_split, t1 = min(kt.total - t0, per_split);
+    if (t1 <= 0 && part > 0) return;
     auto first_key = [&](int i) -> int { return kt.first_key(t0 + i); };
 
     // rows of this wavefront
@@ -524,9 +529,9 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
             for (int e = 0; e < 16; e += 4)
                 *(uint2*)(dst + 32 * d + 2 * e) = make_uint2(bf16_pair(o[d][e] * inv, o[d][e + 1] * inv), bf16_pair(o[d][e + 2] * inv, o[d][e + 3] * inv));
     } else {
-        const int64_t pr = ((int64_t)blockIdx.x * g.splits + blockIdx.y) * BM + (r - first);
-        if (h == 0) g.part_ml[pr] = make_float2(m, l);
-        float* dst = g.part_o + pr * D + 4 * h;
+        const int64_t pr = ((int64_t)block * g.prompt_splits + part) * BM + (r - first);
+        if (h == 0) g.prompt_ml[pr] = make_float2(m, l);
+        float* dst = g.prompt_o + pr * D + 4 * h;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -545,20 +550,20 @@ __global__ __launch_bounds__(256) void attn_prompt_join_kernel(AttnArgs g) {
     const int rows = rt.count * g.p.group, group = g.p.group;
     const int first = rt.tile * BM, base_pos = rt.kv - rt.count, r = first + in_tile;
     const KeyTiles<keys_of(D)> kt(max(base_pos + g.by_group(first), 0), base_pos + g.by_group(min(first + BM - 1, rows - 1)), g.window, g.sinks);
-    const int per = stages_per_split(kt.total, g.splits);
+    const int per = stages_per_split(kt.total, g.prompt_splits);
     if (per >= kt.total || r >= rows) return;
     const int used = (kt.total + per - 1) / per;
-    const int64_t pr = (int64_t)blockIdx.x * g.splits * BM + in_tile;
+    const int64_t pr = (int64_t)blockIdx.x * g.prompt_splits * BM + in_tile;
     float top = kNone;
-    for (int i = 0; i < used; ++i) top = fmaxf(top, g.part_ml[pr + (int64_t)i * BM].x);
+    for (int i = 0; i < used; ++i) top = fmaxf(top, g.prompt_ml[pr + (int64_t)i * BM].x);
     f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
     float l = 0.f;
 #pragma unroll 4
     for (int i = 0; i < used; ++i) {
-        const float2 ml = g.part_ml[pr + (int64_t)i * BM];
+        const float2 ml = g.prompt_ml[pr + (int64_t)i * BM];
         const float w = __builtin_amdgcn_exp2f(ml.x - top);
         l += w * ml.y;
-        acc += *(const f32x4_t*)(g.part_o + (pr + (int64_t)i * BM) * D + c) * w;
+        acc += *(const f32x4_t*)(g.prompt_o + (pr + (int64_t)i * BM) * D + c) * w;
     }
     const float inv = l > 0.f ? 1.f / l : 0.f;
     const int token = g.by_group(r);
@@ -587,17 +592,23 @@ PromptPlan plan_prompt(int64_t tokens, int64_t n_seq, int64_t n_kv, int64_t grou
 }
 
 template <int D, bool I8>
-int launch_prompt(aser_ctx* ctx, const AttnArgs& g, const PromptPlan& p) {
+int launch_prompt(aser_ctx* ctx, AttnArgs& g, const PromptPlan& p) {
     constexpr int KEYS = keys_of(D);
     constexpr size_t lds = slots_of(D) * (2 * KEYS * 2 * D) + 16 + (I8 ? 8 * KEYS * 8 : 0);
-    if (p.tiles * g.p.n_kv > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: too many rows");
-    const unsigned blocks = (unsigned)(p.tiles * g.p.n_kv);
+    static_assert(sizeof(FewShared<D>) <= lds, "the few rows' sums lie where the stages do");
+    const int64_t blocks = p.tiles * g.p.n_kv, pairs = (int64_t)g.p.n_seq * g.row_tiles * g.p.n_kv;
+    const int64_t all = blocks * p.splits + (g.few_rows > 0 ? pairs * g.splits : 0);
+    if (all > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: too many rows");
+    g.prompt_blocks = (int)blocks;
+    g.prompt_all = (int)(blocks * p.splits);
+    g.by_blocks = Divider::by((uint32_t)blocks);
+    g.by_pairs = Divider::by((uint32_t)pairs);
     auto kernel = attn_prompt_kernel<D, I8>;
     ASER_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    kernel<<<dim3(blocks, (unsigned)p.splits), 64 * W, lds, ctx->stream>>>(g);
+    kernel<<<(unsigned)all, 64 * W, lds, ctx->stream>>>(g);
     ASER_TRY(aser_check_launch(ctx, "attn_prompt_kernel"));
     if (p.splits > 1) {
-        attn_prompt_join_kernel<D><<<dim3(blocks, kRows / (256 / (D / 4))), 256, 0, ctx->stream>>>(g);
+        attn_prompt_join_kernel<D><<<dim3((unsigned)blocks, kRows / (256 / (D / 4))), 256, 0, ctx->stream>>>(g);
         return aser_check_launch(ctx, "attn_prompt_join_kernel");
     }
     return ASER_OK;
@@ -609,12 +620,12 @@ size_t aser_attention_prompt_workspace(int64_t tokens, int64_t n_seq, int64_t n_
     return plan_prompt(tokens, n_seq, n_kv, group, head_dim, keys).bytes;
 }
 
-int aser_attention_prompt(aser_ctx* ctx, AttnArgs g, int head_dim, int64_t keys) {
+int aser_attention_prompt(aser_ctx* ctx, AttnArgs g, int head_dim, int64_t keys, size_t ws_at) {
     const bool i8 = g.p.k_scale != nullptr;
     const PromptPlan p = plan_prompt(g.p.tokens, g.p.n_seq, g.p.n_kv, g.p.group, head_dim, keys);
-    g.splits = p.splits;
-    g.part_o = (float*)ctx->ws;
-    g.part_ml = (float2*)((char*)ctx->ws + p.o_bytes);
+    g.prompt_splits = p.splits;
+    g.prompt_o = (float*)((char*)ctx->ws + ws_at);
+    g.prompt_ml = (float2*)((char*)ctx->ws + ws_at + p.o_bytes);
     if (head_dim == 64) return i8 ? launch_prompt<64, true>(ctx, g, p) : launch_prompt<64, false>(ctx, g, p);
     if (head_dim == 128) return i8 ? launch_prompt<128, true>(ctx, g, p) : launch_prompt<128, false>(ctx, g, p);
     return i8 ? launch_prompt<256, true>(ctx, g, p) : launch_prompt<256, false>(ctx, g, p);
