@@ -61,6 +61,18 @@ struct KeyTiles {
     __device__ __forceinline__ int first_key(int i) const { return (i < sink_tiles ? i : main0 + i - sink_tiles) * TILE; }
 };
 
+// Request and row tile of the tile-th pair of them in the kernels for few rows.  A request's first row tile is often the only one with rows, and
+// workgroups go to the XCDs and their shader engines in turn: at every row_tiles-th place those with work would meet on a part of the device (31 tokens over 8192
+// keys each beside a request of 16 new tokens: 373 us, in this order 202).  So the order of a request's row tiles turns from request to request.
+struct FewTile {
+    int seq, row_tile;
+    __device__ __forceinline__ FewTile(const AttnArgs& g, int tile) {
+        seq = g.by_tiles(tile);
+        const int turn = seq + g.by_tiles(seq), x = tile - seq * g.row_tiles - (turn - g.by_tiles(turn) * g.row_tiles);
+        row_tile = x < 0 ? x + g.row_tiles : x;
+    }
+};
+
 // Words that no kernel of this call writes, through the scalar cache: beside copies into LDS the compiler takes vector loads for them, and
 // waits for those together with every copy in flight.
 typedef const __attribute__((address_space(4))) int32_t* ScalarInts;

@@ -41,7 +41,9 @@ __device__ __forceinline__ void few_rows(const AttnArgs& g, int block, int split
     constexpr int KS = D / 32;                    // steps of 32 channels in K Q^T
     constexpr int NB = D / 16;                    // channels of a lane in V^T, and accumulators of O^T
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, grp = lane >> 4;
-    const int tile = g.by_kv(block), kvh = block - tile * g.p.n_kv, s = g.by_tiles(tile), rt = tile - s * g.row_tiles;
+    const int tile = g.by_kv(block), kvh = block - tile * g.p.n_kv;
+    const FewTile ft(g, tile);
+    const int s = ft.seq, rt = ft.row_tile;
     int64_t row0;
     const int count = (int)request_rows(g.p, s, &row0), kv = request_kv_len(g.p, s);
     const int rows = count * g.p.group - rt * 16;                            // rows of this tile, if positive

@@ -19,7 +19,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs g) {
     __shared__ f32x4_t sm[SL][CL];
     __shared__ float sm_w[kMaxSplits], sm_m[4], sm_l[4];
     const int tid = threadIdx.x, cl = tid % CL, sl = tid / CL, r = blockIdx.y;
-    const int tile = g.by_kv(blockIdx.x), kvh = blockIdx.x - tile * g.p.n_kv, s = g.by_tiles(tile), rt = tile - s * g.row_tiles;
+    const int tile = g.by_kv(blockIdx.x), kvh = blockIdx.x - tile * g.p.n_kv;
+    const FewTile ft(g, tile);
+    const int s = ft.seq, rt = ft.row_tile;
     const int64_t pr = (int64_t)blockIdx.x * g.splits * 16 + r;
     float2 ml = g.part_ml[pr + (int64_t)min(tid, g.splits - 1) * 16];
     int64_t row0;
@@ -65,12 +67,13 @@ struct Plan { int most_splits, splits, tiles_per_split, row_tiles; };
 // Splits of the key axis: several thousand workgroups even out requests of different lengths, as long as each of a workgroup's four
 // wavefronts has 8 steps; a call of few requests takes shorter ones, down to two steps, to fill the device.  (Equal shares of all keys
 // for a fixed number of workgroups came out no faster on ragged batches and slower on others.)  keys: the most that a row sees.
-// Workspace is there for most_splits, which grows with the keys (a window asks for no more than none does).
+// Where a call has prompts too, most of the others are single tokens: one row tile of a request is counted (31 tokens over 8192 keys and a prompt of 1000
+// 209 -> 203 us).  Workspace is there for most_splits, which grows with the keys (a window asks for no more than none does).
 Plan plan_few(int64_t n_seq, int64_t n_kv, int64_t group, int64_t max_new, int64_t keys) {
     Plan p;
     const int64_t rows = max_new * group < kFewRows ? max_new * group : kFewRows;
     p.row_tiles = (int)ceil_div64(rows, 16);
-    const int64_t tiles = keys / kTile + 3, pairs = n_seq * n_kv * p.row_tiles;
+    const int64_t tiles = keys / kTile + 3, pairs = n_seq * n_kv * (max_new * group > kFewRows ? 1 : p.row_tiles);
     int64_t splits = ceil_div64(4096, pairs);
     if (splits > tiles / 32) splits = tiles / 32;
     if (splits * pairs < 1024) {

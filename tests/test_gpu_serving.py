@@ -287,6 +287,19 @@ def test_attention_repeats_and_follows_its_stream():
 
 
 
+@pytest.mark.parametrize("kv_heads", [1, 2, 8])
+@pytest.mark.parametrize("longest", [5, 12, 16, 40])
+def test_attention_of_single_tokens_beside_longer_requests(longest, kv_heads):
+    """Requests of one to four row tiles, and a prompt, in one call."""
+    new = [1, longest, 1, 1, 3, 1, max(longest // 2, 1), 1, 0, 1, 4, 1]
+    kv = [700, 90, 1, 333, 64, 2000, 150, 17, 40, 512, 31, 1025]
+    req = Requests(new, kv, 32, seed=longest)
+    heads = 4 * kv_heads
+    cache = make_cache(req, kv_heads, 64, False, 21)
+    q, out = attend(req, cache, heads)
+    check_attention("single tokens beside %d, %d key/value heads" % (longest, kv_heads), req, cache, heads, q, out)
+
+
 @pytest.mark.parametrize("int8", [False, True], ids=["bf16", "int8"])
 @pytest.mark.parametrize("d", [64, 128, 256])
 def test_attention_of_more_rows_than_the_device_holds_at_once(d, int8):
