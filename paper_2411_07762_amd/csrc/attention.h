@@ -33,7 +33,7 @@ struct AttnArgs {
     int splits, tiles_per_split, row_tiles;       // the kernel for few rows: parts of the key axis, their steps, most row tiles of a request
     float* part_o; float2* part_ml;               // results of splits: [row tile and head][split][row][D], [..][split][row] (maximum, sum)
     // the kernel for prompts: the same of its own, and its grid: tiles times heads, times splits, then the few rows' (by_pairs: times splits again)
-    int prompt_splits, prompt_blocks, prompt_all;
+    int prompt_splits, prompt_blocks, prompt_all, prompt_joins;
     Divider by_blocks, by_pairs;
     float* prompt_o; float2* prompt_ml;
 };
@@ -84,7 +84,7 @@ __device__ __forceinline__ uint32_t codes_pair(uint32_t w) {
     return upper_halves((float)(int8_t)(w >> (8 * B)), (float)(int8_t)(w >> (8 * B + 8)));
 }
 
-// prompt_attention.hip: all requests of a call where some may have more than few_rows rows; keys: the most that a row sees.  Its workspace begins at
-// byte ws_at of ctx's.  The requests of few rows are left to be joined.
+// prompt_attention.hip: a call where some request may have more than few_rows rows; keys: the most that a row sees.  Its workspace begins at
+// byte ws_at of ctx's, behind that of the requests of few rows.
 size_t aser_attention_prompt_workspace(int64_t tokens, int64_t n_seq, int64_t n_kv, int64_t group, int head_dim, int64_t keys);
 int aser_attention_prompt(aser_ctx* ctx, AttnArgs g, int head_dim, int64_t keys, size_t ws_at);

@@ -20,6 +20,7 @@
 #include "attention.h"
 
 constexpr int kTile = 32;                         // keys of a step
+constexpr int kMaxSplits = 256;                   // parts of a request's keys: a thread of the join for each
 
 // Loads N words; ONCE: and says that nobody reads them again.
 template <int N, bool ONCE>
@@ -287,4 +288,55 @@ __device__ __forceinline__ void few_rows(const AttnArgs& g, int block, int split
 #pragma unroll
         for (int c = 0; c < PER; c += 4) *(f32x4_t*)(g.part_o + pr * D + ch + c) = (f32x4_t){acc[c], acc[c + 1], acc[c + 2], acc[c + 3]};
     }
+}
+
+// Joins the splits of one row: o = sum_s w_s o_s / sum_s w_s l_s, w_s = exp2(m_s - max m).  The maxima are asked for before the
+// request's length says how many of them there are: one wait less in a kernel that is nothing but waits.
+template <int D>
+struct FewJoin { f32x4_t sm[1024 / D][D / 4]; float w[kMaxSplits], m[4], l[4]; };
+
+// block: as in few_rows; r: row of the tile
+template <int D>
+__device__ __forceinline__ void few_join(const AttnArgs& g, int block, int r, FewJoin<D>& x) {
+    constexpr int CL = D / 4, SL = 256 / CL;      // lanes over channels (4 each), splits side by side
+    const int tid = threadIdx.x, cl = tid % CL, sl = tid / CL;
+    const int tile = g.by_kv(block), kvh = block - tile * g.p.n_kv;
+    const FewTile ft(g, tile);
+    const int s = ft.seq, rt = ft.row_tile;
+    const int64_t pr = (int64_t)block * g.splits * 16 + r;
+    float2 ml = g.part_ml[pr + (int64_t)min(tid, g.splits - 1) * 16];
+    int64_t row0;
+    const int count = (int)request_rows(g.p, s, &row0), kv = request_kv_len(g.p, s), row = rt * 16 + r;
+    if (row >= count * g.p.group || count * g.p.group > g.few_rows) return;
+    const int last_row = min(rt * 16 + 15, count * g.p.group - 1);
+    const KeyTiles<kTile> kt(max(kv - count + g.by_group(rt * 16), 0), kv - count + g.by_group(last_row), g.window, g.sinks);
+    const int used = g.by_split(kt.total + g.tiles_per_split - 1);
+    if (used <= 1) return;
+    if (tid >= used) ml = make_float2(kNone, 0.f);
+    float top = ml.x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if ((tid & 63) == 0) x.m[tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(x.m[0], x.m[1]), fmaxf(x.m[2], x.m[3]));
+    const float w = tid < used ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
+    float ll = w * ml.y;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) ll += __shfl_xor(ll, o);
+    if ((tid & 63) == 0) x.l[tid >> 6] = ll;
+    x.w[tid] = w;
+    __syncthreads();
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int i = sl; i < used; i += SL) acc += *(const f32x4_t*)(g.part_o + (pr + (int64_t)i * 16) * D + 4 * cl) * x.w[i];
+    x.sm[sl][cl] = acc;
+    __syncthreads();
+    if (sl) return;
+#pragma unroll
+    for (int i = 1; i < SL; ++i) acc += x.sm[i][cl];
+    ll = (x.l[0] + x.l[1]) + (x.l[2] + x.l[3]);
+    const float inv = ll > 0.f ? 1.f / ll : 0.f;
+    const int token = g.by_group(row);
+    uint16_t* dst = g.out + (row0 + token) * g.ldo + (int64_t)(kvh * g.p.group + row - token * g.p.group) * D + 4 * cl;
+    *(uint2*)dst = make_uint2(bf16_pair(acc[0] * inv, acc[1] * inv), bf16_pair(acc[2] * inv, acc[3] * inv));
 }

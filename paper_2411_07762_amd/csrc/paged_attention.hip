@@ -3,61 +3,16 @@
 
 namespace {
 
-constexpr int kMaxSplits = 256;                   // a thread of the joining kernel for each
-
 template <int D, bool I8, bool ONCE>
 __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void attn_few_kernel(AttnArgs g) {
     __shared__ FewShared<D> sm;
     few_rows<D, I8, ONCE>(g, blockIdx.x, blockIdx.y, sm);
 }
 
-// Joins the splits of one row: o = sum_s w_s o_s / sum_s w_s l_s, w_s = exp2(m_s - max m).  The maxima are asked for before the
-// request's length says how many of them there are: one wait less in a kernel that is nothing but waits.
 template <int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs g) {
-    constexpr int CL = D / 4, SL = 256 / CL;      // lanes over channels (4 each), splits side by side
-    __shared__ f32x4_t sm[SL][CL];
-    __shared__ float sm_w[kMaxSplits], sm_m[4], sm_l[4];
-    const int tid = threadIdx.x, cl = tid % CL, sl = tid / CL, r = blockIdx.y;
-    const int tile = g.by_kv(blockIdx.x), kvh = blockIdx.x - tile * g.p.n_kv;
-    const FewTile ft(g, tile);
-    const int s = ft.seq, rt = ft.row_tile;
-    const int64_t pr = (int64_t)blockIdx.x * g.splits * 16 + r;
-    float2 ml = g.part_ml[pr + (int64_t)min(tid, g.splits - 1) * 16];
-    int64_t row0;
-    const int count = (int)request_rows(g.p, s, &row0), kv = request_kv_len(g.p, s), row = rt * 16 + r;
-    if (row >= count * g.p.group || count * g.p.group > g.few_rows) return;
-    const int last_row = min(rt * 16 + 15, count * g.p.group - 1);
-    const KeyTiles<kTile> kt(max(kv - count + g.by_group(rt * 16), 0), kv - count + g.by_group(last_row), g.window, g.sinks);
-    const int used = g.by_split(kt.total + g.tiles_per_split - 1);
-    if (used <= 1) return;
-    if (tid >= used) ml = make_float2(kNone, 0.f);
-    float top = ml.x;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    if ((tid & 63) == 0) sm_m[tid >> 6] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
-    const float w = tid < used ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
-    float ll = w * ml.y;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) ll += __shfl_xor(ll, o);
-    if ((tid & 63) == 0) sm_l[tid >> 6] = ll;
-    sm_w[tid] = w;
-    __syncthreads();
-    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int i = sl; i < used; i += SL) acc += *(const f32x4_t*)(g.part_o + (pr + (int64_t)i * 16) * D + 4 * cl) * sm_w[i];
-    sm[sl][cl] = acc;
-    __syncthreads();
-    if (sl) return;
-#pragma unroll
-    for (int i = 1; i < SL; ++i) acc += sm[i][cl];
-    ll = (sm_l[0] + sm_l[1]) + (sm_l[2] + sm_l[3]);
-    const float inv = ll > 0.f ? 1.f / ll : 0.f;
-    const int token = g.by_group(row);
-    uint16_t* dst = g.out + (row0 + token) * g.ldo + (int64_t)(kvh * g.p.group + row - token * g.p.group) * D + 4 * cl;
-    *(uint2*)dst = make_uint2(bf16_pair(acc[0] * inv, acc[1] * inv), bf16_pair(acc[2] * inv, acc[3] * inv));
+    __shared__ FewJoin<D> x;
+    few_join<D>(g, blockIdx.x, blockIdx.y, x);
 }
 
 constexpr int kFewRows = 64;                      // requests of more rows take the kernel for prompts
@@ -95,7 +50,7 @@ int64_t keys_seen(int64_t max_kv, int64_t max_new, int64_t window, int64_t sinks
 // One row tile reads its keys once.  Then the hint that a line is not wanted again pays: 64 requests of up to 8192 tokens, 128 channels, bf16 242 -> 223 us,
 // int8 138 -> 131; not where several row tiles share the keys (142 -> 195 with four).
 template <int D>
-int run_few(aser_ctx* ctx, const AttnArgs& g) {
+int run_few(aser_ctx* ctx, const AttnArgs& g, int64_t max_rows) {
     const dim3 grid((unsigned)((int64_t)g.p.n_seq * g.row_tiles * g.p.n_kv), (unsigned)g.splits);
     const bool once = g.row_tiles == 1;
     if (g.p.k_scale) {
@@ -105,12 +60,9 @@ int run_few(aser_ctx* ctx, const AttnArgs& g) {
         if (once) attn_few_kernel<D, false, true><<<grid, 256, 0, ctx->stream>>>(g);
         else attn_few_kernel<D, false, false><<<grid, 256, 0, ctx->stream>>>(g);
     }
-    return aser_check_launch(ctx, "attn_few_kernel");
-}
-template <int D>
-int join_few(aser_ctx* ctx, const AttnArgs& g, int64_t max_rows) {
+    ASER_TRY(aser_check_launch(ctx, "attn_few_kernel"));
     if (g.splits == 1) return ASER_OK;
-    attn_join_kernel<D><<<dim3((unsigned)(g.p.n_seq * g.row_tiles * g.p.n_kv), (unsigned)(max_rows < 16 ? max_rows : 16)), 256, 0, ctx->stream>>>(g);
+    attn_join_kernel<D><<<dim3(grid.x, (unsigned)(max_rows < 16 ? max_rows : 16)), 256, 0, ctx->stream>>>(g);
     return aser_check_launch(ctx, "attn_join_kernel");
 }
 
@@ -165,10 +117,9 @@ extern "C" int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ld
     g.part_ml = (float2*)((char*)ctx->ws + o_bytes);
     if (max_rows > kFewRows) {
         if (g.p.n_seq == 1) g.few_rows = -1;      // one request: it is for the kernel for prompts, whatever it is
-        ASER_TRY(aser_attention_prompt(ctx, g, cache->head_dim, keys, few));
-        if (g.p.n_seq == 1) return ASER_OK;
-    } else {
-        ASER_TRY(cache->head_dim == 64 ? run_few<64>(ctx, g) : cache->head_dim == 128 ? run_few<128>(ctx, g) : run_few<256>(ctx, g));
+        return aser_attention_prompt(ctx, g, cache->head_dim, keys, few);
     }
-    return cache->head_dim == 64 ? join_few<64>(ctx, g, max_rows) : cache->head_dim == 128 ? join_few<128>(ctx, g, max_rows) : join_few<256>(ctx, g, max_rows);
+    if (cache->head_dim == 64) return run_few<64>(ctx, g, max_rows);
+    if (cache->head_dim == 128) return run_few<128>(ctx, g, max_rows);
+    return run_few<256>(ctx, g, max_rows);
 }

@@ -539,12 +539,22 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
     }
 }
 
-// Joins the splits of a row tile: o = sum_s w_s o_s / sum_s w_s l_s, w_s = exp2(m_s - max m); four channels of a row per thread.
+// Joins the splits of a row tile: o = sum_s w_s o_s / sum_s w_s l_s, w_s = exp2(m_s - max m); four channels of a row per thread.  Behind the prompts'
+// workgroups come those of the rows of requests that have few.
+template <int D>
+constexpr int join_blocks = kRows / (256 / (D / 4));       // of a row tile and head
+
 template <int D>
 __global__ __launch_bounds__(256) void attn_prompt_join_kernel(AttnArgs g) {
     constexpr int CL = D / 4, R = 256 / CL, BM = kRows;
-    const int tid = threadIdx.x, c = tid % CL * 4, in_tile = blockIdx.y * R + tid / CL;
-    const int u = g.by_kv(blockIdx.x), kvh = blockIdx.x - u * g.p.n_kv;
+    __shared__ FewJoin<D> few;
+    if ((int)blockIdx.x >= g.prompt_joins) {
+        const int b = blockIdx.x - g.prompt_joins;
+        few_join<D>(g, b >> 4, b & 15, few);
+        return;
+    }
+    const int tid = threadIdx.x, block = blockIdx.x / join_blocks<D>, c = tid % CL * 4, in_tile = blockIdx.x % join_blocks<D> * R + tid / CL;
+    const int u = g.by_kv(block), kvh = block - u * g.p.n_kv;
     const RowTile rt(g, u, BM, tid & 63);
     if (rt.seq < 0) return;
     const int rows = rt.count * g.p.group, group = g.p.group;
@@ -553,7 +563,7 @@ __global__ __launch_bounds__(256) void attn_prompt_join_kernel(AttnArgs g) {
     const int per = stages_per_split(kt.total, g.prompt_splits);
     if (per >= kt.total || r >= rows) return;
     const int used = (kt.total + per - 1) / per;
-    const int64_t pr = (int64_t)blockIdx.x * g.prompt_splits * BM + in_tile;
+    const int64_t pr = (int64_t)block * g.prompt_splits * BM + in_tile;
     float top = kNone;
     for (int i = 0; i < used; ++i) top = fmaxf(top, g.prompt_ml[pr + (int64_t)i * BM].x);
     f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
@@ -607,11 +617,12 @@ int launch_prompt(aser_ctx* ctx, AttnArgs& g, const PromptPlan& p) {
     ASER_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
     kernel<<<(unsigned)all, 64 * W, lds, ctx->stream>>>(g);
     ASER_TRY(aser_check_launch(ctx, "attn_prompt_kernel"));
-    if (p.splits > 1) {
-        attn_prompt_join_kernel<D><<<dim3((unsigned)blocks, kRows / (256 / (D / 4))), 256, 0, ctx->stream>>>(g);
-        return aser_check_launch(ctx, "attn_prompt_join_kernel");
-    }
-    return ASER_OK;
+    const int64_t joins = p.splits > 1 ? blocks * join_blocks<D> : 0, few = g.few_rows > 0 && g.splits > 1 ? pairs * 16 : 0;
+    if (joins + few == 0) return ASER_OK;
+    if (joins + few > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: too many rows");
+    g.prompt_joins = (int)joins;
+    attn_prompt_join_kernel<D><<<(unsigned)(joins + few), 256, 0, ctx->stream>>>(g);
+    return aser_check_launch(ctx, "attn_prompt_join_kernel");
 }
 
 }  // namespace
