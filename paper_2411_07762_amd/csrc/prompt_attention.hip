@@ -1,4 +1,4 @@
-// Attention of prompts over the paged cache: the formulas and the transposed products of paged_attention.hip on tiles that the
+// Attention of prompts over the paged cache: the formulas and the transposed products of few_rows.h on tiles that the
 // matrix instructions bound instead of memory, 4 D operations per visible key, row and head.
 //
 // A wavefront owns 32 rows (a row: one query head of one new token; the heads that share a key/value head lie next to each
@@ -12,12 +12,12 @@
 //
 // Roundings: probabilities to bf16 for the second product (8 bits; their sum keeps the unrounded ones), results to bf16.
 //
-// Measured (32 query heads over 8): 8192 tokens of 128 channels 513 us, 1.07 PFLOP/s; the same matrix instructions alone, without
-// loads and softmax, take 362 us: at this length the clock gives way to the power that they draw, 1.7 GHz against 2.2 for 1024
+// Measured (32 query heads over 8): 8192 tokens of 128 channels 502 to 522 us on different devices, 1.05 to 1.1 PFLOP/s; the same
+// matrix instructions alone, without loads and softmax, take 362 us: at this length the clock gives way to the power that they draw, 1.7 GHz against 2.2 for 1024
 // tokens (28 us), where the length of a step counts: 600 cycles to begin the copies, 1050 for the softmax, 1130 for the products.
-// Two prompts of 6001 and 3034 tokens under a window of 1024: 176 us.  64 channels: 8192 tokens 287 us, bound by the vector unit, whose
+// Two prompts of 6001 and 3034 tokens under a window of 1024: 173 us.  64 channels: 8192 tokens 290 to 305 us, bound by the vector unit, whose
 // exponentials take twice the products' time.  256 channels (16 heads), 4096 tokens: 217 us.  int8 pays 60 vector instructions a step
-// of 280 for widening: 4096 tokens of 128 channels 185 us.
+// of 280 for widening: 4096 tokens of 128 channels 188 us.
 #include "few_rows.h"
 
 namespace {
