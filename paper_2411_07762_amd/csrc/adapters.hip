@@ -371,7 +371,8 @@ AdPlan plan_adapters(int64_t rows, int64_t n, int r) {
     const bool few = rows <= kFewRows;
     p.tok = few ? 16 : 16 * kManyTiles;
     p.tiles = (int)(few ? ceil_div64(rows, p.tok) * rows : ceil_div64(rows, p.tok) + kMaxAdapters + 1);
-    // parts of the channel axis: about 512 workgroups, at least 256 channels each
+    // parts of the channel axis: about 512 workgroups, at least 256 channels each (1024 workgroups: 4099 rows of 4096 inputs, 14336 outputs 140 -> 153 us,
+    // whose many blocks of outputs add the parts each; 3434 rows of 7459 inputs, 869 outputs 64.5 -> 59.1)
     const int64_t groups = few ? rows : ceil_div64(rows, p.tok);
     int64_t parts = ceil_div64(512, groups);
     if (parts > ceil_div64(n, 256)) parts = ceil_div64(n, 256);
