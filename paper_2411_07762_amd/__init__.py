@@ -222,6 +222,18 @@ def _dtype_code(t) -> int:
     return code
 
 
+_DTYPES = {}
+
+
+def _dtype(name: str):
+    """The torch dtype of that name (importing this package does not import torch)."""
+    dtype = _DTYPES.get(name)
+    if dtype is None:
+        import torch
+        dtype = _DTYPES[name] = getattr(torch, name)
+    return dtype
+
+
 class Context:
     """Owns an aser_ctx bound to a device and a HIP stream (torch's current stream by default)."""
 
@@ -512,6 +524,17 @@ def _token_rows(t, tokens: int):
     return t.data_ptr(), ld, cols
 
 
+def _head_weights(t, channels: int):
+    """Address of a norm's weights; the kernel reads `channels` floats from it on."""
+    if t is None:
+        return None
+    if t.dtype != _dtype("float32"):
+        raise TypeError("norm weights must be float32")
+    if t.numel() != channels or not t.is_contiguous():
+        raise ValueError("norm weights must be contiguous, one for each channel of a head")
+    return t.data_ptr()
+
+
 def aser_kv_append(ctx: Context, q, k, v, cache: KvCache, batch: KvBatch, q_out, *, rope_cos=None, rope_sin=None, interleaved: bool = False,
                    q_norm=None, k_norm=None, eps: float = 1e-6) -> int:
     """q, k, v: tokens x (heads * channels), bfloat16 or float32 alike (q and q_out may be None); rope_cos, rope_sin: positions x
@@ -519,13 +542,18 @@ def aser_kv_append(ctx: Context, q, k, v, cache: KvCache, batch: KvBatch, q_out,
     dt, tokens, opts = _dtype_code(k), batch.tokens, None
     if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
         raise TypeError("q, k and v must have one dtype")
+    if (rope_cos is None) != (rope_sin is None):
+        raise ValueError("rope_cos and rope_sin go together")
     if rope_cos is not None or q_norm is not None or k_norm is not None:
         n_pos = half = 0
         if rope_cos is not None:
+            if rope_cos.dtype != _dtype("float32") or rope_sin.dtype != rope_cos.dtype:
+                raise TypeError("rope_cos and rope_sin must be float32")
             n_pos, half = rope_cos.shape
             if not (rope_cos.is_contiguous() and rope_sin.is_contiguous() and rope_sin.shape == rope_cos.shape):
                 raise ValueError("rope_cos and rope_sin must be contiguous and alike")
-        opts = ctypes.byref(aser_qk_opts(_ptr(rope_cos), _ptr(rope_sin), _ptr(q_norm), _ptr(k_norm), n_pos, 2 * half, 1 if interleaved else 0, eps))
+        opts = ctypes.byref(aser_qk_opts(_ptr(rope_cos), _ptr(rope_sin), _head_weights(q_norm, cache.head_dim), _head_weights(k_norm, cache.head_dim),
+                                         n_pos, 2 * half, 1 if interleaved else 0, eps))
     kp, ldk, _ = _token_rows(k, tokens)
     vp, ldv, _ = _token_rows(v, tokens)
     qp = op = None

@@ -1,0 +1,70 @@
+"""What the Python binding of the serving operators refuses before it hands addresses to the library: a stub stands for the library,
+so that a call that is let through is seen and nothing runs."""
+import pytest
+import torch
+
+import paper_2411_07762_amd as aser
+
+
+class Library:
+    """Takes every call, remembers its name and returns ASER_OK."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append(name)
+            return aser.ASER_OK
+        return call
+
+
+@pytest.fixture
+def ctx():
+    c = aser.Context.__new__(aser.Context)
+    c._lib, c.handle, c.device, c._ws, c._ws_bytes = Library(), 1, torch.zeros(1).get_device(), None, 0
+    return c
+
+
+def zeros(*shape, dtype=torch.float32):
+    return torch.zeros(*shape, dtype=dtype)
+
+
+TOKENS, HEADS, KV, D, PAGE = 6, 4, 2, 64, 16
+
+
+def cache():
+    return aser.KvCache(*(zeros(5, KV, PAGE, D, dtype=torch.bfloat16) for _ in range(2)))
+
+
+def batch(columns=3, max_kv=40):
+    ints = torch.int32
+    return aser.KvBatch(zeros(3, dtype=ints), zeros(2, dtype=ints), zeros(2, columns, dtype=ints), tokens=TOKENS, max_new=4, max_kv=max_kv)
+
+
+def append(ctx, **kw):
+    a = dict(q=zeros(TOKENS, HEADS * D), k=zeros(TOKENS, KV * D), v=zeros(TOKENS, KV * D), out=zeros(TOKENS, HEADS * D, dtype=torch.bfloat16),
+             rope_cos=zeros(64, D // 2), rope_sin=zeros(64, D // 2), q_norm=zeros(D), k_norm=zeros(D))
+    a.update(kw)
+    return aser.aser_kv_append(ctx, a.pop("q"), a.pop("k"), a.pop("v"), a.pop("cache", None) or cache(), a.pop("batch", None) or batch(), a.pop("out"), **a)
+
+
+def refused(ctx, error, call, **kw):
+    with pytest.raises(error):
+        call(ctx, **kw)
+    assert not ctx._lib.calls, "the library was called"
+
+
+@pytest.mark.parametrize("kw,error", [
+    (dict(q_norm=zeros(D, dtype=torch.bfloat16)), TypeError), (dict(k_norm=zeros(D, dtype=torch.float64)), TypeError),
+    (dict(q_norm=zeros(3)), ValueError), (dict(k_norm=zeros(2 * D)), ValueError),
+    (dict(k_norm=zeros(2 * D)[::2]), ValueError),
+    (dict(rope_cos=zeros(64, D // 2, dtype=torch.bfloat16), rope_sin=zeros(64, D // 2, dtype=torch.bfloat16)), TypeError),
+    (dict(rope_sin=zeros(64, D // 2, dtype=torch.bfloat16)), TypeError), (dict(rope_sin=None), ValueError),
+    (dict(rope_cos=None, q_norm=None, k_norm=None), ValueError), (dict(rope_cos=None), ValueError), (dict(rope_sin=zeros(63, D // 2)), ValueError),
+    (dict(rope_cos=zeros(64, D)[:, ::2]), ValueError),
+])
+def test_append_refuses_tables_and_weights_that_the_kernel_would_misread(ctx, kw, error):
+    refused(ctx, error, append, **kw)
+    assert append(ctx) == aser.ASER_OK and ctx._lib.calls == ["aser_kv_append"]
+    assert append(ctx, rope_cos=None, rope_sin=None, q_norm=None, k_norm=zeros(1, D)) == aser.ASER_OK
