@@ -484,7 +484,7 @@ class KvCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.c = aser_kv_cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), k.shape[0], k.stride(0), k.stride(1), k.stride(2),
                                ASER_KV_INT8 if k.dtype == torch.int8 else ASER_KV_BF16, k.shape[2], k.shape[1], k.shape[3])
-        self.ref, self.head_dim = ctypes.byref(self.c), k.shape[3]
+        self.ref, self.head_dim, self.kv_width = ctypes.byref(self.c), k.shape[3], k.shape[1] * k.shape[3]
 
     @classmethod
     def empty(cls, n_pages: int, n_kv: int, page_size: int, head_dim: int, int8: bool = False, device: int = 0):
@@ -524,6 +524,13 @@ def _token_rows(t, tokens: int):
     return t.data_ptr(), ld, cols
 
 
+def _heads(width: int, cache: KvCache) -> int:
+    heads, rest = divmod(width, cache.head_dim)
+    if rest:
+        raise ValueError("queries must have whole heads")
+    return heads
+
+
 def _head_weights(t, channels: int):
     """Address of a norm's weights; the kernel reads `channels` floats from it on."""
     if t is None:
@@ -554,8 +561,10 @@ def aser_kv_append(ctx: Context, q, k, v, cache: KvCache, batch: KvBatch, q_out,
                 raise ValueError("rope_cos and rope_sin must be contiguous and alike")
         opts = ctypes.byref(aser_qk_opts(_ptr(rope_cos), _ptr(rope_sin), _head_weights(q_norm, cache.head_dim), _head_weights(k_norm, cache.head_dim),
                                          n_pos, 2 * half, 1 if interleaved else 0, eps))
-    kp, ldk, _ = _token_rows(k, tokens)
-    vp, ldv, _ = _token_rows(v, tokens)
+    kp, ldk, k_width = _token_rows(k, tokens)
+    vp, ldv, v_width = _token_rows(v, tokens)
+    if k_width < cache.kv_width or v_width < cache.kv_width:
+        raise ValueError("k and v must have the channels of all key/value heads")
     qp = op = None
     ldq = ldo = heads = 0
     if q is not None:
@@ -563,7 +572,7 @@ def aser_kv_append(ctx: Context, q, k, v, cache: KvCache, batch: KvBatch, q_out,
         op, ldo, out_width = _token_rows(q_out, tokens)
         if _dtype_code(q_out) != ASER_DTYPE_BF16 or out_width < width:
             raise TypeError("q_out must be bfloat16, as wide as q")
-        heads = width // cache.head_dim
+        heads = _heads(width, cache)
     return ctx._lib.aser_kv_append(ctx.handle, qp, ldq, heads, kp, ldk, vp, ldv, dt, opts, cache.ref, batch.ref, op, ldo)
 
 
@@ -577,7 +586,7 @@ def aser_paged_attention(ctx: Context, q, cache: KvCache, batch: KvBatch, out, *
     op, ldo, out_width = _token_rows(out, batch.tokens)
     if _dtype_code(q) != ASER_DTYPE_BF16 or out.dtype != q.dtype or out_width < width:
         raise TypeError("q and out must be bfloat16, out as wide as q")
-    return ctx._lib.aser_paged_attention(ctx.handle, qp, ldq, width // cache.head_dim, cache.ref, batch.ref, scale, window, sinks, op, ldo)
+    return ctx._lib.aser_paged_attention(ctx.handle, qp, ldq, _heads(width, cache), cache.ref, batch.ref, scale, window, sinks, op, ldo)
 
 
 def aser_adapter_workspace_bytes(rows: int, n: int, m: int, r: int) -> int:

@@ -68,3 +68,22 @@ def test_append_refuses_tables_and_weights_that_the_kernel_would_misread(ctx, kw
     refused(ctx, error, append, **kw)
     assert append(ctx) == aser.ASER_OK and ctx._lib.calls == ["aser_kv_append"]
     assert append(ctx, rope_cos=None, rope_sin=None, q_norm=None, k_norm=zeros(1, D)) == aser.ASER_OK
+
+
+def attention(ctx, **kw):
+    a = dict(q=zeros(TOKENS, HEADS * D, dtype=torch.bfloat16), out=zeros(TOKENS, HEADS * D, dtype=torch.bfloat16))
+    a.update(kw)
+    return aser.aser_paged_attention(ctx, a["q"], a.get("cache") or cache(), a.get("batch") or batch(), a["out"], scale=0.1)
+
+
+def test_heads_that_the_rows_do_not_have_are_refused(ctx):
+    """A slice of fewer heads' columns than the cache has reads its neighbours', and past the last row."""
+    fused = zeros(TOKENS, 3 * KV * D)
+    for name in "kv":
+        refused(ctx, ValueError, append, **{name: fused[:, :KV * D - D]})
+        refused(ctx, ValueError, append, **{name: fused[:, :KV * D - 1]})
+    refused(ctx, ValueError, append, q=zeros(TOKENS, HEADS * D + 8), out=zeros(TOKENS, HEADS * D + 8, dtype=torch.bfloat16))
+    refused(ctx, ValueError, attention, q=zeros(TOKENS, HEADS * D - 16, dtype=torch.bfloat16))
+    assert append(ctx, k=fused[:, :KV * D], v=fused[:, KV * D:2 * KV * D]) == aser.ASER_OK
+    assert append(ctx, q=None, out=None) == aser.ASER_OK
+    assert attention(ctx, q=zeros(TOKENS, D * KV, dtype=torch.bfloat16)) == aser.ASER_OK
