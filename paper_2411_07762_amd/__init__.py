@@ -603,8 +603,10 @@ def aser_adapter_forward(ctx: Context, X, adapter, A, B, scale, Y0, Y) -> int:
         raise ValueError("A must be adapters x r x n and B adapters x m x r, contiguous")
     if _dtype_code(A) != ASER_DTYPE_BF16 or B.dtype != A.dtype or _dtype_code(Y) != ASER_DTYPE_F32 or (Y0 is not None and Y0.dtype != Y.dtype):
         raise TypeError("A and B must be bfloat16, Y0 and Y float32")
-    if adapter.shape[0] != rows or adapter.element_size() != 4 or (scale is not None and scale.shape[0] < n_adapters):
-        raise ValueError("adapter has an int32 for each row of X, scale a float32 for each adapter")
+    if adapter.dtype != _dtype("int32") or (scale is not None and scale.dtype != Y.dtype):
+        raise TypeError("adapter must be int32, scale float32")
+    if adapter.shape[0] != rows or not adapter.is_contiguous() or (scale is not None and (scale.shape[0] < n_adapters or not scale.is_contiguous())):
+        raise ValueError("adapter has an int32 for each row of X, scale a float32 for each adapter, contiguous")
     xp, ldx, _ = _token_rows(X, rows)
     yp, ldy, width = _token_rows(Y, rows)
     y0p, ldy0, width0 = (None, m, m) if Y0 is None else _token_rows(Y0, rows)

@@ -87,3 +87,23 @@ def test_heads_that_the_rows_do_not_have_are_refused(ctx):
     assert append(ctx, k=fused[:, :KV * D], v=fused[:, KV * D:2 * KV * D]) == aser.ASER_OK
     assert append(ctx, q=None, out=None) == aser.ASER_OK
     assert attention(ctx, q=zeros(TOKENS, D * KV, dtype=torch.bfloat16)) == aser.ASER_OK
+
+
+def adapters(ctx, **kw):
+    a = dict(X=zeros(TOKENS, 32), adapter=zeros(TOKENS, dtype=torch.int32), A=zeros(3, 4, 32, dtype=torch.bfloat16), B=zeros(3, 20, 4, dtype=torch.bfloat16),
+             scale=zeros(3), Y0=None, Y=zeros(TOKENS, 20))
+    a.update(kw)
+    return aser.aser_adapter_forward(ctx, a["X"], a["adapter"], a["A"], a["B"], a["scale"], a["Y0"], a["Y"])
+
+
+@pytest.mark.parametrize("kw,error", [
+    (dict(adapter=zeros(TOKENS)), TypeError), (dict(adapter=zeros(TOKENS, dtype=torch.int64)), TypeError),
+    (dict(adapter=zeros(2 * TOKENS, dtype=torch.int32)[::2]), ValueError), (dict(adapter=zeros(TOKENS + 1, dtype=torch.int32)), ValueError),
+    (dict(adapter=zeros(1, dtype=torch.int32).expand(TOKENS)), ValueError),
+    (dict(scale=zeros(3, dtype=torch.bfloat16)), TypeError), (dict(scale=zeros(3, dtype=torch.float64)), TypeError),
+    (dict(scale=zeros(2)), ValueError), (dict(scale=zeros(6)[::2]), ValueError), (dict(scale=zeros(1).expand(3)), ValueError),
+])
+def test_adapters_refuse_numbers_and_scales_that_the_kernel_would_misread(ctx, kw, error):
+    refused(ctx, error, adapters, **kw)
+    assert adapters(ctx) == aser.ASER_OK and adapters(ctx, scale=None) == aser.ASER_OK and adapters(ctx, scale=zeros(4)) == aser.ASER_OK
+    assert adapters(ctx, X=zeros(1, 32), adapter=zeros(TOKENS, dtype=torch.int32)[:1], Y=zeros(1, 20)) == aser.ASER_OK
