@@ -484,7 +484,7 @@ class KvCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.c = aser_kv_cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), k.shape[0], k.stride(0), k.stride(1), k.stride(2),
                                ASER_KV_INT8 if k.dtype == torch.int8 else ASER_KV_BF16, k.shape[2], k.shape[1], k.shape[3])
-        self.ref, self.head_dim, self.kv_width = ctypes.byref(self.c), k.shape[3], k.shape[1] * k.shape[3]
+        self.ref, self.head_dim, self.kv_width, self.page_size = ctypes.byref(self.c), k.shape[3], k.shape[1] * k.shape[3], k.shape[2]
 
     @classmethod
     def empty(cls, n_pages: int, n_kv: int, page_size: int, head_dim: int, int8: bool = False, device: int = 0):
@@ -512,7 +512,12 @@ class KvBatch:
         self.start, self.kv_len, self.pages = start, kv_len, pages
         ld = pages.stride(0) if n_seq > 1 else pages.shape[1]
         self.c = aser_kv_batch(_ptr(start), _ptr(kv_len), _ptr(pages), ld, tokens, n_seq, max_new, max_kv)
-        self.ref, self.tokens = ctypes.byref(self.c), tokens
+        self.ref, self.tokens, self.columns, self.max_kv = ctypes.byref(self.c), tokens, pages.shape[1], max_kv
+
+
+def _check_table(cache: KvCache, batch: KvBatch):
+    if batch.columns * cache.page_size < batch.max_kv:
+        raise ValueError("the page table must have a column for every page of max_kv tokens")
 
 
 def _token_rows(t, tokens: int):
@@ -547,6 +552,7 @@ def aser_kv_append(ctx: Context, q, k, v, cache: KvCache, batch: KvBatch, q_out,
     """q, k, v: tokens x (heads * channels), bfloat16 or float32 alike (q and q_out may be None); rope_cos, rope_sin: positions x
     (rotated channels / 2) float32; q_norm, k_norm: channels of a head, float32."""
     dt, tokens, opts = _dtype_code(k), batch.tokens, None
+    _check_table(cache, batch)
     if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
         raise TypeError("q, k and v must have one dtype")
     if (rope_cos is None) != (rope_sin is None):
@@ -582,6 +588,7 @@ def aser_paged_attention_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads
 
 def aser_paged_attention(ctx: Context, q, cache: KvCache, batch: KvBatch, out, *, scale: float, window: int = 0, sinks: int = 0) -> int:
     """q, out: tokens x (heads * channels), bfloat16."""
+    _check_table(cache, batch)
     qp, ldq, width = _token_rows(q, batch.tokens)
     op, ldo, out_width = _token_rows(out, batch.tokens)
     if _dtype_code(q) != ASER_DTYPE_BF16 or out.dtype != q.dtype or out_width < width:

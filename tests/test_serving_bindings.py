@@ -107,3 +107,17 @@ def test_adapters_refuse_numbers_and_scales_that_the_kernel_would_misread(ctx, k
     refused(ctx, error, adapters, **kw)
     assert adapters(ctx) == aser.ASER_OK and adapters(ctx, scale=None) == aser.ASER_OK and adapters(ctx, scale=zeros(4)) == aser.ASER_OK
     assert adapters(ctx, X=zeros(1, 32), adapter=zeros(TOKENS, dtype=torch.int32)[:1], Y=zeros(1, 20)) == aser.ASER_OK
+
+
+@pytest.mark.parametrize("call", [append, attention], ids=["append", "attention"])
+def test_page_table_has_a_column_for_every_page(ctx, call):
+    """A slice of columns has the wider table's leading dimension: its own are what counts."""
+    table = zeros(2, 8, dtype=torch.int32)
+
+    def of(pages, max_kv=40):
+        return aser.KvBatch(zeros(3, dtype=torch.int32), zeros(2, dtype=torch.int32), pages, tokens=TOKENS, max_new=4, max_kv=max_kv)
+
+    refused(ctx, ValueError, call, batch=of(table[:, :2]))
+    refused(ctx, ValueError, call, batch=of(table[:, 6:]))
+    refused(ctx, ValueError, call, batch=of(zeros(2, 3, dtype=torch.int32), 49))
+    assert call(ctx, batch=of(table[:, :3])) == aser.ASER_OK and call(ctx, batch=of(table[:, 5:], 48)) == aser.ASER_OK
