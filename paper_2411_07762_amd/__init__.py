@@ -222,16 +222,15 @@ def _dtype_code(t) -> int:
     return code
 
 
-_DTYPES = {}
+_TYPES = None
 
 
-def _dtype(name: str):
-    """The torch dtype of that name (importing this package does not import torch)."""
-    dtype = _DTYPES.get(name)
-    if dtype is None:
-        import torch
-        dtype = _DTYPES[name] = getattr(torch, name)
-    return dtype
+def _types():
+    """torch's bfloat16, float32 and int32, kept in _TYPES (importing this package does not import torch)."""
+    global _TYPES
+    import torch
+    _TYPES = torch.bfloat16, torch.float32, torch.int32
+    return _TYPES
 
 
 class Context:
@@ -481,6 +480,7 @@ class KvCache:
         for sc in (k_scale, v_scale):
             if sc is not None and (sc.dtype != torch.float32 or tuple(sc.shape) != tuple(k.shape[:3]) or not sc.is_contiguous()):
                 raise ValueError("scales must be contiguous float32, pages x heads x slots")
+        self.device = _same_device(k, v, k_scale, v_scale)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.c = aser_kv_cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), k.shape[0], k.stride(0), k.stride(1), k.stride(2),
                                ASER_KV_INT8 if k.dtype == torch.int8 else ASER_KV_BF16, k.shape[2], k.shape[1], k.shape[3])
@@ -509,24 +509,52 @@ class KvBatch:
             raise TypeError("start, kv_len and pages must be int32, start and kv_len contiguous")
         if pages.shape[1] > 1 and pages.stride(1) != 1:
             raise ValueError("the page table must have unit column stride")
+        self.device = _same_device(start, kv_len, pages)
         self.start, self.kv_len, self.pages = start, kv_len, pages
         ld = pages.stride(0) if n_seq > 1 else pages.shape[1]
         self.c = aser_kv_batch(_ptr(start), _ptr(kv_len), _ptr(pages), ld, tokens, n_seq, max_new, max_kv)
         self.ref, self.tokens, self.columns, self.max_kv = ctypes.byref(self.c), tokens, pages.shape[1], max_kv
 
 
-def _check_table(cache: KvCache, batch: KvBatch):
+def _check_batch(device: int, cache: KvCache, batch: KvBatch):
+    if cache.device != device or batch.device != device:
+        raise ValueError("cache and batch must be on the context's device")
     if batch.columns * cache.page_size < batch.max_kv:
         raise ValueError("the page table must have a column for every page of max_kv tokens")
 
 
-def _token_rows(t, tokens: int):
-    """(address, leading dimension, columns) of a matrix with a row for each token of a batch."""
-    rows, cols = t.shape
+_ELSEWHERE = "every tensor must be on the context's device"
+
+
+def _same_device(*tensors) -> int:
+    devices = {t.get_device() for t in tensors if t is not None}
+    if len(devices) != 1:
+        raise ValueError("the tensors must be on one device")
+    return devices.pop()
+
+
+def _rows(t, rows: int, dtype, device: int):
+    """(address, leading dimension, columns) of a matrix of at least `rows` rows.  A kernel that follows an address on another device faults."""
+    have, cols = t.shape
     ld, unit = t.stride()
-    if rows < tokens or unit != 1:
-        raise ValueError("token matrices need a row for each of the batch's tokens and unit column stride")
+    if have < rows or unit != 1:
+        raise ValueError("matrices need a row for each token and unit column stride")
+    if t.dtype != dtype:
+        raise TypeError("%s expected, got %s" % (dtype, t.dtype))
+    if t.get_device() != device:
+        raise ValueError(_ELSEWHERE)
     return t.data_ptr(), ld, cols
+
+
+def _floats(t, f32, device: int):
+    """Address of a dense float32 tensor."""
+    if t.dtype != f32:
+        raise TypeError("tables, weights and scales must be float32")
+    if not t.is_contiguous():
+        raise ValueError("tables, weights and scales must be contiguous")
+    if t.get_device() != device:
+        raise ValueError(_ELSEWHERE)
+    return t.data_ptr()
 
 
 def _heads(width: int, cache: KvCache) -> int:
@@ -536,48 +564,45 @@ def _heads(width: int, cache: KvCache) -> int:
     return heads
 
 
-def _head_weights(t, channels: int):
-    """Address of a norm's weights; the kernel reads `channels` floats from it on."""
-    if t is None:
-        return None
-    if t.dtype != _dtype("float32"):
-        raise TypeError("norm weights must be float32")
-    if t.numel() != channels or not t.is_contiguous():
-        raise ValueError("norm weights must be contiguous, one for each channel of a head")
-    return t.data_ptr()
-
-
 def aser_kv_append(ctx: Context, q, k, v, cache: KvCache, batch: KvBatch, q_out, *, rope_cos=None, rope_sin=None, interleaved: bool = False,
                    q_norm=None, k_norm=None, eps: float = 1e-6) -> int:
     """q, k, v: tokens x (heads * channels), bfloat16 or float32 alike (q and q_out may be None); rope_cos, rope_sin: positions x
     (rotated channels / 2) float32; q_norm, k_norm: channels of a head, float32."""
-    dt, tokens, opts = _dtype_code(k), batch.tokens, None
-    _check_table(cache, batch)
-    if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
-        raise TypeError("q, k and v must have one dtype")
+    bf16, f32, _ = _TYPES or _types()
+    dtype, tokens, device, opts = k.dtype, batch.tokens, ctx.device, None
+    dt = ASER_DTYPE_F32 if dtype == f32 else _dtype_code(k)
+    _check_batch(device, cache, batch)
     if (rope_cos is None) != (rope_sin is None):
         raise ValueError("rope_cos and rope_sin go together")
     if rope_cos is not None or q_norm is not None or k_norm is not None:
+        # the kernel reads n_pos x half floats of the tables and a float for each channel of a head of the weights
         n_pos = half = 0
+        cos = sin = qn = kn = None
         if rope_cos is not None:
-            if rope_cos.dtype != _dtype("float32") or rope_sin.dtype != rope_cos.dtype:
-                raise TypeError("rope_cos and rope_sin must be float32")
-            n_pos, half = rope_cos.shape
-            if not (rope_cos.is_contiguous() and rope_sin.is_contiguous() and rope_sin.shape == rope_cos.shape):
-                raise ValueError("rope_cos and rope_sin must be contiguous and alike")
-        opts = ctypes.byref(aser_qk_opts(_ptr(rope_cos), _ptr(rope_sin), _head_weights(q_norm, cache.head_dim), _head_weights(k_norm, cache.head_dim),
-                                         n_pos, 2 * half, 1 if interleaved else 0, eps))
-    kp, ldk, k_width = _token_rows(k, tokens)
-    vp, ldv, v_width = _token_rows(v, tokens)
+            cos, sin = _floats(rope_cos, f32, device), _floats(rope_sin, f32, device)
+            n_pos, half = shape = rope_cos.shape
+            if rope_sin.shape != shape:
+                raise ValueError("rope_cos and rope_sin must be alike")
+        if q_norm is not None:
+            qn = _floats(q_norm, f32, device)
+            if q_norm.numel() != cache.head_dim:
+                raise ValueError("q_norm must have a weight for each channel of a head")
+        if k_norm is not None:
+            kn = _floats(k_norm, f32, device)
+            if k_norm.numel() != cache.head_dim:
+                raise ValueError("k_norm must have a weight for each channel of a head")
+        opts = ctypes.byref(aser_qk_opts(cos, sin, qn, kn, n_pos, 2 * half, 1 if interleaved else 0, eps))
+    kp, ldk, k_width = _rows(k, tokens, dtype, device)
+    vp, ldv, v_width = _rows(v, tokens, dtype, device)
     if k_width < cache.kv_width or v_width < cache.kv_width:
         raise ValueError("k and v must have the channels of all key/value heads")
     qp = op = None
     ldq = ldo = heads = 0
     if q is not None:
-        qp, ldq, width = _token_rows(q, tokens)
-        op, ldo, out_width = _token_rows(q_out, tokens)
-        if _dtype_code(q_out) != ASER_DTYPE_BF16 or out_width < width:
-            raise TypeError("q_out must be bfloat16, as wide as q")
+        qp, ldq, width = _rows(q, tokens, dtype, device)
+        op, ldo, out_width = _rows(q_out, tokens, bf16, device)
+        if out_width < width:
+            raise ValueError("q_out must be as wide as q")
         heads = _heads(width, cache)
     return ctx._lib.aser_kv_append(ctx.handle, qp, ldq, heads, kp, ldk, vp, ldv, dt, opts, cache.ref, batch.ref, op, ldo)
 
@@ -588,11 +613,12 @@ def aser_paged_attention_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads
 
 def aser_paged_attention(ctx: Context, q, cache: KvCache, batch: KvBatch, out, *, scale: float, window: int = 0, sinks: int = 0) -> int:
     """q, out: tokens x (heads * channels), bfloat16."""
-    _check_table(cache, batch)
-    qp, ldq, width = _token_rows(q, batch.tokens)
-    op, ldo, out_width = _token_rows(out, batch.tokens)
-    if _dtype_code(q) != ASER_DTYPE_BF16 or out.dtype != q.dtype or out_width < width:
-        raise TypeError("q and out must be bfloat16, out as wide as q")
+    bf16, device, tokens = (_TYPES or _types())[0], ctx.device, batch.tokens
+    _check_batch(device, cache, batch)
+    qp, ldq, width = _rows(q, tokens, bf16, device)
+    op, ldo, out_width = _rows(out, tokens, bf16, device)
+    if out_width < width:
+        raise ValueError("out must be as wide as q")
     return ctx._lib.aser_paged_attention(ctx.handle, qp, ldq, _heads(width, cache), cache.ref, batch.ref, scale, window, sinks, op, ldo)
 
 
@@ -603,24 +629,24 @@ def aser_adapter_workspace_bytes(rows: int, n: int, m: int, r: int) -> int:
 def aser_adapter_forward(ctx: Context, X, adapter, A, B, scale, Y0, Y) -> int:
     """X: rows x n; adapter: rows int32; A: adapters x r x n and B: adapters x m x r, contiguous bfloat16; scale: adapters float32
     or None; Y0 (None: zeros) and Y: rows x m float32."""
-    n_adapters, r, n = A.shape
-    rows, cols = X.shape
-    m = B.shape[1]
-    if cols != n or tuple(B.shape) != (n_adapters, m, r) or not (A.is_contiguous() and B.is_contiguous()):
+    (n_adapters, r, n), (rows, cols), (b_adapters, m, b_r) = A.shape, X.shape, B.shape
+    device, (bf16, f32, i32) = ctx.device, _TYPES or _types()
+    if cols != n or b_adapters != n_adapters or b_r != r or not (A.is_contiguous() and B.is_contiguous()):
         raise ValueError("A must be adapters x r x n and B adapters x m x r, contiguous")
-    if _dtype_code(A) != ASER_DTYPE_BF16 or B.dtype != A.dtype or _dtype_code(Y) != ASER_DTYPE_F32 or (Y0 is not None and Y0.dtype != Y.dtype):
-        raise TypeError("A and B must be bfloat16, Y0 and Y float32")
-    if adapter.dtype != _dtype("int32") or (scale is not None and scale.dtype != Y.dtype):
-        raise TypeError("adapter must be int32, scale float32")
-    if adapter.shape[0] != rows or not adapter.is_contiguous() or (scale is not None and (scale.shape[0] < n_adapters or not scale.is_contiguous())):
-        raise ValueError("adapter has an int32 for each row of X, scale a float32 for each adapter, contiguous")
-    xp, ldx, _ = _token_rows(X, rows)
-    yp, ldy, width = _token_rows(Y, rows)
-    y0p, ldy0, width0 = (None, m, m) if Y0 is None else _token_rows(Y0, rows)
+    if A.dtype != bf16 or B.dtype != bf16 or adapter.dtype != i32:
+        raise TypeError("A and B must be bfloat16, adapter int32")
+    if A.get_device() != device or B.get_device() != device or adapter.get_device() != device:
+        raise ValueError(_ELSEWHERE)
+    if adapter.shape[0] != rows or not adapter.is_contiguous() or (scale is not None and scale.shape[0] < n_adapters):
+        raise ValueError("adapter has an int32 for each row of X, contiguous, scale a float32 for each adapter")
+    dt = _dtype_code(X)
+    xp, ldx, _ = _rows(X, rows, X.dtype, device)
+    yp, ldy, width = _rows(Y, rows, f32, device)
+    y0p, ldy0, width0 = (None, m, m) if Y0 is None else _rows(Y0, rows, f32, device)
     if width < m or width0 < m:
         raise ValueError("Y0 and Y must be as wide as B is high")
-    return ctx._lib.aser_adapter_forward(ctx.handle, xp, _dtype_code(X), rows, n, ldx, adapter.data_ptr(), A.data_ptr(), B.data_ptr(),
-                                         _ptr(scale), n_adapters, r, m, y0p, ldy0, yp, ldy)
+    return ctx._lib.aser_adapter_forward(ctx.handle, xp, dt, rows, n, ldx, adapter.data_ptr(), A.data_ptr(), B.data_ptr(),
+                                         None if scale is None else _floats(scale, f32, device), n_adapters, r, m, y0p, ldy0, yp, ldy)
 
 
 # ----------------------------------------------------------------------------------- one layer, end to end

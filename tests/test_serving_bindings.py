@@ -121,3 +121,46 @@ def test_page_table_has_a_column_for_every_page(ctx, call):
     refused(ctx, ValueError, call, batch=of(table[:, 6:]))
     refused(ctx, ValueError, call, batch=of(zeros(2, 3, dtype=torch.int32), 49))
     assert call(ctx, batch=of(table[:, :3])) == aser.ASER_OK and call(ctx, batch=of(table[:, 5:], 48)) == aser.ASER_OK
+
+
+class There(torch.Tensor):
+    """A tensor that says it is on device 3."""
+
+    def get_device(self):
+        return 3
+
+
+def there(*shape, dtype=torch.float32):
+    return torch.zeros(*shape, dtype=dtype).as_subclass(There)
+
+
+def test_tensors_of_another_device_than_the_context_are_refused(ctx):
+    """The address of a host tensor, or of another device's, would fault in the kernel."""
+    ints, half, rows = torch.int32, torch.bfloat16, (TOKENS, HEADS * D)
+    args = {append: dict(q=(rows,), k=((TOKENS, KV * D),), v=((TOKENS, KV * D),), out=(rows, half), rope_cos=((64, D // 2),), rope_sin=((64, D // 2),), q_norm=((D,),), k_norm=((D,),)),
+            attention: dict(q=(rows, half), out=(rows, half)),
+            adapters: dict(X=((TOKENS, 32),), adapter=((TOKENS,), ints), A=((3, 4, 32), half), B=((3, 20, 4), half), scale=((3,),), Y=((TOKENS, 20),), Y0=((TOKENS, 20),))}
+    for call, names in args.items():
+        for name, (shape, *dtype) in names.items():
+            refused(ctx, ValueError, call, **{name: there(*shape, **dict(zip(["dtype"], dtype)))})
+    pages = (5, KV, PAGE, D)
+    with pytest.raises(ValueError):
+        aser.KvCache(zeros(*pages, dtype=half), there(*pages, dtype=half))
+    for at in range(2):
+        scales = [zeros(*pages[:3]), zeros(*pages[:3])]
+        scales[at] = there(*pages[:3])
+        with pytest.raises(ValueError):
+            aser.KvCache(zeros(*pages, dtype=torch.int8), zeros(*pages, dtype=torch.int8), *scales)
+    for at in range(3):
+        parts = [zeros(3, dtype=ints), zeros(2, dtype=ints), zeros(2, 3, dtype=ints)]
+        parts[at] = there(*parts[at].shape, dtype=ints)
+        with pytest.raises(ValueError):
+            aser.KvBatch(*parts, tokens=TOKENS, max_new=4, max_kv=40)
+    cache_there = aser.KvCache(there(*pages, dtype=half), there(*pages, dtype=half))
+    batch_there = aser.KvBatch(there(3, dtype=ints), there(2, dtype=ints), there(2, 3, dtype=ints), tokens=TOKENS, max_new=4, max_kv=40)
+    for call in (append, attention):
+        refused(ctx, ValueError, call, cache=cache_there)
+        refused(ctx, ValueError, call, batch=batch_there)
+    ctx.device = 0                                        # everything else on the host
+    for call in (append, attention, adapters):
+        refused(ctx, ValueError, call)
