@@ -94,6 +94,8 @@ extern "C" int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ld
     if (window < 0 || sinks < 0) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: negative window or sinks");
     if (!(scale - scale == 0.f)) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "paged_attention: scale is not finite");
     if (batch->tokens == 0 || batch->max_new == 0) return ASER_OK;
+    // A window that no key can fall out of is none.  Beside tokens in front of position 0 the first key of a wider one would leave 32 bits.
+    if (window >= batch->max_kv) window = 0;
     const int64_t keys = keys_seen(batch->max_kv, batch->max_new, window, window > 0 ? sinks : 0), max_rows = (int64_t)batch->max_new * g.p.group;
     const Plan plan = plan_few(g.p.n_seq, g.p.n_kv, g.p.group, batch->max_new, keys);
     g.q = q; g.ldq = ldq; g.out = out; g.ldo = ldo;
