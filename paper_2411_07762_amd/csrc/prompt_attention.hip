@@ -255,6 +255,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
 
     const int mine = idle ? 0 : max(min(kt.count_up_to(wp_hi) - t0, t1), 0);     // stages that this wavefront works on: those behind lie past its rows
     bool missing = false;                          // some page that the tile may look at is not there
+    bool far = false;                              // some row's maximum is beyond 2^24
     f32x16_t sc[SUB];                              // logits of a stage, rows and keys as S^T has them
     bf16x8_t pb[SUB][2];                           // its probabilities
     auto logits = [&](int i) {
@@ -322,6 +323,17 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
             l *= shrink;
 #pragma unroll
             for (int d = 0; d < DB; ++d) o[d] *= shrink;
+            far = __ballot((fabsf(m) > 0x1p24f) & (m > kNone)) != 0;
+        }
+        // The maximum has been rounded, the products below are not: up to 2^24 that is a factor of 2 for all keys alike, beyond 2^31 it would take
+        // every exponential out of range.  So there the logits are rounded as the maximum is.
+        float factor = c;
+        if (far) {
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sc[u][e] *= c;
+            factor = 1.f;
         }
         float sum[2] = {0.f, 0.f};                 // of the unrounded probabilities
 #pragma unroll
@@ -331,7 +343,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
             for (int e4 = 0; e4 < 4; ++e4) {
                 float p[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sc[u][4 * e4 + e], c, -m));
+                for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sc[u][4 * e4 + e], factor, -m));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum[e & 1] += p[e];
                 if constexpr (I8) {
