@@ -7,7 +7,7 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
-constexpr float kNone = -1e30f;                   // running maximum before any key
+constexpr float kNone = -3.402823466e38f;         // running maximum before any key: the lowest finite value, so that every logit above it counts
 
 // n / d for 0 <= n < 2^31 as (n m) >> (31 + s): with 2^s >= d and m = floor(2^(31 + s) / d) + 1 the product is above n 2^(31 + s) / d by less than
 // 2^(31 + s) / d.  A division by a number that is not known to the compiler takes some 150 cycles.

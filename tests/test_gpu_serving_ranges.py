@@ -33,7 +33,7 @@ def test_attention_under_a_window_beyond_every_key(new, window, sinks):
 @pytest.mark.parametrize("int8", [False, True], ids=["bf16", "int8"])
 @pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("new", [1, 70], ids=["few", "prompt"])
-@pytest.mark.parametrize("power", [34])
+@pytest.mark.parametrize("power", [34, 101])
 @pytest.mark.parametrize("sign", [1.0, -1.0])
 def test_attention_where_all_logits_are_far_from_zero(sign, power, new, d, int8):
     """All visible keys have one logit, of about 2^34 d or 2^101 d and either sign: every one counts the same.  Then one key has the largest: it alone counts."""
