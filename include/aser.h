@@ -402,7 +402,8 @@ int aser_compensated_forward(aser_ctx* ctx, const int8_t* x_codes, const float* 
  * may be shared with others for reading; pages that new tokens are stored to belong to one request. */
 typedef enum aser_kv_dtype {
     ASER_KV_BF16 = 0,
-    ASER_KV_INT8 = 1    /* per token and head: scale = max_i |u_i| / 127 (1 if zero), code = rint_half_even(u_i / scale)  */
+    ASER_KV_INT8 = 1    /* per token and head: scale = max_i |u_i| / 127 (1 if zero), code = rint_half_even(u_i / scale); a head with a NaN or an
+                           infinity has the scale NaN, so that what sees it is NaN too                                       */
 } aser_kv_dtype;
 
 /* Element (page, head, slot, channel) of k and of v is at page * page_stride + head * head_stride + slot * slot_stride

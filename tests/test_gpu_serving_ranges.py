@@ -61,3 +61,40 @@ def test_attention_where_all_logits_are_far_from_zero(sign, power, new, d, int8)
         ctx.check(aser.aser_paged_attention(ctx, q, cache, batch, out, scale=1.0))
         torch.cuda.synchronize()
         check_attention("one logit" if not one else "one key", req, cache, 4, q, out, scale=1.0)
+
+
+# ------------------------------------------------------------------------------------------------ append
+@pytest.mark.parametrize("norm", [False, True], ids=["plain", "norm"])
+def test_append_to_an_int8_cache_keeps_what_is_not_finite(norm):
+    """A head with a NaN or an infinity has the scale NaN, and attention that sees it gives NaN; every other head is stored as without it."""
+    say("append int8 not finite norm=%s" % norm)
+    new, d, kv_heads, heads = [7, 1], 64, 2, 4
+    req = Requests(new, [20, 40], 16)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(6)
+    q, k, v = (torch.randn(8, n * d, generator=g, device=DEV) for n in (heads, kv_heads, kv_heads))
+    kn = torch.ones(d, device=DEV) if norm else None
+    bad_k, bad_v = torch.zeros(8, kv_heads, dtype=torch.bool), torch.zeros(8, kv_heads, dtype=torch.bool)
+    results = []
+    for spoil in (False, True):
+        if spoil:
+            k[1, :d], k[2, d + 5], k[3, 11], v[4, d + 63], v[5, 0] = float("nan"), float("nan"), float("inf"), -float("inf"), float("nan")
+            bad_k[1, 0] = bad_k[2, 1] = bad_k[3, 0] = bad_v[4, 1] = bad_v[5, 0] = True
+        cache = make_cache(req, kv_heads, d, True, 12)
+        out = torch.empty(8, heads * d, dtype=torch.bfloat16, device=DEV)
+        ctx = new_ctx()
+        ctx.check(aser.aser_kv_append(ctx, q, k, v, cache, req.batch(), out, k_norm=kn))
+        torch.cuda.synchronize()
+        results.append((cache, out))
+    (clean, _), (cache, out) = results
+    at = torch.cat([torch.arange(13, 20), torch.tensor([39])])
+    page = torch.from_numpy(np.concatenate([req.pages[0][np.arange(13, 20) // 16], req.pages[1][39 // 16:39 // 16 + 1]])).long()
+    for name, bad in (("k", bad_k), ("v", bad_v)):
+        scale, ref = (getattr(c, name + "_scale").cpu()[page, :, at % 16] for c in (cache, clean))
+        codes, ref_codes = (getattr(c, name).cpu()[page, :, at % 16] for c in (cache, clean))
+        assert scale[bad].isnan().all()
+        assert torch.equal(scale[~bad], ref[~bad]) and torch.equal(codes[~bad], ref_codes[~bad])
+    q, got = attend(req, cache, heads)
+    got = f64(got).reshape(8, kv_heads, heads // kv_heads, d)
+    assert np.isnan(got[:7][[1, 2, 3, 4, 5, 6]][:, 0]).all() and np.isnan(got[2:7, 1]).all()
+    assert np.isfinite(got[7]).all()
