@@ -475,7 +475,8 @@ int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ldq, int32_t 
  * DEVICE, one int32 per row.  A: n_adapters x r x n and B: n_adapters x m x r, bf16, dense; scale: n_adapters fp32 or
  * NULL (1).  Y0, Y: rows x m fp32; Y may be Y0 (in place: rows without an adapter are then not touched); Y0 NULL: zeros.
  * r <= 128 (adapters of smaller rank are padded with zeros), n_adapters <= 4096; any n and m.  The operands are used with
- * all their bits (fp32 X and the inner products as three bf16 terms), sums are fp32; deterministic.  Asynchronous.
+ * all their bits (fp32 X and the inner products as three bf16 terms, by the fp32 instruction where those do not hold them), sums are fp32; an
+ * infinity or a NaN has on its row the effect that it has in fp32, on others none; deterministic.  Asynchronous.
  * Needs aser_adapter_workspace_bytes of workspace.  rows == 0 is a no-op. */
 size_t aser_adapter_workspace_bytes(int64_t rows, int64_t n, int64_t m, int32_t r);
 int aser_adapter_forward(aser_ctx* ctx, const void* X, int x_dtype, int64_t rows, int64_t n, int64_t ldx, const int32_t* adapter,

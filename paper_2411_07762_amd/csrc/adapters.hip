@@ -8,7 +8,9 @@
 //
 // Both products are formed transposed (rank or output in the rows of the 16 x 16 accumulator, token in its columns), so a lane
 // holds four consecutive ranks or outputs of one token and loads and stores 16 bytes.  A and B are bf16; fp32 X and the
-// fp32 P enter the bf16 instruction as three terms that add up to all 24 bits (v = v1 + v2 + v3, each the rounded rest).
+// fp32 P enter the bf16 instruction as three terms that add up to all 24 bits (v = v1 + v2 + v3, each the rounded rest).  Rows where they do not (values
+// below 1e-33 or so, the largest finite ones, infinities) are done again by the fp32 instruction, which for a whole call of such rows takes three times as
+// long: 4099 rows 140 -> 465 us.  Looking whether there are any costs 1 %.
 // Measured: 4099 rows of 4096 fp32 inputs, 14336 outputs, rank 64, 6 adapters: sorting 8.4 us, P 22 to 24 (67 MB of X, 2.9 TB/s), Y 106 to 108
 // (470 MB of Y0 and Y, 4.4 TB/s; a plain copy reaches 5.3); 48 rows, 4096 by 4096, rank 16, 16 adapters 3.9 + 5.3.
 #include "bf16_pair.h"
@@ -125,8 +127,13 @@ struct TileRows {
 __device__ __forceinline__ bf16x8_t pack8(const float x[8]) {
     return __builtin_bit_cast(bf16x8_t, make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7])));
 }
-// x as three bf16 terms
-__device__ __forceinline__ void three_terms(float x[8], bf16x8_t t[3]) {
+// x as three bf16 terms.  Returns the bits of what they leave, 0 unless some value is out of their range: some last bits of one below 1e-33 or so fall under
+// the smallest bf16 value, one above the largest rounds to an infinity, and from an infinity or a NaN nothing can be taken away.
+__device__ __forceinline__ uint32_t three_terms(const float v[8], bf16x8_t t[3]) {
+#pragma clang fp contract(off)                     // a product that v is the rounded value of would leave its own last bits
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = v[j];
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
         t[k] = pack8(x);
@@ -138,6 +145,32 @@ __device__ __forceinline__ void three_terms(float x[8], bf16x8_t t[3]) {
             x[2 * j + 1] -= __uint_as_float(u[j] & 0xFFFF0000u);
         }
     }
+    uint32_t rest = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) rest |= __float_as_uint(x[j]);
+    return rest;
+}
+// One step of 32 with the terms of x, and with x itself by eight fp32 instructions (each takes one of a lane's eight: the order of a step is free as long as
+// both operands agree).  The second takes several times as long and is for columns whose x has no three terms.
+__device__ __forceinline__ f32x4_t terms_step(bf16x8_t a, const bf16x8_t t[3], f32x4_t acc) {
+#pragma unroll
+    for (int k = 2; k >= 0; --k) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, t[k], acc, 0, 0, 0);
+    return acc;
+}
+__device__ __forceinline__ f32x4_t exact_step(bf16x8_t a, const float x[8], f32x4_t acc) {
+    const uint4 w = __builtin_bit_cast(uint4, a);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(u[j] << 16), x[2 * j], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(u[j] & 0xFFFF0000u), x[2 * j + 1], acc, 0, 0, 0);
+    }
+    return acc;
+}
+// Bit c: some lane of column c says so.  A column is decided by its own values, so a row's result does not depend on the other rows of its tile.
+__device__ __forceinline__ uint32_t columns_where(bool lane_says) {
+    const uint64_t b = __ballot(lane_says), h = b | b >> 32;
+    return (uint32_t)(h | h >> 16) & 0xFFFFu;
 }
 
 // Eight consecutive values of a row of n, from column c on; zeros past its end.  Rows start where they like: the loads take 16 bytes from any
@@ -201,6 +234,7 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdArgs g) {
     for (int x = 0; x < NT; ++x)
 #pragma unroll
         for (int i = 0; i < RT; ++i) acc[x][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    uint32_t rest[NT] = {};
     for (int64_t c = c0 + 32 * wave; c < c1; c += 128) {
         const int64_t at = c + 8 * grp;
         const bool last = c + 32 > g.n;
@@ -220,13 +254,35 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdArgs g) {
         }
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
-            bf16x8_t t[3];
-            if (F32) three_terms(xf[x], t);
-            else t[0] = xb[x];
+            if constexpr (F32) {
+                bf16x8_t t[3];
+                rest[x] |= three_terms(xf[x], t);
 #pragma unroll
-            for (int i = 0; i < RT; ++i)
+                for (int i = 0; i < RT; ++i) acc[x][i] = terms_step(a[i], t, acc[x][i]);
+            } else {
 #pragma unroll
-                for (int k = F32 ? 2 : 0; k >= 0; --k) acc[x][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], t[k], acc[x][i], 0, 0, 0);
+                for (int i = 0; i < RT; ++i) acc[x][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], xb[x], acc[x][i], 0, 0, 0);
+            }
+        }
+    }
+    if constexpr (F32) {
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            const uint32_t exact = columns_where(rest[x] != 0);
+            if (exact == 0) continue;
+            // rare: these columns again, with all bits, one tile of ranks after the other
+            const float* x_row = (const float*)g.X + (int64_t)max(tr.row[x], 0) * g.ldx;
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                for (int64_t c = c0 + 32 * wave; c < c1; c += 128) {
+                    float xs[8];
+                    row8_f32(x_row, c + 8 * grp, g.n, c + 32 > g.n, xs);
+                    v = exact_step(row8(a_row + min(16 * i + col, g.r - 1) * g.n, c + 8 * grp, g.n, c + 32 > g.n), xs, v);
+                }
+                acc[x][i] = exact >> col & 1 ? v : acc[x][i];
+            }
         }
     }
     if (wave)
@@ -287,9 +343,10 @@ __global__ __launch_bounds__(256, NT > 1 ? 3 : 4) void adapter_up_kernel(AdArgs 
         }
     }
     bf16x8_t t[NT][KS][3];
+    uint32_t exact[NT];                            // columns whose P has no three terms
     const uint16_t* b = g.B;
+    const float s = some && g.scale ? g.scale[tr.adapter] : 1.f;
     if (some) {
-        const float s = g.scale ? g.scale[tr.adapter] : 1.f;
         b += (int64_t)tr.adapter * g.m * g.r;
         f32x4_t* sums = (f32x4_t*)sm;              // [wave][NT][KS][2][lane]
         // a wavefront adds every fourth part, the four sums meet
@@ -312,7 +369,8 @@ __global__ __launch_bounds__(256, NT > 1 ? 3 : 4) void adapter_up_kernel(AdArgs 
             }
         __syncthreads();
 #pragma unroll
-        for (int x = 0; x < NT; ++x)
+        for (int x = 0; x < NT; ++x) {
+            uint32_t rest = 0;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 f32x4_t w[2];
@@ -322,9 +380,11 @@ __global__ __launch_bounds__(256, NT > 1 ? 3 : 4) void adapter_up_kernel(AdArgs 
                     constexpr int NEXT = NT * KS * 2 * 64;
                     w[j] = (at[0] + at[NEXT]) + (at[2 * NEXT] + at[3 * NEXT]);
                 }
-                float p[8] = {w[0][0] * s, w[0][1] * s, w[0][2] * s, w[0][3] * s, w[1][0] * s, w[1][1] * s, w[1][2] * s, w[1][3] * s};
-                three_terms(p, t[x][k]);
+                const float p[8] = {w[0][0] * s, w[0][1] * s, w[0][2] * s, w[0][3] * s, w[1][0] * s, w[1][1] * s, w[1][2] * s, w[1][3] * s};
+                rest |= three_terms(p, t[x][k]);
             }
+            exact[x] = columns_where(rest != 0);
+        }
         __syncthreads();                           // before the turns below overwrite the sums
     }
     if (o0 >= g.m) return;
@@ -339,12 +399,42 @@ __global__ __launch_bounds__(256, NT > 1 ? 3 : 4) void adapter_up_kernel(AdArgs 
             for (int k = 0; k < KS; ++k) {
                 const bf16x8_t w = row8(b + row * g.r, 32 * k + 8 * grp, g.r, 32 * k + 32 > g.r);
 #pragma unroll
-                for (int x = 0; x < NT; ++x)
-#pragma unroll
-                    for (int e = 2; e >= 0; --e) acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, t[x][k][e], acc[x], 0, 0, 0);
+                for (int x = 0; x < NT; ++x) acc[x] = terms_step(w, t[x][k], acc[x]);
             }
 #pragma unroll
             for (int x = 0; x < NT; ++x) *(f32x4_t*)(turn + (16 * x + col) * PITCH + 16 * i + 4 * grp) = acc[x];
+        }
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            if (exact[x] == 0) continue;
+            // rare: these columns again, with all bits; P from its parts once more, added in the same order
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+                f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                for (int k0 = 0; k0 < g.r; k0 += 32) {
+                    const int at = k0 + 8 * grp;
+                    f32x4_t pair[2][2] = {};
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        f32x4_t u = {0.f, 0.f, 0.f, 0.f}, v = u;
+#pragma unroll 1
+                        for (int part = w; part < g.parts && tr.row[x] >= 0 && at < g.rp; part += 4) {
+                            const float* src = g.P + ((int64_t)part * g.rows + tr.row[x]) * g.rp + at;
+                            u += *(const f32x4_t*)src;
+                            v += *(const f32x4_t*)(src + 4);
+                        }
+                        pair[w / 2][0] = w % 2 ? pair[w / 2][0] + u : u;
+                        pair[w / 2][1] = w % 2 ? pair[w / 2][1] + v : v;
+                    }
+                    const f32x4_t lo = pair[0][0] + pair[1][0], hi = pair[0][1] + pair[1][1];
+                    float p[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) p[j] = at + j < g.r ? (j < 4 ? lo[j % 4] : hi[j % 4]) * s : 0.f;   // behind the rank: an infinity of X has left NaN
+                    acc = exact_step(row8(b + min(o0 + 16 * i + col, g.m - 1) * g.r, at, g.r, k0 + 32 > g.r), p, acc);
+                }
+                if (exact[x] >> col & 1) *(f32x4_t*)(turn + (16 * x + col) * PITCH + 16 * i + 4 * grp) = acc;
+            }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();

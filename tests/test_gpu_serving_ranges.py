@@ -98,3 +98,69 @@ def test_append_to_an_int8_cache_keeps_what_is_not_finite(norm):
     got = f64(got).reshape(8, kv_heads, heads // kv_heads, d)
     assert np.isnan(got[:7][[1, 2, 3, 4, 5, 6]][:, 0]).all() and np.isnan(got[2:7, 1]).all()
     assert np.isfinite(got[7]).all()
+
+
+# ------------------------------------------------------------------------------------------------ adapters
+def adapt(X, ids, A, B, scale=None, Y0=None):
+    rows, m = X.shape[0], B.shape[1]
+    out = torch.full((rows, m), 7.0, device=DEV)
+    ctx = new_ctx()
+    ctx.ensure_workspace(aser.aser_adapter_workspace_bytes(rows, X.shape[1], m, A.shape[1]))
+    ctx.check(aser.aser_adapter_forward(ctx, X, ids, A, B, scale, Y0, out))
+    torch.cuda.synchronize()
+    return out
+
+
+@pytest.mark.parametrize("r", [13, 72])
+@pytest.mark.parametrize("rows", [5, 70])
+@pytest.mark.parametrize("scale", [1e-37, 1e-36, 1e-33, 1e-30, 1e30])
+def test_adapters_keep_all_bits_at_any_scale(scale, rows, r):
+    """Inputs, or inner products alone, of a size whose lower bits three bf16 terms do not hold: the bound of the other sizes.  (The fp32 instruction
+    adds n / 4 + r / 4 times instead of n / 32 + r / 32, each time at half an ulp: 87 to 102 of the 149 halves that the bound has.)"""
+    say("adapters at %g, %d rows" % (scale, rows))
+    n, m, na = 333, 201, 3
+    g = torch.Generator(device=DEV)
+    g.manual_seed(rows)
+
+    def rand(*shape):
+        return torch.randn(*shape, generator=g, device=DEV)
+
+    ids = torch.randint(0, na, (rows,), generator=g, device=DEV, dtype=torch.int32)
+    for x_scale, a_scale in ((scale, 1.0), (1.0, scale)):
+        X, A, B = rand(rows, n) * x_scale, (rand(na, r, n) * a_scale).to(torch.bfloat16), (rand(na, m, r) / scale).to(torch.bfloat16)
+        got = f64(adapt(X, ids, A, B))
+        want, size = orc.adapters(f64(X), ids.cpu().numpy(), f64(A), f64(B), None, np.zeros((rows, m)))
+        bar = 2.0 ** -23 * (n / 32 + r / 32 + 64) * size
+        rel = np.linalg.norm(got - want) / np.linalg.norm(want)
+        say("x %g, A %g: largest error / bound %.3f, relative %.2e" % (x_scale, a_scale, (np.abs(got - want) / bar).max(), rel))
+        assert (np.abs(got - want) <= bar).all()
+        assert rel <= 1e-6
+
+
+@pytest.mark.parametrize("rows", [9, 100])
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("n,r", [(256, 16), (259, 13)])
+def test_adapters_of_inputs_that_are_not_finite(n, r, x, rows):
+    """An infinity gives an infinity where the formula does, a NaN a NaN; the largest finite values, which round to an infinity in bf16, give what they
+    should; and rows beside them keep their bits."""
+    say("adapters not finite n=%d r=%d %s %d rows" % (n, r, x, rows))
+    m, na = 130, 2
+    g = torch.Generator(device=DEV)
+    g.manual_seed(n)
+    A, B = (torch.rand(na, *s, generator=g, device=DEV) * 1e-3 + 1e-4 for s in ((r, n), (m, r)))
+    A, B = A.to(torch.bfloat16), B.to(torch.bfloat16)
+    X = torch.randn(rows, n, generator=g, device=DEV)
+    X = X.to(torch.bfloat16) if x == "bf16" else X
+    ids = torch.arange(rows, device=DEV, dtype=torch.int32) % na
+    y0 = torch.randn(rows, m, generator=g, device=DEV)
+    before = adapt(X, ids, A, B, None, y0)
+    inf = float("inf")
+    X[0, 3], X[1, n - 1], X[2, 5], X[3, 0], X[3, 40] = inf, -inf, float("nan"), inf, -inf
+    X[4, 7] = 3.4e38 if x == "f32" else torch.finfo(torch.bfloat16).max
+    X[5, 9] = -torch.finfo(X.dtype).max
+    got = adapt(X, ids, A, B, None, y0)
+    assert torch.equal(got[6:], before[6:])
+    got = f64(got)
+    assert (got[0] == inf).all() and (got[1] == -inf).all() and np.isnan(got[2:4]).all()
+    want, size = orc.adapters(f64(X[4:6]), ids[4:6].cpu().numpy(), f64(A), f64(B), None, f64(y0[4:6]))
+    assert (np.abs(got[4:6] - want) <= 2.0 ** -23 * (n / 32 + r / 32 + 64) * size).all()
