@@ -450,7 +450,7 @@ typedef struct aser_qk_opts {
  * may be NULL together (no queries wanted).  Computed in fp32, rounded once.  A new token whose position is outside
  * [0, max_kv) or on a page that is not there stores nothing; outside [0, max_kv) its row of q_out is left alone too.
  * All rows 16-byte aligned (pointers, and leading dimensions in bytes).  n_heads is a multiple of n_kv.  tokens == 0 is
- * a no-op.  Asynchronous, needs no workspace. */
+ * a no-op, whatever the matrices' pointers.  Asynchronous, needs no workspace. */
 int aser_kv_append(aser_ctx* ctx, const void* q, int64_t ldq, int32_t n_heads, const void* k, int64_t ldk, const void* v, int64_t ldv,
                    int32_t x_dtype, const aser_qk_opts* opts, const aser_kv_cache* cache, const aser_kv_batch* batch,
                    uint16_t* q_out, int64_t ldqo);
@@ -464,7 +464,8 @@ int aser_kv_append(aser_ctx* ctx, const void* q, int64_t ldq, int32_t n_heads, c
  * q, out: tokens x (n_heads * head_dim) bf16, rows 16-byte aligned; out must not overlap q.  window == 0: no window,
  * sinks is then not looked at.  Products of bf16 numbers summed in fp32; for the second product probabilities are rounded
  * to bf16 (requests of at most 64 rows, a row being a new token and head of a key/value head: to two bf16 terms), their sum is not.  Deterministic.  Asynchronous.
- * Needs aser_paged_attention_workspace_bytes of workspace (which reads of the structs what is on the host). */
+ * tokens == 0 is a no-op, whatever the matrices' pointers.  Needs aser_paged_attention_workspace_bytes of workspace (which reads of the structs what
+ * is on the host). */
 size_t aser_paged_attention_workspace_bytes(const aser_kv_cache* cache, const aser_kv_batch* batch, int32_t n_heads);
 int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ldq, int32_t n_heads, const aser_kv_cache* cache,
                          const aser_kv_batch* batch, float scale, int32_t window, int32_t sinks, uint16_t* out, int64_t ldo);
@@ -477,7 +478,7 @@ int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ldq, int32_t 
  * r <= 128 (adapters of smaller rank are padded with zeros), n_adapters <= 4096; any n and m.  The operands are used with
  * all their bits (fp32 X and the inner products as three bf16 terms, by the fp32 instruction where those do not hold them), sums are fp32; an
  * infinity or a NaN has on its row the effect that it has in fp32, on others none; deterministic.  Asynchronous.
- * Needs aser_adapter_workspace_bytes of workspace.  rows == 0 is a no-op. */
+ * Needs aser_adapter_workspace_bytes of workspace.  rows == 0 is a no-op, whatever the pointers of X, adapter, Y0 and Y. */
 size_t aser_adapter_workspace_bytes(int64_t rows, int64_t n, int64_t m, int32_t r);
 int aser_adapter_forward(aser_ctx* ctx, const void* X, int x_dtype, int64_t rows, int64_t n, int64_t ldx, const int32_t* adapter,
                          const uint16_t* A, const uint16_t* B, const float* scale, int32_t n_adapters, int32_t r, int64_t m,

@@ -507,9 +507,9 @@ extern "C" int aser_adapter_forward(aser_ctx* ctx, const void* X, int x_dtype, i
                                     const uint16_t* A, const uint16_t* B, const float* scale, int32_t n_adapters, int32_t r, int64_t m,
                                     const float* Y0, int64_t ldy0, float* Y, int64_t ldy) {
     if (!ctx) return ASER_ERR_INVALID_ARG;
-    if (!X || !adapter || !A || !B || !Y) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "adapter_forward: null pointer");
+    if (!A || !B || (rows != 0 && (!X || !adapter || !Y))) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "adapter_forward: null pointer");
     if (x_dtype != ASER_DTYPE_BF16 && x_dtype != ASER_DTYPE_F32) ASER_FAIL(ctx, ASER_ERR_DTYPE, "adapter_forward: dtype must be bf16 or f32");
-    if (rows < 0 || rows > INT32_MAX / 32 || n <= 0 || m <= 0 || ldx < n || ldy < m || (Y0 && ldy0 < m) || (Y0 == Y && ldy0 != ldy) || m > ((int64_t)1 << 23))
+    if (rows < 0 || rows > INT32_MAX / 32 || n <= 0 || m <= 0 || ldx < n || ldy < m || (Y0 && (ldy0 < m || (Y0 == Y && ldy0 != ldy))) || m > ((int64_t)1 << 23))
         ASER_FAIL(ctx, ASER_ERR_SHAPE, "adapter_forward: bad shape");
     if (r <= 0 || r > 128 || n_adapters <= 0 || n_adapters > kMaxAdapters) ASER_FAIL(ctx, ASER_ERR_SHAPE, "adapter_forward: r must be in [1, 128], n_adapters in [1, 4096]");
     const bool f32 = x_dtype == ASER_DTYPE_F32;

@@ -187,10 +187,10 @@ extern "C" int aser_kv_append(aser_ctx* ctx, const void* q, int64_t ldq, int32_t
                               int32_t x_dtype, const aser_qk_opts* opts, const aser_kv_cache* cache, const aser_kv_batch* batch,
                               uint16_t* q_out, int64_t ldqo) {
     if (!ctx) return ASER_ERR_INVALID_ARG;
-    if (!k || !v || (q == nullptr) != (q_out == nullptr)) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "kv_append: null pointer");
     if (x_dtype != ASER_DTYPE_BF16 && x_dtype != ASER_DTYPE_F32) ASER_FAIL(ctx, ASER_ERR_DTYPE, "kv_append: dtype must be bf16 or f32");
     AppendArgs g{};
     ASER_TRY(aser_paged_args(ctx, "kv_append", cache, batch, q ? n_heads : (cache ? cache->n_kv : 1), &g.p));
+    if (batch->tokens != 0 && (!k || !v || (q == nullptr) != (q_out == nullptr))) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "kv_append: null pointer");
     const int D = cache->head_dim, size = x_dtype == ASER_DTYPE_F32 ? 4 : 2;
     if (ldk < (int64_t)cache->n_kv * D || ldv < (int64_t)cache->n_kv * D || (q && (ldq < (int64_t)n_heads * D || ldqo < (int64_t)n_heads * D)))
         ASER_FAIL(ctx, ASER_ERR_SHAPE, "kv_append: leading dimension below the heads' channels");

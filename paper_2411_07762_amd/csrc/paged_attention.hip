@@ -85,9 +85,9 @@ extern "C" size_t aser_paged_attention_workspace_bytes(const aser_kv_cache* c, c
 extern "C" int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ldq, int32_t n_heads, const aser_kv_cache* cache,
                                     const aser_kv_batch* batch, float scale, int32_t window, int32_t sinks, uint16_t* out, int64_t ldo) {
     if (!ctx) return ASER_ERR_INVALID_ARG;
-    if (!q || !out) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "paged_attention: null pointer");
     AttnArgs g{};
     ASER_TRY(aser_paged_args(ctx, "paged_attention", cache, batch, n_heads, &g.p));
+    if (batch->tokens != 0 && (!q || !out)) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "paged_attention: null pointer");
     const int64_t width = (int64_t)n_heads * cache->head_dim;
     if (ldq < width || ldo < width) ASER_FAIL(ctx, ASER_ERR_SHAPE, "paged_attention: leading dimension below the heads' channels");
     if (!aser_rows_aligned(q, ldq, 2) || !aser_rows_aligned(out, ldo, 2)) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "paged_attention: rows must be 16-byte aligned");

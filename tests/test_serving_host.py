@@ -110,3 +110,20 @@ def test_workspace_queries():
     assert lib.aser_paged_attention_workspace_bytes(cache(), batch(n_seq=1, max_kv=100000), 32) > 256
     assert aser.aser_adapter_workspace_bytes(0, 8, 8, 8) == 256
     assert aser.aser_adapter_workspace_bytes(48, 4096, 4096, 16) >= 48 * 16 * 4
+
+
+def test_matrices_without_rows_have_no_address(ctx):
+    """A framework's matrix of no rows has a null pointer: still a no-op, and everything else is still checked."""
+    assert attention(ctx, cache(), batch(tokens=0), q=None, out=None) == aser.ASER_OK
+    assert append(ctx, cache(), batch(tokens=0), q=None, k=None, v=None, q_out=None) == aser.ASER_OK
+    assert append(ctx, cache(), batch(tokens=0), k=None, v=None, q_out=None) == aser.ASER_OK
+    assert attention(ctx, cache(head_dim=96), batch(tokens=0), q=None, out=None) == aser.ASER_ERR_SHAPE
+    assert append(ctx, cache(), batch(tokens=0, start=None), q=None, k=None, v=None, q_out=None) == aser.ASER_ERR_INVALID_ARG
+    assert attention(ctx, cache(), None, q=None, out=None) == aser.ASER_ERR_INVALID_ARG
+    assert append(ctx, cache(), None, q=None, k=None, v=None, q_out=None) == aser.ASER_ERR_INVALID_ARG
+
+    def adapters(rows, X=None, ids=None, A=P, Y=None, n=64):
+        return ctx._lib.aser_adapter_forward(ctx.handle, X, 0, rows, n, 64, ids, A, P, None, 3, 8, 32, None, 32, Y, 32)
+    assert adapters(0) == aser.ASER_OK
+    assert adapters(0, A=None) == aser.ASER_ERR_INVALID_ARG and adapters(0, n=0) == aser.ASER_ERR_SHAPE
+    assert adapters(1) == adapters(1, X=P) == adapters(1, X=P, ids=P) == adapters(1, ids=P, Y=P) == aser.ASER_ERR_INVALID_ARG
