@@ -164,3 +164,113 @@ def test_adapters_of_inputs_that_are_not_finite(n, r, x, rows):
     assert (got[0] == inf).all() and (got[1] == -inf).all() and np.isnan(got[2:4]).all()
     want, size = orc.adapters(f64(X[4:6]), ids[4:6].cpu().numpy(), f64(A), f64(B), None, f64(y0[4:6]))
     assert (np.abs(got[4:6] - want) <= 2.0 ** -23 * (n / 32 + r / 32 + 64) * size).all()
+
+
+@pytest.mark.parametrize("kv_heads,d", [(1, 64), (2, 64), (1, 128), (2, 256)])
+def test_attention_of_more_requests_than_a_wavefront_looks_at_once(kv_heads, d):
+    """130 requests, most of them single tokens, prompts on both sides of numbers 64 and 128; one key/value head: keys of prompts in parts."""
+    say("attention of 130 requests, %d key/value heads of %d" % (kv_heads, d))
+    new, kv = [1] * 130, [1 + (37 * s) % 190 for s in range(130)]
+    for s, n in ((3, 40), (62, 33), (63, 70), (64, 40), (65, 2), (100, 0), (127, 35), (128, 130), (129, 41)):
+        new[s], kv[s] = n, n + 900 + s
+    req = Requests(new, kv, 32, seed=kv_heads)
+    cache = make_cache(req, kv_heads, d, False, 21)
+    q, out = attend(req, cache, 4 * kv_heads)
+    check_attention("130 requests", req, cache, 4 * kv_heads, q, out)
+    q, out = attend(req, cache, 4 * kv_heads, window=50, sinks=3)
+    check_attention("130 requests, window", req, cache, 4 * kv_heads, q, out, window=50, sinks=3)
+
+
+@pytest.mark.parametrize("kv,heads,kv_heads,d,int8", [(70001, 4, 1, 64, False), (70001, 2, 1, 64, True), (33003, 8, 2, 128, False), (40000, 2, 1, 256, False)])
+def test_attention_in_more_parts_than_a_wavefront_joins_at_once(kv, heads, kv_heads, d, int8):
+    """One token over an axis that is cut into 115 to 244 parts."""
+    say("attention over %d keys" % kv)
+    req = Requests([1], [kv], 64)
+    cache = make_cache(req, kv_heads, d, int8, 4)
+    q, out = attend(req, cache, heads)
+    check_attention("%d keys" % kv, req, cache, heads, q, out)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("new", [[1, 2], [100, 37]], ids=["few", "prompt"])
+def test_attention_ignores_int8_scales_that_nobody_sees(new, d):
+    """NaN and infinities as scales of slots past the request's tokens, of keys that left the window and of pages that the table does not name."""
+    say("attention unseen scales %s d=%d" % (new, d))
+    req = Requests(new, [200, 45], 16, spare=3)
+    for window, sinks in ((48, 4), (0, 0)):
+        cache = make_cache(req, 2, d, True, 7)
+        used = np.zeros((req.n_pages, req.page), bool)
+        for s in range(2):
+            low = req.kv[s] - new[s] - window + 1 if window else 0
+            for p in range(req.kv[s]):
+                used[req.pages[s, p // 16], p % 16] = p >= low or p < sinks
+        hide = torch.from_numpy(~used).to(DEV)[:, None, :]
+        cache.k_scale.masked_fill_(hide, float("nan"))
+        cache.v_scale.masked_fill_(hide, float("inf"))
+        cache.v_scale[:, 1].masked_fill_(hide[:, 0], float("nan"))
+        q, out = attend(req, cache, 8, window=window, sinks=sinks)
+        check_attention("unseen scales", req, cache, 8, q, out, window=window, sinks=sinks)
+    for at, bad in ((3, -1), (5, req.n_pages), (7, 2 ** 31 - 1)):
+        req.pages[0, at] = bad
+    cache = make_cache(req, 2, d, True, 8)
+    cache.k_scale[0] = float("nan")                        # the page that is read in place of one that is not there
+    cache.v_scale[0] = float("inf")
+    free = sorted(set(range(1, req.n_pages)) - set(req.pages.reshape(-1).tolist()))
+    req.pages[req.pages == 0] = free[0]
+    q, out = attend(req, cache, 8)
+    check_attention("missing pages", req, cache, 8, q, out)
+
+
+TWO_TERMS = [
+    # new, kv, heads, kv_heads, d, page, int8, window, sinks
+    ([1], [77], 32, 8, 128, 64, False, 0, 0),
+    ([1, 1], [5003, 60], 16, 4, 128, 32, False, 0, 0),
+    ([1] * 3, [2049, 31, 400], 8, 2, 256, 64, False, 0, 0),
+    ([4, 1, 7, 2], [60, 9, 30, 900], 8, 4, 64, 32, False, 0, 0),
+    ([1, 1, 2], [4097, 1300, 50], 32, 4, 64, 16, True, 0, 0),
+    ([1] * 5, [31, 32, 33, 64, 700], 16, 4, 128, 128, True, 0, 0),
+    ([1, 3, 1], [40, 500, 4001], 8, 2, 128, 32, False, 64, 4),
+]
+
+
+@pytest.mark.parametrize("new,kv,heads,kv_heads,d,page,int8,window,sinks", TWO_TERMS, ids=[str(i) for i in range(len(TWO_TERMS))])
+@pytest.mark.parametrize("beside", [False, True], ids=["alone", "beside_a_prompt"])
+def test_few_rows_keep_probabilities_to_two_terms(new, kv, heads, kv_heads, d, page, int8, window, sinks, beside):
+    """Requests of at most 64 rows: the result's rounding (2^-8 of it), what two bf16 terms leave of the probabilities (2^-16 of sum p |v|) and fp32 arithmetic
+    (1e-4 of that sum).  Over all outputs the roundings of the results come to 1.5e-3 to 1.7e-3 of the norm: their mean square is a third of the largest
+    one's over the binades' mean.  The same sums with probabilities rounded once to bf16 do not pass."""
+    say("attention two terms %s %s beside=%s" % (new, kv, beside))
+    if beside:
+        new, kv = list(new) + [100], list(kv) + [120]
+    req = Requests(new, kv, page)
+    cache = make_cache(req, kv_heads, d, int8, 5)
+    q, out = attend(req, cache, heads, window=window, sinks=sinks)
+    k, v = numbers(cache)
+    rows = slice(0, int(req.start[len(new) - beside]))
+    qn = f64(q).reshape(req.tokens, heads, d)
+    want, size = orc.attention(qn, k, v, req.pages, req.start, req.kv_len, d ** -0.5, window, sinks)
+
+    def passes(got):
+        err = np.abs(got - want)[rows]
+        rel = np.linalg.norm(err) / np.linalg.norm(want[rows])
+        bar = BF16 * np.abs(want[rows]) + (2.0 ** -16 + 1e-4) * size[rows]
+        say("largest error / bound %.2f, relative %.2e" % ((err / bar).max(), rel))
+        return bool((err <= bar).all()) and rel <= 1.9e-3
+
+    assert passes(f64(out).reshape(want.shape))
+
+    def rounded(x):
+        return torch.from_numpy(np.asarray(x, np.float32)).to(torch.bfloat16).float().numpy().astype(np.float64)
+
+    once = np.zeros_like(want)
+    for s in range(len(new) - beside):
+        n = kv[s]
+        j = np.arange(n)
+        at = req.pages[s][j // page]
+        ok = orc.visible(orc.positions_of(req.start, req.kv_len, s), n, window, sinks)
+        for h in range(heads):
+            kh, vh = k[at, h * kv_heads // heads, j % page], v[at, h * kv_heads // heads, j % page]
+            logits = np.where(ok, qn[req.start[s]:req.start[s + 1], h] @ kh.T * d ** -0.5, -np.inf)
+            p = np.exp(logits - logits.max(1, keepdims=True))
+            once[req.start[s]:req.start[s + 1], h] = rounded(rounded(p) @ vh / p.sum(1, keepdims=True))
+    assert not passes(once)
