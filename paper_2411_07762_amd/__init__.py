@@ -516,11 +516,10 @@ class KvBatch:
         self.ref, self.tokens, self.columns, self.max_kv = ctypes.byref(self.c), tokens, pages.shape[1], max_kv
 
 
-def _check_batch(device: int, cache: KvCache, batch: KvBatch):
+def _refuse(device: int, cache: KvCache, batch: KvBatch):
     if cache.device != device or batch.device != device:
-        raise ValueError("cache and batch must be on the context's device")
-    if batch.columns * cache.page_size < batch.max_kv:
-        raise ValueError("the page table must have a column for every page of max_kv tokens")
+        raise ValueError(_ELSEWHERE)
+    raise ValueError("the page table must have a column for every page of max_kv tokens")
 
 
 _ELSEWHERE = "every tensor must be on the context's device"
@@ -546,22 +545,21 @@ def _rows(t, rows: int, dtype, device: int):
     return t.data_ptr(), ld, cols
 
 
-def _floats(t, f32, device: int):
-    """Address of a dense float32 tensor."""
-    if t.dtype != f32:
-        raise TypeError("tables, weights and scales must be float32")
-    if not t.is_contiguous():
-        raise ValueError("tables, weights and scales must be contiguous")
-    if t.get_device() != device:
-        raise ValueError(_ELSEWHERE)
-    return t.data_ptr()
-
-
-def _heads(width: int, cache: KvCache) -> int:
-    heads, rest = divmod(width, cache.head_dim)
-    if rest:
-        raise ValueError("queries must have whole heads")
-    return heads
+def _floats(tensors, f32, device: int) -> list:
+    """Addresses of dense float32 tensors, None where one is None."""
+    found = []
+    for t in tensors:
+        if t is None:
+            found.append(None)
+            continue
+        if t.dtype != f32:
+            raise TypeError("tables, weights and scales must be float32")
+        if not t.is_contiguous():
+            raise ValueError("tables, weights and scales must be contiguous")
+        if t.get_device() != device:
+            raise ValueError(_ELSEWHERE)
+        found.append(t.data_ptr())
+    return found
 
 
 def aser_kv_append(ctx: Context, q, k, v, cache: KvCache, batch: KvBatch, q_out, *, rope_cos=None, rope_sin=None, interleaved: bool = False,
@@ -571,27 +569,20 @@ def aser_kv_append(ctx: Context, q, k, v, cache: KvCache, batch: KvBatch, q_out,
     bf16, f32, _ = _TYPES or _types()
     dtype, tokens, device, opts = k.dtype, batch.tokens, ctx.device, None
     dt = ASER_DTYPE_F32 if dtype == f32 else _dtype_code(k)
-    _check_batch(device, cache, batch)
+    if cache.device != device or batch.device != device or batch.columns * cache.page_size < batch.max_kv:
+        _refuse(device, cache, batch)
     if (rope_cos is None) != (rope_sin is None):
         raise ValueError("rope_cos and rope_sin go together")
     if rope_cos is not None or q_norm is not None or k_norm is not None:
         # the kernel reads n_pos x half floats of the tables and a float for each channel of a head of the weights
         n_pos = half = 0
-        cos = sin = qn = kn = None
         if rope_cos is not None:
-            cos, sin = _floats(rope_cos, f32, device), _floats(rope_sin, f32, device)
             n_pos, half = shape = rope_cos.shape
             if rope_sin.shape != shape:
                 raise ValueError("rope_cos and rope_sin must be alike")
-        if q_norm is not None:
-            qn = _floats(q_norm, f32, device)
-            if q_norm.numel() != cache.head_dim:
-                raise ValueError("q_norm must have a weight for each channel of a head")
-        if k_norm is not None:
-            kn = _floats(k_norm, f32, device)
-            if k_norm.numel() != cache.head_dim:
-                raise ValueError("k_norm must have a weight for each channel of a head")
-        opts = ctypes.byref(aser_qk_opts(cos, sin, qn, kn, n_pos, 2 * half, 1 if interleaved else 0, eps))
+        if (q_norm is not None and q_norm.numel() != cache.head_dim) or (k_norm is not None and k_norm.numel() != cache.head_dim):
+            raise ValueError("q_norm and k_norm must have a weight for each channel of a head")
+        opts = ctypes.byref(aser_qk_opts(*_floats((rope_cos, rope_sin, q_norm, k_norm), f32, device), n_pos, 2 * half, 1 if interleaved else 0, eps))
     kp, ldk, k_width = _rows(k, tokens, dtype, device)
     vp, ldv, v_width = _rows(v, tokens, dtype, device)
     if k_width < cache.kv_width or v_width < cache.kv_width:
@@ -601,9 +592,9 @@ def aser_kv_append(ctx: Context, q, k, v, cache: KvCache, batch: KvBatch, q_out,
     if q is not None:
         qp, ldq, width = _rows(q, tokens, dtype, device)
         op, ldo, out_width = _rows(q_out, tokens, bf16, device)
-        if out_width < width:
-            raise ValueError("q_out must be as wide as q")
-        heads = _heads(width, cache)
+        heads, rest = divmod(width, cache.head_dim)
+        if rest or out_width < width:
+            raise ValueError("q must have whole heads, q_out must be as wide")
     return ctx._lib.aser_kv_append(ctx.handle, qp, ldq, heads, kp, ldk, vp, ldv, dt, opts, cache.ref, batch.ref, op, ldo)
 
 
@@ -614,12 +605,14 @@ def aser_paged_attention_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads
 def aser_paged_attention(ctx: Context, q, cache: KvCache, batch: KvBatch, out, *, scale: float, window: int = 0, sinks: int = 0) -> int:
     """q, out: tokens x (heads * channels), bfloat16."""
     bf16, device, tokens = (_TYPES or _types())[0], ctx.device, batch.tokens
-    _check_batch(device, cache, batch)
+    if cache.device != device or batch.device != device or batch.columns * cache.page_size < batch.max_kv:
+        _refuse(device, cache, batch)
     qp, ldq, width = _rows(q, tokens, bf16, device)
     op, ldo, out_width = _rows(out, tokens, bf16, device)
-    if out_width < width:
-        raise ValueError("out must be as wide as q")
-    return ctx._lib.aser_paged_attention(ctx.handle, qp, ldq, _heads(width, cache), cache.ref, batch.ref, scale, window, sinks, op, ldo)
+    heads, rest = divmod(width, cache.head_dim)
+    if rest or out_width < width:
+        raise ValueError("q must have whole heads, out must be as wide")
+    return ctx._lib.aser_paged_attention(ctx.handle, qp, ldq, heads, cache.ref, batch.ref, scale, window, sinks, op, ldo)
 
 
 def aser_adapter_workspace_bytes(rows: int, n: int, m: int, r: int) -> int:
@@ -646,7 +639,7 @@ def aser_adapter_forward(ctx: Context, X, adapter, A, B, scale, Y0, Y) -> int:
     if width < m or width0 < m:
         raise ValueError("Y0 and Y must be as wide as B is high")
     return ctx._lib.aser_adapter_forward(ctx.handle, xp, dt, rows, n, ldx, adapter.data_ptr(), A.data_ptr(), B.data_ptr(),
-                                         None if scale is None else _floats(scale, f32, device), n_adapters, r, m, y0p, ldy0, yp, ldy)
+                                         _floats((scale,), f32, device)[0], n_adapters, r, m, y0p, ldy0, yp, ldy)
 
 
 # ----------------------------------------------------------------------------------- one layer, end to end
