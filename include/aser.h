@@ -460,10 +460,12 @@ int aser_kv_append(aser_ctx* ctx, const void* q, int64_t ldq, int32_t n_heads, c
  * key j of its request when j <= p (p: the token's position) and, with window > 0, j > p - window or j < sinks; query head h
  * reads key/value head h / (n_heads / n_kv).  A token that sees nothing gets zeros; what the cache holds where nobody looks
  * (slots past kv_len, pages that are not there) does not matter, NaN included.  What some new token of a request sees has to
- * be finite (a value that is not makes NaN of the request's tokens, also of those that do not see it).
+ * be finite (a value that is not makes NaN of the request's tokens, also of those that do not see it), and scale q.k log2(e) within the range of fp32.
  * q, out: tokens x (n_heads * head_dim) bf16, rows 16-byte aligned; out must not overlap q.  window == 0: no window,
  * sinks is then not looked at.  Products of bf16 numbers summed in fp32; for the second product probabilities are rounded
- * to bf16 (requests of at most 64 rows, a row being a new token and head of a key/value head: to two bf16 terms), their sum is not.  Deterministic.  Asynchronous.
+ * to bf16, their sum is not.  A row being a new token and head of a key/value head, they are rounded to two bf16 terms in calls with
+ * max_new * n_heads / n_kv <= 64, and for requests of at most 64 rows in calls of several requests (a call of one request goes by max_new alone).
+ * Deterministic.  Asynchronous.
  * tokens == 0 is a no-op, whatever the matrices' pointers.  Needs aser_paged_attention_workspace_bytes of workspace (which reads of the structs what
  * is on the host). */
 size_t aser_paged_attention_workspace_bytes(const aser_kv_cache* cache, const aser_kv_batch* batch, int32_t n_heads);
@@ -475,7 +477,7 @@ int aser_paged_attention(aser_ctx* ctx, const uint16_t* q, int64_t ldq, int32_t 
  * and Y[t] = Y0[t] where adapter[t] is outside [0, n_adapters) (no adapter).  X: rows x n, bf16 or fp32 (ldx).  adapter:
  * DEVICE, one int32 per row.  A: n_adapters x r x n and B: n_adapters x m x r, bf16, dense; scale: n_adapters fp32 or
  * NULL (1).  Y0, Y: rows x m fp32; Y may be Y0 (in place: rows without an adapter are then not touched); Y0 NULL: zeros.
- * r <= 128 (adapters of smaller rank are padded with zeros), n_adapters <= 4096; any n and m.  The operands are used with
+ * r <= 128 (adapters of smaller rank are padded with zeros), n_adapters <= 4096, m <= 2^23; any n.  The operands are used with
  * all their bits (fp32 X and the inner products as three bf16 terms, by the fp32 instruction where those do not hold them), sums are fp32; an
  * infinity or a NaN has on its row the effect that it has in fp32, on others none; deterministic.  Asynchronous.
  * Needs aser_adapter_workspace_bytes of workspace.  rows == 0 is a no-op, whatever the pointers of X, adapter, Y0 and Y. */

@@ -1,7 +1,7 @@
 // Low-rank adapters of many requests beside a projection that they share:
 //     Y[t] = Y0[t] + s_a (x_t A_a^T) B_a^T,   a the adapter of row t.
 // Rows with the same adapter are taken 16 or 32 at a time, so that an adapter is read once for so many of its rows, wherever they
-// are in the batch: the sum is the same for a row whatever its neighbours.  Two launches, P = x A^T in parts of the channel axis
+// are in the batch: for a given number of rows (which sets the parts of the channel axis) the sum is the same for a row whatever its neighbours.  Two launches, P = x A^T in parts of the channel axis
 // and Y = Y0 + s P B^T, which adds the parts in their order; a third in front sorts the rows by adapter when there are
 // more than 64 of them (up to 64 the groups are formed by a ballot in every wavefront).  A few operations per byte of A, B,
 // X and Y: bound by memory, or by the launches when few rows come.
@@ -11,8 +11,8 @@
 // fp32 P enter the bf16 instruction as three terms that add up to all 24 bits (v = v1 + v2 + v3, each the rounded rest).  Rows where they do not (values
 // below 1e-33 or so, the largest finite ones, infinities) are done again by the fp32 instruction, which for a whole call of such rows takes three times as
 // long: 4099 rows 140 -> 465 us.  Looking whether there are any costs 1 %.
-// Measured: 4099 rows of 4096 fp32 inputs, 14336 outputs, rank 64, 6 adapters: sorting 8.4 us, P 22 to 24 (67 MB of X, 2.9 TB/s), Y 106 to 108
-// (470 MB of Y0 and Y, 4.4 TB/s; a plain copy reaches 5.3); 48 rows, 4096 by 4096, rank 16, 16 adapters 3.9 + 5.3.
+// Measured: 4099 rows of 4096 fp32 inputs, 14336 outputs, rank 64, 6 adapters: sorting 8.7 us, P 23 to 24 (67 MB of X, 2.8 TB/s), Y 106 to 109
+// (470 MB of Y0 and Y, 4.4 TB/s; a plain copy reaches 5.3); 48 rows, 4096 by 4096, rank 16, 16 adapters 4.2 + 5.8.
 #include "bf16_pair.h"
 #include "aser_internal.h"
 

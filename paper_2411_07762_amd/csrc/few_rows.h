@@ -11,10 +11,10 @@
 // D / 16 channels of its 8 keys and a byte permute per pair of keys turns them round.
 // Bound by reading the cache: 4 D bytes per key and head against 64 D / 16 matrix operations of 16 columns.  The keys of a request are cut
 // into parts for different workgroups, whose results a second launch joins: a single request would otherwise keep a workgroup per
-// key/value head busy and no more.  Probabilities enter the second product as two bf16 terms (16 bits; one term put an error of 2^-9 where
-// the results' own rounding is 2^-9 too, and the second costs nothing beside the loads).
-// Measured: 64 requests of 1600 to 8192 tokens, 128 channels, 32 query heads over 8: 215 us, 6.0 TB/s (a plain read reaches 6.65); one request of
-// 32771 tokens 23 us + 4.4 to join; 40 requests of up to 12003 on an int8 cache of 64 channels 64 us, 5.1 TB/s, where widening the codes counts too;
+// key/value head busy and no more.  Probabilities enter the second product as two bf16 terms (16 bits; one term puts an error of up to 2^-8
+// where the results' own rounding is 2^-8 too, and the second costs nothing beside the loads).
+// Measured: 64 requests of 1600 to 8192 tokens, 128 channels, 32 query heads over 8: 214 us, 6.0 TB/s (a plain read reaches 6.65); one request of
+// 32771 tokens 23 us + 4.5 to join; 40 requests of up to 12003 on an int8 cache of 64 channels 64 us, 5.1 TB/s, where widening the codes counts too;
 // 16 requests with 4 new tokens each, 32 heads over 32, under a window of 2048 with 4 sinks 86 us, 6.3 TB/s.
 #pragma once
 #include "attention.h"
@@ -213,7 +213,7 @@ __device__ __forceinline__ void few_rows(const AttnArgs& g, int block, int split
             l += p[e];
             if (I8) p[e] *= f.vs[e];
         }
-        // two bf16 terms, 2^-17 together: the second product is far from bounding this kernel
+        // two bf16 terms, 2^-16 together: the second product is far from bounding this kernel
         const uint4 p1 = make_uint4(bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3]), bf16_pair(p[4], p[5]), bf16_pair(p[6], p[7]));
         const uint32_t pw[4] = {p1.x, p1.y, p1.z, p1.w};
 #pragma unroll

@@ -8,7 +8,7 @@
 // heads at a time and stays with its token, whose angles it loads once; with few tokens the heads of a token are spread over
 // several wavefronts instead.
 // Measured: 11070 tokens of 5 prompts, fp32, 32 + 8 + 8 heads of 128 channels with norms and rotation 83 us, 5.0 TB/s (a plain copy
-// reaches 5.3); into an int8 cache 11000 tokens of 5 prompts 81 us; 96 single tokens 7.0 us, one 4.2, of which an empty launch takes 2.
+// reaches 5.3); into an int8 cache 11000 tokens of 5 prompts 81 us; 96 single tokens 6.7 us, one 4.5, of which an empty launch takes 2.
 #include "bf16_pair.h"
 #include "paged_kv.h"
 

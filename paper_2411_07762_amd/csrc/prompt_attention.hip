@@ -12,12 +12,13 @@
 //
 // Roundings: probabilities to bf16 for the second product (8 bits; their sum keeps the unrounded ones), results to bf16.
 //
-// Measured (32 query heads over 8): 8192 tokens of 128 channels 502 to 522 us on different devices, 1.05 to 1.1 PFLOP/s; the same
+// Measured (32 query heads over 8): 8192 tokens of 128 channels 493 to 522 us on different devices, 1.05 to 1.11 PFLOP/s (525 to 562 back to back under a trace); the same
 // matrix instructions alone, without loads and softmax, take 362 us: at this length the clock gives way to the power that they draw, 1.7 GHz against 2.2 for 1024
 // tokens (28 us), where the length of a step counts: 600 cycles to begin the copies, 1050 for the softmax, 1130 for the products.
-// Two prompts of 6001 and 3034 tokens under a window of 1024: 173 us.  64 channels: 8192 tokens 290 to 305 us, bound by the vector unit, whose
-// exponentials take twice the products' time.  256 channels (16 heads), 4096 tokens: 217 us.  int8 pays 60 vector instructions a step
-// of 280 for widening: 4096 tokens of 128 channels 188 us.
+// Two prompts of 6001 and 3034 tokens under a window of 1024: 171 to 176 us.  64 channels: 8192 tokens 290 to 307 us, bound by the vector unit: the 32
+// exponentials of a step alone take as long as its products (512 cycles each), and the rest of the softmax comes on top.  256 channels (16 heads), 4096 tokens:
+// 233 us, one wavefront a SIMD, so that nothing runs beside its softmax.  int8 pays 60 vector instructions a step of 280 for widening: 4096 tokens of 128
+// channels 187 us.
 #include "few_rows.h"
 
 namespace {
@@ -84,7 +85,8 @@ constexpr int W = 4;                              // wavefronts of a workgroup
 constexpr int kRows = 32 * W;                     // rows of its tile
 
 // Keys of a stage, and slots for stages in LDS: two workgroups of up to 128 channels fit a compute unit, of 256 one does and has more stages on
-// their way.  Stages of 32 keys for 128 channels: 588 us for 8192 tokens, of 64 530; four slots and one workgroup of 64 channels: 347, two slots 323.
+// their way.  Stages of 32 keys for 128 channels: 8192 tokens 519 -> 539 us, 1024 28 -> 33, 4096 on an int8 cache 188 -> 214, only under the window 172 -> 164;
+// four slots for 64 channels: 8192 tokens 307 -> 339.
 constexpr int keys_of(int d) { return d == 256 ? 32 : 64; }
 constexpr int slots_of(int d) { return d == 256 ? 4 : 2; }
 
@@ -476,8 +478,8 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 ? 3 : 2) void attn_p
     // Step i: copies of the keys of stage i + AHEAD and the values of the stage before it begun, into slots that were read last in step i - 1;
     // softmax of stage i; products P V of stage i and K Q of stage i + 1; what step i + 1 needs waited for; barrier.  int8: the keys of stage i + 2 and
     // the values of stage i + 1 land, the next ones are fetched.  While one workgroup of the compute unit is at its softmax (vector unit), the other
-    // one may be at its products (matrix unit): two of four wavefronts each were as fast as one of eight whose halves a second barrier kept
-    // half a step apart (530 and 523 us for 8192 tokens; without it 571), and faster where there are few rows (3 x 200 tokens behind 1500: 46 -> 37).
+    // one may be at its products (matrix unit).  One workgroup of eight wavefronts whose halves a second barrier kept half a step apart took 523 us for 8192
+    // tokens (without that barrier 571) and 46 for 3 x 200 behind 1500, where this takes 31.
     // Copies spread over the softmax took as long as together before it.
     auto begin = [&](int i) {                      // of a step, before its softmax: copies on their way
         if constexpr (!I8) {

@@ -191,6 +191,7 @@ def test_attention_in_more_parts_than_a_wavefront_joins_at_once(kv, heads, kv_he
     check_attention("%d keys" % kv, req, cache, heads, q, out)
 
 
+@pytest.mark.filterwarnings("ignore:invalid value encountered:RuntimeWarning")    # codes times scales that nobody sees
 @pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("new", [[1, 2], [100, 37]], ids=["few", "prompt"])
 def test_attention_ignores_int8_scales_that_nobody_sees(new, d):
