@@ -24,6 +24,17 @@
  *   aser_paged_attention    attention of new tokens over that cache, single ones and prompts
  *   aser_adapter_forward    low-rank adapters of single requests beside a shared projection
  *
+ * with weights and activations in microscaled 4-bit floats instead of integers:
+ *
+ *   aser_mx4_quantize       rows to four-bit floats with a power of two for each 32 of them
+ *   aser_mx4_forward        the compensated layer on them
+ *
+ * and, for layers of experts on such weights:
+ *
+ *   aser_route_experts      each row's experts, their weights, and the rows' order by expert
+ *   aser_expert_forward     the experts' products, each row with its expert
+ *   aser_expert_combine     the weighted sum of a row's experts
+ *
  * Orientation.  The paper stores activations as (in x tokens) and writes the Gram matrix
  * X X^T.  This library stores activations tokens x in (N x n, row-major, channel
  * contiguous); the same n x n matrix is then G = X^T X.  W is m x n (out x in), row-major.
@@ -485,6 +496,96 @@ size_t aser_adapter_workspace_bytes(int64_t rows, int64_t n, int64_t m, int32_t 
 int aser_adapter_forward(aser_ctx* ctx, const void* X, int x_dtype, int64_t rows, int64_t n, int64_t ldx, const int32_t* adapter,
                          const uint16_t* A, const uint16_t* B, const float* scale, int32_t n_adapters, int32_t r, int64_t m,
                          const float* Y0, int64_t ldy0, float* Y, int64_t ldy);
+
+/* ------------------------------------------------------------------------------------------------------------
+ * Microscaled 4 bits.  A row's channels are taken in blocks of 32; a value is 2^(b - 127) times a four-bit float, b the
+ * block's scale byte.  The code of such a float has the sign in bit 3 and one of the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6 in
+ * the other three bits.  b = 255: the block is NaN.
+ *
+ * `count` matrices of rows x n behind each other (experts; 1 otherwise).  Rows are padded with zeros (codes and scale bytes)
+ * to width = n rounded up to a multiple of 128.
+ *   codes:  count x rows x width / 2 bytes, two codes a byte, the even channel in the low half
+ *   scales: count x (width / 128) x rows words of four bytes; byte i of word w of a row belongs to block 4 w + i.  (A lane
+ *           of a matrix instruction takes a word at a time, and neighbouring lanes neighbouring rows.) */
+typedef struct aser_mx4 {
+    uint8_t* codes;      /* DEVICE, 16-byte aligned */
+    uint8_t* scales;     /* DEVICE, 16-byte aligned */
+    int64_t rows, n;
+    int32_t count;
+} aser_mx4;
+
+/* Quantizes the count * rows rows of X (bf16 or fp32, ldx), weights or tokens:
+ *     u = X[t][i] / mdiag[i]  (IEEE fp32; mdiag NULL: X itself),  e = floor(log2(max_block |u|)) - 2, but at least -127
+ *     b = e + 127,  code = u / 2^e rounded to the nearest of the sixteen (ties to the even code, beyond 6 to 6)
+ * so a block's largest value keeps its power of two.  Blocks of zeros: b = 0; blocks with a NaN or an infinity: b = 255, codes 0.
+ * values (NULL or count * rows rows of the type of X, ldv): the numbers that the codes stand for, exactly; what
+ * aser_quant_target wants of a weight quantizer.  It may be X itself (ldv == ldx).  Padding is written too; values has no padding.
+ * rows == 0 is a no-op.  Asynchronous, needs no workspace. */
+int aser_mx4_quantize(aser_ctx* ctx, const void* X, int x_dtype, int64_t ldx, const float* mdiag, const aser_mx4* out, void* values,
+                      int64_t ldv);
+
+/* The compensated layer on such codes: with x of T rows and w of m rows, both of n channels,
+ *     Y[t][o] = sum_i x[t][i] w[o][i] + sum_k P[t][k] L_A[o][k],   P[t][k] = sum_i x[t][i] L_B[k][i]
+ * L_A: m x r, L_B: r x n, bf16, dense; r == 0: no compensation (both may be NULL); r <= 128.
+ * swiglu != 0: the first half of the outputs are gates (m even), and Y[t][o] = z / (1 + exp(-z)) Z[t][m / 2 + o], z = Z[t][o], Z the
+ * sums above; Y then has m / 2 columns.  Y: bf16 or fp32 (y_dtype, ldy), rounded once.  Sums are fp32, P too (three bf16 terms, all 24 bits); a NaN
+ * block of a token is its row's, one of a weight its output's.  Deterministic.  Asynchronous.  rows == 0 is a no-op.
+ * Needs aser_mx4_forward_workspace_bytes(T, n, m, r) bytes of workspace. */
+size_t aser_mx4_forward_workspace_bytes(int64_t rows, int64_t n, int64_t m, int32_t r);
+int aser_mx4_forward(aser_ctx* ctx, const aser_mx4* x, const aser_mx4* w, const uint16_t* L_A, const uint16_t* L_B, int32_t r,
+                     int32_t swiglu, void* Y, int32_t y_dtype, int64_t ldy);
+
+/* Which rows go to which experts.  rows tokens choose top_k of n_experts each; a pair is a token and one of its choices, pair
+ * t * top_k + j being choice j of token t.  All DEVICE, dense; aser_route_experts writes them, and a caller with a router of its own may.
+ *   ids      rows x top_k: expert of each pair, -1 for none       weights  rows x top_k: its weight
+ *   offsets  n_experts + 1: expert e has the positions offsets[e] .. offsets[e + 1] - 1 of the pairs sorted by expert
+ *   order    rows x top_k: the pair at each position (pairs without an expert are left out; -1 behind the last)
+ *   place    rows x top_k: the position of each pair, -1 for none
+ * What they say is read on the device only and never trusted with an address: positions and pairs are clamped to their ranges. */
+typedef struct aser_expert_plan {
+    int32_t* ids;
+    float* weights;
+    int32_t* offsets;
+    int32_t* order;
+    int32_t* place;
+    int64_t rows;
+    int32_t top_k;       /* 1 .. 32                      */
+    int32_t n_experts;   /* 1 .. 1024, at least top_k    */
+} aser_expert_plan;
+
+typedef struct aser_route_opts {
+    int32_t sigmoid;       /* scores: 0 softmax over all experts, 1 sigmoid of each logit                                          */
+    int32_t n_groups;      /* experts in groups of n_experts / n_groups neighbours, 1 .. 64                                        */
+    int32_t top_groups;    /* only experts of so many groups may be chosen, 1 .. n_groups                                          */
+    int32_t group_top;     /* a group is worth its largest c (1), or the sum of its two largest (2; of its one if only one can be chosen) */
+    int32_t renormalize;   /* != 0: a row's weights are divided by their sum (by nothing if that is 0)                               */
+    float scale;           /* and multiplied by this at last                                                                       */
+} aser_route_opts;
+
+/* Scores s of logits (rows x n_experts, bf16 or fp32, ldl) are computed in 64 bits.  Chosen are the top_k experts of the largest c = s + bias (fp32,
+ * n_experts; NULL: none; without a bias the scores are ordered as the logits are, and unless groups are summed c is the
+ * logit), of equal ones the lower number; groups likewise.  Weights are made of s, not of c.
+ * An expert whose logit is -inf or NaN, or whose c is NaN or -inf, is never chosen, and such logits do not count in the softmax; a logit of
+ * +inf counts as the largest finite number.  Where fewer than top_k can be chosen, the row ends with ids of -1 and weights of 0.
+ * Positions keep the pairs of an expert in their order.  Deterministic.  Asynchronous.  Needs aser_route_workspace_bytes of workspace.
+ * rows == 0 sets offsets to 0 and does nothing else. */
+size_t aser_route_workspace_bytes(int64_t rows, int32_t n_experts, int32_t top_k);
+int aser_route_experts(aser_ctx* ctx, const void* logits, int32_t x_dtype, int64_t ldl, const float* bias, const aser_route_opts* opts,
+                       const aser_expert_plan* plan);
+
+/* aser_mx4_forward of every position with its expert: w has n_experts matrices, L_A (n_experts x m x r) and L_B (n_experts x r x n)
+ * as many.  Row p of Y is position p (rows * top_k rows).  gather != 0: position p reads row order[p] / top_k of x, which has a row for each
+ * token; 0: row p of x, which has rows * top_k.  Rows of Y behind offsets[n_experts] are left as they are.
+ * Needs aser_expert_forward_workspace_bytes(rows * top_k, n, m, n_experts, r) bytes of workspace. */
+size_t aser_expert_forward_workspace_bytes(int64_t positions, int64_t n, int64_t m, int32_t n_experts, int32_t r);
+int aser_expert_forward(aser_ctx* ctx, const aser_mx4* x, const aser_mx4* w, const aser_expert_plan* plan, int32_t gather,
+                        const uint16_t* L_A, const uint16_t* L_B, int32_t r, int32_t swiglu, void* Y, int32_t y_dtype, int64_t ldy);
+
+/* out[t] = Y0[t] + sum_j weights[t][j] Y[place[t][j]]; pairs whose place is outside [0, rows * top_k) add nothing.  Y: rows * top_k x m, y_dtype;
+ * out and Y0 (NULL: zeros): rows x m, out_dtype; out may be Y0 (ldo == ldy0).  Summed in fp32 in the order of j, rounded once.  Asynchronous, needs no
+ * workspace.  rows == 0 is a no-op. */
+int aser_expert_combine(aser_ctx* ctx, const void* Y, int32_t y_dtype, int64_t ldy, int64_t m, const aser_expert_plan* plan, const void* Y0,
+                        int64_t ldy0, void* out, int32_t out_dtype, int64_t ldo);
 
 /* Measurement aid (not a step of the method; bench.py reports it next to the nominal peaks): the rate, in
  * 10^12 operations per second, that a loop of nothing but MFMA instructions reaches on the device, with

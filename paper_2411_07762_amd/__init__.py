@@ -45,6 +45,8 @@ EXPORTS = (
     "aser_layer_workspace_bytes", "aser_smoothed_weight", "aser_quant_target",
     "aser_kv_append", "aser_paged_attention", "aser_paged_attention_workspace_bytes",
     "aser_adapter_forward", "aser_adapter_workspace_bytes",
+    "aser_mx4_quantize", "aser_mx4_forward", "aser_mx4_forward_workspace_bytes",
+    "aser_route_experts", "aser_route_workspace_bytes", "aser_expert_forward", "aser_expert_forward_workspace_bytes", "aser_expert_combine",
 )
 
 
@@ -82,6 +84,22 @@ class aser_kv_batch(ctypes.Structure):
 class aser_qk_opts(ctypes.Structure):
     _fields_ = [("rope_cos", ctypes.c_void_p), ("rope_sin", ctypes.c_void_p), ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p),
                 ("n_pos", ctypes.c_int64), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class aser_mx4(ctypes.Structure):
+    """Mirror of the C struct of the same name; Mx4 fills one from tensors."""
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64), ("n", ctypes.c_int64), ("count", ctypes.c_int32)]
+
+
+class aser_expert_plan(ctypes.Structure):
+    """Mirror of the C struct of the same name; ExpertPlan fills one from tensors."""
+    _fields_ = [("ids", ctypes.c_void_p), ("weights", ctypes.c_void_p), ("offsets", ctypes.c_void_p), ("order", ctypes.c_void_p),
+                ("place", ctypes.c_void_p), ("rows", ctypes.c_int64), ("top_k", ctypes.c_int32), ("n_experts", ctypes.c_int32)]
+
+
+class aser_route_opts(ctypes.Structure):
+    _fields_ = [("sigmoid", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("top_groups", ctypes.c_int32), ("group_top", ctypes.c_int32),
+                ("renormalize", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 class AserError(RuntimeError):
@@ -179,6 +197,23 @@ def load_library() -> ctypes.CDLL:
     lib.aser_adapter_workspace_bytes.argtypes = [i64, i64, i64, i32]
     lib.aser_adapter_forward.restype = ctypes.c_int
     lib.aser_adapter_forward.argtypes = [vp, vp, ctypes.c_int, i64, i64, i64, vp, vp, vp, vp, i32, i32, i64, vp, i64, vp, i64]
+    mx, plan = ctypes.POINTER(aser_mx4), ctypes.POINTER(aser_expert_plan)
+    lib.aser_mx4_quantize.restype = ctypes.c_int
+    lib.aser_mx4_quantize.argtypes = [vp, vp, ctypes.c_int, i64, vp, mx, vp, i64]
+    lib.aser_mx4_forward_workspace_bytes.restype = ctypes.c_size_t
+    lib.aser_mx4_forward_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.aser_mx4_forward.restype = ctypes.c_int
+    lib.aser_mx4_forward.argtypes = [vp, mx, mx, vp, vp, i32, i32, vp, i32, i64]
+    lib.aser_route_workspace_bytes.restype = ctypes.c_size_t
+    lib.aser_route_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.aser_route_experts.restype = ctypes.c_int
+    lib.aser_route_experts.argtypes = [vp, vp, i32, i64, vp, ctypes.POINTER(aser_route_opts), plan]
+    lib.aser_expert_forward_workspace_bytes.restype = ctypes.c_size_t
+    lib.aser_expert_forward_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+    lib.aser_expert_forward.restype = ctypes.c_int
+    lib.aser_expert_forward.argtypes = [vp, mx, mx, plan, i32, vp, vp, i32, i32, vp, i32, i64]
+    lib.aser_expert_combine.restype = ctypes.c_int
+    lib.aser_expert_combine.argtypes = [vp, vp, i32, i64, i64, plan, vp, i64, vp, i32, i64]
     lib.aser_mfma_rate_probe.restype = ctypes.c_int
     lib.aser_mfma_rate_probe.argtypes = [vp, i32, i32, i32, ctypes.POINTER(ctypes.c_double)]
     _lib = lib
@@ -640,6 +675,153 @@ def aser_adapter_forward(ctx: Context, X, adapter, A, B, scale, Y0, Y) -> int:
         raise ValueError("Y0 and Y must be as wide as B is high")
     return ctx._lib.aser_adapter_forward(ctx.handle, xp, dt, rows, n, ldx, adapter.data_ptr(), A.data_ptr(), B.data_ptr(),
                                          _floats((scale,), f32, device)[0], n_adapters, r, m, y0p, ldy0, yp, ldy)
+
+
+# ----------------------------------------------------------------------------------- microscaled 4 bits, experts
+class Mx4:
+    """Matrices in microscaled 4 bits from their tensors (C struct aser_mx4): codes, rows x width / 2, and scales, width / 128 x rows x 4, uint8 and
+    contiguous, width being n rounded up to a multiple of 128; with one more dimension in front for several matrices (experts)."""
+
+    def __init__(self, codes, scales, n: int):
+        import torch
+        width = (n + 127) // 128 * 128
+        front = tuple(codes.shape[:-2])
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+            raise TypeError("codes and scales must be uint8")
+        if codes.dim() not in (2, 3) or codes.shape[-1] != width // 2 or tuple(scales.shape) != front + (width // 128, codes.shape[-2], 4):
+            raise ValueError("codes must be (matrices x) rows x width / 2, scales (matrices x) width / 128 x rows x 4")
+        if not (codes.is_contiguous() and scales.is_contiguous()):
+            raise ValueError("codes and scales must be contiguous")
+        self.device = _same_device(codes, scales)
+        self.codes, self.scales, self.n, self.rows, self.count = codes, scales, n, codes.shape[-2], front[0] if front else 1
+        self.c = aser_mx4(_ptr(codes), _ptr(scales), self.rows, n, self.count)
+        self.ref = ctypes.byref(self.c)
+
+    @classmethod
+    def empty(cls, rows: int, n: int, count: Optional[int] = None, device: int = 0):
+        """Room for one matrix, or with count for several."""
+        import torch
+        width, front = (n + 127) // 128 * 128, () if count is None else (count,)
+        make = lambda *shape: torch.empty(front + shape, dtype=torch.uint8, device="cuda:%d" % device)     # noqa: E731
+        return cls(make(rows, width // 2), make(width // 128, rows, 4), n)
+
+
+class ExpertPlan:
+    """Which rows go to which experts (C struct aser_expert_plan), from its tensors: ids, order and place, rows x top_k (order and place may be flat), int32,
+    weights, rows x top_k float32, offsets, n_experts + 1 int32; all contiguous."""
+
+    def __init__(self, ids, weights, offsets, order, place):
+        import torch
+        if ids.dim() != 2 or weights.shape != ids.shape or order.numel() != ids.numel() or place.numel() != ids.numel() or offsets.dim() != 1:
+            raise ValueError("ids, weights, order and place have rows x top_k entries, offsets n_experts + 1")
+        if any(t.dtype != torch.int32 for t in (ids, offsets, order, place)) or weights.dtype != torch.float32:
+            raise TypeError("ids, offsets, order and place must be int32, weights float32")
+        if not all(t.is_contiguous() for t in (ids, weights, offsets, order, place)):
+            raise ValueError("the arrays of a plan must be contiguous")
+        self.device = _same_device(ids, weights, offsets, order, place)
+        self.ids, self.weights, self.offsets, self.order, self.place = ids, weights, offsets, order, place
+        (self.rows, self.top_k), self.n_experts = ids.shape, offsets.shape[0] - 1
+        self.positions = self.rows * self.top_k
+        self.c = aser_expert_plan(_ptr(ids), _ptr(weights), _ptr(offsets), _ptr(order), _ptr(place), self.rows, self.top_k, self.n_experts)
+        self.ref = ctypes.byref(self.c)
+
+    @classmethod
+    def empty(cls, rows: int, top_k: int, n_experts: int, device: int = 0):
+        import torch
+        make = lambda *shape: torch.empty(shape, dtype=torch.int32, device="cuda:%d" % device)             # noqa: E731
+        return cls(make(rows, top_k), make(rows, top_k).view(torch.float32), make(n_experts + 1), make(rows * top_k), make(rows * top_k))
+
+
+def aser_mx4_quantize(ctx: Context, X, out: Mx4, *, mdiag=None, values=None) -> int:
+    """X: (matrices x) rows x n, bfloat16 or float32; mdiag: n float32; values: like X (may be X)."""
+    device, f32 = ctx.device, (_TYPES or _types())[1]
+    if X.dim() == 3:
+        X = X.view(-1, X.shape[-1])
+        values = None if values is None else values.view(-1, values.shape[-1])
+    if out.device != device:
+        raise ValueError(_ELSEWHERE)
+    rows, dt = out.rows * out.count, _dtype_code(X)
+    xp, ldx, n = _rows(X, rows, X.dtype, device)
+    if n != out.n or X.shape[0] != rows or (mdiag is not None and mdiag.numel() != n):
+        raise ValueError("X must have the rows and channels of the result, mdiag a float32 for each channel")
+    vp, ldv, width = (None, n, n) if values is None else _rows(values, rows, X.dtype, device)
+    if width < n:
+        raise ValueError("values must be as wide as X")
+    return ctx._lib.aser_mx4_quantize(ctx.handle, xp, dt, ldx, _floats((mdiag,), f32, device)[0], out.ref, vp, ldv)
+
+
+def _product(ctx: Context, x: Mx4, w: Mx4, Y, rows: int, L_A, L_B, swiglu: bool):
+    """(address of L_A, of L_B, rank, swiglu, address of Y, its type, its leading dimension) after the checks that the library cannot make."""
+    device, bf16 = ctx.device, (_TYPES or _types())[0]
+    if x.device != device or w.device != device:
+        raise ValueError(_ELSEWHERE)
+    r, la, lb = 0, None, None
+    if (L_A is None) != (L_B is None):
+        raise ValueError("L_A and L_B go together")
+    if L_A is not None:
+        r = L_A.shape[-1]
+        front = tuple(w.codes.shape[:-2])
+        if tuple(L_A.shape) != front + (w.rows, r) or tuple(L_B.shape) != front + (r, w.n) or not (L_A.is_contiguous() and L_B.is_contiguous()):
+            raise ValueError("L_A must be (matrices x) outputs x r and L_B (matrices x) r x channels, contiguous")
+        if L_A.dtype != bf16 or L_B.dtype != bf16:
+            raise TypeError("L_A and L_B must be bfloat16")
+        if L_A.get_device() != device or L_B.get_device() != device:
+            raise ValueError(_ELSEWHERE)
+        la, lb = (L_A.data_ptr(), L_B.data_ptr()) if r else (None, None)
+    yp, ldy, width = _rows(Y, rows, Y.dtype, device)
+    if width < (w.rows // 2 if swiglu else w.rows):
+        raise ValueError("Y must have a column for each output")
+    return la, lb, r, 1 if swiglu else 0, yp, _dtype_code(Y), ldy
+
+
+def aser_mx4_forward_workspace_bytes(rows: int, n: int, m: int, r: int) -> int:
+    return int(load_library().aser_mx4_forward_workspace_bytes(rows, n, m, r))
+
+
+def aser_mx4_forward(ctx: Context, x: Mx4, w: Mx4, Y, *, L_A=None, L_B=None, swiglu: bool = False) -> int:
+    """Y: rows x outputs (half as many if swiglu), bfloat16 or float32; L_A: outputs x r and L_B: r x channels, contiguous bfloat16."""
+    return ctx._lib.aser_mx4_forward(ctx.handle, x.ref, w.ref, *_product(ctx, x, w, Y, x.rows, L_A, L_B, swiglu))
+
+
+def aser_route_workspace_bytes(rows: int, n_experts: int, top_k: int) -> int:
+    return int(load_library().aser_route_workspace_bytes(rows, n_experts, top_k))
+
+
+def aser_route_experts(ctx: Context, logits, plan: ExpertPlan, *, bias=None, sigmoid: bool = False, groups: int = 1, top_groups: int = 1, group_top: int = 1,
+                       renormalize: bool = True, scale: float = 1.0) -> int:
+    """logits: rows x experts, bfloat16 or float32; bias: experts float32.  Fills the plan."""
+    device, f32 = ctx.device, (_TYPES or _types())[1]
+    if plan.device != device:
+        raise ValueError(_ELSEWHERE)
+    lp, ldl, experts = _rows(logits, plan.rows, logits.dtype, device)
+    if experts != plan.n_experts or (bias is not None and bias.numel() != experts):
+        raise ValueError("logits and bias must have a column for each expert")
+    opts = aser_route_opts(1 if sigmoid else 0, groups, top_groups, group_top, 1 if renormalize else 0, scale)
+    return ctx._lib.aser_route_experts(ctx.handle, lp, _dtype_code(logits), ldl, _floats((bias,), f32, device)[0], ctypes.byref(opts), plan.ref)
+
+
+def aser_expert_forward_workspace_bytes(positions: int, n: int, m: int, n_experts: int, r: int) -> int:
+    return int(load_library().aser_expert_forward_workspace_bytes(positions, n, m, n_experts, r))
+
+
+def aser_expert_forward(ctx: Context, x: Mx4, w: Mx4, plan: ExpertPlan, Y, *, gather: bool, L_A=None, L_B=None, swiglu: bool = False) -> int:
+    """Y: positions x outputs (half as many if swiglu), bfloat16 or float32; L_A: experts x outputs x r and L_B: experts x r x channels, bfloat16."""
+    if plan.device != ctx.device:
+        raise ValueError(_ELSEWHERE)
+    return ctx._lib.aser_expert_forward(ctx.handle, x.ref, w.ref, plan.ref, 1 if gather else 0, *_product(ctx, x, w, Y, plan.positions, L_A, L_B, swiglu))
+
+
+def aser_expert_combine(ctx: Context, Y, plan: ExpertPlan, out, *, Y0=None) -> int:
+    """Y: positions x m, out and Y0 (None: zeros): rows x m, bfloat16 or float32."""
+    device = ctx.device
+    if plan.device != device:
+        raise ValueError(_ELSEWHERE)
+    yp, ldy, m = _rows(Y, plan.positions, Y.dtype, device)
+    op, ldo, out_width = _rows(out, plan.rows, out.dtype, device)
+    y0p, ldy0, width0 = (None, m, m) if Y0 is None else _rows(Y0, plan.rows, out.dtype, device)
+    if out_width != m or width0 < m:
+        raise ValueError("out and Y0 must be as wide as Y")
+    return ctx._lib.aser_expert_combine(ctx.handle, yp, _dtype_code(Y), ldy, m, plan.ref, y0p, ldy0, op, _dtype_code(out), ldo)
 
 
 # ----------------------------------------------------------------------------------- one layer, end to end

@@ -1,0 +1,403 @@
+// Routing of rows to experts, and the weighted sum of what the experts made of them.
+//
+// Routing: a wavefront has a row, its lanes the experts lane, lane + 64, ...  Scores are computed in 64 bits, so that experts are told apart where fp32 would
+// round their scores to one number.  The top_k largest are found one after the other.  A workgroup has 32 rows: bit t of an expert's word says that row t chose it,
+// so the number of a pair among its expert's pairs is a count of bits, and the order by expert is the same whatever the timing.  Up
+// to 32 rows are ordered in the same launch; more in two further ones, a running sum over the workgroups for each expert and the placing.
+#include "bf16_pair.h"
+#include "mx4.h"
+
+namespace {
+
+constexpr int kTok = 32, kWaves = 8;
+constexpr double kMinus = -__builtin_huge_val();
+
+struct RouteArgs {
+    const void* logits; int64_t ldl;
+    const float* bias;
+    aser_route_opts o;
+    int32_t* ids; float* weights; int32_t* offsets; int32_t* order; int32_t* place;
+    int64_t rows;
+    int top_k, experts;
+    int32_t* counts;      // [expert][workgroup]; more than one workgroup
+    int32_t* totals;      // [expert]
+    int groups;           // workgroups
+};
+
+__device__ __forceinline__ double wave_max(double v) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) v = fmax(v, __shfl_xor(v, d));
+    return v;
+}
+
+// Running sum over the experts: offs[e] = sum of count(e') for e' < e, offs[experts] the total.  One wavefront.
+template <class COUNT>
+__device__ __forceinline__ void sum_experts(int experts, int32_t* offs, COUNT count) {
+    const int lane = threadIdx.x & 63;
+    int32_t before = 0;
+    for (int e0 = 0; e0 < experts; e0 += 64) {
+        const int32_t mine = e0 + lane < experts ? count(e0 + lane) : 0;
+        int32_t upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int32_t v = __shfl_up(upto, d);
+            if (lane >= d) upto += v;
+        }
+        if (e0 + lane < experts) offs[e0 + lane] = before + upto - mine;
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    if (lane == 0) offs[experts] = before;
+}
+
+// Places the pairs of 32 rows: marks[e] has the rows that chose e, first[e] the position of the first of them.
+__device__ __forceinline__ void place_pairs(const RouteArgs& g, int64_t row0, const uint32_t* marks, const int32_t* first, int32_t total) {
+    const int64_t left = (g.rows - row0) * g.top_k, pairs = g.rows * g.top_k;
+    const int here = left < kTok * g.top_k ? (int)left : kTok * g.top_k;
+    for (int i = threadIdx.x; i < here; i += kWaves * 64) {
+        const int64_t pair = row0 * g.top_k + i;
+        const int32_t e = g.ids[pair];
+        const int t = i / g.top_k;
+        int32_t at = -1;
+        if (e >= 0) {
+            at = first[e] + __popc(marks[e] & ((1u << t) - 1u));
+            g.order[at] = (int32_t)pair;
+        }
+        g.place[pair] = at;
+        if (pair >= total && pair < pairs) g.order[pair] = -1;
+    }
+}
+
+template <int V, bool F32>
+__global__ __launch_bounds__(kWaves * 64) void route_kernel(RouteArgs g) {
+    extern __shared__ __align__(16) char smem[];
+    double* const cbuf = (double*)smem;                                     // [wavefront][expert], if there are groups
+    uint32_t* const marks = (uint32_t*)(smem + (g.o.n_groups > 1 ? (size_t)kWaves * g.experts * 8 : 0));
+    int32_t* const first = (int32_t*)(marks + g.experts);                   // experts + 1
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row0 = (int64_t)blockIdx.x * kTok;
+    for (int e = threadIdx.x; e < g.experts; e += kWaves * 64) marks[e] = 0;
+    __syncthreads();
+    const bool by_logit = !g.bias && (g.o.n_groups == 1 || g.o.group_top == 1);
+    for (int t = wave; t < kTok && row0 + t < g.rows; t += kWaves) {
+        const int64_t row = row0 + t;
+        double s[V], c[V];
+        double top = kMinus;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int e = lane + 64 * j;
+            float l = -__builtin_huge_valf();
+            if (e < g.experts) l = F32 ? ((const float*)g.logits)[row * g.ldl + e] : __uint_as_float((uint32_t)((const uint16_t*)g.logits)[row * g.ldl + e] << 16);
+            if (!(l == l)) l = -__builtin_huge_valf();
+            if (l > 3.402823466e38f) l = 3.402823466e38f;
+            s[j] = l;
+            top = fmax(top, s[j]);
+        }
+        const double l_top = wave_max(top);
+        double sum = 0.0;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const double l = s[j];
+            const bool off = l == kMinus;
+            if (g.o.sigmoid) s[j] = off ? 0.0 : 1.0 / (1.0 + exp(-l));
+            else s[j] = off ? 0.0 : exp(l - l_top);
+            sum += s[j];
+            c[j] = l;
+        }
+        if (!g.o.sigmoid) {
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+#pragma unroll
+            for (int j = 0; j < V; ++j) s[j] = sum > 0.0 ? s[j] / sum : 0.0;
+        }
+        if (!by_logit) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int e = lane + 64 * j;
+                double v = s[j];
+                if (g.bias && e < g.experts) v += (double)g.bias[e];
+                c[j] = c[j] == kMinus || !(v == v) ? kMinus : v;
+            }
+        }
+        if (g.o.n_groups > 1) {
+            double* const mine = cbuf + (size_t)wave * g.experts;
+            const int size = g.experts / g.o.n_groups;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (lane + 64 * j < g.experts) mine[lane + 64 * j] = c[j];
+            __builtin_amdgcn_wave_barrier();
+            double worth = kMinus;
+            if (lane < g.o.n_groups) {
+                double second = kMinus;
+                for (int i = 0; i < size; ++i) {
+                    const double v = mine[lane * size + i];
+                    if (v > worth) { second = worth; worth = v; }
+                    else if (v > second) second = v;
+                }
+                if (g.o.group_top == 2 && second > kMinus) worth += second;
+            }
+            int ahead = 0;
+            for (int i = 0; i < g.o.n_groups; ++i) {
+                const double v = __shfl(worth, i);
+                ahead += v > worth || (v == worth && i < lane);
+            }
+            const uint64_t open = __ballot(lane < g.o.n_groups && ahead < g.o.top_groups);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int e = lane + 64 * j;
+                if (e < g.experts && !((open >> (e / size)) & 1)) c[j] = kMinus;
+            }
+        }
+        int my_id = -1;
+        double my_s = 0.0;
+        for (int k = 0; k < g.top_k; ++k) {
+            double best = kMinus, score = 0.0;
+            int at = INT32_MAX;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (c[j] > best) { best = c[j]; at = lane + 64 * j; score = s[j]; }
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const double v = __shfl_xor(best, d), sv = __shfl_xor(score, d);
+                const int a = __shfl_xor(at, d);
+                if (v > best || (v == best && a < at)) { best = v; at = a; score = sv; }
+            }
+            if (!(best > kMinus)) break;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (at == lane + 64 * j) c[j] = kMinus;
+            if (lane == k) { my_id = at; my_s = score; }
+        }
+        if (g.o.renormalize) {
+            double total = my_s;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
+            if (total > 0.0) my_s /= total;
+        }
+        if (lane < g.top_k) {
+            g.ids[row * g.top_k + lane] = my_id;
+            g.weights[row * g.top_k + lane] = (float)(my_s * (double)g.o.scale);
+            if (my_id >= 0) atomicOr(&marks[my_id], 1u << t);
+        }
+    }
+    __syncthreads();
+    if (g.groups > 1) {
+        for (int e = threadIdx.x; e < g.experts; e += kWaves * 64) g.counts[(int64_t)e * g.groups + blockIdx.x] = __popc(marks[e]);
+        return;
+    }
+    if (wave == 0) sum_experts(g.experts, first, [&](int e) { return __popc(marks[e]); });
+    __syncthreads();
+    for (int e = threadIdx.x; e <= g.experts; e += kWaves * 64) g.offsets[e] = first[e];
+    place_pairs(g, row0, marks, first, first[g.experts]);
+}
+
+// counts[e][*] to the numbers of pairs in the workgroups before, totals[e] their sum.  A wavefront has an expert.
+__global__ __launch_bounds__(64) void route_sum_kernel(RouteArgs g) {
+    const int lane = threadIdx.x;
+    int32_t* const mine = g.counts + (int64_t)blockIdx.x * g.groups;
+    int32_t before = 0;
+    for (int i0 = 0; i0 < g.groups; i0 += 64) {
+        const int32_t v = i0 + lane < g.groups ? mine[i0 + lane] : 0;
+        int32_t upto = v;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int32_t u = __shfl_up(upto, d);
+            if (lane >= d) upto += u;
+        }
+        if (i0 + lane < g.groups) mine[i0 + lane] = before + upto - v;
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    if (lane == 0) g.totals[blockIdx.x] = before;
+}
+
+__global__ __launch_bounds__(kWaves * 64) void route_place_kernel(RouteArgs g) {
+    extern __shared__ __align__(16) char smem[];
+    uint32_t* const marks = (uint32_t*)smem;
+    int32_t* const first = (int32_t*)(marks + g.experts);
+    const int64_t row0 = (int64_t)blockIdx.x * kTok;
+    for (int e = threadIdx.x; e < g.experts; e += kWaves * 64) marks[e] = 0;
+    __syncthreads();
+    const int64_t left = (g.rows - row0) * g.top_k;
+    const int here = left < kTok * g.top_k ? (int)left : kTok * g.top_k;
+    for (int i = threadIdx.x; i < here; i += kWaves * 64) {
+        const int32_t e = g.ids[row0 * g.top_k + i];
+        if (e >= 0) atomicOr(&marks[e], 1u << (i / g.top_k));
+    }
+    if (threadIdx.x < 64) sum_experts(g.experts, first, [&](int e) { return g.totals[e]; });
+    __syncthreads();
+    const int32_t total = first[g.experts];
+    if (blockIdx.x == 0)
+        for (int e = threadIdx.x; e <= g.experts; e += kWaves * 64) g.offsets[e] = first[e];
+    __syncthreads();
+    for (int e = threadIdx.x; e < g.experts; e += kWaves * 64) first[e] += g.counts[(int64_t)e * g.groups + blockIdx.x];
+    __syncthreads();
+    place_pairs(g, row0, marks, first, total);
+}
+
+__global__ __launch_bounds__(256) void route_none_kernel(int32_t* offsets, int n) {
+    for (int e = threadIdx.x; e <= n; e += 256) offsets[e] = 0;
+}
+
+template <int V>
+int launch_route(aser_ctx* ctx, const RouteArgs& g, bool f32) {
+    const size_t lds = (g.o.n_groups > 1 ? (size_t)kWaves * g.experts * 8 : 0) + (2 * (size_t)g.experts + 1) * 4;
+    auto kernel = f32 ? route_kernel<V, true> : route_kernel<V, false>;
+    if (lds > 65536) ASER_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    kernel<<<(unsigned)g.groups, kWaves * 64, lds, ctx->stream>>>(g);
+    return aser_check_launch(ctx, "route_kernel");
+}
+
+// ---------------------------------------------------------------------------------------------------------------- the weighted sum
+struct CombineArgs {
+    const void* Y; int64_t ldy, m;
+    const int32_t* place; const float* weights;
+    int64_t positions;
+    int top_k;
+    const void* Y0; int64_t ldy0;
+    void* out; int64_t ldo;
+    bool vec;
+};
+
+template <bool F32>
+__device__ __forceinline__ float element(const void* p, int64_t at) {
+    return F32 ? ((const float*)p)[at] : __uint_as_float((uint32_t)((const uint16_t*)p)[at] << 16);
+}
+template <bool F32>
+__device__ __forceinline__ void eight(const void* p, int64_t at, int here, bool vec, float* v) {
+    if (vec && here == 8) {
+        if (F32) {
+            const float4 a = *(const float4*)((const float*)p + at), b = *(const float4*)((const float*)p + at + 4);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+            const uint4 a = *(const uint4*)((const uint16_t*)p + at);
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < here ? element<F32>(p, at + i) : 0.f;
+}
+
+// A workgroup has 2048 columns of a token, a thread eight.
+template <bool YF32, bool OF32>
+__global__ __launch_bounds__(256) void combine_kernel(CombineArgs g) {
+    const int64_t t = blockIdx.x, c = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 8;
+    if (c >= g.m) return;
+    const int here = (int)(g.m - c < 8 ? g.m - c : 8);
+    float sum[8];
+    if (g.Y0) eight<OF32>(g.Y0, t * g.ldy0 + c, here, g.vec, sum);
+    else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+    }
+    for (int j = 0; j < g.top_k; ++j) {
+        const int32_t at = g.place[t * g.top_k + j];
+        if (at < 0 || at >= g.positions) continue;
+        const float w = g.weights[t * g.top_k + j];
+        float v[8];
+        eight<YF32>(g.Y, (int64_t)at * g.ldy + c, here, g.vec, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, v[i], sum[i]);
+    }
+    const int64_t o = t * g.ldo + c;
+    if (g.vec && here == 8) {
+        if (OF32) {
+            *(float4*)((float*)g.out + o) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            *(float4*)((float*)g.out + o + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
+        } else {
+            *(uint4*)((uint16_t*)g.out + o) = make_uint4(bf16_pair(sum[0], sum[1]), bf16_pair(sum[2], sum[3]), bf16_pair(sum[4], sum[5]), bf16_pair(sum[6], sum[7]));
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (i >= here) continue;
+        if (OF32) ((float*)g.out)[o + i] = sum[i];
+        else ((uint16_t*)g.out)[o + i] = (uint16_t)bf16_pair(sum[i], sum[i]);
+    }
+}
+
+bool row16(const void* p, int64_t ld, int64_t size) { return !((uintptr_t)p & 15) && !(ld * size & 15); }
+
+}  // namespace
+
+int aser_plan_check(aser_ctx* ctx, const char* who, const aser_expert_plan* p) {
+    if (!p) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "%s: null plan", who);
+    if (p->rows < 0 || p->n_experts <= 0 || p->n_experts > 1024 || p->top_k <= 0 || p->top_k > 32 || p->top_k > p->n_experts || p->rows > INT32_MAX / 32 / p->top_k)
+        ASER_FAIL(ctx, ASER_ERR_SHAPE, "%s: needs 1 to 1024 experts, 1 to 32 of them for a row, and less than 2^26 pairs", who);
+    if (((uintptr_t)p->ids | (uintptr_t)p->weights | (uintptr_t)p->offsets | (uintptr_t)p->order | (uintptr_t)p->place) & 3)
+        ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "%s: misaligned plan", who);
+    return ASER_OK;
+}
+
+extern "C" size_t aser_route_workspace_bytes(int64_t rows, int32_t n_experts, int32_t top_k) {
+    (void)top_k;
+    if (rows <= kTok || n_experts <= 0) return kAserWsTail;
+    return align_up((size_t)(ceil_div64(rows, kTok) + 1) * n_experts * 4, 256) + kAserWsTail;
+}
+
+extern "C" int aser_route_experts(aser_ctx* ctx, const void* logits, int32_t x_dtype, int64_t ldl, const float* bias, const aser_route_opts* opts,
+                                  const aser_expert_plan* plan) {
+    if (!ctx) return ASER_ERR_INVALID_ARG;
+    if (!opts) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "route_experts: null options");
+    if (x_dtype != ASER_DTYPE_BF16 && x_dtype != ASER_DTYPE_F32) ASER_FAIL(ctx, ASER_ERR_DTYPE, "route_experts: dtype must be bf16 or f32");
+    ASER_TRY(aser_plan_check(ctx, "route_experts", plan));
+    const int experts = plan->n_experts;
+    if (opts->n_groups < 1 || opts->n_groups > 64 || experts % opts->n_groups || opts->top_groups < 1 || opts->top_groups > opts->n_groups || opts->group_top < 1 ||
+        opts->group_top > 2)
+        ASER_FAIL(ctx, ASER_ERR_SHAPE, "route_experts: 1 to 64 groups of as many experts, 1 to n_groups of them open, a group worth its one or two best");
+    if (!(opts->scale - opts->scale == 0.f)) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "route_experts: scale is not finite");
+    if (!plan->offsets || (plan->rows != 0 && (!logits || !plan->ids || !plan->weights || !plan->order || !plan->place)))
+        ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "route_experts: null pointer");
+    if (ldl < experts) ASER_FAIL(ctx, ASER_ERR_SHAPE, "route_experts: leading dimension below the number of experts");
+    const bool f32 = x_dtype == ASER_DTYPE_F32;
+    if (((uintptr_t)logits & (f32 ? 3 : 1)) || ((uintptr_t)bias & 3)) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "route_experts: misaligned pointer");
+    if (plan->rows == 0) {
+        ASER_TRY(aser_prepare_device(ctx));
+        route_none_kernel<<<1, 256, 0, ctx->stream>>>(plan->offsets, experts);
+        return aser_check_launch(ctx, "route_none_kernel");
+    }
+    const size_t need = aser_route_workspace_bytes(plan->rows, experts, plan->top_k);
+    RouteArgs g{logits, ldl, bias, *opts, plan->ids, plan->weights, plan->offsets, plan->order, plan->place, plan->rows, plan->top_k, experts, nullptr, nullptr,
+                (int)ceil_div64(plan->rows, kTok)};
+    if (g.groups > 1) {
+        if (!ctx->ws || ctx->ws_bytes < need) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "route_experts: workspace too small");
+        g.counts = (int32_t*)ctx->ws;
+        g.totals = g.counts + (int64_t)g.groups * experts;
+    }
+    ASER_TRY(aser_prepare_device(ctx));
+    if (experts <= 64) ASER_TRY(launch_route<1>(ctx, g, f32));
+    else if (experts <= 128) ASER_TRY(launch_route<2>(ctx, g, f32));
+    else if (experts <= 256) ASER_TRY(launch_route<4>(ctx, g, f32));
+    else if (experts <= 512) ASER_TRY(launch_route<8>(ctx, g, f32));
+    else ASER_TRY(launch_route<16>(ctx, g, f32));
+    if (g.groups == 1) return ASER_OK;
+    route_sum_kernel<<<(unsigned)experts, 64, 0, ctx->stream>>>(g);
+    ASER_TRY(aser_check_launch(ctx, "route_sum_kernel"));
+    route_place_kernel<<<(unsigned)g.groups, kWaves * 64, (2 * (size_t)experts + 1) * 4, ctx->stream>>>(g);
+    return aser_check_launch(ctx, "route_place_kernel");
+}
+
+extern "C" int aser_expert_combine(aser_ctx* ctx, const void* Y, int32_t y_dtype, int64_t ldy, int64_t m, const aser_expert_plan* plan, const void* Y0, int64_t ldy0,
+                                   void* out, int32_t out_dtype, int64_t ldo) {
+    if (!ctx) return ASER_ERR_INVALID_ARG;
+    if ((y_dtype != ASER_DTYPE_BF16 && y_dtype != ASER_DTYPE_F32) || (out_dtype != ASER_DTYPE_BF16 && out_dtype != ASER_DTYPE_F32))
+        ASER_FAIL(ctx, ASER_ERR_DTYPE, "expert_combine: dtypes must be bf16 or f32");
+    ASER_TRY(aser_plan_check(ctx, "expert_combine", plan));
+    if (plan->rows != 0 && (!Y || !out || !plan->place || !plan->weights)) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "expert_combine: null pointer");
+    if (m <= 0 || m > ((int64_t)1 << 24) || ldy < m || ldo < m || (Y0 && (ldy0 < m || (Y0 == out && ldy0 != ldo)))) ASER_FAIL(ctx, ASER_ERR_SHAPE, "expert_combine: bad shape");
+    const bool yf = y_dtype == ASER_DTYPE_F32, of = out_dtype == ASER_DTYPE_F32;
+    if (((uintptr_t)Y & (yf ? 3 : 1)) || (((uintptr_t)Y0 | (uintptr_t)out) & (of ? 3 : 1))) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "expert_combine: misaligned pointer");
+    if (plan->rows == 0) return ASER_OK;
+    CombineArgs g{Y, ldy, m, plan->place, plan->weights, plan->rows * plan->top_k, plan->top_k, Y0, ldy0, out, ldo, false};
+    g.vec = row16(Y, ldy, yf ? 4 : 2) && row16(out, ldo, of ? 4 : 2) && (!Y0 || row16(Y0, ldy0, of ? 4 : 2));
+    const dim3 grid((unsigned)plan->rows, (unsigned)ceil_div64(m, 2048));
+    ASER_TRY(aser_prepare_device(ctx));
+    if (yf) of ? combine_kernel<true, true><<<grid, 256, 0, ctx->stream>>>(g) : combine_kernel<true, false><<<grid, 256, 0, ctx->stream>>>(g);
+    else of ? combine_kernel<false, true><<<grid, 256, 0, ctx->stream>>>(g) : combine_kernel<false, false><<<grid, 256, 0, ctx->stream>>>(g);
+    return aser_check_launch(ctx, "combine_kernel");
+}
