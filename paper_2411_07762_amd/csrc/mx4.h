@@ -20,6 +20,21 @@ struct MxGroups {
     }
 };
 
+// Tiles of bm positions that there are.
+__device__ __forceinline__ int64_t mx4_tiles(const MxGroups& g, int bm) {
+    if (!g.offsets) return (g.positions + bm - 1) / bm;
+    const int lane = threadIdx.x & 63;
+    const int32_t most = (int32_t)g.positions;
+    int32_t sum = 0;
+    for (int e = lane; e < g.count; e += 64) {
+        const int32_t a = g.offsets[e], b = g.offsets[e + 1];
+        const int32_t s = a < 0 ? 0 : a > most ? most : a, t = b > most ? most : b;
+        sum += t > s ? (t - s + bm - 1) / bm : 0;
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    return __builtin_amdgcn_readfirstlane(sum);
+}
 // Workgroup `tile`'s matrix, first position and number of positions.  False: there is no such tile.  Every wavefront looks for itself: a
 // lane has a group, and the running sum of the groups' tiles says whose the tile is.
 __device__ __forceinline__ bool mx4_find_tile(const MxGroups& g, int64_t tile, int bm, int* e, int64_t* p0, int* rows) {
