@@ -503,10 +503,11 @@ int aser_adapter_forward(aser_ctx* ctx, const void* X, int x_dtype, int64_t rows
  * the other three bits.  b = 255: the block is NaN.
  *
  * `count` matrices of rows x n behind each other (experts; 1 otherwise).  Rows are padded with zeros (codes and scale bytes)
- * to width = n rounded up to a multiple of 128.
- *   codes:  count x rows x width / 2 bytes, two codes a byte, the even channel in the low half
- *   scales: count x (width / 128) x rows words of four bytes; byte i of word w of a row belongs to block 4 w + i.  (A lane
- *           of a matrix instruction takes a word at a time, and neighbouring lanes neighbouring rows.) */
+ * to width = n rounded up to a multiple of 128, and cut into words of 128 channels; 16 rows are a panel (the last one may have rows
+ * that are not there: room for them, which nobody reads), and a word of a panel's rows lies side by side:
+ *   codes:  count x panels x (width / 128) x 16 x 64 bytes, two codes a byte, the even channel in the low half
+ *   scales: count x panels x (width / 128) x 16 x 4 bytes, byte i of word w of a row belongs to its block 4 w + i
+ * (What a matrix instruction takes of 16 rows is a kilobyte in a row, and what a product with few rows reads of the other matrix is one stream.) */
 typedef struct aser_mx4 {
     uint8_t* codes;      /* DEVICE, 16-byte aligned */
     uint8_t* scales;     /* DEVICE, 16-byte aligned */

@@ -679,31 +679,40 @@ def aser_adapter_forward(ctx: Context, X, adapter, A, B, scale, Y0, Y) -> int:
 
 # ----------------------------------------------------------------------------------- microscaled 4 bits, experts
 class Mx4:
-    """Matrices in microscaled 4 bits from their tensors (C struct aser_mx4): codes, rows x width / 2, and scales, width / 128 x rows x 4, uint8 and
-    contiguous, width being n rounded up to a multiple of 128; with one more dimension in front for several matrices (experts)."""
+    """Matrices in microscaled 4 bits from their tensors (C struct aser_mx4), uint8 and contiguous, in the library's layout when `rows` is given: codes, panels x
+    words x 16 x 64, and scales, panels x words x 16 x 4, panels being ceil(rows / 16) and words ceil(n / 128); with one more dimension in front
+    for several matrices (experts).  Without it codes are rows x 64 words and scales words x rows x 4, and are laid out anew (copies)."""
 
-    def __init__(self, codes, scales, n: int):
+    def __init__(self, codes, scales, n: int, rows: Optional[int] = None):
         import torch
-        width = (n + 127) // 128 * 128
-        front = tuple(codes.shape[:-2])
+        words = (n + 127) // 128
         if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
             raise TypeError("codes and scales must be uint8")
-        if codes.dim() not in (2, 3) or codes.shape[-1] != width // 2 or tuple(scales.shape) != front + (width // 128, codes.shape[-2], 4):
-            raise ValueError("codes must be (matrices x) rows x width / 2, scales (matrices x) width / 128 x rows x 4")
+        self.device = _same_device(codes, scales)
+        if rows is None:
+            if codes.dim() not in (2, 3) or tuple(scales.shape) != tuple(codes.shape[:-2]) + (words, codes.shape[-2], 4) or codes.shape[-1] != 64 * words:
+                raise ValueError("codes must be (matrices x) rows x 64 words, scales (matrices x) words x rows x 4")
+            rows, pad = codes.shape[-2], -codes.shape[-2] % 16
+            laid = []
+            for t in (codes.unflatten(-1, (words, 64)), scales.transpose(-3, -2)):
+                t = torch.nn.functional.pad(t, (0, 0, 0, 0, 0, pad)) if pad else t
+                laid.append(t.unflatten(-3, ((rows + pad) // 16, 16)).transpose(-3, -2).contiguous())
+            codes, scales = laid
+        front, shape = tuple(codes.shape[:-4]), ((rows + 15) // 16, words, 16)
+        if codes.dim() not in (4, 5) or tuple(codes.shape) != front + shape + (64,) or tuple(scales.shape) != front + shape + (4,):
+            raise ValueError("codes must be (matrices x) panels x words x 16 x 64, scales (matrices x) panels x words x 16 x 4")
         if not (codes.is_contiguous() and scales.is_contiguous()):
             raise ValueError("codes and scales must be contiguous")
-        self.device = _same_device(codes, scales)
-        self.codes, self.scales, self.n, self.rows, self.count = codes, scales, n, codes.shape[-2], front[0] if front else 1
-        self.c = aser_mx4(_ptr(codes), _ptr(scales), self.rows, n, self.count)
+        self.codes, self.scales, self.n, self.rows, self.count, self.front = codes, scales, n, rows, front[0] if front else 1, front
+        self.c = aser_mx4(_ptr(codes), _ptr(scales), rows, n, self.count)
         self.ref = ctypes.byref(self.c)
 
     @classmethod
     def empty(cls, rows: int, n: int, count: Optional[int] = None, device: int = 0):
         """Room for one matrix, or with count for several."""
         import torch
-        width, front = (n + 127) // 128 * 128, () if count is None else (count,)
-        make = lambda *shape: torch.empty(front + shape, dtype=torch.uint8, device="cuda:%d" % device)     # noqa: E731
-        return cls(make(rows, width // 2), make(width // 128, rows, 4), n)
+        shape = (() if count is None else (count,)) + ((rows + 15) // 16, (n + 127) // 128, 16)
+        return cls(*(torch.empty(shape + (k,), dtype=torch.uint8, device="cuda:%d" % device) for k in (64, 4)), n, rows)
 
 
 class ExpertPlan:
@@ -760,8 +769,7 @@ def _product(ctx: Context, x: Mx4, w: Mx4, Y, rows: int, L_A, L_B, swiglu: bool)
         raise ValueError("L_A and L_B go together")
     if L_A is not None:
         r = L_A.shape[-1]
-        front = tuple(w.codes.shape[:-2])
-        if tuple(L_A.shape) != front + (w.rows, r) or tuple(L_B.shape) != front + (r, w.n) or not (L_A.is_contiguous() and L_B.is_contiguous()):
+        if tuple(L_A.shape) != w.front + (w.rows, r) or tuple(L_B.shape) != w.front + (r, w.n) or not (L_A.is_contiguous() and L_B.is_contiguous()):
             raise ValueError("L_A must be (matrices x) outputs x r and L_B (matrices x) r x channels, contiguous")
         if L_A.dtype != bf16 or L_B.dtype != bf16:
             raise TypeError("L_A and L_B must be bfloat16")

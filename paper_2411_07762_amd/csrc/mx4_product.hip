@@ -13,27 +13,30 @@ namespace {
 
 typedef int v4i_t __attribute__((ext_vector_type(4)));
 typedef int v8i_t __attribute__((ext_vector_type(8)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 struct MxArgs {
     MxGroups groups;
-    const uint8_t* xc; const uint32_t* xs; int64_t x_rows;
-    const uint8_t* wc; const uint32_t* ws; int64_t m;      // rows of a weight matrix
+    const uint8_t* xc; const uint32_t* xs;
+    const uint8_t* wc; const uint32_t* ws; int64_t m, w_size;   // rows of a weight matrix, units from one to the next
     int64_t n; int words;
-    const uint16_t* la; const uint16_t* lb; int r, rp;      // rp: r rounded up to 16
-    float* P; int parts; int part_words;                    // [part][position][rp]
+    const uint16_t* la; const uint16_t* lb; int r;
+    int64_t la_ld;                                          // rows of L_A: r, or what they are padded to
+    float* P; int parts, part_words, rp;                    // few rows: [part][position][rp] fp32, rp: r rounded up to 16
+    uint16_t* planes; int lr_steps;                         // many rows: [term][position][32 lr_steps / terms] bf16; steps of 32 ranks and one term
     void* Y; int64_t ldy; int64_t outs;                     // columns of Y
-    bool vec;                                               // four columns of Y at a time
-    bool la_vec, lb_vec;                                    // rows of the factors in 16-byte loads
+    bool vec;                                               // 16 bytes (few rows: four columns) of Y at a time
+    bool lb_vec;                                            // rows of L_B in 16-byte loads
 };
 
 // Four-bit operands are the first four registers of the instruction's eight.
 __device__ __forceinline__ v8i_t wide(const v4i_t& v) { return v8i_t{v[0], v[1], v[2], v[3], 0, 0, 0, 0}; }
-template <int B>
 __device__ __forceinline__ f32x4_t mfma16(const v4i_t& a, uint32_t sa, const v4i_t& b, uint32_t sb, const f32x4_t& c) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(a), wide(b), c, 4, 4, B, (int)sa, B, (int)sb);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(a), wide(b), c, 4, 4, 0, (int)sa, 0, (int)sb);
 }
 
 __device__ __forceinline__ float gated(float gate, float up) { return gate / (1.f + expf(-gate)) * up; }
@@ -55,149 +58,189 @@ __device__ __forceinline__ void store4(const MxArgs& g, int64_t p, int64_t o, co
 }
 
 // ---------------------------------------------------------------------------------------------------------------- P = x L_B^T
-// 16 positions a workgroup; four wavefronts share a part of the channels, a scale word at a time: lane group q = lane / 16 has block q of it, 32 channels of
-// its token, which become bf16 (exactly) eight at a time and meet 64 bytes of each row of L_B.  Ranks are in the rows of the accumulator.
-template <int RF>
-__global__ __launch_bounds__(256) void mx4_down_kernel(MxArgs g) {
-    __shared__ __align__(16) float part[4][RF][64][4];
+// 16 NT positions and 16 RF ranks a workgroup; W wavefronts share a part of the channels, a word at a time with the next one's loads in flight: lane group q =
+// lane / 16 has block q of it, 32 channels of its token, which become bf16 (exactly) eight at a time and meet 64 bytes of each row of L_B.  Ranks are in the rows
+// of the accumulator.  TERMS = 0: fp32 sums of the part; otherwise (one part) the sum as so many bf16 terms, each what the ones before leave, rounded.
+template <int RF, int NT, int W, int TERMS>
+__global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_tiles) {
+    extern __shared__ __align__(16) float part[];            // [wavefront][fragment][lane][4]
     const int lane = threadIdx.x & 63, li = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int pt = blockIdx.x % g.parts;
+    const int rt = blockIdx.x % rank_tiles, rest = blockIdx.x / rank_tiles, pt = rest % g.parts;
     int e, rows;
     int64_t p0;
-    if (!mx4_find_tile(g.groups, blockIdx.x / g.parts, 16, &e, &p0, &rows)) return;
-    const int64_t row = mx4_row(g.groups, p0 + (li < rows ? li : rows - 1));
-    const uint8_t* const xc = g.xc + row * g.words * 64 + 16 * q;
-    const uint32_t* const xs = g.xs + row;
-    const uint16_t* const lb = g.lb + (int64_t)e * g.r * g.n;
-    f32x4_t acc[RF];
+    if (!mx4_find_tile(g.groups, rest / g.parts, 16 * NT, &e, &p0, &rows)) return;
+    int64_t xat[NT];
 #pragma unroll
-    for (int f = 0; f < RF; ++f) acc[f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < NT; ++t) xat[t] = mx4_at(mx4_row(g.groups, p0 + (16 * t + li < rows ? 16 * t + li : rows - 1)), g.words);
+    const uint16_t* const lb = g.lb + (int64_t)e * g.r * g.n + 32 * q;
+    f32x4_t acc[RF][NT];
+#pragma unroll
+    for (int f = 0; f < RF; ++f)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[f][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     const int first = pt * g.part_words, last = first + g.part_words < g.words ? first + g.part_words : g.words;
-    for (int w = first + wave; w < last; w += 4) {
-        const v4i_t codes = *(const v4i_t*)(xc + (int64_t)w * 64);
-        const uint32_t byte = (xs[(int64_t)w * g.x_rows] >> (8 * q)) & 255u;
-        const float scale = byte == 0 ? __uint_as_float(0x00400000u) : byte == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(byte << 23);
-        const int64_t c0 = (int64_t)w * kMxWord + 32 * q;
+    v4i_t codes[2][NT];
+    uint32_t scale[2][NT];
+    uint4 a[2][RF][4];
+    auto load = [&](int u, int w) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            typedef float pair_t __attribute__((ext_vector_type(2)));
-            const uint32_t w4 = (uint32_t)codes[j];
-            const pair_t v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w4, 1.f, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w4, 1.f, 1),
-                         v2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w4, 1.f, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w4, 1.f, 3);
-            const uint4 xv = make_uint4(upper_halves(v0[0] * scale, v0[1] * scale), upper_halves(v1[0] * scale, v1[1] * scale),
-                                        upper_halves(v2[0] * scale, v2[1] * scale), upper_halves(v3[0] * scale, v3[1] * scale));
-            const bf16x8_t b = __builtin_bit_cast(bf16x8_t, xv);
-            const int64_t c = c0 + 8 * j;
+        for (int t = 0; t < NT; ++t) {
+            const int64_t at = xat[t] + (int64_t)w * kMxNext;
+            codes[u][t] = *(const v4i_t*)(g.xc + at * 64 + 16 * q);
+            scale[u][t] = g.xs[at];
+        }
+        const int64_t c0 = (int64_t)w * kMxWord;
 #pragma unroll
-            for (int f = 0; f < RF; ++f) {
-                const int k = 16 * f + li;
-                uint4 a = make_uint4(0u, 0u, 0u, 0u);
-                if (k < g.r) {
-                    const uint16_t* src = lb + (int64_t)k * g.n + c;
-                    if (g.lb_vec) {                          // n is a multiple of 8: eight channels are there or none
-                        if (c < g.n) a = *(const uint4*)src;
-                    } else {
-                        uint32_t h[8];
+        for (int f = 0; f < RF; ++f) {
+            const int k = 16 * (rt * RF + f) + li;
+            const uint16_t* src = lb + (int64_t)k * g.n + c0;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) h[i] = c + i < g.n ? src[i] : 0u;
-                        a = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
-                    }
+            for (int j = 0; j < 4; ++j) {
+                a[u][f][j] = make_uint4(0u, 0u, 0u, 0u);
+                if (k >= g.r) continue;
+                const int64_t c = c0 + 32 * q + 8 * j;
+                if (g.lb_vec) {                              // n is a multiple of 8: eight channels are there or none
+                    if (c < g.n) a[u][f][j] = *(const uint4*)(src + 8 * j);
+                } else {
+                    uint32_t h[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) h[i] = c + i < g.n ? src[8 * j + i] : 0u;
+                    a[u][f][j] = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
                 }
-                acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), b, acc[f], 0, 0, 0);
             }
         }
+    };
+    auto multiply = [&](int u) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const float by = __uint_as_float(((scale[u][t] >> (8 * q)) & 255u) << 23);        // the conversion takes the exponent field for what it is in a scale byte
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t w4 = (uint32_t)codes[u][t][j];
+                const bf16x2_t v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 1),
+                               v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 3);
+                const bf16x8_t b = {v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+#pragma unroll
+                for (int f = 0; f < RF; ++f) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a[u][f][j]), b, acc[f][t], 0, 0, 0);
+            }
+        }
+    };
+    if (first + wave < last) load(0, first + wave);
+    for (int w = first + wave; w < last; w += 2 * W) {
+        if (w + W < last) load(1, w + W);
+        multiply(0);
+        if (w + 2 * W < last) load(0, w + 2 * W);
+        if (w + W < last) multiply(1);
     }
+    f32x4_t* const mine = (f32x4_t*)part + lane;
 #pragma unroll
-    for (int f = 0; f < RF; ++f) *(f32x4_t*)part[wave][f][lane] = acc[f];
+    for (int f = 0; f < RF; ++f)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) mine[(wave * RF * NT + f * NT + t) * 64] = acc[f][t];
     __syncthreads();
-    for (int f = wave; f < RF; f += 4) {                     // ranks 16 f + 4 q .. + 3 of token li
-        f32x4_t sum = *(const f32x4_t*)part[0][f][lane];
+    for (int i = wave; i < RF * NT; i += W) {                // ranks 16 f + 4 q .. + 3 of token li
+        f32x4_t sum = mine[i * 64];
 #pragma unroll
-        for (int w = 1; w < 4; ++w) sum += *(const f32x4_t*)part[w][f][lane];
-        if (li < rows) *(f32x4_t*)(g.P + ((int64_t)pt * g.groups.positions + p0 + li) * g.rp + 16 * f + 4 * q) = sum;
+        for (int w = 1; w < W; ++w) sum += mine[(w * RF * NT + i) * 64];
+        const int k = 16 * (rt * RF + i / NT) + 4 * q, at = 16 * (i % NT) + li;
+        if (at >= rows) continue;
+        if (TERMS == 0) {
+            if (k < g.rp) *(f32x4_t*)(g.P + ((int64_t)pt * g.groups.positions + p0 + at) * g.rp + k) = sum;
+            continue;
+        }
+        const int64_t width = g.lr_steps / (TERMS ? TERMS : 1) * 32;
+        if (k >= width) continue;
+        uint16_t* dst = g.planes + (p0 + at) * width + k;
+#pragma unroll
+        for (int u = 0; u < TERMS; ++u, dst += g.groups.positions * width) {
+            const uint32_t w0 = bf16_pair(sum[0], sum[1]), w1 = bf16_pair(sum[2], sum[3]);
+            *(uint2*)dst = make_uint2(w0, w1);
+            sum -= f32x4_t{__uint_as_float(w0 << 16), __uint_as_float(w0 & 0xFFFF0000u), __uint_as_float(w1 << 16), __uint_as_float(w1 & 0xFFFF0000u)};
+        }
     }
 }
 
+// L_A with its rows padded with zeros to a multiple of 32 ranks, where the tiles cannot take it as it is.
+__global__ __launch_bounds__(256) void mx4_pad_kernel(const uint16_t* __restrict__ la, int64_t rows, int r, int width, uint16_t* __restrict__ out) {
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, row = i / width;
+    const int k = (int)(i - row * width);
+    if (row >= rows) return;
+    uint32_t v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = k + u < r ? la[row * r + k + u] : 0u;
+    *(uint4*)(out + i) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+}
+
 // ---------------------------------------------------------------------------------------------------------------- few rows of a matrix
-// A workgroup has 16 outputs (of each half, if gated) of up to 16 NT positions; its W wavefronts share the channels in chunks of 512, of which lane
-// group q has the four blocks of word 4 c + q: one word of scales for four instructions, 64 bytes of codes a lane.  Outputs are in the rows of the
-// accumulator, so a lane has four neighbouring ones of a position.  The sums of the wavefronts meet in LDS in a fixed order.
-template <int NA, int NT, int W, bool F32>
+// A workgroup has 16 FA rows of the weights (gated: half of them gates, the others their values) and up to 16 NT positions; its W wavefronts take the words of
+// the channels in turn, U of them ahead.  A fragment of a word, a panel's 16 rows, is a kilobyte of memory in a row; a lane's 16 bytes are block lane / 16 of row
+// lane % 16.  Outputs are in the rows of the accumulator, so a lane has four neighbouring ones of a position.  The sums of the wavefronts meet in LDS in a fixed
+// order.
+template <int FA, int NT, int W, int U, bool GATED, bool F32>
 __global__ __launch_bounds__(64 * W) void mx4_few_kernel(MxArgs g) {
     extern __shared__ __align__(16) float part[];            // [wavefront][fragment][lane][4]
+    constexpr int OF = GATED ? FA / 2 : FA;                  // fragments of outputs
     const int lane = threadIdx.x & 63, li = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int e, rows;
     int64_t p0;
     if (!mx4_find_tile(g.groups, blockIdx.y, 16 * NT, &e, &p0, &rows)) return;
-    const int64_t o0 = (int64_t)blockIdx.x * 16, o = o0 + li < g.outs ? o0 + li : g.outs - 1;     // past the end: the last one again, not stored
-    const uint8_t* ac[NA];
-    const uint32_t* as[NA];
+    const int64_t o0 = (int64_t)blockIdx.x * (16 * OF);
+    int64_t arow[FA], aat[FA], bat[NT];
 #pragma unroll
-    for (int a = 0; a < NA; ++a) {
-        const int64_t row = o + a * g.outs;
-        ac[a] = g.wc + ((int64_t)e * g.m + row) * g.words * 64;
-        as[a] = g.ws + (int64_t)e * g.words * g.m + row;
+    for (int a = 0; a < FA; ++a) {
+        const int64_t o = o0 + 16 * (a % OF) + li;           // past the end: the last one again, not stored
+        arow[a] = (a >= OF ? g.outs : 0) + (o < g.outs ? o : g.outs - 1);
+        aat[a] = e * g.w_size + mx4_at(arow[a], g.words);
     }
-    const uint8_t* bc[NT];
-    const uint32_t* bs[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int at = 16 * t + li;
-        const int64_t row = mx4_row(g.groups, p0 + (at < rows ? at : rows - 1));
-        bc[t] = g.xc + row * g.words * 64;
-        bs[t] = g.xs + row;
-    }
-    f32x4_t acc[NA][NT];
+    for (int t = 0; t < NT; ++t) bat[t] = mx4_at(mx4_row(g.groups, p0 + (16 * t + li < rows ? 16 * t + li : rows - 1)), g.words);
+    const uint8_t* const wc = g.wc + 16 * q;
+    const uint8_t* const xc = g.xc + 16 * q;
+    f32x4_t acc[FA][NT];
 #pragma unroll
-    for (int a = 0; a < NA; ++a)
+    for (int a = 0; a < FA; ++a)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[a][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int c = wave; 4 * c < g.words; c += W) {
-        const bool there = 4 * c + q < g.words;
-        const int64_t w = there ? 4 * c + q : g.words - 1;
-        v4i_t av[NA][4], bv[NT][4];
-        uint32_t sa[NA], sb[NT];
+    v4i_t av[U][FA], bv[U][NT];
+    uint32_t sa[U][FA], sb[U][NT];
+    auto load = [&](int u, int w) {
 #pragma unroll
-        for (int a = 0; a < NA; ++a) {
-            sa[a] = as[a][w * g.m];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) av[a][j] = *(const v4i_t*)(ac[a] + w * 64 + 16 * j);
+        for (int a = 0; a < FA; ++a) {
+            const int64_t at = aat[a] + (int64_t)w * kMxNext;
+            av[u][a] = *(const v4i_t*)(wc + at * 64);
+            sa[u][a] = g.ws[at];
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            sb[t] = bs[t][w * g.x_rows];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) bv[t][j] = *(const v4i_t*)(bc[t] + w * 64 + 16 * j);
+            const int64_t at = bat[t] + (int64_t)w * kMxNext;
+            bv[u][t] = *(const v4i_t*)(xc + at * 64);
+            sb[u][t] = g.xs[at];
         }
-        if (!there) {                                        // words past the end: zeros, at scales that keep them so
+    };
 #pragma unroll
-            for (int a = 0; a < NA; ++a) {
-                sa[a] = 0x7F7F7F7Fu;
+    for (int u = 0; u < U; ++u)
+        if (wave + u * W < g.words) load(u, wave + u * W);
+    for (int w = wave; w < g.words; w += U * W) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) av[a][j] = v4i_t{0, 0, 0, 0};
+        for (int u = 0; u < U; ++u) {
+            if (w + u * W < g.words) {
+#pragma unroll
+                for (int a = 0; a < FA; ++a)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) acc[a][t] = mfma16(av[u][a], sa[u][a] >> (8 * q), bv[u][t], sb[u][t] >> (8 * q), acc[a][t]);
             }
-#pragma unroll
-            for (int t = 0; t < NT; ++t) sb[t] = 0x7F7F7F7Fu;
+            if (w + (u + U) * W < g.words) load(u, w + (u + U) * W);
         }
-#pragma unroll
-        for (int a = 0; a < NA; ++a)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                acc[a][t] = mfma16<0>(av[a][0], sa[a], bv[t][0], sb[t], acc[a][t]);
-                acc[a][t] = mfma16<1>(av[a][1], sa[a], bv[t][1], sb[t], acc[a][t]);
-                acc[a][t] = mfma16<2>(av[a][2], sa[a], bv[t][2], sb[t], acc[a][t]);
-                acc[a][t] = mfma16<3>(av[a][3], sa[a], bv[t][3], sb[t], acc[a][t]);
-            }
     }
     if (g.P) {                                               // four ranks an instruction, in fp32; the wavefronts share them
         const uint16_t* la = g.la + (int64_t)e * g.m * g.r;
         for (int k0 = 4 * wave; k0 < g.r; k0 += 4 * W) {
             const int k = k0 + q;
-            float lv[NA], pv[NT];
+            float lv[FA], pv[NT];
 #pragma unroll
-            for (int a = 0; a < NA; ++a) lv[a] = k < g.r ? __uint_as_float((uint32_t)la[(o + a * g.outs) * g.r + k] << 16) : 0.f;
+            for (int a = 0; a < FA; ++a) lv[a] = k < g.r ? __uint_as_float((uint32_t)la[arow[a] * g.r + k] << 16) : 0.f;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const int at = 16 * t + li;
@@ -206,42 +249,43 @@ __global__ __launch_bounds__(64 * W) void mx4_few_kernel(MxArgs g) {
                 for (int p = 0; p < g.parts; ++p) pv[t] += src[(int64_t)p * g.groups.positions * g.rp];
             }
 #pragma unroll
-            for (int a = 0; a < NA; ++a)
+            for (int a = 0; a < FA; ++a)
 #pragma unroll
                 for (int t = 0; t < NT; ++t) acc[a][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(lv[a], pv[t], acc[a][t], 0, 0, 0);
         }
     }
     f32x4_t* const mine = (f32x4_t*)part + lane;
 #pragma unroll
-    for (int a = 0; a < NA; ++a)
+    for (int a = 0; a < FA; ++a)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) mine[((wave * NA + a) * NT + t) * 64] = acc[a][t];
+        for (int t = 0; t < NT; ++t) mine[((wave * FA + a) * NT + t) * 64] = acc[a][t];
     __syncthreads();
-    for (int t = wave; t < NT; t += W) {
-        f32x4_t z[NA];
+    for (int i = wave; i < OF * NT; i += W) {
+        const int a = i / NT, t = i % NT;
+        f32x4_t z = mine[(a * NT + t) * 64], up = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (GATED) up = mine[((a + OF) * NT + t) * 64];
 #pragma unroll
-        for (int a = 0; a < NA; ++a) {
-            z[a] = mine[(a * NT + t) * 64];
-#pragma unroll
-            for (int w = 1; w < W; ++w) z[a] += mine[((w * NA + a) * NT + t) * 64];
+        for (int w = 1; w < W; ++w) {
+            z += mine[((w * FA + a) * NT + t) * 64];
+            if (GATED) up += mine[((w * FA + a + OF) * NT + t) * 64];
         }
         float y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = NA == 2 ? gated(z[0][i], z[NA - 1][i]) : z[0][i];
+        for (int u = 0; u < 4; ++u) y[u] = GATED ? gated(z[u], up[u]) : z[u];
         const int at = 16 * t + li;
-        if (at < rows) store4<F32>(g, p0 + at, o0 + 4 * q, y);
+        if (at < rows) store4<F32>(g, p0 + at, o0 + 16 * a + 4 * q, y);
     }
 }
 
 // ---------------------------------------------------------------------------------------------------------------- many rows of a matrix
-// A workgroup has 64 MF outputs of 64 NF positions, a wavefront (2 x 2 of them, one for each SIMD) 32 MF x 32 NF.  A step is a scale word, 128 channels: 64 bytes of
-// codes of every row and a word of scales go straight from memory into LDS, in 16-byte chunks whose place in a row is turned by the row so that 32 rows' reads meet all banks; a ring of
+// A workgroup has 64 MF outputs of 64 NF positions, a wavefront (2 x 2 of them, one for each SIMD) 32 MF x 32 NF.  A step is a word of the channels: 64 bytes of
+// codes and a word of scales of every row go straight from memory into LDS, in 16-byte chunks whose place in a row is turned by the row so that 32 rows' reads meet all banks; a ring of
 // four stages keeps three steps of loads in flight, one barrier a step.  The loads are inline assembly because the compiler would
 // make every LDS read wait for all of them.  Half h = lane / 32 of the lanes holds blocks h and 2 + h of a step, one for each of its two instructions
 // per pair of fragments, whose scales are bytes 0 and 2 of its word shifted by h bytes.
 // Gated, a wavefront's first MF / 2 fragments are gates and the others the values that belong to them.
 // Workgroup b runs on XCD b % 8; an XCD's tiles are numbered in panels of kPanel tiles of positions, so that its 32 workgroups share few slabs of either operand.
-constexpr int kStages = 4, kPanel = 4;
+constexpr int kPanel = 4;
 
 __device__ __forceinline__ int chunk_at(int r, int c) { return r * 64 + ((c ^ ((r >> 2) & 3)) << 4); }
 
@@ -250,8 +294,12 @@ __device__ __forceinline__ f32x16_t mfma32(const v4i_t& a, uint32_t sa, const v4
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(a), wide(b), c, 4, 4, B, (int)sa, B, (int)sb);
 }
 
-template <int MF, int NF, bool GATED, bool F32>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void mx4_tile_kernel(MxArgs g, int out_tiles) {
+__device__ __forceinline__ f32x16_t mfma32_bf16(const v4i_t& a, const v4i_t& b, const f32x16_t& c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+template <int MF, int NF, int ST, int WG, bool GATED, bool F32>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) void mx4_tile_kernel(MxArgs g, int out_tiles) {
     extern __shared__ __align__(16) char smem[];
     constexpr int BM = 64 * MF, BN = 64 * NF;
     constexpr int A_BYTES = BM * 64, B_BYTES = BN * 64, SA = A_BYTES + B_BYTES, SB = SA + BM * 4, STAGE = SB + BN * 4;
@@ -285,31 +333,30 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
 
     // what this lane fetches: chunk lane % 4 of a row's slab of 64 bytes, 16 rows an instruction, and words of scales, 64 rows an instruction
     const char *ga[MF], *gb[NF], *gs[2];
-    const int64_t pitch = (int64_t)g.words * 64;
     const int ch = (lane & 3) ^ ((lane >> 4) & 3);
 #pragma unroll
-    for (int t = 0; t < MF; ++t) ga[t] = (const char*)g.wc + ((int64_t)e * g.m + weight_row(16 * (MF * wave + t) + (lane >> 2))) * pitch + 16 * ch;
+    for (int t = 0; t < MF; ++t) ga[t] = (const char*)g.wc + (e * g.w_size + mx4_at(weight_row(16 * (MF * wave + t) + (lane >> 2)), g.words)) * 64 + 16 * ch;
 #pragma unroll
-    for (int t = 0; t < NF; ++t) gb[t] = (const char*)g.xc + token_row(16 * (NF * wave + t) + (lane >> 2)) * pitch + 16 * ch;
-    gs[0] = (const char*)(g.ws + (int64_t)e * g.words * g.m + weight_row(64 * (wave % MF) + lane));
-    gs[1] = (const char*)(g.xs + token_row(64 * (wave % NF) + lane));
-    const int64_t sa_step = g.m * 4, sb_step = g.x_rows * 4;
+    for (int t = 0; t < NF; ++t) gb[t] = (const char*)g.xc + mx4_at(token_row(16 * (NF * wave + t) + (lane >> 2)), g.words) * 64 + 16 * ch;
+    gs[0] = (const char*)(g.ws + e * g.w_size + mx4_at(weight_row(64 * (wave % MF) + lane), g.words));
+    gs[1] = (const char*)(g.xs + mx4_at(token_row(64 * (wave % NF) + lane), g.words));
+    int64_t next_a = kMxNext * 64, next_b = kMxNext * 64, next_s = kMxNext * 4;      // bytes to the following stage
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-    // load number t of a stage
-    auto issue = [&](int64_t s, int t) {
-        const uint32_t slot = ring + (uint32_t)(s & (kStages - 1)) * STAGE;
+    // load number t of a stage, to the slot at byte `at` of the ring
+    auto issue = [&](uint32_t at, int t) {
+        const uint32_t slot = ring + at;
         if (t < MF) {
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(slot + (uint32_t)(MF * wave + t) * 1024), "v"(ga[t]) : "memory", "m0");
-            ga[t] += 64;
+            ga[t] += next_a;
         } else if (t < MF + NF) {
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(slot + A_BYTES + (uint32_t)(NF * wave + t - MF) * 1024), "v"(gb[t - MF]) : "memory", "m0");
-            gb[t - MF] += 64;
+            gb[t - MF] += next_b;
         } else if (t == MF + NF) {
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(slot + SA + (uint32_t)(wave % MF) * 256), "v"(gs[0]) : "memory", "m0");
-            gs[0] += sa_step;
+            gs[0] += next_s;
         } else {
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(slot + SB + (uint32_t)(wave % NF) * 256), "v"(gs[1]) : "memory", "m0");
-            gs[1] += sb_step;
+            gs[1] += next_s;
         }
     };
     auto wait = [&](int stages) {                            // until at most the loads of so many later stages are in flight
@@ -343,22 +390,50 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         if (t < MF) a1[t] = *(const v4i_t*)(st + (offa[t] ^ 32));
         else b1[t - MF] = *(const v4i_t*)(st + (offb[t - MF] ^ 32));
     };
-    const int64_t steps = g.words;
-    for (int64_t s = 0; s < kStages - 1 && s < steps; ++s)
+    // Behind the words of the channels come the steps of the low-rank branch, 32 ranks of L_A and of one term of P each: 64 bytes a row as well.
+    constexpr int TERMS = F32 ? 3 : 2;
+    const int words = g.words, steps = words + g.lr_steps;
+    auto turn_to_ranks = [&]() {
+        const int64_t width = 64 * (int64_t)(g.lr_steps / TERMS);        // bytes of a row of P
 #pragma unroll
-        for (int t = 0; t < LOADS; ++t) issue(s, t);
-    wait(steps >= 3 ? 2 : steps == 2 ? 1 : 0);
+        for (int t = 0; t < MF; ++t) ga[t] = (const char*)g.la + ((int64_t)e * g.m + weight_row(16 * (MF * wave + t) + (lane >> 2))) * g.la_ld * 2 + 16 * ch;
+#pragma unroll
+        for (int t = 0; t < NF; ++t) {
+            const int r = 16 * (NF * wave + t) + (lane >> 2);
+            gb[t] = (const char*)g.planes + (p0 + (r < rows ? r : rows - 1)) * width + 16 * ch;
+        }
+        gs[0] -= next_s;                                     // scales are not looked at: the last word's again
+        gs[1] -= next_s;
+        next_s = 0;
+    };
+    // before the loads of stage s
+    auto aim = [&](int s) {
+        if (s < words) return;
+        if (s == words) turn_to_ranks();
+        const int term = (s - words) % TERMS;
+        const int64_t plane = g.groups.positions * 64 * (int64_t)(g.lr_steps / TERMS);
+        next_a = term == TERMS - 1 ? 64 : 0;
+        next_b = term == TERMS - 1 ? 64 - (TERMS - 1) * plane : plane;
+    };
+    for (int s = 0; s < ST - 1 && s < steps; ++s) {
+        aim(s);
+#pragma unroll
+        for (int t = 0; t < LOADS; ++t) issue((uint32_t)s * STAGE, t);
+    }
+    wait(steps >= ST - 1 ? ST - 2 : steps - 1);
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < 2 * (MF + NF); ++t) read0(smem, t);
     constexpr int M = MF * NF;                               // instructions of a half step
     constexpr int R0 = 2 * (MF + NF), R1 = MF + NF;
     constexpr int W = M > 4 ? 1 : 0;                         // the barrier's place in the second half
-    auto step = [&](int64_t s, auto steady_tag) {
-        constexpr bool STEADY = decltype(steady_tag)::value;
-        const char* st = smem + (int)(s & (kStages - 1)) * STAGE;
-        const char* sn = smem + (int)((s + 1) & (kStages - 1)) * STAGE;
-        const bool more = STEADY || s + 1 < steps, fetch = STEADY || s + kStages - 1 < steps;
+    uint32_t cur = 0;                                        // the step's slot
+    auto step = [&](int s, auto steady_tag, auto ranks_tag) {
+        constexpr bool STEADY = decltype(steady_tag)::value, RANKS = decltype(ranks_tag)::value;
+        const uint32_t next = cur + STAGE == ST * STAGE ? 0 : cur + STAGE, put = cur == 0 ? (ST - 1) * STAGE : cur - STAGE;
+        const char *st = smem + cur, *sn = smem + next;
+        const bool more = STEADY || s + 1 < steps, fetch = STEADY || s + ST - 1 < steps;
+        if (!STEADY && fetch) aim(s + ST - 1);
 #pragma unroll
         for (int i = 0; i < MF; ++i) sa[i] = na[i] >> (8 * h);
 #pragma unroll
@@ -367,19 +442,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
 #pragma unroll
         for (int k = 0; k < M; ++k) {
             const int i = k / NF, j = k % NF;
-            acc[i][j] = mfma32<0>(a0[i], sa[i], b0[j], sb[j], acc[i][j]);
+            acc[i][j] = RANKS ? mfma32_bf16(a0[i], b0[j], acc[i][j]) : mfma32<0>(a0[i], sa[i], b0[j], sb[j], acc[i][j]);
 #pragma unroll
             for (int t = 0; t < R1; ++t)
                 if (t * (M / 2) / R1 == k) read1(st, t);
             __builtin_amdgcn_sched_barrier(0);
         }
-        // second half: the wait for the next stage, the reads of its first half, the loads of stage s + 3
+        // second half: the wait for the next stage, the reads of its first half, the loads of the last stage that has a slot
 #pragma unroll
         for (int k = 0; k < M; ++k) {
             const int i = k / NF, j = k % NF;
-            acc[i][j] = mfma32<2>(a1[i], sa[i], b1[j], sb[j], acc[i][j]);
+            acc[i][j] = RANKS ? mfma32_bf16(a1[i], b1[j], acc[i][j]) : mfma32<2>(a1[i], sa[i], b1[j], sb[j], acc[i][j]);
             if (k == W && more) {
-                wait((STEADY || s + 2 < steps) ? 1 : 0);
+                wait(ST == 4 && (STEADY || s + 2 < steps) ? 1 : 0);
                 __syncthreads();                             // everyone's share has landed, and everyone is done with stage s - 1
             }
 #pragma unroll
@@ -387,70 +462,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
                 if (more && W + 1 + t * (M / 2 - W) / R0 == k) read0(sn, t);
 #pragma unroll
             for (int t = 0; t < LOADS; ++t)
-                if (fetch && M / 2 + t * (M / 2) / LOADS == k) issue(s + kStages - 1, t);
+                if (fetch && M / 2 + t * (M / 2) / LOADS == k) issue(put, t);
             __builtin_amdgcn_sched_barrier(0);
         }
+        cur = next;
     };
-    int64_t s = 0;
-    for (; s + kStages - 1 < steps; ++s) step(s, std::true_type{});
-    for (; s < steps; ++s) step(s, std::false_type{});
+    int s = 0;
+    for (; s + ST - 1 < words; ++s) step(s, std::true_type{}, std::false_type{});
+    for (; s < words; ++s) step(s, std::false_type{}, std::false_type{});
+    for (; s < steps; ++s) step(s, std::false_type{}, std::true_type{});
 
-    if (g.P) {                                               // the low-rank branch on the same accumulators: P as three bf16 terms that hold all its bits
-        const uint16_t* const la = g.la + (int64_t)e * g.m * g.r;
-        const uint16_t* lr[MF];
-#pragma unroll
-        for (int i = 0; i < MF; ++i) lr[i] = la + weight_row(wa * 32 * MF + 32 * i + li) * g.r;
-        const float* pr[NF];
-#pragma unroll
-        for (int j = 0; j < NF; ++j) {
-            const int at = wb * 32 * NF + 32 * j + li;
-            pr[j] = g.P + (p0 + (at < rows ? at : rows - 1)) * g.rp;
-        }
-        const int64_t part = g.groups.positions * g.rp;
-#pragma nounroll
-        for (int k0 = 0; k0 < g.r; k0 += 16) {
-            const int k = k0 + 8 * h;
-            bf16x8_t pv[NF][3];
-#pragma unroll
-            for (int j = 0; j < NF; ++j) {
-                float v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = 0.f;
-                for (int p = 0; p < g.parts; ++p) {
-                    const float4 x = *(const float4*)(pr[j] + p * part + k), y = *(const float4*)(pr[j] + p * part + k + 4);
-                    v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
-                }
-#pragma unroll
-                for (int u = 0; u < 3; ++u) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        w[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
-                        v[2 * i] -= __uint_as_float(w[i] << 16);
-                        v[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
-                    }
-                    pv[j][u] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < MF; ++i) {
-                uint4 a = make_uint4(0u, 0u, 0u, 0u);
-                if (g.la_vec) {
-                    if (k < g.r) a = *(const uint4*)(lr[i] + k);
-                } else {
-                    uint32_t q[8];
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) q[u] = k + u < g.r ? lr[i][k + u] : 0u;
-                    a = make_uint4(q[0] | q[1] << 16, q[2] | q[3] << 16, q[4] | q[5] << 16, q[6] | q[7] << 16);
-                }
-                const bf16x8_t av = __builtin_bit_cast(bf16x8_t, a);
-#pragma unroll
-                for (int j = 0; j < NF; ++j)
-#pragma unroll
-                    for (int u = 2; u >= 0; --u) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, pv[j][u], acc[i][j], 0, 0, 0);
-            }
-        }
-    }
     // acc[i][j][k]: output 32 i + 8 (k / 4) + 4 h + k % 4, position 32 j + li of the wavefront's.  32 positions at a time are turned through LDS (the wavefront's own
     // part of it), so that rows of Y are written in whole lines.
     constexpr int OF = GATED ? MF / 2 : MF;                  // fragments of outputs
@@ -504,53 +525,73 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     }
 }
 
-template <int NA, int NT, int W>
-void launch_few(const MxArgs& g, dim3 grid, bool f32, hipStream_t s) {
-    const size_t lds = (size_t)W * NA * NT * 1024;
-    if (f32) mx4_few_kernel<NA, NT, W, true><<<grid, 64 * W, lds, s>>>(g);
-    else mx4_few_kernel<NA, NT, W, false><<<grid, 64 * W, lds, s>>>(g);
+template <int FA, int NT, int W, int U, bool GATED>
+int launch_few_one(aser_ctx* ctx, const MxArgs& g, bool f32) {
+    const size_t lds = (size_t)W * FA * NT * 1024;
+    const int64_t tiles = g.groups.most_tiles(16 * NT);
+    if (tiles > 65535) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: too many rows");
+    const dim3 grid((unsigned)ceil_div64(g.outs, 16 * (GATED ? FA / 2 : FA)), (unsigned)tiles);
+    if (f32) mx4_few_kernel<FA, NT, W, U, GATED, true><<<grid, 64 * W, lds, ctx->stream>>>(g);
+    else mx4_few_kernel<FA, NT, W, U, GATED, false><<<grid, 64 * W, lds, ctx->stream>>>(g);
+    return aser_check_launch(ctx, "mx4_few_kernel");
+}
+template <int FA, int NT, int W, int U>
+int launch_few(aser_ctx* ctx, const MxArgs& g, bool gated, bool f32) {
+    return gated ? launch_few_one<FA, NT, W, U, true>(ctx, g, f32) : launch_few_one<FA, NT, W, U, false>(ctx, g, f32);
 }
 
-template <int MF, int NF, bool GATED, bool F32>
+template <int MF, int NF, int ST, int WG, bool GATED, bool F32>
 int launch_tile_one(aser_ctx* ctx, const MxArgs& g) {
-    constexpr int kRing = kStages * (64 * MF + 64 * NF) * 68, kTurn = 4 * 32 * ((GATED ? MF / 2 : MF) * 32 * (F32 ? 4 : 2) + 16), kLds = kRing > kTurn ? kRing : kTurn;
-    static_assert(kLds <= 160 * 1024, "the ring and the turned outputs have to fit the LDS of a compute unit");
-    const auto kernel = mx4_tile_kernel<MF, NF, GATED, F32>;
+    constexpr int kRing = ST * (64 * MF + 64 * NF) * 68, kTurn = 4 * 32 * ((GATED ? MF / 2 : MF) * 32 * (F32 ? 4 : 2) + 16), kLds = kRing > kTurn ? kRing : kTurn;
+    static_assert(kLds * WG <= 160 * 1024, "the ring and the turned outputs have to fit the LDS of a compute unit");
+    const auto kernel = mx4_tile_kernel<MF, NF, ST, WG, GATED, F32>;
     ASER_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds));
     const int64_t out_tiles = ceil_div64(g.outs, GATED ? 32 * MF : 64 * MF), grid = ceil_div64(g.groups.most_tiles(64 * NF) * out_tiles, 8) * 8;
     if (grid > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: too many rows times outputs");
     kernel<<<(unsigned)grid, 256, kLds, ctx->stream>>>(g, (int)out_tiles);
     return aser_check_launch(ctx, "mx4_tile_kernel");
 }
-template <int MF, int NF>
+template <int MF, int NF, int ST, int WG>
 int launch_tile(aser_ctx* ctx, const MxArgs& g, bool gated, bool f32) {
-    if (gated) return f32 ? launch_tile_one<MF, NF, true, true>(ctx, g) : launch_tile_one<MF, NF, true, false>(ctx, g);
-    return f32 ? launch_tile_one<MF, NF, false, true>(ctx, g) : launch_tile_one<MF, NF, false, false>(ctx, g);
+    if (gated) return f32 ? launch_tile_one<MF, NF, ST, WG, true, true>(ctx, g) : launch_tile_one<MF, NF, ST, WG, true, false>(ctx, g);
+    return f32 ? launch_tile_one<MF, NF, ST, WG, false, true>(ctx, g) : launch_tile_one<MF, NF, ST, WG, false, false>(ctx, g);
 }
 
 struct Plan {
     int nt;                  // 16 nt positions a workgroup
-    int nf;                  // not 0: 64 nf positions a workgroup, 256 outputs
-    int parts, part_words;   // of the channels, for P
-    size_t p_bytes;
+    bool many;               // tiles through LDS instead
+    int parts, part_words;   // few rows: of the channels, for P
+    size_t p_bytes, la_bytes;
 };
 
-Plan plan_product(int64_t positions, int64_t n, int32_t count, int32_t r) {
+Plan plan_product(int64_t positions, int64_t n, int64_t m, int32_t count, int32_t r) {
     Plan p{};
     const int64_t each = ceil_div64(positions, count < positions ? count : positions);
     p.nt = each <= 16 ? 1 : each <= 32 ? 2 : 4;
-    p.nf = each <= 64 ? 0 : each <= 128 ? 2 : 4;
+    p.many = each > 64;
     const int64_t words = mx4_words(n), tiles = ceil_div64(positions, 16);
-    int64_t parts = tiles >= 256 ? 1 : ceil_div64(256, tiles);
-    if (parts > ceil_div64(words, 8)) parts = ceil_div64(words, 8);
+    int64_t parts = p.many || tiles >= 256 ? 1 : ceil_div64(256, tiles);
+    if (parts > ceil_div64(words, 4)) parts = ceil_div64(words, 4);
     p.part_words = (int)ceil_div64(words, parts);
     p.parts = (int)ceil_div64(words, p.part_words);
-    p.p_bytes = r > 0 ? align_up((size_t)p.parts * positions * align_up(r, 16) * 4, 256) : 0;
+    if (r <= 0) return p;
+    if (p.many) {
+        p.p_bytes = align_up((size_t)positions * align_up(r, 32) * 2 * 3, 256);
+        p.la_bytes = align_up((size_t)count * m * align_up(r, 32) * 2, 256);
+    } else {
+        p.p_bytes = align_up((size_t)p.parts * positions * align_up(r, 16) * 4, 256);
+    }
     return p;
 }
 
-template <int RF>
-void launch_down(const MxArgs& g, unsigned grid, hipStream_t s) { mx4_down_kernel<RF><<<grid, 256, 0, s>>>(g); }
+template <int RF, int NT, int W, int TERMS>
+int launch_down(aser_ctx* ctx, const MxArgs& g) {
+    const int rank_tiles = (int)ceil_div64(TERMS ? g.lr_steps / (TERMS ? TERMS : 1) * 32 : g.rp, 16 * RF);
+    const int64_t grid = g.groups.most_tiles(16 * NT) * g.parts * rank_tiles;
+    if (grid > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: too many rows");
+    mx4_down_kernel<RF, NT, W, TERMS><<<(unsigned)grid, 64 * W, (size_t)W * RF * NT * 1024, ctx->stream>>>(g, rank_tiles);
+    return aser_check_launch(ctx, "mx4_down_kernel");
+}
 
 int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx4* w, const MxGroups& groups, const uint16_t* L_A, const uint16_t* L_B, int32_t r,
                 int32_t swiglu, void* Y, int32_t y_dtype, int64_t ldy) {
@@ -565,49 +606,48 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
     if (((uintptr_t)Y & (f32 ? 3 : 1)) || (((uintptr_t)L_A | (uintptr_t)L_B) & 1)) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "%s: misaligned pointer", who);
     if (groups.positions == 0) return ASER_OK;
     if (!Y) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "%s: null pointer", who);
-    const Plan p = plan_product(groups.positions, w->n, w->count, r);
-    if (p.p_bytes && (!ctx->ws || ctx->ws_bytes < p.p_bytes + kAserWsTail)) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "%s: workspace too small", who);
+    const Plan p = plan_product(groups.positions, w->n, w->rows, w->count, r);
+    if (r > 0 && (!ctx->ws || ctx->ws_bytes < p.p_bytes + p.la_bytes + kAserWsTail)) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "%s: workspace too small", who);
     MxArgs g{};
     g.groups = groups;
-    g.xc = x->codes; g.xs = (const uint32_t*)x->scales; g.x_rows = x->rows;
-    g.wc = w->codes; g.ws = (const uint32_t*)w->scales; g.m = w->rows;
     g.n = w->n; g.words = (int)mx4_words(w->n);
-    g.la = L_A; g.lb = L_B; g.r = r; g.rp = (int)align_up(r, 16);
-    g.P = r > 0 ? (float*)ctx->ws : nullptr; g.parts = p.parts; g.part_words = p.part_words;
+    g.xc = x->codes; g.xs = (const uint32_t*)x->scales;
+    g.wc = w->codes; g.ws = (const uint32_t*)w->scales; g.m = w->rows; g.w_size = mx4_size(w->rows, g.words);
+    g.la = L_A; g.lb = L_B; g.r = r; g.la_ld = r;
+    g.parts = p.parts; g.part_words = p.part_words; g.rp = (int)align_up(r, 16);
     g.Y = Y; g.ldy = ldy; g.outs = outs;
-    // the kernel for many rows stores 16 bytes at a time, the other one four columns
-    const int64_t unit = p.nf || f32 ? 16 : 8, size = f32 ? 4 : 2;
+    const int64_t unit = p.many || f32 ? 16 : 8, size = f32 ? 4 : 2;
     g.vec = !((uintptr_t)Y & (unit - 1)) && !(ldy * size & (unit - 1));
-    g.la_vec = !((uintptr_t)L_A & 15) && !(r & 7);
     g.lb_vec = !((uintptr_t)L_B & 15) && !(w->n & 7);
-    const int64_t down = groups.most_tiles(16) * p.parts, tiles = groups.most_tiles(16 * p.nt);
-    if (down > INT32_MAX || tiles > 65535) ASER_FAIL(ctx, ASER_ERR_SHAPE, "%s: too many rows", who);
     ASER_TRY(aser_prepare_device(ctx));
-    if (r > 0) {
-        switch (g.rp / 16) {
-            case 1: launch_down<1>(g, (unsigned)down, ctx->stream); break;
-            case 2: launch_down<2>(g, (unsigned)down, ctx->stream); break;
-            case 3: launch_down<3>(g, (unsigned)down, ctx->stream); break;
-            case 4: launch_down<4>(g, (unsigned)down, ctx->stream); break;
-            case 5: launch_down<5>(g, (unsigned)down, ctx->stream); break;
-            case 6: launch_down<6>(g, (unsigned)down, ctx->stream); break;
-            case 7: launch_down<7>(g, (unsigned)down, ctx->stream); break;
-            default: launch_down<8>(g, (unsigned)down, ctx->stream); break;
+    if (!p.many) {
+        if (r > 0) {
+            g.P = (float*)ctx->ws;
+            ASER_TRY((launch_down<1, 1, 4, 0>(ctx, g)));
         }
-        ASER_TRY(aser_check_launch(ctx, "mx4_down_kernel"));
+        if (p.nt == 1) return swiglu ? launch_few_one<2, 1, 8, 4, true>(ctx, g, f32) : launch_few_one<1, 1, 8, 4, false>(ctx, g, f32);
+        return p.nt == 2 ? launch_few<2, 2, 4, 4>(ctx, g, swiglu, f32) : launch_few<4, 4, 4, 2>(ctx, g, swiglu, f32);
     }
-    if (p.nf) return p.nf == 2 ? launch_tile<4, 2>(ctx, g, swiglu, f32) : launch_tile<4, 4>(ctx, g, swiglu, f32);
-    const dim3 grid((unsigned)ceil_div64(outs, 16), (unsigned)tiles);
-    if (swiglu) {
-        if (p.nt == 1) launch_few<2, 1, 8>(g, grid, f32, ctx->stream);
-        else if (p.nt == 2) launch_few<2, 2, 4>(g, grid, f32, ctx->stream);
-        else launch_few<2, 4, 4>(g, grid, f32, ctx->stream);
-    } else {
-        if (p.nt == 1) launch_few<1, 1, 8>(g, grid, f32, ctx->stream);
-        else if (p.nt == 2) launch_few<1, 2, 4>(g, grid, f32, ctx->stream);
-        else launch_few<1, 4, 4>(g, grid, f32, ctx->stream);
+    if (r > 0) {
+        const int terms = f32 ? 3 : 2, width = (int)align_up(r, 32);
+        g.planes = (uint16_t*)ctx->ws;
+        g.lr_steps = width / 32 * terms;
+        ASER_TRY(f32 ? width > 32 ? (launch_down<4, 2, 8, 3>(ctx, g)) : (launch_down<2, 2, 8, 3>(ctx, g))
+                     : width > 32 ? (launch_down<4, 2, 8, 2>(ctx, g)) : (launch_down<2, 2, 8, 2>(ctx, g)));
+        if (r != width || ((uintptr_t)L_A & 15)) {
+            uint16_t* const padded = (uint16_t*)((char*)ctx->ws + p.p_bytes);
+            const int64_t rows = w->rows * w->count, grid = ceil_div64(rows * width, 2048);
+            if (grid > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "%s: L_A is too large", who);
+            mx4_pad_kernel<<<(unsigned)grid, 256, 0, ctx->stream>>>(L_A, rows, r, width, padded);
+            ASER_TRY(aser_check_launch(ctx, "mx4_pad_kernel"));
+            g.la = padded;
+            g.la_ld = width;
+        }
     }
-    return aser_check_launch(ctx, "mx4_few_kernel");
+#ifndef CFG
+#define CFG 4, 2, 3, 2
+#endif
+    return launch_tile<CFG>(ctx, g, swiglu, f32);
 }
 
 }  // namespace
@@ -627,7 +667,8 @@ extern "C" int aser_mx4_forward(aser_ctx* ctx, const aser_mx4* x, const aser_mx4
 
 extern "C" size_t aser_expert_forward_workspace_bytes(int64_t positions, int64_t n, int64_t m, int32_t n_experts, int32_t r) {
     if (positions <= 0 || n <= 0 || m <= 0 || n_experts <= 0) return kAserWsTail;
-    return plan_product(positions, n, n_experts, r).p_bytes + kAserWsTail;
+    const Plan p = plan_product(positions, n, m, n_experts, r);
+    return p.p_bytes + p.la_bytes + kAserWsTail;
 }
 
 extern "C" int aser_expert_forward(aser_ctx* ctx, const aser_mx4* x, const aser_mx4* w, const aser_expert_plan* plan, int32_t gather, const uint16_t* L_A,

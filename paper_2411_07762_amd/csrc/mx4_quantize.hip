@@ -5,7 +5,7 @@
 // scale byte: no logarithm.  u is scaled by a product with a power of two (exact: what leaves the range of fp32 below rounds to 0 anyway), rounded and packed two at a
 // time by the conversion instruction.
 // A group of 16 lanes has a scale word of a row, 128 channels, a lane 8 of them: 16 bytes of bf16 or twice 16 of fp32.  Neighbouring
-// groups have neighbouring rows, whose words lie side by side.  Bound by memory.
+// groups have neighbouring rows, whose codes and scales lie side by side.  Bound by memory.
 #include "bf16_pair.h"
 #include "mx4.h"
 
@@ -87,14 +87,12 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(QuantArgs g) {
     codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, u[4] * by, u[5] * by, 1.f, 2);
     codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, u[6] * by, u[7] * by, 1.f, 3);
     if (bad) codes = 0;
-    ((uint32_t*)g.codes)[(row * g.words + word) * 16 + li] = codes;
     uint32_t w = byte << (8 * (li >> 2));
     w |= __shfl_xor(w, 4);
     w |= __shfl_xor(w, 8);
-    if (li == 0) {
-        const int64_t e = row / g.rows;
-        g.scales[(e * g.words + word) * g.rows + (row - e * g.rows)] = w;
-    }
+    const int64_t e = row / g.rows, at0 = e * mx4_size(g.rows, g.words) + mx4_at(row - e * g.rows, g.words) + word * kMxNext;
+    ((uint32_t*)g.codes)[at0 * 16 + li] = codes;
+    if (li == 0) g.scales[at0] = w;
     if (!VALUES || here == 0) return;
     pair_t v2[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 1),
                     __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 3)};
