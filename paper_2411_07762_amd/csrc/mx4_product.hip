@@ -23,14 +23,13 @@ struct MxArgs {
     MxGroups groups;
     const uint8_t* xc; const uint32_t* xs;
     const uint8_t* wc; const uint32_t* ws; int64_t m, w_size;   // rows of a weight matrix, units from one to the next
-    int64_t n; int words;
+    int words;
     const uint16_t* la; const uint16_t* lb; int r;
-    int64_t la_ld;                                          // rows of L_A: r, or what they are padded to
+    int64_t la_ld, lb_ld;                                   // their rows: r and n, or what they are padded to
     float* P; int parts, part_words, rp;                    // few rows: [part][position][rp] fp32, rp: r rounded up to 16
     uint16_t* planes; int lr_steps;                         // many rows: [term][position][32 lr_steps / terms] bf16; steps of 32 ranks and one term
     void* Y; int64_t ldy; int64_t outs;                     // columns of Y
     bool vec;                                               // 16 bytes (few rows: four columns) of Y at a time
-    bool lb_vec;                                            // rows of L_B in 16-byte loads
 };
 
 // Four-bit operands are the first four registers of the instruction's eight.
@@ -58,9 +57,9 @@ __device__ __forceinline__ void store4(const MxArgs& g, int64_t p, int64_t o, co
 }
 
 // ---------------------------------------------------------------------------------------------------------------- P = x L_B^T
-// 16 NT positions and 16 RF ranks a workgroup; W wavefronts share a part of the channels, a word at a time with the next one's loads in flight: lane group q =
-// lane / 16 has block q of it, 32 channels of its token, which become bf16 (exactly) eight at a time and meet 64 bytes of each row of L_B.  Ranks are in the rows
-// of the accumulator.  TERMS = 0: fp32 sums of the part; otherwise (one part) the sum as so many bf16 terms, each what the ones before leave, rounded.
+// 16 NT positions and 16 RF ranks a workgroup; W wavefronts share a part of the channels, a word at a time with the next one's loads in flight.  Of each of its four blocks lane
+// group q = lane / 16 has channels 8 q .. + 7 of its token, which become bf16 (exactly), and of its row of L_B: the four groups together read 64 bytes of a row
+// (16 bytes a lane of a row's 256, each on its own, took 20 us instead of TODO for 4099 tokens of 4096 channels and 64 ranks).  Ranks are in the rows of the accumulator.  TERMS = 0: fp32 sums of the part; otherwise (one part) the sum as so many bf16 terms, each what the ones before leave, rounded.
 template <int RF, int NT, int W, int TERMS>
 __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_tiles) {
     extern __shared__ __align__(16) float part[];            // [wavefront][fragment][lane][4]
@@ -73,12 +72,15 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
     int64_t xat[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) xat[t] = mx4_at(mx4_row(g.groups, p0 + (16 * t + li < rows ? 16 * t + li : rows - 1)), g.words);
-    const uint16_t* const lb = g.lb + (int64_t)e * g.r * g.n + 32 * q;
+    const uint16_t* lrow[RF];
     f32x4_t acc[RF][NT];
 #pragma unroll
-    for (int f = 0; f < RF; ++f)
+    for (int f = 0; f < RF; ++f) {
+        const int k = 16 * (rt * RF + f) + li;
+        lrow[f] = g.lb + ((int64_t)e * g.r + (k < g.r ? k : g.r - 1)) * g.lb_ld;
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[f][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
     const int first = pt * g.part_words, last = first + g.part_words < g.words ? first + g.part_words : g.words;
     v4i_t codes[2][NT];
     uint32_t scale[2][NT];
@@ -87,36 +89,25 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int64_t at = xat[t] + (int64_t)w * kMxNext;
-            codes[u][t] = *(const v4i_t*)(g.xc + at * 64 + 16 * q);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) codes[u][t][j] = *(const int*)(g.xc + at * 64 + 16 * j + 4 * q);
             scale[u][t] = g.xs[at];
         }
-        const int64_t c0 = (int64_t)w * kMxWord;
+        const int64_t c0 = (int64_t)w * kMxWord + 8 * q;
+        // Behind the last channel the last ones are read again, against zeros of x; ranks that are not there read the last row, and what becomes of them is not kept.
 #pragma unroll
-        for (int f = 0; f < RF; ++f) {
-            const int k = 16 * (rt * RF + f) + li;
-            const uint16_t* src = lb + (int64_t)k * g.n + c0;
+        for (int j = 0; j < 4; ++j) {
+            const int64_t c = c0 + 32 * j < g.lb_ld ? c0 + 32 * j : g.lb_ld - 8;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                a[u][f][j] = make_uint4(0u, 0u, 0u, 0u);
-                if (k >= g.r) continue;
-                const int64_t c = c0 + 32 * q + 8 * j;
-                if (g.lb_vec) {                              // n is a multiple of 8: eight channels are there or none
-                    if (c < g.n) a[u][f][j] = *(const uint4*)(src + 8 * j);
-                } else {
-                    uint32_t h[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) h[i] = c + i < g.n ? src[8 * j + i] : 0u;
-                    a[u][f][j] = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
-                }
-            }
+            for (int f = 0; f < RF; ++f) a[u][f][j] = *(const uint4*)(lrow[f] + c);
         }
     };
     auto multiply = [&](int u) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const float by = __uint_as_float(((scale[u][t] >> (8 * q)) & 255u) << 23);        // the conversion takes the exponent field for what it is in a scale byte
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
+                const float by = __uint_as_float(((scale[u][t] >> (8 * j)) & 255u) << 23);    // the conversion takes the exponent field for what it is in a scale byte
                 const uint32_t w4 = (uint32_t)codes[u][t][j];
                 const bf16x2_t v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 1),
                                v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 3);
@@ -145,6 +136,9 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
         for (int w = 1; w < W; ++w) sum += mine[(w * RF * NT + i) * 64];
         const int k = 16 * (rt * RF + i / NT) + 4 * q, at = 16 * (i % NT) + li;
         if (at >= rows) continue;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (k + u >= g.r) sum[u] = 0.f;
         if (TERMS == 0) {
             if (k < g.rp) *(f32x4_t*)(g.P + ((int64_t)pt * g.groups.positions + p0 + at) * g.rp + k) = sum;
             continue;
@@ -161,10 +155,10 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
     }
 }
 
-// L_A with its rows padded with zeros to a multiple of 32 ranks, where the tiles cannot take it as it is.
-__global__ __launch_bounds__(256) void mx4_pad_kernel(const uint16_t* __restrict__ la, int64_t rows, int r, int width, uint16_t* __restrict__ out) {
+// A factor with its rows of r padded with zeros, where it cannot be read in pieces of 16 bytes as it is (L_B), or not in pieces of 64 (L_A of many rows).
+__global__ __launch_bounds__(256) void mx4_pad_kernel(const uint16_t* __restrict__ la, int64_t rows, int64_t r, int64_t width, uint16_t* __restrict__ out) {
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, row = i / width;
-    const int k = (int)(i - row * width);
+    const int64_t k = i - row * width;
     if (row >= rows) return;
     uint32_t v[8];
 #pragma unroll
@@ -177,6 +171,8 @@ __global__ __launch_bounds__(256) void mx4_pad_kernel(const uint16_t* __restrict
 // the channels in turn, U of them ahead.  A fragment of a word, a panel's 16 rows, is a kilobyte of memory in a row; a lane's 16 bytes are block lane / 16 of row
 // lane % 16.  Outputs are in the rows of the accumulator, so a lane has four neighbouring ones of a position.  The sums of the wavefronts meet in LDS in a fixed
 // order.
+constexpr int kMostParts = 4;                                // of the channels, for P of few rows
+
 template <int FA, int NT, int W, int U, bool GATED, bool F32>
 __global__ __launch_bounds__(64 * W) void mx4_few_kernel(MxArgs g) {
     extern __shared__ __align__(16) float part[];            // [wavefront][fragment][lane][4]
@@ -222,6 +218,38 @@ __global__ __launch_bounds__(64 * W) void mx4_few_kernel(MxArgs g) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
         if (wave + u * W < g.words) load(u, wave + u * W);
+    // the low-rank branch: 16 ranks at a time, each such chunk by one wavefront, four ranks an instruction, in fp32.  P's parts are summed into LDS; lane group q has
+    // ranks 4 q .. + 3 of a chunk, of its four outputs' rows of L_A here and of P later
+    constexpr int CHUNKS = 8 / W;
+    uint32_t lv[CHUNKS][FA][2];
+    if (g.P) {
+        const uint16_t* const la = g.la + (int64_t)e * g.m * g.r;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int a = 0; a < FA; ++a) {
+                const int k = 16 * (wave + c * W) + 4 * q;
+                const uint16_t* const src = la + arow[a] * g.r + k;
+                uint32_t h[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) h[i] = k + i < g.r ? src[i] : 0u;
+                lv[c][a][0] = h[0] | h[1] << 16;
+                lv[c][a][1] = h[2] | h[3] << 16;
+            }
+        const int four = g.rp / 4;
+        const int64_t next = g.groups.positions * g.rp;
+        for (int i = threadIdx.x; i < 16 * NT * four; i += 64 * W) {
+            const int at = i / four, k = 4 * (i - at * four);
+            const float* src = g.P + (p0 + (at < rows ? at : rows - 1)) * g.rp + k;
+            f32x4_t sum = *(const f32x4_t*)src;
+            f32x4_t more[kMostParts - 1];
+#pragma unroll
+            for (int p = 1; p < kMostParts; ++p) more[p - 1] = p < g.parts ? *(const f32x4_t*)(src + p * next) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int p = 1; p < kMostParts; ++p) sum += more[p - 1];
+            *(f32x4_t*)(part + at * (g.rp + 4) + k) = sum;
+        }
+    }
     for (int w = wave; w < g.words; w += U * W) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -234,25 +262,23 @@ __global__ __launch_bounds__(64 * W) void mx4_few_kernel(MxArgs g) {
             if (w + (u + U) * W < g.words) load(u, w + (u + U) * W);
         }
     }
-    if (g.P) {                                               // four ranks an instruction, in fp32; the wavefronts share them
-        const uint16_t* la = g.la + (int64_t)e * g.m * g.r;
-        for (int k0 = 4 * wave; k0 < g.r; k0 += 4 * W) {
-            const int k = k0 + q;
-            float lv[FA], pv[NT];
+    if (g.P) {
+        __syncthreads();
 #pragma unroll
-            for (int a = 0; a < FA; ++a) lv[a] = k < g.r ? __uint_as_float((uint32_t)la[arow[a] * g.r + k] << 16) : 0.f;
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int k0 = 16 * (wave + c * W);
+            if (k0 >= g.rp) break;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const int at = 16 * t + li;
-                const float* src = g.P + (p0 + (at < rows ? at : rows - 1)) * g.rp + k;
-                pv[t] = 0.f;
-                for (int p = 0; p < g.parts; ++p) pv[t] += src[(int64_t)p * g.groups.positions * g.rp];
+                const f32x4_t pv = *(const f32x4_t*)(part + (16 * t + li) * (g.rp + 4) + k0 + 4 * q);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int a = 0; a < FA; ++a)
+                        acc[a][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(i & 1 ? lv[c][a][i >> 1] & 0xFFFF0000u : lv[c][a][i >> 1] << 16), pv[i], acc[a][t], 0, 0, 0);
             }
-#pragma unroll
-            for (int a = 0; a < FA; ++a)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) acc[a][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(lv[a], pv[t], acc[a][t], 0, 0, 0);
         }
+        __syncthreads();
     }
     f32x4_t* const mine = (f32x4_t*)part + lane;
 #pragma unroll
@@ -527,12 +553,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
 
 template <int FA, int NT, int W, int U, bool GATED>
 int launch_few_one(aser_ctx* ctx, const MxArgs& g, bool f32) {
-    const size_t lds = (size_t)W * FA * NT * 1024;
+    size_t lds = (size_t)W * FA * NT * 1024;                 // the sums of the wavefronts; before them P, if there is one
+    const size_t ranks = g.P ? (size_t)16 * NT * (g.rp + 4) * 4 : 0;
+    if (lds < ranks) lds = ranks;
     const int64_t tiles = g.groups.most_tiles(16 * NT);
     if (tiles > 65535) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: too many rows");
     const dim3 grid((unsigned)ceil_div64(g.outs, 16 * (GATED ? FA / 2 : FA)), (unsigned)tiles);
-    if (f32) mx4_few_kernel<FA, NT, W, U, GATED, true><<<grid, 64 * W, lds, ctx->stream>>>(g);
-    else mx4_few_kernel<FA, NT, W, U, GATED, false><<<grid, 64 * W, lds, ctx->stream>>>(g);
+    const auto kernel = f32 ? mx4_few_kernel<FA, NT, W, U, GATED, true> : mx4_few_kernel<FA, NT, W, U, GATED, false>;
+    if (lds > 65536) ASER_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    kernel<<<grid, 64 * W, lds, ctx->stream>>>(g);
     return aser_check_launch(ctx, "mx4_few_kernel");
 }
 template <int FA, int NT, int W, int U>
@@ -557,24 +586,51 @@ int launch_tile(aser_ctx* ctx, const MxArgs& g, bool gated, bool f32) {
     return f32 ? launch_tile_one<MF, NF, ST, WG, false, true>(ctx, g) : launch_tile_one<MF, NF, ST, WG, false, false>(ctx, g);
 }
 
+// Rows of the weights of a workgroup, wavefronts, words ahead.  TODO
+int run_few(aser_ctx* ctx, const MxArgs& g, int nt, int64_t matrices, bool gated, bool f32) {
+#ifdef FEW
+    return launch_few<FEW>(ctx, g, gated, f32);
+#endif
+    if (nt == 2) return launch_few<2, 2, 4, 2>(ctx, g, gated, f32);
+    if (nt == 3) return launch_few<2, 3, 4, 2>(ctx, g, gated, f32);
+    if (nt == 4) return launch_few<2, 4, 4, 2>(ctx, g, gated, f32);
+    const int64_t panels = matrices * ceil_div64(g.m, 16);
+    if (panels >= 8192) return launch_few<4, 1, 4, 2>(ctx, g, gated, f32);
+    if (gated || panels >= 1024) return launch_few<2, 1, 8, 2>(ctx, g, gated, f32);
+    return launch_few_one<1, 1, 8, 4, false>(ctx, g, f32);
+}
+
+int run_many(aser_ctx* ctx, const MxArgs& g, bool gated, bool f32) {
+#ifdef CFG
+    return launch_tile<CFG>(ctx, g, gated, f32);
+#endif
+    auto tiles = [&](int mf, int nf) { return g.groups.most_tiles(64 * nf) * ceil_div64(g.m, 64 * mf); };
+    if (tiles(4, 2) >= 512) return launch_tile<4, 2, 3, 2>(ctx, g, gated, f32);
+    if (tiles(2, 2) >= 256) return launch_tile<2, 2, 4, 2>(ctx, g, gated, f32);
+    return launch_tile<2, 1, 4, 2>(ctx, g, gated, f32);
+}
+
 struct Plan {
     int nt;                  // 16 nt positions a workgroup
     bool many;               // tiles through LDS instead
     int parts, part_words;   // few rows: of the channels, for P
-    size_t p_bytes, la_bytes;
+    size_t p_bytes, la_bytes, lb_bytes;      // P, and the factors should they have to be padded
+    size_t all() const { return p_bytes + la_bytes + lb_bytes; }
 };
 
 Plan plan_product(int64_t positions, int64_t n, int64_t m, int32_t count, int32_t r) {
     Plan p{};
     const int64_t each = ceil_div64(positions, count < positions ? count : positions);
-    p.nt = each <= 16 ? 1 : each <= 32 ? 2 : 4;
-    p.many = each > 64;
+    p.nt = (int)(each <= 64 ? ceil_div64(each, 16) : 4);
+    p.many = each > 64 && ceil_div64(positions, 64) * ceil_div64(m, 32) > 512;
     const int64_t words = mx4_words(n), tiles = ceil_div64(positions, 16);
     int64_t parts = p.many || tiles >= 256 ? 1 : ceil_div64(256, tiles);
-    if (parts > ceil_div64(words, 4)) parts = ceil_div64(words, 4);
+    if (parts > ceil_div64(words, 8)) parts = ceil_div64(words, 8);
+    if (parts > kMostParts) parts = kMostParts;
     p.part_words = (int)ceil_div64(words, parts);
     p.parts = (int)ceil_div64(words, p.part_words);
     if (r <= 0) return p;
+    p.lb_bytes = align_up((size_t)count * r * align_up(n, 8) * 2, 256);
     if (p.many) {
         p.p_bytes = align_up((size_t)positions * align_up(r, 32) * 2 * 3, 256);
         p.la_bytes = align_up((size_t)count * m * align_up(r, 32) * 2, 256);
@@ -582,6 +638,13 @@ Plan plan_product(int64_t positions, int64_t n, int64_t m, int32_t count, int32_
         p.p_bytes = align_up((size_t)p.parts * positions * align_up(r, 16) * 4, 256);
     }
     return p;
+}
+
+int pad_rows(aser_ctx* ctx, const uint16_t* f, int64_t rows, int64_t r, int64_t width, uint16_t* out) {
+    const int64_t grid = ceil_div64(rows * width, 2048);
+    if (grid > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: the factors are too large");
+    mx4_pad_kernel<<<(unsigned)grid, 256, 0, ctx->stream>>>(f, rows, r, width, out);
+    return aser_check_launch(ctx, "mx4_pad_kernel");
 }
 
 template <int RF, int NT, int W, int TERMS>
@@ -607,26 +670,30 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
     if (groups.positions == 0) return ASER_OK;
     if (!Y) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "%s: null pointer", who);
     const Plan p = plan_product(groups.positions, w->n, w->rows, w->count, r);
-    if (r > 0 && (!ctx->ws || ctx->ws_bytes < p.p_bytes + p.la_bytes + kAserWsTail)) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "%s: workspace too small", who);
+    if (r > 0 && (!ctx->ws || ctx->ws_bytes < p.all() + kAserWsTail)) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "%s: workspace too small", who);
     MxArgs g{};
     g.groups = groups;
-    g.n = w->n; g.words = (int)mx4_words(w->n);
+    g.words = (int)mx4_words(w->n);
     g.xc = x->codes; g.xs = (const uint32_t*)x->scales;
     g.wc = w->codes; g.ws = (const uint32_t*)w->scales; g.m = w->rows; g.w_size = mx4_size(w->rows, g.words);
-    g.la = L_A; g.lb = L_B; g.r = r; g.la_ld = r;
+    g.la = L_A; g.lb = L_B; g.r = r; g.la_ld = r; g.lb_ld = w->n;
     g.parts = p.parts; g.part_words = p.part_words; g.rp = (int)align_up(r, 16);
     g.Y = Y; g.ldy = ldy; g.outs = outs;
     const int64_t unit = p.many || f32 ? 16 : 8, size = f32 ? 4 : 2;
     g.vec = !((uintptr_t)Y & (unit - 1)) && !(ldy * size & (unit - 1));
-    g.lb_vec = !((uintptr_t)L_B & 15) && !(w->n & 7);
     ASER_TRY(aser_prepare_device(ctx));
+    if (r > 0 && (((uintptr_t)L_B & 15) || (w->n & 7))) {
+        uint16_t* const padded = (uint16_t*)((char*)ctx->ws + p.p_bytes + p.la_bytes);
+        g.lb_ld = align_up(w->n, 8);
+        ASER_TRY(pad_rows(ctx, L_B, (int64_t)w->count * r, w->n, g.lb_ld, padded));
+        g.lb = padded;
+    }
     if (!p.many) {
         if (r > 0) {
             g.P = (float*)ctx->ws;
             ASER_TRY((launch_down<1, 1, 4, 0>(ctx, g)));
         }
-        if (p.nt == 1) return swiglu ? launch_few_one<2, 1, 8, 4, true>(ctx, g, f32) : launch_few_one<1, 1, 8, 4, false>(ctx, g, f32);
-        return p.nt == 2 ? launch_few<2, 2, 4, 4>(ctx, g, swiglu, f32) : launch_few<4, 4, 4, 2>(ctx, g, swiglu, f32);
+        return run_few(ctx, g, p.nt, w->count < groups.positions ? w->count : groups.positions, swiglu, f32);
     }
     if (r > 0) {
         const int terms = f32 ? 3 : 2, width = (int)align_up(r, 32);
@@ -636,18 +703,12 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
                      : width > 32 ? (launch_down<4, 2, 8, 2>(ctx, g)) : (launch_down<2, 2, 8, 2>(ctx, g)));
         if (r != width || ((uintptr_t)L_A & 15)) {
             uint16_t* const padded = (uint16_t*)((char*)ctx->ws + p.p_bytes);
-            const int64_t rows = w->rows * w->count, grid = ceil_div64(rows * width, 2048);
-            if (grid > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "%s: L_A is too large", who);
-            mx4_pad_kernel<<<(unsigned)grid, 256, 0, ctx->stream>>>(L_A, rows, r, width, padded);
-            ASER_TRY(aser_check_launch(ctx, "mx4_pad_kernel"));
+            ASER_TRY(pad_rows(ctx, L_A, w->rows * w->count, r, width, padded));
             g.la = padded;
             g.la_ld = width;
         }
     }
-#ifndef CFG
-#define CFG 4, 2, 3, 2
-#endif
-    return launch_tile<CFG>(ctx, g, swiglu, f32);
+    return run_many(ctx, g, swiglu, f32);
 }
 
 }  // namespace
@@ -668,7 +729,7 @@ extern "C" int aser_mx4_forward(aser_ctx* ctx, const aser_mx4* x, const aser_mx4
 extern "C" size_t aser_expert_forward_workspace_bytes(int64_t positions, int64_t n, int64_t m, int32_t n_experts, int32_t r) {
     if (positions <= 0 || n <= 0 || m <= 0 || n_experts <= 0) return kAserWsTail;
     const Plan p = plan_product(positions, n, m, n_experts, r);
-    return p.p_bytes + p.la_bytes + kAserWsTail;
+    return p.all() + kAserWsTail;
 }
 
 extern "C" int aser_expert_forward(aser_ctx* ctx, const aser_mx4* x, const aser_mx4* w, const aser_expert_plan* plan, int32_t gather, const uint16_t* L_A,
