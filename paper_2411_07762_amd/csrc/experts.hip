@@ -1,7 +1,8 @@
 // Routing of rows to experts, and the weighted sum of what the experts made of them.
 //
 // Routing: a wavefront has a row, its lanes the experts lane, lane + 64, ...  Scores are computed in 64 bits, so that experts are told apart where fp32 would
-// round their scores to one number.  The top_k largest are found one after the other.  A workgroup has 32 rows: bit t of an expert's word says that row t chose it,
+// round their scores to one number.  The top_k largest are found one after the other, by the upper halves of keys of 64 bits that order as the numbers do; only where lanes
+// agree in them the lower halves are looked at.  A workgroup has 32 rows: bit t of an expert's word says that row t chose it,
 // so the number of a pair among its expert's pairs is a count of bits, and the order by expert is the same whatever the timing.  Up
 // to 32 rows are ordered in the same launch; more in two further ones, a running sum over the workgroups for each expert and the placing.
 #include "bf16_pair.h"
@@ -9,7 +10,7 @@
 
 namespace {
 
-constexpr int kTok = 32, kWaves = 8;
+constexpr int kTok = 32, kWaves = 16;
 constexpr double kMinus = -__builtin_huge_val();
 
 struct RouteArgs {
@@ -22,12 +23,48 @@ struct RouteArgs {
     int32_t* counts;      // [expert][workgroup]; more than one workgroup
     int32_t* totals;      // [expert]
     int groups;           // workgroups
+    int per_bits;         // 2^per_bits lanes look at a group of experts
 };
 
-__device__ __forceinline__ double wave_max(double v) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v = fmax(v, __shfl_xor(v, d));
-    return v;
+// Steps of a reduction over a wavefront by the data-parallel moves: after the six of them lane 63 has the result of all.  Lanes that a move does not reach get `idle`.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t v, uint32_t idle) { return (uint32_t)__builtin_amdgcn_update_dpp((int)idle, (int)v, CTRL, ROWS, 15, false); }
+template <class F>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t v, uint32_t idle, F join) {
+    v = join(v, moved<0x111, 15>(v, idle));       // from 1, 2, 4, 8 lanes below within a row of 16, then from the rows before
+    v = join(v, moved<0x112, 15>(v, idle));
+    v = join(v, moved<0x114, 15>(v, idle));
+    v = join(v, moved<0x118, 15>(v, idle));
+    v = join(v, moved<0x142, 10>(v, idle));
+    v = join(v, moved<0x143, 12>(v, idle));
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) { return wave_reduce(v, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; }); }
+__device__ __forceinline__ uint32_t wave_min(uint32_t v) { return wave_reduce(v, 0xFFFFFFFFu, [](uint32_t a, uint32_t b) { return a < b ? a : b; }); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double v) {                 // 0 where no lane is reached
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint64_t lo = moved<CTRL, ROWS>((uint32_t)b, 0u), hi = moved<CTRL, ROWS>((uint32_t)(b >> 32), 0u);
+    return __builtin_bit_cast(double, lo | hi << 32);
+}
+__device__ __forceinline__ double lane_value(double v, int lane) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint64_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+    return __builtin_bit_cast(double, lo | hi << 32);
+}
+__device__ __forceinline__ double wave_sum(double v) {
+    v += moved<0x111, 15>(v);
+    v += moved<0x112, 15>(v);
+    v += moved<0x114, 15>(v);
+    v += moved<0x118, 15>(v);
+    v += moved<0x142, 10>(v);
+    v += moved<0x143, 12>(v);
+    return lane_value(v, 63);
+}
+// Numbers of 64 bits as whole numbers in the same order; no number that is not -inf or NaN has a key below 2^52.
+__device__ __forceinline__ uint64_t key_of(double v) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v + 0.0);       // one zero
+    return b >> 63 ? ~b : b | (uint64_t)1 << 63;
 }
 
 // Running sum over the experts: offs[e] = sum of count(e') for e' < e, offs[experts] the total.  One wavefront.
@@ -81,42 +118,43 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(RouteArgs g) {
     for (int t = wave; t < kTok && row0 + t < g.rows; t += kWaves) {
         const int64_t row = row0 + t;
         double s[V], c[V];
-        double top = kMinus;
+        float l[V], top = -__builtin_huge_valf();
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int e = lane + 64 * j;
-            float l = -__builtin_huge_valf();
-            if (e < g.experts) l = F32 ? ((const float*)g.logits)[row * g.ldl + e] : __uint_as_float((uint32_t)((const uint16_t*)g.logits)[row * g.ldl + e] << 16);
-            if (!(l == l)) l = -__builtin_huge_valf();
-            if (l > 3.402823466e38f) l = 3.402823466e38f;
-            s[j] = l;
-            top = fmax(top, s[j]);
+            l[j] = -__builtin_huge_valf();
+            if (e < g.experts) l[j] = F32 ? ((const float*)g.logits)[row * g.ldl + e] : __uint_as_float((uint32_t)((const uint16_t*)g.logits)[row * g.ldl + e] << 16);
+            if (!(l[j] == l[j])) l[j] = -__builtin_huge_valf();
+            if (l[j] > 3.402823466e38f) l[j] = 3.402823466e38f;
+            top = fmaxf(top, l[j]);
         }
-        const double l_top = wave_max(top);
-        double sum = 0.0;
+        if (g.o.sigmoid) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const double l = s[j];
-            const bool off = l == kMinus;
-            if (g.o.sigmoid) s[j] = off ? 0.0 : 1.0 / (1.0 + exp(-l));
-            else s[j] = off ? 0.0 : exp(l - l_top);
-            sum += s[j];
-            c[j] = l;
-        }
-        if (!g.o.sigmoid) {
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-#pragma unroll
-            for (int j = 0; j < V; ++j) s[j] = sum > 0.0 ? s[j] / sum : 0.0;
-        }
-        if (!by_logit) {
+            for (int j = 0; j < V; ++j) s[j] = l[j] == -__builtin_huge_valf() ? 0.0 : 1.0 / (1.0 + exp(-(double)l[j]));
+        } else {
+            // the largest logit, by the keys of 32 bits that order floats
+            const uint32_t tb = __float_as_uint(top + 0.f), most = wave_max(tb >> 31 ? ~tb : tb | 0x80000000u);
+            const double l_top = __uint_as_float(most >> 31 ? most & 0x7FFFFFFFu : ~most);
+            double sum = 0.0;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const int e = lane + 64 * j;
-                double v = s[j];
-                if (g.bias && e < g.experts) v += (double)g.bias[e];
-                c[j] = c[j] == kMinus || !(v == v) ? kMinus : v;
+                s[j] = l[j] == -__builtin_huge_valf() ? 0.0 : exp((double)l[j] - l_top);
+                sum += s[j];
             }
+            sum = wave_sum(sum);
+            const double by = sum > 0.0 ? sum : 1.0;
+#pragma unroll
+            for (int j = 0; j < V; ++j) s[j] = s[j] / by;
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int e = lane + 64 * j;
+            double v = l[j];
+            if (!by_logit) {
+                v = s[j];
+                if (g.bias && e < g.experts) v += (double)g.bias[e];
+            }
+            c[j] = l[j] == -__builtin_huge_valf() || !(v == v) ? kMinus : v;
         }
         if (g.o.n_groups > 1) {
             double* const mine = cbuf + (size_t)wave * g.experts;
@@ -125,54 +163,64 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(RouteArgs g) {
             for (int j = 0; j < V; ++j)
                 if (lane + 64 * j < g.experts) mine[lane + 64 * j] = c[j];
             __builtin_amdgcn_wave_barrier();
-            double worth = kMinus;
-            if (lane < g.o.n_groups) {
-                double second = kMinus;
-                for (int i = 0; i < size; ++i) {
-                    const double v = mine[lane * size + i];
-                    if (v > worth) { second = worth; worth = v; }
-                    else if (v > second) second = v;
+            // `per` lanes look at a group's members in turn, and join what they found
+            const int per = 1 << g.per_bits, group = lane >> g.per_bits;
+            double worth = kMinus, second = kMinus;
+            if (group < g.o.n_groups)
+                for (int i = lane & (per - 1); i < size; i += per) {
+                    const double v = mine[group * size + i];
+                    second = fmax(second, fmin(worth, v));
+                    worth = fmax(worth, v);
                 }
-                if (g.o.group_top == 2 && second > kMinus) worth += second;
+            for (int d = 1; d < per; d *= 2) {
+                const double w2 = __shfl_xor(worth, d), s2 = __shfl_xor(second, d);
+                second = fmax(fmax(second, s2), fmin(worth, w2));
+                worth = fmax(worth, w2);
             }
+            if (g.o.group_top == 2 && second > kMinus) worth += second;
             int ahead = 0;
             for (int i = 0; i < g.o.n_groups; ++i) {
-                const double v = __shfl(worth, i);
-                ahead += v > worth || (v == worth && i < lane);
+                const double v = lane_value(worth, i << g.per_bits);
+                ahead += v > worth || (v == worth && i < group);
             }
-            const uint64_t open = __ballot(lane < g.o.n_groups && ahead < g.o.top_groups);
+            const uint64_t open = __ballot(group < g.o.n_groups && ahead < g.o.top_groups);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const int e = lane + 64 * j;
-                if (e < g.experts && !((open >> (e / size)) & 1)) c[j] = kMinus;
+                if (e < g.experts && !((open >> ((e / size) << g.per_bits)) & 1)) c[j] = kMinus;
             }
         }
+        uint64_t key[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) key[j] = c[j] > kMinus ? key_of(c[j]) : 0;
         int my_id = -1;
-        double my_s = 0.0;
+        double my_s = 0.0, total = 0.0;
         for (int k = 0; k < g.top_k; ++k) {
-            double best = kMinus, score = 0.0;
-            int at = INT32_MAX;
+            uint64_t best = 0;
+            int at = 0;
+            double score = 0.0;
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                if (c[j] > best) { best = c[j]; at = lane + 64 * j; score = s[j]; }
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const double v = __shfl_xor(best, d), sv = __shfl_xor(score, d);
-                const int a = __shfl_xor(at, d);
-                if (v > best || (v == best && a < at)) { best = v; at = a; score = sv; }
+                if (key[j] > best) { best = key[j]; at = j; score = s[j]; }
+            const uint32_t high = wave_max((uint32_t)(best >> 32));
+            if (high == 0) break;                            // nothing is left: keys of numbers are above 2^32
+            uint64_t who = __ballot((uint32_t)(best >> 32) == high);
+            if (__popcll(who) > 1) {                         // several lanes agree in the upper half: the lower one, then the lowest expert
+                const bool mine = (uint32_t)(best >> 32) == high;
+                const uint32_t low = wave_max(mine ? (uint32_t)best : 0u);
+                const bool same = mine && (uint32_t)best == low;
+                const uint32_t e = wave_min(same ? (uint32_t)(lane + 64 * at) : 0xFFFFFFFFu);
+                who = (uint64_t)1 << (e & 63);
             }
-            if (!(best > kMinus)) break;
+            const int owner = __builtin_ctzll(who), j_of = __builtin_amdgcn_readlane(at, owner);
+            score = lane_value(score, owner);
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                if (at == lane + 64 * j) c[j] = kMinus;
-            if (lane == k) { my_id = at; my_s = score; }
+                if (lane == owner && j == j_of) key[j] = 0;
+            if (lane == k) { my_id = owner + 64 * j_of; my_s = score; }
+            total += score;
         }
-        if (g.o.renormalize) {
-            double total = my_s;
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
-            if (total > 0.0) my_s /= total;
-        }
+        if (g.o.renormalize && total > 0.0) my_s /= total;
         if (lane < g.top_k) {
             g.ids[row * g.top_k + lane] = my_id;
             g.weights[row * g.top_k + lane] = (float)(my_s * (double)g.o.scale);
@@ -364,6 +412,7 @@ extern "C" int aser_route_experts(aser_ctx* ctx, const void* logits, int32_t x_d
     const size_t need = aser_route_workspace_bytes(plan->rows, experts, plan->top_k);
     RouteArgs g{logits, ldl, bias, *opts, plan->ids, plan->weights, plan->offsets, plan->order, plan->place, plan->rows, plan->top_k, experts, nullptr, nullptr,
                 (int)ceil_div64(plan->rows, kTok)};
+    while ((opts->n_groups << (g.per_bits + 1)) <= 64) ++g.per_bits;
     if (g.groups > 1) {
         if (!ctx->ws || ctx->ws_bytes < need) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "route_experts: workspace too small");
         g.counts = (int32_t*)ctx->ws;

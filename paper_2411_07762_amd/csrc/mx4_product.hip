@@ -117,12 +117,18 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
             }
         }
     };
-    if (first + wave < last) load(0, first + wave);
-    for (int w = first + wave; w < last; w += 2 * W) {
-        if (w + W < last) load(1, w + W);
+    // The rows of L_B are a power of two apart more often than not, so that all workgroups would read one channel of the L2 at a time: they begin at different words.
+    const int count = first + wave < last ? (last - first - wave + W - 1) / W : 0, turn = count ? (rest / g.parts) % count : 0;
+    auto word = [&](int i) {
+        const int at = i + turn;
+        return first + wave + W * (at < count ? at : at - count);
+    };
+    if (count > 0) load(0, word(0));
+    for (int i = 0; i < count; i += 2) {
+        if (i + 1 < count) load(1, word(i + 1));
         multiply(0);
-        if (w + 2 * W < last) load(0, w + 2 * W);
-        if (w + W < last) multiply(1);
+        if (i + 2 < count) load(0, word(i + 2));
+        if (i + 1 < count) multiply(1);
     }
     f32x4_t* const mine = (f32x4_t*)part + lane;
 #pragma unroll
