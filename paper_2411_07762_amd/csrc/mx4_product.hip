@@ -26,6 +26,7 @@ struct MxArgs {
     int words;
     const uint16_t* la; const uint16_t* lb; int r;
     int64_t la_ld, lb_ld;                                   // their rows: r and n, or what they are padded to
+    int lb_frags;                                           // many rows: L_B is arranged, with so many times 16 ranks
     float* P; int parts, part_words, rp;                    // few rows: [part][position][rp] fp32, rp: r rounded up to 16
     uint16_t* planes; int lr_steps;                         // many rows: [term][position][32 lr_steps / terms] bf16; steps of 32 ranks and one term
     void* Y; int64_t ldy; int64_t outs;                     // columns of Y
@@ -57,12 +58,16 @@ __device__ __forceinline__ void store4(const MxArgs& g, int64_t p, int64_t o, co
 }
 
 // ---------------------------------------------------------------------------------------------------------------- P = x L_B^T
-// 16 NT positions and 16 RF ranks a workgroup; W wavefronts share a part of the channels, a word at a time with the next one's loads in flight.  Of each of its four blocks lane
-// group q = lane / 16 has channels 8 q .. + 7 of its token, which become bf16 (exactly), and of its row of L_B: the four groups together read 64 bytes of a row
-// (16 bytes a lane of a row's 256, each on its own, took 20 us instead of TODO for 4099 tokens of 4096 channels and 64 ranks).  Ranks are in the rows of the accumulator.  TERMS = 0: fp32 sums of the part; otherwise (one part) the sum as so many bf16 terms, each what the ones before leave, rounded.
-template <int RF, int NT, int W, int TERMS>
+// 16 NT positions and 16 RF ranks a workgroup; W wavefronts share a part of the channels, a word at a time with the loads of U words in flight.  Ranks are in the
+// rows of the accumulator; tokens become bf16 on the way, exactly.
+// TERMS = 0, few rows: fp32 sums of the part.  L_B is read as it is: of each of a word's four blocks lane group q = lane / 16 has channels 8 q .. + 7.
+// Otherwise the sum (of one part) as so many bf16 terms, each what the ones before leave, rounded; and lane group q has block q, of L_B in the order
+// of the lanes (mx4_arrange_kernel).  Lanes next to each other have different rows, and a load of 16 bytes from 64 places occupies a compute unit's address unit
+// for 64 cycles where one from a kilobyte in a row takes 16: with L_B as it is 4099 tokens of 4096 channels, 64 ranks take 25 us.
+template <int RF, int NT, int W, int U, int TERMS>
 __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_tiles) {
     extern __shared__ __align__(16) float part[];            // [wavefront][fragment][lane][4]
+    constexpr bool ARRANGED = TERMS > 0;
     const int lane = threadIdx.x & 63, li = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rt = blockIdx.x % rank_tiles, rest = blockIdx.x / rank_tiles, pt = rest % g.parts;
@@ -73,6 +78,7 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
 #pragma unroll
     for (int t = 0; t < NT; ++t) xat[t] = mx4_at(mx4_row(g.groups, p0 + (16 * t + li < rows ? 16 * t + li : rows - 1)), g.words);
     const uint16_t* lrow[RF];
+    const uint4* const arranged = (const uint4*)g.lb + ((int64_t)e * g.words * g.lb_frags + rt * RF) * 256 + lane;
     f32x4_t acc[RF][NT];
 #pragma unroll
     for (int f = 0; f < RF; ++f) {
@@ -82,15 +88,17 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
         for (int t = 0; t < NT; ++t) acc[f][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
     const int first = pt * g.part_words, last = first + g.part_words < g.words ? first + g.part_words : g.words;
-    v4i_t codes[2][NT];
-    uint32_t scale[2][NT];
-    uint4 a[2][RF][4];
+    v4i_t codes[U][NT];
+    uint32_t scale[U][NT];
+    uint4 a[U][RF][4];
     auto load = [&](int u, int w) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int64_t at = xat[t] + (int64_t)w * kMxNext;
+            if (ARRANGED) codes[u][t] = *(const v4i_t*)(g.xc + at * 64 + 16 * q);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) codes[u][t][j] = *(const int*)(g.xc + at * 64 + 16 * j + 4 * q);
+            for (int j = 0; j < 4; ++j)
+                if (!ARRANGED) codes[u][t][j] = *(const int*)(g.xc + at * 64 + 16 * j + 4 * q);
             scale[u][t] = g.xs[at];
         }
         const int64_t c0 = (int64_t)w * kMxWord + 8 * q;
@@ -99,15 +107,15 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
         for (int j = 0; j < 4; ++j) {
             const int64_t c = c0 + 32 * j < g.lb_ld ? c0 + 32 * j : g.lb_ld - 8;
 #pragma unroll
-            for (int f = 0; f < RF; ++f) a[u][f][j] = *(const uint4*)(lrow[f] + c);
+            for (int f = 0; f < RF; ++f) a[u][f][j] = ARRANGED ? arranged[(int64_t)w * g.lb_frags * 256 + (f * 4 + j) * 64] : *(const uint4*)(lrow[f] + c);
         }
     };
     auto multiply = [&](int u) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float by = __uint_as_float(((scale[u][t] >> (8 * j)) & 255u) << 23);    // the conversion takes the exponent field for what it is in a scale byte
+                const float by = __uint_as_float(((scale[u][t] >> (8 * (ARRANGED ? q : j))) & 255u) << 23);      // the conversion takes the exponent field for a scale byte
                 const uint32_t w4 = (uint32_t)codes[u][t][j];
                 const bf16x2_t v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 1),
                                v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 3);
@@ -115,20 +123,18 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
 #pragma unroll
                 for (int f = 0; f < RF; ++f) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a[u][f][j]), b, acc[f][t], 0, 0, 0);
             }
+    };
+    const int count = first + wave < last ? (last - first - wave + W - 1) / W : 0;
+    auto word = [&](int i) { return first + wave + W * i; };
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (u < count) load(u, word(u));
+    for (int i = 0; i < count; i += U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i + u < count) multiply(u);
+            if (i + u + U < count) load(u, word(i + u + U));
         }
-    };
-    // The rows of L_B are a power of two apart more often than not, so that all workgroups would read one channel of the L2 at a time: they begin at different words.
-    const int count = first + wave < last ? (last - first - wave + W - 1) / W : 0, turn = count ? (rest / g.parts) % count : 0;
-    auto word = [&](int i) {
-        const int at = i + turn;
-        return first + wave + W * (at < count ? at : at - count);
-    };
-    if (count > 0) load(0, word(0));
-    for (int i = 0; i < count; i += 2) {
-        if (i + 1 < count) load(1, word(i + 1));
-        multiply(0);
-        if (i + 2 < count) load(0, word(i + 2));
-        if (i + 1 < count) multiply(1);
     }
     f32x4_t* const mine = (f32x4_t*)part + lane;
 #pragma unroll
@@ -159,6 +165,28 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
             sum -= f32x4_t{__uint_as_float(w0 << 16), __uint_as_float(w0 & 0xFFFF0000u), __uint_as_float(w1 << 16), __uint_as_float(w1 & 0xFFFF0000u)};
         }
     }
+}
+
+// L_B in the order in which a wavefront with ARRANGED above takes it: [matrix][word][16 ranks][eighths of a block][lane][8 channels], zeros where there is no rank or no channel.
+__global__ __launch_bounds__(256) void mx4_arrange_kernel(const uint16_t* __restrict__ lb, int64_t units, int words, int frags, int r, int64_t n, bool vec, uint4* __restrict__ out) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= units) return;
+    const int lane = (int)(i & 63), j = (int)(i >> 6) & 3;
+    const int64_t piece = i >> 8, ew = piece / frags, e = ew / words;
+    const int k = (int)(piece - ew * frags) * 16 + (lane & 15);
+    const int64_t c = (ew - e * words) * kMxWord + 32 * (lane >> 4) + 8 * j;
+    const uint16_t* const src = lb + (e * r + k) * n + c;
+    uint32_t v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = 0u;
+    if (k < r && vec && c < n) {                             // rows on 16-byte boundaries, n a multiple of 8
+        out[i] = *(const uint4*)src;
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+        if (k < r && c + u < n) v[u] = src[u];
+    out[i] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
 }
 
 // A factor with its rows of r padded with zeros, where it cannot be read in pieces of 16 bytes as it is (L_B), or not in pieces of 64 (L_A of many rows).
@@ -331,7 +359,7 @@ __device__ __forceinline__ f32x16_t mfma32_bf16(const v4i_t& a, const v4i_t& b, 
 }
 
 template <int MF, int NF, int ST, int WG, bool GATED, bool F32>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) void mx4_tile_kernel(MxArgs g, int out_tiles) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) void mx4_tile_kernel(MxArgs g, uint32_t out_tiles) {
     extern __shared__ __align__(16) char smem[];
     constexpr int BM = 64 * MF, BN = 64 * NF;
     constexpr int A_BYTES = BM * 64, B_BYTES = BN * 64, SA = A_BYTES + B_BYTES, SB = SA + BM * 4, STAGE = SB + BN * 4;
@@ -340,15 +368,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wa = wave >> 1, wb = wave & 1;
 
-    const int64_t tiles = mx4_tiles(g.groups, BN), total = tiles * out_tiles, per_xcd = (total + 7) / 8;
-    const int64_t id = (int64_t)(blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    const uint32_t tiles = mx4_tiles(g.groups, BN), total = tiles * out_tiles, per_xcd = (total + 7) / 8;
+    const uint32_t id = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= per_xcd || id >= total) return;
-    const int64_t panel = id / (kPanel * (int64_t)out_tiles), in_panel = id - panel * kPanel * out_tiles;
-    const int64_t high = tiles - panel * kPanel < kPanel ? tiles - panel * kPanel : kPanel;
+    const uint32_t panel = id / (kPanel * out_tiles), in_panel = id - panel * kPanel * out_tiles;
+    const uint32_t high = tiles - panel * kPanel < kPanel ? tiles - panel * kPanel : kPanel;
     int e, rows;
     int64_t p0;
     if (!mx4_find_tile(g.groups, panel * kPanel + in_panel % high, BN, &e, &p0, &rows)) return;
-    const int64_t o0 = (in_panel / high) * (GATED ? BM / 2 : BM);
+    const int64_t o0 = (int64_t)(in_panel / high) * (GATED ? BM / 2 : BM);
     // weight row of row r of the tile; past the end the last one, whose sums are not stored
     auto weight_row = [&](int r) {
         int64_t o, base = 0;
@@ -504,46 +532,51 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
     for (; s < words; ++s) step(s, std::false_type{}, std::false_type{});
     for (; s < steps; ++s) step(s, std::false_type{}, std::true_type{});
 
-    // acc[i][j][k]: output 32 i + 8 (k / 4) + 4 h + k % 4, position 32 j + li of the wavefront's.  32 positions at a time are turned through LDS (the wavefront's own
-    // part of it), so that rows of Y are written in whole lines.
+    // acc[i][j][k]: output 32 i + 8 (k / 4) + 4 h + k % 4, position 32 j + li of the wavefront's.  They are turned through the wavefront's part of the ring, as many
+    // positions at a time as it holds, so that rows of Y are written in whole lines; the 16-byte chunks of a row change places by the row, which keeps both the writes
+    // and the reads off each other's banks.
     constexpr int OF = GATED ? MF / 2 : MF;                  // fragments of outputs
-    constexpr int SIZE = F32 ? 4 : 2, ROW = OF * 32 * SIZE + 16;
+    constexpr int SIZE = F32 ? 4 : 2, ROW = OF * 32 * SIZE, CHUNKS = ROW / 16;
+    constexpr int FIT = ST * STAGE / 4 / (32 * ROW), BATCH = FIT >= NF ? NF : FIT >= 2 && NF % 2 == 0 ? 2 : 1;
+    static_assert(FIT >= 1, "the ring has to hold 32 positions of every wavefront");
+    auto chunk_of = [](int r, int c) { return c ^ (CHUNKS >= 16 ? r & 15 : r / (16 / (CHUNKS < 16 ? CHUNKS : 16)) & (CHUNKS - 1)); };
     const int64_t ow = o0 + wa * 32 * OF;
     __syncthreads();
-    char* const mine = smem + wave * (32 * ROW);
+    char* const mine = smem + wave * (BATCH * 32 * ROW);
 #pragma unroll
-    for (int j = 0; j < NF; ++j) {
-        const int first = wb * 32 * NF + 32 * j;
-        const int here = rows - first;                       // positions of these 32 that are there
+    for (int j0 = 0; j0 < NF; j0 += BATCH) {
 #pragma unroll
-        for (int i = 0; i < OF; ++i)
+        for (int jj = 0; jj < BATCH; ++jj) {
+            const int j = j0 + jj;
+            char* const row = mine + (32 * jj + li) * ROW;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float y[4];
+            for (int i = 0; i < OF; ++i)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) y[u] = GATED ? gated(acc[i][j][4 * k + u], acc[MF - OF + i][j][4 * k + u]) : acc[i][j][4 * k + u];
-                const int o = 32 * i + 8 * k + 4 * h;
-                if (!g.vec) {
-                    if (li < here) store4<F32>(g, p0 + first + li, ow + o, y);
-                } else if (F32) {
-                    *(float4*)(mine + li * ROW + o * 4) = make_float4(y[0], y[1], y[2], y[3]);
-                } else {
-                    *(uint2*)(mine + li * ROW + o * 2) = make_uint2(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]));
+                for (int k = 0; k < 4; ++k) {
+                    float y[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) y[u] = GATED ? gated(acc[i][j][4 * k + u], acc[MF - OF + i][j][4 * k + u]) : acc[i][j][4 * k + u];
+                    const int o = 32 * i + 8 * k + 4 * h;
+                    if (F32) *(float4*)(row + 16 * chunk_of(li, o / 4)) = make_float4(y[0], y[1], y[2], y[3]);
+                    else *(uint2*)(row + 16 * chunk_of(li, o / 8) + 8 * h) = make_uint2(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]));
                 }
-            }
-        if (!g.vec) continue;
+        }
         __builtin_amdgcn_wave_barrier();
-        constexpr int EACH = 16 / SIZE, PER = OF * 32 / EACH, ROWS = 64 / PER;      // outputs of a lane, lanes of a row, rows an instruction
-        const int o = (lane % PER) * EACH;
+        constexpr int EACH = 16 / SIZE, ROWS = 64 / CHUNKS;  // outputs of a lane, rows an instruction
+        const int c = lane % CHUNKS, o = c * EACH, r0 = lane / CHUNKS, base = wb * 32 * NF + 32 * j0;
+        char* dst = (char*)g.Y + ((p0 + base + r0) * g.ldy + ow + o) * SIZE;
+        const int64_t next = ROWS * g.ldy * SIZE;
+        if (g.vec && base + 32 * BATCH <= rows && ow + 32 * OF <= g.outs) {
 #pragma unroll
-        for (int t = 0; t < 32; t += ROWS) {
-            const int r = t + lane / PER;
-            const uint4 v = *(const uint4*)(mine + r * ROW + o * SIZE);
-            if (r >= here) continue;
-            char* const dst = (char*)g.Y + ((p0 + first + r) * g.ldy + ow + o) * SIZE;
-            if (ow + o + EACH <= g.outs) {
-                *(uint4*)dst = v;
-            } else {
+            for (int t = 0; t < 32 * BATCH; t += ROWS, dst += next) *(uint4*)dst = *(const uint4*)(mine + (t + r0) * ROW + 16 * chunk_of((t + r0) & 31, c));
+        } else {                                             // the last positions or outputs, or rows of Y that 16 bytes do not fit
+#pragma nounroll
+            for (int t = r0; t < 32 * BATCH && base + t < rows; t += ROWS, dst += next) {
+                const uint4 v = *(const uint4*)(mine + t * ROW + 16 * chunk_of(t & 31, c));
+                if (g.vec && ow + o + EACH <= g.outs) {
+                    *(uint4*)dst = v;
+                    continue;
+                }
                 const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                 for (int u = 0; u < EACH; ++u) {
@@ -577,13 +610,13 @@ int launch_few(aser_ctx* ctx, const MxArgs& g, bool gated, bool f32) {
 
 template <int MF, int NF, int ST, int WG, bool GATED, bool F32>
 int launch_tile_one(aser_ctx* ctx, const MxArgs& g) {
-    constexpr int kRing = ST * (64 * MF + 64 * NF) * 68, kTurn = 4 * 32 * ((GATED ? MF / 2 : MF) * 32 * (F32 ? 4 : 2) + 16), kLds = kRing > kTurn ? kRing : kTurn;
-    static_assert(kLds * WG <= 160 * 1024, "the ring and the turned outputs have to fit the LDS of a compute unit");
+    constexpr int kLds = ST * (64 * MF + 64 * NF) * 68;
+    static_assert(kLds * WG <= 160 * 1024, "the rings have to fit the LDS of a compute unit");
     const auto kernel = mx4_tile_kernel<MF, NF, ST, WG, GATED, F32>;
     ASER_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds));
     const int64_t out_tiles = ceil_div64(g.outs, GATED ? 32 * MF : 64 * MF), grid = ceil_div64(g.groups.most_tiles(64 * NF) * out_tiles, 8) * 8;
     if (grid > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: too many rows times outputs");
-    kernel<<<(unsigned)grid, 256, kLds, ctx->stream>>>(g, (int)out_tiles);
+    kernel<<<(unsigned)grid, 256, kLds, ctx->stream>>>(g, (uint32_t)out_tiles);
     return aser_check_launch(ctx, "mx4_tile_kernel");
 }
 template <int MF, int NF, int ST, int WG>
@@ -620,7 +653,7 @@ struct Plan {
     int nt;                  // 16 nt positions a workgroup
     bool many;               // tiles through LDS instead
     int parts, part_words;   // few rows: of the channels, for P
-    size_t p_bytes, la_bytes, lb_bytes;      // P, and the factors should they have to be padded
+    size_t p_bytes, la_bytes, lb_bytes;      // P, and the factors as the kernels want them
     size_t all() const { return p_bytes + la_bytes + lb_bytes; }
 };
 
@@ -636,12 +669,13 @@ Plan plan_product(int64_t positions, int64_t n, int64_t m, int32_t count, int32_
     p.part_words = (int)ceil_div64(words, parts);
     p.parts = (int)ceil_div64(words, p.part_words);
     if (r <= 0) return p;
-    p.lb_bytes = align_up((size_t)count * r * align_up(n, 8) * 2, 256);
     if (p.many) {
         p.p_bytes = align_up((size_t)positions * align_up(r, 32) * 2 * 3, 256);
         p.la_bytes = align_up((size_t)count * m * align_up(r, 32) * 2, 256);
+        p.lb_bytes = align_up((size_t)count * words * kMxWord * align_up(r, 32) * 2, 256);
     } else {
         p.p_bytes = align_up((size_t)p.parts * positions * align_up(r, 16) * 4, 256);
+        p.lb_bytes = align_up((size_t)count * r * align_up(n, 8) * 2, 256);
     }
     return p;
 }
@@ -653,12 +687,12 @@ int pad_rows(aser_ctx* ctx, const uint16_t* f, int64_t rows, int64_t r, int64_t 
     return aser_check_launch(ctx, "mx4_pad_kernel");
 }
 
-template <int RF, int NT, int W, int TERMS>
+template <int RF, int NT, int W, int U, int TERMS>
 int launch_down(aser_ctx* ctx, const MxArgs& g) {
     const int rank_tiles = (int)ceil_div64(TERMS ? g.lr_steps / (TERMS ? TERMS : 1) * 32 : g.rp, 16 * RF);
     const int64_t grid = g.groups.most_tiles(16 * NT) * g.parts * rank_tiles;
     if (grid > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: too many rows");
-    mx4_down_kernel<RF, NT, W, TERMS><<<(unsigned)grid, 64 * W, (size_t)W * RF * NT * 1024, ctx->stream>>>(g, rank_tiles);
+    mx4_down_kernel<RF, NT, W, U, TERMS><<<(unsigned)grid, 64 * W, (size_t)W * RF * NT * 1024, ctx->stream>>>(g, rank_tiles);
     return aser_check_launch(ctx, "mx4_down_kernel");
 }
 
@@ -688,16 +722,17 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
     const int64_t unit = p.many || f32 ? 16 : 8, size = f32 ? 4 : 2;
     g.vec = !((uintptr_t)Y & (unit - 1)) && !(ldy * size & (unit - 1));
     ASER_TRY(aser_prepare_device(ctx));
-    if (r > 0 && (((uintptr_t)L_B & 15) || (w->n & 7))) {
-        uint16_t* const padded = (uint16_t*)((char*)ctx->ws + p.p_bytes + p.la_bytes);
-        g.lb_ld = align_up(w->n, 8);
-        ASER_TRY(pad_rows(ctx, L_B, (int64_t)w->count * r, w->n, g.lb_ld, padded));
-        g.lb = padded;
-    }
+    const bool lb_vec = !((uintptr_t)L_B & 15) && !(w->n & 7);
+    uint16_t* const lb_room = (uint16_t*)((char*)ctx->ws + p.p_bytes + p.la_bytes);
     if (!p.many) {
         if (r > 0) {
             g.P = (float*)ctx->ws;
-            ASER_TRY((launch_down<1, 1, 4, 0>(ctx, g)));
+            if (!lb_vec) {
+                g.lb_ld = align_up(w->n, 8);
+                ASER_TRY(pad_rows(ctx, L_B, (int64_t)w->count * r, w->n, g.lb_ld, lb_room));
+                g.lb = lb_room;
+            }
+            ASER_TRY((launch_down<1, 1, 4, 2, 0>(ctx, g)));
         }
         return run_few(ctx, g, p.nt, w->count < groups.positions ? w->count : groups.positions, swiglu, f32);
     }
@@ -705,8 +740,16 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
         const int terms = f32 ? 3 : 2, width = (int)align_up(r, 32);
         g.planes = (uint16_t*)ctx->ws;
         g.lr_steps = width / 32 * terms;
-        ASER_TRY(f32 ? width > 32 ? (launch_down<4, 2, 8, 3>(ctx, g)) : (launch_down<2, 2, 8, 3>(ctx, g))
-                     : width > 32 ? (launch_down<4, 2, 8, 2>(ctx, g)) : (launch_down<2, 2, 8, 2>(ctx, g)));
+        g.lb_frags = width / 16;
+        const int64_t units = (int64_t)w->count * g.words * g.lb_frags * 256, grid = ceil_div64(units, 256);
+        if (grid > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "%s: the factors are too large", who);
+        mx4_arrange_kernel<<<(unsigned)grid, 256, 0, ctx->stream>>>(L_B, units, g.words, g.lb_frags, r, w->n, lb_vec, (uint4*)lb_room);
+        ASER_TRY(aser_check_launch(ctx, "mx4_arrange_kernel"));
+        g.lb = lb_room;
+#ifndef DOWN
+#define DOWN 2, 2, 4, 4
+#endif
+        ASER_TRY(f32 ? (launch_down<DOWN, 3>(ctx, g)) : (launch_down<DOWN, 2>(ctx, g)));
         if (r != width || ((uintptr_t)L_A & 15)) {
             uint16_t* const padded = (uint16_t*)((char*)ctx->ws + p.p_bytes);
             ASER_TRY(pad_rows(ctx, L_A, w->rows * w->count, r, width, padded));
