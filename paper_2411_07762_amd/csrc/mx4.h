@@ -25,8 +25,8 @@ struct MxGroups {
 };
 
 // Tiles of bm positions that there are.
-__device__ __forceinline__ int64_t mx4_tiles(const MxGroups& g, int bm) {
-    if (!g.offsets) return (g.positions + bm - 1) / bm;
+__device__ __forceinline__ uint32_t mx4_tiles(const MxGroups& g, int bm) {
+    if (!g.offsets) return (uint32_t)((g.positions + bm - 1) / bm);
     const int lane = threadIdx.x & 63;
     const int32_t most = (int32_t)g.positions;
     int32_t sum = 0;
@@ -39,19 +39,20 @@ __device__ __forceinline__ int64_t mx4_tiles(const MxGroups& g, int bm) {
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     return __builtin_amdgcn_readfirstlane(sum);
 }
-// Workgroup `tile`'s matrix, first position and number of positions.  False: there is no such tile.  Every wavefront looks for itself: a
-// lane has a group, and the running sum of the groups' tiles says whose the tile is.
-__device__ __forceinline__ bool mx4_find_tile(const MxGroups& g, int64_t tile, int bm, int* e, int64_t* p0, int* rows) {
+// Tiles of bm positions, `across` of them beside each other for other outputs, numbered matrix by matrix: the matrix that number id belongs to, its first position, the
+// number of its positions, and id's place among its tiles.  False: there is no such tile.  Every wavefront looks for itself: a lane has a matrix, and the
+// running sum of their tiles says whose the number is.
+__device__ __forceinline__ bool mx4_find(const MxGroups& g, uint32_t id, int bm, uint32_t across, int* e, int64_t* first, int* count, uint32_t* place) {
     if (!g.offsets) {
-        const int64_t left = g.positions - tile * bm;
         *e = 0;
-        *p0 = tile * bm;
-        *rows = (int)(left < bm ? left : bm);
-        return left > 0;
+        *first = 0;
+        *count = (int)g.positions;
+        *place = id;
+        return (int64_t)(id / across) * bm < g.positions;
     }
     const int lane = threadIdx.x & 63;
     const int32_t most = (int32_t)g.positions;
-    int32_t before = 0;
+    uint32_t before = 0;
     for (int e0 = 0; e0 < g.count; e0 += 64) {
         int32_t s = 0, n = 0;
         if (e0 + lane < g.count) {
@@ -60,26 +61,36 @@ __device__ __forceinline__ bool mx4_find_tile(const MxGroups& g, int64_t tile, i
             const int32_t t = b > most ? most : b;
             n = t > s ? t - s : 0;
         }
-        const int32_t mine = (n + bm - 1) / bm;
-        int32_t upto = mine;
+        const uint32_t mine = (uint32_t)((n + bm - 1) / bm);
+        uint32_t upto = mine;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
-            const int32_t v = __shfl_up(upto, d);
+            const uint32_t v = __shfl_up(upto, d);
             if (lane >= d) upto += v;
         }
-        const uint64_t over = __ballot(before + upto > tile);
+        const uint64_t over = __ballot((before + upto) * across > id);
         if (over) {
             const int at = __builtin_ctzll(over);
-            const int32_t i = (int32_t)tile - before - __builtin_amdgcn_readlane(upto - mine, at), first = __builtin_amdgcn_readlane(s, at);
-            const int32_t left = __builtin_amdgcn_readlane(n, at) - i * bm;
             *e = e0 + at;
-            *p0 = first + (int64_t)i * bm;
-            *rows = left < bm ? left : bm;
+            *first = __builtin_amdgcn_readlane(s, at);
+            *count = __builtin_amdgcn_readlane(n, at);
+            *place = id - (before + (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), at)) * across;
             return true;
         }
-        before += __builtin_amdgcn_readlane(upto, 63);
+        before += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
     }
     return false;
+}
+// The same for one tile across: the tile's matrix, first position and number of positions.
+__device__ __forceinline__ bool mx4_find_tile(const MxGroups& g, uint32_t tile, int bm, int* e, int64_t* p0, int* rows) {
+    int count;
+    uint32_t place;
+    int64_t first;
+    if (!mx4_find(g, tile, bm, 1, e, &first, &count, &place)) return false;
+    const int left = count - (int)place * bm;
+    *p0 = first + (int64_t)place * bm;
+    *rows = left < bm ? left : bm;
+    return true;
 }
 __device__ __forceinline__ int64_t mx4_row(const MxGroups& g, int64_t p) {
     if (!g.order) return p;

@@ -39,7 +39,13 @@ __device__ __forceinline__ f32x4_t mfma16(const v4i_t& a, uint32_t sa, const v4i
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(a), wide(b), c, 4, 4, 0, (int)sa, 0, (int)sb);
 }
 
-__device__ __forceinline__ float gated(float gate, float up) { return gate / (1.f + expf(-gate)) * up; }
+// gate / (1 + exp(-gate)) * up.  For a bf16 result the exponential and the reciprocal of the instructions do, a few 2^-22 off where the result is rounded to 2^-9; the
+// functions of fp32 take five times as many instructions.
+template <bool F32>
+__device__ __forceinline__ float gated(float gate, float up) {
+    if (F32) return gate / (1.f + expf(-gate)) * up;
+    return gate * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(gate * -1.44269504f)) * up;
+}
 
 template <bool F32>
 __device__ __forceinline__ void store4(const MxArgs& g, int64_t p, int64_t o, const float* y) {
@@ -331,7 +337,7 @@ __global__ __launch_bounds__(64 * W) void mx4_few_kernel(MxArgs g) {
         }
         float y[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) y[u] = GATED ? gated(z[u], up[u]) : z[u];
+        for (int u = 0; u < 4; ++u) y[u] = GATED ? gated<F32>(z[u], up[u]) : z[u];
         const int at = 16 * t + li;
         if (at < rows) store4<F32>(g, p0 + at, o0 + 16 * a + 4 * q, y);
     }
@@ -344,7 +350,8 @@ __global__ __launch_bounds__(64 * W) void mx4_few_kernel(MxArgs g) {
 // make every LDS read wait for all of them.  Half h = lane / 32 of the lanes holds blocks h and 2 + h of a step, one for each of its two instructions
 // per pair of fragments, whose scales are bytes 0 and 2 of its word shifted by h bytes.
 // Gated, a wavefront's first MF / 2 fragments are gates and the others the values that belong to them.
-// Workgroup b runs on XCD b % 8; an XCD's tiles are numbered in panels of kPanel tiles of positions, so that its 32 workgroups share few slabs of either operand.
+// Workgroup b runs on XCD b % 8; an XCD's tiles are numbered matrix by matrix in panels of kPanel tiles of positions, so that its workgroups share few slabs of either operand
+// and a matrix is read once where its positions make no more than a panel.
 constexpr int kPanel = 4;
 
 __device__ __forceinline__ int chunk_at(int r, int c) { return r * 64 + ((c ^ ((r >> 2) & 3)) << 4); }
@@ -368,15 +375,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wa = wave >> 1, wb = wave & 1;
 
-    const uint32_t tiles = mx4_tiles(g.groups, BN), total = tiles * out_tiles, per_xcd = (total + 7) / 8;
+    const uint32_t total = mx4_tiles(g.groups, BN) * out_tiles, per_xcd = (total + 7) / 8;
     const uint32_t id = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= per_xcd || id >= total) return;
-    const uint32_t panel = id / (kPanel * out_tiles), in_panel = id - panel * kPanel * out_tiles;
-    const uint32_t high = tiles - panel * kPanel < kPanel ? tiles - panel * kPanel : kPanel;
-    int e, rows;
-    int64_t p0;
-    if (!mx4_find_tile(g.groups, panel * kPanel + in_panel % high, BN, &e, &p0, &rows)) return;
-    const int64_t o0 = (int64_t)(in_panel / high) * (GATED ? BM / 2 : BM);
+    int e, count;
+    int64_t first_p;
+    uint32_t in;
+    mx4_find(g.groups, id, BN, out_tiles, &e, &first_p, &count, &in);
+    const uint32_t tiles = (uint32_t)(count + BN - 1) / BN, panel = in / (kPanel * out_tiles), in_panel = in - panel * kPanel * out_tiles;
+    const uint32_t high = tiles - panel * kPanel < kPanel ? tiles - panel * kPanel : kPanel, across = in_panel / high;
+    const int before = (int)(panel * kPanel + in_panel - across * high) * BN, rows = count - before < BN ? count - before : BN;
+    const int64_t p0 = first_p + before, o0 = (int64_t)across * (GATED ? BM / 2 : BM);
     // weight row of row r of the tile; past the end the last one, whose sums are not stored
     auto weight_row = [&](int r) {
         int64_t o, base = 0;
@@ -419,11 +428,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
             gs[1] += next_s;
         }
     };
-    auto wait = [&](int stages) {                            // until at most the loads of so many later stages are in flight
-        if (stages == 2) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * LOADS) : "memory");
-        else if (stages == 1) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(LOADS) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-    };
+    auto wait_for = [&](auto most) { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(decltype(most)::value) : "memory"); };       // until at most so many loads are in flight
 
     int offa[MF], offb[NF];
 #pragma unroll
@@ -440,15 +445,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
             for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
     v4i_t a0[MF], a1[MF], b0[NF], b1[NF];
     uint32_t sa[MF], sb[NF], na[MF], nb[NF];
-    auto read0 = [&](const char* st, int t) {                // operand t of a step's first instruction, then the words of scales
-        if (t < MF) a0[t] = *(const v4i_t*)(st + offa[t]);
-        else if (t < MF + NF) b0[t - MF] = *(const v4i_t*)(st + offb[t - MF]);
-        else if (t < 2 * MF + NF) na[t - MF - NF] = *(const uint32_t*)(st + offsa + 128 * (t - MF - NF));
-        else nb[t - 2 * MF - NF] = *(const uint32_t*)(st + offsb + 128 * (t - 2 * MF - NF));
+    // the operands of a step's first instructions and the words of scales, in the order in which they are wanted
+    auto read0 = [&](const char* st, int t) {
+        if (t < NF) b0[t] = *(const v4i_t*)(st + offb[t]);
+        else if (t == NF) a0[0] = *(const v4i_t*)(st + offa[0]);
+        else if (t < 2 * NF + 1) nb[t - NF - 1] = *(const uint32_t*)(st + offsb + 128 * (t - NF - 1));
+        else if (t < 2 * NF + MF + 1) na[t - 2 * NF - 1] = *(const uint32_t*)(st + offsa + 128 * (t - 2 * NF - 1));
+        else a0[t - 2 * NF - MF] = *(const v4i_t*)(st + offa[t - 2 * NF - MF]);
     };
     auto read1 = [&](const char* st, int t) {                // the second's: the neighbouring pair of chunks
-        if (t < MF) a1[t] = *(const v4i_t*)(st + (offa[t] ^ 32));
-        else b1[t - MF] = *(const v4i_t*)(st + (offb[t - MF] ^ 32));
+        if (t < NF) b1[t] = *(const v4i_t*)(st + (offb[t] ^ 32));
+        else a1[t - NF] = *(const v4i_t*)(st + (offa[t - NF] ^ 32));
     };
     // Behind the words of the channels come the steps of the low-rank branch, 32 ranks of L_A and of one term of P each: 64 bytes a row as well.
     constexpr int TERMS = F32 ? 3 : 2;
@@ -475,12 +482,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
         next_a = term == TERMS - 1 ? 64 : 0;
         next_b = term == TERMS - 1 ? 64 - (TERMS - 1) * plane : plane;
     };
+    // Of a stage's loads the first EARLY are issued in the second half of a step, the others in the first half of the next: all at once they would wait for each other.
+    // Three slots only leave no time for that.
+    constexpr int EARLY = ST == 4 ? LOADS / 2 : LOADS;
     for (int s = 0; s < ST - 1 && s < steps; ++s) {
         aim(s);
 #pragma unroll
-        for (int t = 0; t < LOADS; ++t) issue((uint32_t)s * STAGE, t);
+        for (int t = 0; t < LOADS; ++t)
+            if (s < ST - 2 || t < EARLY) issue((uint32_t)s * STAGE, t);
     }
-    wait(steps >= ST - 1 ? ST - 2 : steps - 1);
+    if (steps >= ST - 1) wait_for(std::integral_constant<int, (ST - 3) * LOADS + EARLY>{});
+    else if (ST == 4 && steps == 2) wait_for(std::integral_constant<int, LOADS>{});
+    else wait_for(std::integral_constant<int, 0>{});
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < 2 * (MF + NF); ++t) read0(smem, t);
@@ -493,7 +506,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
         const uint32_t next = cur + STAGE == ST * STAGE ? 0 : cur + STAGE, put = cur == 0 ? (ST - 1) * STAGE : cur - STAGE;
         const char *st = smem + cur, *sn = smem + next;
         const bool more = STEADY || s + 1 < steps, fetch = STEADY || s + ST - 1 < steps;
-        if (!STEADY && fetch) aim(s + ST - 1);
+        const bool rest = EARLY < LOADS && (STEADY || s + ST - 2 < steps);
+        const uint32_t late = put == 0 ? (ST - 1) * STAGE : put - STAGE;      // the slot of the stage before
 #pragma unroll
         for (int i = 0; i < MF; ++i) sa[i] = na[i] >> (8 * h);
 #pragma unroll
@@ -505,24 +519,29 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
             acc[i][j] = RANKS ? mfma32_bf16(a0[i], b0[j], acc[i][j]) : mfma32<0>(a0[i], sa[i], b0[j], sb[j], acc[i][j]);
 #pragma unroll
             for (int t = 0; t < R1; ++t)
-                if (t * (M / 2) / R1 == k) read1(st, t);
+                if (t * (M - 1) / R1 == k) read1(st, t);
+#pragma unroll
+            for (int t = EARLY; t < LOADS; ++t)
+                if (rest && (t - EARLY) * M / (LOADS - EARLY) == k) issue(late, t);
             __builtin_amdgcn_sched_barrier(0);
         }
-        // second half: the wait for the next stage, the reads of its first half, the loads of the last stage that has a slot
+        // second half: the wait for the next stage, the reads of its first half, loads of the last stage that has a slot
 #pragma unroll
         for (int k = 0; k < M; ++k) {
             const int i = k / NF, j = k % NF;
             acc[i][j] = RANKS ? mfma32_bf16(a1[i], b1[j], acc[i][j]) : mfma32<2>(a1[i], sa[i], b1[j], sb[j], acc[i][j]);
             if (k == W && more) {
-                wait(ST == 4 && (STEADY || s + 2 < steps) ? 1 : 0);
+                if (ST == 4 && (STEADY || s + 2 < steps)) wait_for(std::integral_constant<int, LOADS>{});
+                else wait_for(std::integral_constant<int, 0>{});
                 __syncthreads();                             // everyone's share has landed, and everyone is done with stage s - 1
+                if (!STEADY && fetch) aim(s + ST - 1);
             }
 #pragma unroll
             for (int t = 0; t < R0; ++t)
-                if (more && W + 1 + t * (M / 2 - W) / R0 == k) read0(sn, t);
+                if (more && W + 1 + t * (M - W - 1) / R0 == k) read0(sn, t);
 #pragma unroll
-            for (int t = 0; t < LOADS; ++t)
-                if (fetch && M / 2 + t * (M / 2) / LOADS == k) issue(put, t);
+            for (int t = 0; t < EARLY; ++t)
+                if (fetch && W + 1 + t * (M - W - 1) / EARLY == k) issue(put, t);
             __builtin_amdgcn_sched_barrier(0);
         }
         cur = next;
@@ -555,7 +574,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
                 for (int k = 0; k < 4; ++k) {
                     float y[4];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) y[u] = GATED ? gated(acc[i][j][4 * k + u], acc[MF - OF + i][j][4 * k + u]) : acc[i][j][4 * k + u];
+                    for (int u = 0; u < 4; ++u) y[u] = GATED ? gated<F32>(acc[i][j][4 * k + u], acc[MF - OF + i][j][4 * k + u]) : acc[i][j][4 * k + u];
                     const int o = 32 * i + 8 * k + 4 * h;
                     if (F32) *(float4*)(row + 16 * chunk_of(li, o / 4)) = make_float4(y[0], y[1], y[2], y[3]);
                     else *(uint2*)(row + 16 * chunk_of(li, o / 8) + 8 * h) = make_uint2(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]));
