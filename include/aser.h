@@ -505,9 +505,9 @@ int aser_adapter_forward(aser_ctx* ctx, const void* X, int x_dtype, int64_t rows
  * `count` matrices of rows x n behind each other (experts; 1 otherwise).  Rows are padded with zeros (codes and scale bytes)
  * to width = n rounded up to a multiple of 128, and cut into words of 128 channels; 16 rows are a panel (the last one may have rows
  * that are not there: room for them, which nobody reads), and a word of a panel's rows lies side by side:
- *   codes:  count x panels x (width / 128) x 16 x 64 bytes, two codes a byte, the even channel in the low half
+ *   codes:  count x panels x (width / 128) x 4 blocks x 16 rows x 16 bytes, two codes a byte, the even channel in the low half
  *   scales: count x panels x (width / 128) x 16 x 4 bytes, byte i of word w of a row belongs to its block 4 w + i
- * (What a matrix instruction takes of 16 rows is a kilobyte in a row, and what a product with few rows reads of the other matrix is one stream.) */
+ * (What a matrix instruction takes of 16 rows is a kilobyte in the order of its lanes, and what a product with few rows reads of the other matrix is one stream.) */
 typedef struct aser_mx4 {
     uint8_t* codes;      /* DEVICE, 16-byte aligned */
     uint8_t* scales;     /* DEVICE, 16-byte aligned */

@@ -680,7 +680,7 @@ def aser_adapter_forward(ctx: Context, X, adapter, A, B, scale, Y0, Y) -> int:
 # ----------------------------------------------------------------------------------- microscaled 4 bits, experts
 class Mx4:
     """Matrices in microscaled 4 bits from their tensors (C struct aser_mx4), uint8 and contiguous, in the library's layout when `rows` is given: codes, panels x
-    words x 16 x 64, and scales, panels x words x 16 x 4, panels being ceil(rows / 16) and words ceil(n / 128); with one more dimension in front
+    words x 4 x 16 x 16, and scales, panels x words x 16 x 4, panels being ceil(rows / 16) and words ceil(n / 128); with one more dimension in front
     for several matrices (experts).  Without it codes are rows x 64 words and scales words x rows x 4, and are laid out anew (copies)."""
 
     def __init__(self, codes, scales, n: int, rows: Optional[int] = None):
@@ -693,14 +693,16 @@ class Mx4:
             if codes.dim() not in (2, 3) or tuple(scales.shape) != tuple(codes.shape[:-2]) + (words, codes.shape[-2], 4) or codes.shape[-1] != 64 * words:
                 raise ValueError("codes must be (matrices x) rows x 64 words, scales (matrices x) words x rows x 4")
             rows, pad = codes.shape[-2], -codes.shape[-2] % 16
-            laid = []
-            for t in (codes.unflatten(-1, (words, 64)), scales.transpose(-3, -2)):
-                t = torch.nn.functional.pad(t, (0, 0, 0, 0, 0, pad)) if pad else t
-                laid.append(t.unflatten(-3, ((rows + pad) // 16, 16)).transpose(-3, -2).contiguous())
-            codes, scales = laid
-        front, shape = tuple(codes.shape[:-4]), ((rows + 15) // 16, words, 16)
-        if codes.dim() not in (4, 5) or tuple(codes.shape) != front + shape + (64,) or tuple(scales.shape) != front + shape + (4,):
-            raise ValueError("codes must be (matrices x) panels x words x 16 x 64, scales (matrices x) panels x words x 16 x 4")
+            codes, scales = codes.unflatten(-1, (words, 4, 16)), scales.transpose(-3, -2)                       # rows first
+            if pad:
+                codes = torch.nn.functional.pad(codes, (0, 0, 0, 0, 0, 0, 0, pad))
+                scales = torch.nn.functional.pad(scales, (0, 0, 0, 0, 0, pad))
+            panels = (rows + pad) // 16
+            codes = codes.unflatten(-4, (panels, 16)).movedim(-4, -2).contiguous()
+            scales = scales.unflatten(-3, (panels, 16)).transpose(-3, -2).contiguous()
+        front, panels = tuple(scales.shape[:-4]), (rows + 15) // 16
+        if scales.dim() not in (4, 5) or tuple(codes.shape) != front + (panels, words, 4, 16, 16) or tuple(scales.shape) != front + (panels, words, 16, 4):
+            raise ValueError("codes must be (matrices x) panels x words x 4 x 16 x 16, scales (matrices x) panels x words x 16 x 4")
         if not (codes.is_contiguous() and scales.is_contiguous()):
             raise ValueError("codes and scales must be contiguous")
         self.codes, self.scales, self.n, self.rows, self.count, self.front = codes, scales, n, rows, front[0] if front else 1, front
@@ -711,8 +713,8 @@ class Mx4:
     def empty(cls, rows: int, n: int, count: Optional[int] = None, device: int = 0):
         """Room for one matrix, or with count for several."""
         import torch
-        shape = (() if count is None else (count,)) + ((rows + 15) // 16, (n + 127) // 128, 16)
-        return cls(*(torch.empty(shape + (k,), dtype=torch.uint8, device="cuda:%d" % device) for k in (64, 4)), n, rows)
+        shape = (() if count is None else (count,)) + ((rows + 15) // 16, (n + 127) // 128)
+        return cls(*(torch.empty(shape + more, dtype=torch.uint8, device="cuda:%d" % device) for more in ((4, 16, 16), (16, 4))), n, rows)
 
 
 class ExpertPlan:

@@ -5,9 +5,11 @@
 static const int64_t kMxWord = 128;         // channels of a scale word: four blocks of 32, 64 bytes of codes
 
 static inline int64_t mx4_words(int64_t n) { return ceil_div64(n, kMxWord); }
-// Place of word 0 of a row, in units of 64 bytes of codes or 4 of scales; the next word is kMxNext further.  Matrix e begins at e * mx4_size.
+// Rows are in panels of 16: the word of scales of a row is at mx4_at, in words, the following one kMxNext further; the 16 bytes of codes of block q are at
+// 16 mx4_code + 256 q bytes, those of the following word 64 kMxNext bytes further.  Matrix e begins e mx4_size words and 64 times as many bytes behind the first.
 static const int kMxNext = 16;
 __host__ __device__ static inline int64_t mx4_at(int64_t row, int64_t words) { return (row >> 4) * words * 16 + (row & 15); }
+__host__ __device__ static inline int64_t mx4_code(int64_t row, int64_t words) { return (row >> 4) * words * 64 + (row & 15); }
 __host__ __device__ static inline int64_t mx4_size(int64_t rows, int64_t words) { return ((rows + 15) >> 4) * words * 16; }
 // Checks of structs that have been given; `who` names the entry point.  Which arrays of a plan a call needs is its own matter.
 int aser_plan_check(aser_ctx* ctx, const char* who, const aser_expert_plan* p);

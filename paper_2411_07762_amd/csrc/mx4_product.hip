@@ -80,9 +80,13 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
     int e, rows;
     int64_t p0;
     if (!mx4_find_tile(g.groups, rest / g.parts, 16 * NT, &e, &p0, &rows)) return;
-    int64_t xat[NT];
+    int64_t xat[NT], xcode[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) xat[t] = mx4_at(mx4_row(g.groups, p0 + (16 * t + li < rows ? 16 * t + li : rows - 1)), g.words);
+    for (int t = 0; t < NT; ++t) {
+        const int64_t row = mx4_row(g.groups, p0 + (16 * t + li < rows ? 16 * t + li : rows - 1));
+        xat[t] = mx4_at(row, g.words);
+        xcode[t] = mx4_code(row, g.words) * 16;
+    }
     const uint16_t* lrow[RF];
     const uint4* const arranged = (const uint4*)g.lb + ((int64_t)e * g.words * g.lb_frags + rt * RF) * 256 + lane;
     f32x4_t acc[RF][NT];
@@ -100,12 +104,12 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
     auto load = [&](int u, int w) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int64_t at = xat[t] + (int64_t)w * kMxNext;
-            if (ARRANGED) codes[u][t] = *(const v4i_t*)(g.xc + at * 64 + 16 * q);
+            const uint8_t* const code = g.xc + xcode[t] + (int64_t)w * 1024;
+            if (ARRANGED) codes[u][t] = *(const v4i_t*)(code + 256 * q);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (!ARRANGED) codes[u][t][j] = *(const int*)(g.xc + at * 64 + 16 * j + 4 * q);
-            scale[u][t] = g.xs[at];
+                if (!ARRANGED) codes[u][t][j] = *(const int*)(code + 256 * j + 4 * q);
+            scale[u][t] = g.xs[xat[t] + (int64_t)w * kMxNext];
         }
         const int64_t c0 = (int64_t)w * kMxWord + 8 * q;
         // Behind the last channel the last ones are read again, against zeros of x; ranks that are not there read the last row, and what becomes of them is not kept.
@@ -195,6 +199,17 @@ __global__ __launch_bounds__(256) void mx4_arrange_kernel(const uint16_t* __rest
     out[i] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
 }
 
+// The tokens of the positions in their order, so that tiles read them as they read any matrix: on their own, 16 bytes of a row here and there would take
+// the address unit four times as long.  A workgroup has a panel, its threads the rows' blocks and words of scales.
+__global__ __launch_bounds__(256) void mx4_gather_kernel(MxGroups groups, const uint8_t* __restrict__ xc, const uint32_t* __restrict__ xs, int words, uint8_t* __restrict__ oc, uint32_t* __restrict__ os) {
+    const int li = threadIdx.x & 15;
+    const int64_t p = (int64_t)blockIdx.x * 16 + li, row = mx4_row(groups, p < groups.positions ? p : groups.positions - 1);
+    const uint4* const from = (const uint4*)xc + mx4_code(row, words);
+    uint4* const to = (uint4*)oc + (int64_t)blockIdx.x * words * 64 + li;
+    for (int i = threadIdx.x >> 4; i < 4 * words; i += 16) to[16 * i] = from[16 * i];
+    for (int i = threadIdx.x >> 4; i < words; i += 16) os[((int64_t)blockIdx.x * words + i) * 16 + li] = xs[mx4_at(row, words) + (int64_t)i * kMxNext];
+}
+
 // A factor with its rows of r padded with zeros, where it cannot be read in pieces of 16 bytes as it is (L_B), or not in pieces of 64 (L_A of many rows).
 __global__ __launch_bounds__(256) void mx4_pad_kernel(const uint16_t* __restrict__ la, int64_t rows, int64_t r, int64_t width, uint16_t* __restrict__ out) {
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, row = i / width;
@@ -208,13 +223,13 @@ __global__ __launch_bounds__(256) void mx4_pad_kernel(const uint16_t* __restrict
 
 // ---------------------------------------------------------------------------------------------------------------- few rows of a matrix
 // A workgroup has 16 FA rows of the weights (gated: half of them gates, the others their values) and up to 16 NT positions; its W wavefronts take the words of
-// the channels in turn, U of them ahead.  A fragment of a word, a panel's 16 rows, is a kilobyte of memory in a row; a lane's 16 bytes are block lane / 16 of row
-// lane % 16.  Outputs are in the rows of the accumulator, so a lane has four neighbouring ones of a position.  The sums of the wavefronts meet in LDS in a fixed
+// the channels in turn, U of them ahead.  A fragment of a word, a panel's 16 rows, is a kilobyte of memory in the order of the lanes; a lane's 16 bytes are block
+// lane / 16 of row lane % 16.  Outputs are in the rows of the accumulator, so a lane has four neighbouring ones of a position.  The sums of the wavefronts meet in LDS in a fixed
 // order.
 constexpr int kMostParts = 4;                                // of the channels, for P of few rows
 
 template <int FA, int NT, int W, int U, bool GATED, bool F32>
-__global__ __launch_bounds__(64 * W) void mx4_few_kernel(MxArgs g) {
+__global__ __launch_bounds__(64 * W, NT == 1 ? (U > 2 ? 5 : 6) : NT == 2 ? 4 : 3) void mx4_few_kernel(MxArgs g) {
     extern __shared__ __align__(16) float part[];            // [wavefront][fragment][lane][4]
     constexpr int OF = GATED ? FA / 2 : FA;                  // fragments of outputs
     const int lane = threadIdx.x & 63, li = lane & 15, q = lane >> 4;
@@ -223,17 +238,20 @@ __global__ __launch_bounds__(64 * W) void mx4_few_kernel(MxArgs g) {
     int64_t p0;
     if (!mx4_find_tile(g.groups, blockIdx.y, 16 * NT, &e, &p0, &rows)) return;
     const int64_t o0 = (int64_t)blockIdx.x * (16 * OF);
-    int64_t arow[FA], aat[FA], bat[NT];
+    int64_t arow[FA], aat[FA], bat[NT], acode[FA], bcode[NT];
 #pragma unroll
     for (int a = 0; a < FA; ++a) {
         const int64_t o = o0 + 16 * (a % OF) + li;           // past the end: the last one again, not stored
         arow[a] = (a >= OF ? g.outs : 0) + (o < g.outs ? o : g.outs - 1);
         aat[a] = e * g.w_size + mx4_at(arow[a], g.words);
+        acode[a] = e * g.w_size * 64 + mx4_code(arow[a], g.words) * 16 + 256 * q;
     }
 #pragma unroll
-    for (int t = 0; t < NT; ++t) bat[t] = mx4_at(mx4_row(g.groups, p0 + (16 * t + li < rows ? 16 * t + li : rows - 1)), g.words);
-    const uint8_t* const wc = g.wc + 16 * q;
-    const uint8_t* const xc = g.xc + 16 * q;
+    for (int t = 0; t < NT; ++t) {
+        const int64_t row = mx4_row(g.groups, p0 + (16 * t + li < rows ? 16 * t + li : rows - 1));
+        bat[t] = mx4_at(row, g.words);
+        bcode[t] = mx4_code(row, g.words) * 16 + 256 * q;
+    }
     f32x4_t acc[FA][NT];
 #pragma unroll
     for (int a = 0; a < FA; ++a)
@@ -244,15 +262,13 @@ __global__ __launch_bounds__(64 * W) void mx4_few_kernel(MxArgs g) {
     auto load = [&](int u, int w) {
 #pragma unroll
         for (int a = 0; a < FA; ++a) {
-            const int64_t at = aat[a] + (int64_t)w * kMxNext;
-            av[u][a] = *(const v4i_t*)(wc + at * 64);
-            sa[u][a] = g.ws[at];
+            av[u][a] = *(const v4i_t*)(g.wc + acode[a] + (int64_t)w * 1024);
+            sa[u][a] = g.ws[aat[a] + (int64_t)w * kMxNext];
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int64_t at = bat[t] + (int64_t)w * kMxNext;
-            bv[u][t] = *(const v4i_t*)(xc + at * 64);
-            sb[u][t] = g.xs[at];
+            bv[u][t] = *(const v4i_t*)(g.xc + bcode[t] + (int64_t)w * 1024);
+            sb[u][t] = g.xs[bat[t] + (int64_t)w * kMxNext];
         }
     };
 #pragma unroll
@@ -345,8 +361,8 @@ __global__ __launch_bounds__(64 * W) void mx4_few_kernel(MxArgs g) {
 
 // ---------------------------------------------------------------------------------------------------------------- many rows of a matrix
 // A workgroup has 64 MF outputs of 64 NF positions, a wavefront (2 x 2 of them, one for each SIMD) 32 MF x 32 NF.  A step is a word of the channels: 64 bytes of
-// codes and a word of scales of every row go straight from memory into LDS, in 16-byte chunks whose place in a row is turned by the row so that 32 rows' reads meet all banks; a ring of
-// four stages keeps three steps of loads in flight, one barrier a step.  The loads are inline assembly because the compiler would
+// codes and a word of scales of every row go straight from memory into LDS, a panel's kilobyte as it is, block by block, so that 16 lanes read 256 bytes in a row; a ring
+// of ST stages, one barrier a step.  The loads are inline assembly because the compiler would
 // make every LDS read wait for all of them.  Half h = lane / 32 of the lanes holds blocks h and 2 + h of a step, one for each of its two instructions
 // per pair of fragments, whose scales are bytes 0 and 2 of its word shifted by h bytes.
 // Gated, a wavefront's first MF / 2 fragments are gates and the others the values that belong to them.
@@ -354,6 +370,7 @@ __global__ __launch_bounds__(64 * W) void mx4_few_kernel(MxArgs g) {
 // and a matrix is read once where its positions make no more than a panel.
 constexpr int kPanel = 4;
 
+__device__ __forceinline__ int block_at(int r, int q) { return (r >> 4) * 1024 + q * 256 + (r & 15) * 16; }
 __device__ __forceinline__ int chunk_at(int r, int c) { return r * 64 + ((c ^ ((r >> 2) & 3)) << 4); }
 
 template <int B>
@@ -398,15 +415,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
         }
         return base + (o < g.outs ? o : g.outs - 1);
     };
-    auto token_row = [&](int r) { return mx4_row(g.groups, p0 + (r < rows ? r : rows - 1)); };
+    auto token_row = [&](int r) { return p0 + (r < rows ? r : rows - 1); };      // many rows: in order
 
-    // what this lane fetches: chunk lane % 4 of a row's slab of 64 bytes, 16 rows an instruction, and words of scales, 64 rows an instruction
+    // what this lane fetches: 16 rows an instruction, of row lane % 16 block lane / 16, and words of scales, 64 rows an instruction
     const char *ga[MF], *gb[NF], *gs[2];
-    const int ch = (lane & 3) ^ ((lane >> 4) & 3);
 #pragma unroll
-    for (int t = 0; t < MF; ++t) ga[t] = (const char*)g.wc + (e * g.w_size + mx4_at(weight_row(16 * (MF * wave + t) + (lane >> 2)), g.words)) * 64 + 16 * ch;
+    for (int t = 0; t < MF; ++t) ga[t] = (const char*)g.wc + e * g.w_size * 64 + mx4_code(weight_row(16 * (MF * wave + t) + (lane & 15)), g.words) * 16 + 256 * (lane >> 4);
 #pragma unroll
-    for (int t = 0; t < NF; ++t) gb[t] = (const char*)g.xc + mx4_at(token_row(16 * (NF * wave + t) + (lane >> 2)), g.words) * 64 + 16 * ch;
+    for (int t = 0; t < NF; ++t) gb[t] = (const char*)g.xc + mx4_code(token_row(16 * (NF * wave + t) + (lane & 15)), g.words) * 16 + 256 * (lane >> 4);
     gs[0] = (const char*)(g.ws + e * g.w_size + mx4_at(weight_row(64 * (wave % MF) + lane), g.words));
     gs[1] = (const char*)(g.xs + mx4_at(token_row(64 * (wave % NF) + lane), g.words));
     int64_t next_a = kMxNext * 64, next_b = kMxNext * 64, next_s = kMxNext * 4;      // bytes to the following stage
@@ -432,9 +448,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
 
     int offa[MF], offb[NF];
 #pragma unroll
-    for (int i = 0; i < MF; ++i) offa[i] = chunk_at(wa * 32 * MF + 32 * i + li, h);
+    for (int i = 0; i < MF; ++i) offa[i] = block_at(wa * 32 * MF + 32 * i + li, h);
 #pragma unroll
-    for (int j = 0; j < NF; ++j) offb[j] = A_BYTES + chunk_at(wb * 32 * NF + 32 * j + li, h);
+    for (int j = 0; j < NF; ++j) offb[j] = A_BYTES + block_at(wb * 32 * NF + 32 * j + li, h);
     const int offsa = SA + (wa * 32 * MF + li) * 4, offsb = SB + (wb * 32 * NF + li) * 4;
     f32x16_t acc[MF][NF];
 #pragma unroll
@@ -453,14 +469,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
         else if (t < 2 * NF + MF + 1) na[t - 2 * NF - 1] = *(const uint32_t*)(st + offsa + 128 * (t - 2 * NF - 1));
         else a0[t - 2 * NF - MF] = *(const v4i_t*)(st + offa[t - 2 * NF - MF]);
     };
-    auto read1 = [&](const char* st, int t) {                // the second's: the neighbouring pair of chunks
-        if (t < NF) b1[t] = *(const v4i_t*)(st + (offb[t] ^ 32));
-        else a1[t - NF] = *(const v4i_t*)(st + (offa[t - NF] ^ 32));
+    auto read1 = [&](const char* st, int t, bool ranks) {    // the second's: two blocks on, or the neighbouring pair of chunks
+        if (t < NF) b1[t] = *(const v4i_t*)(st + (ranks ? offb[t] ^ 32 : offb[t] + 512));
+        else a1[t - NF] = *(const v4i_t*)(st + (ranks ? offa[t - NF] ^ 32 : offa[t - NF] + 512));
+    };
+    auto read_ranks = [&]() {                                // from here on stages of ranks are read
+#pragma unroll
+        for (int i = 0; i < MF; ++i) offa[i] = chunk_at(wa * 32 * MF + 32 * i + li, h);
+#pragma unroll
+        for (int j = 0; j < NF; ++j) offb[j] = A_BYTES + chunk_at(wb * 32 * NF + 32 * j + li, h);
     };
     // Behind the words of the channels come the steps of the low-rank branch, 32 ranks of L_A and of one term of P each: 64 bytes a row as well.
     constexpr int TERMS = F32 ? 3 : 2;
     const int words = g.words, steps = words + g.lr_steps;
     auto turn_to_ranks = [&]() {
+        const int ch = (lane & 3) ^ ((lane >> 4) & 3);       // of row lane / 4 the chunk that goes to place lane % 4
         const int64_t width = 64 * (int64_t)(g.lr_steps / TERMS);        // bytes of a row of P
 #pragma unroll
         for (int t = 0; t < MF; ++t) ga[t] = (const char*)g.la + ((int64_t)e * g.m + weight_row(16 * (MF * wave + t) + (lane >> 2))) * g.la_ld * 2 + 16 * ch;
@@ -519,7 +542,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
             acc[i][j] = RANKS ? mfma32_bf16(a0[i], b0[j], acc[i][j]) : mfma32<0>(a0[i], sa[i], b0[j], sb[j], acc[i][j]);
 #pragma unroll
             for (int t = 0; t < R1; ++t)
-                if (t * (M - 1) / R1 == k) read1(st, t);
+                if (t * (M - 1) / R1 == k) read1(st, t, RANKS);
 #pragma unroll
             for (int t = EARLY; t < LOADS; ++t)
                 if (rest && (t - EARLY) * M / (LOADS - EARLY) == k) issue(late, t);
@@ -535,6 +558,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
                 else wait_for(std::integral_constant<int, 0>{});
                 __syncthreads();                             // everyone's share has landed, and everyone is done with stage s - 1
                 if (!STEADY && fetch) aim(s + ST - 1);
+                if (!STEADY && s + 1 == words) read_ranks();
             }
 #pragma unroll
             for (int t = 0; t < R0; ++t)
@@ -653,8 +677,8 @@ int run_few(aser_ctx* ctx, const MxArgs& g, int nt, int64_t matrices, bool gated
     if (nt == 3) return launch_few<2, 3, 4, 2>(ctx, g, gated, f32);
     if (nt == 4) return launch_few<2, 4, 4, 2>(ctx, g, gated, f32);
     const int64_t panels = matrices * ceil_div64(g.m, 16);
-    if (panels >= 8192) return launch_few<4, 1, 4, 2>(ctx, g, gated, f32);
-    if (gated || panels >= 1024) return launch_few<2, 1, 8, 2>(ctx, g, gated, f32);
+    if (panels >= 1024) return launch_few<2, 1, 4, 2>(ctx, g, gated, f32);
+    if (gated) return launch_few<2, 1, 8, 2>(ctx, g, gated, f32);
     return launch_few_one<1, 1, 8, 4, false>(ctx, g, f32);
 }
 
@@ -672,8 +696,9 @@ struct Plan {
     int nt;                  // 16 nt positions a workgroup
     bool many;               // tiles through LDS instead
     int parts, part_words;   // few rows: of the channels, for P
+    size_t x_bytes;                          // many rows of experts: their codes and scales in order
     size_t p_bytes, la_bytes, lb_bytes;      // P, and the factors as the kernels want them
-    size_t all() const { return p_bytes + la_bytes + lb_bytes; }
+    size_t all() const { return x_bytes + p_bytes + la_bytes + lb_bytes; }
 };
 
 Plan plan_product(int64_t positions, int64_t n, int64_t m, int32_t count, int32_t r) {
@@ -687,6 +712,7 @@ Plan plan_product(int64_t positions, int64_t n, int64_t m, int32_t count, int32_
     if (parts > kMostParts) parts = kMostParts;
     p.part_words = (int)ceil_div64(words, parts);
     p.parts = (int)ceil_div64(words, p.part_words);
+    if (p.many && count > 1) p.x_bytes = align_up((size_t)mx4_size(positions, words) * 68, 256);
     if (r <= 0) return p;
     if (p.many) {
         p.p_bytes = align_up((size_t)positions * align_up(r, 32) * 2 * 3, 256);
@@ -729,7 +755,7 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
     if (groups.positions == 0) return ASER_OK;
     if (!Y) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "%s: null pointer", who);
     const Plan p = plan_product(groups.positions, w->n, w->rows, w->count, r);
-    if (r > 0 && (!ctx->ws || ctx->ws_bytes < p.all() + kAserWsTail)) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "%s: workspace too small", who);
+    if (p.all() > 0 && (!ctx->ws || ctx->ws_bytes < p.all() + kAserWsTail)) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "%s: workspace too small", who);
     MxArgs g{};
     g.groups = groups;
     g.words = (int)mx4_words(w->n);
@@ -742,10 +768,11 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
     g.vec = !((uintptr_t)Y & (unit - 1)) && !(ldy * size & (unit - 1));
     ASER_TRY(aser_prepare_device(ctx));
     const bool lb_vec = !((uintptr_t)L_B & 15) && !(w->n & 7);
-    uint16_t* const lb_room = (uint16_t*)((char*)ctx->ws + p.p_bytes + p.la_bytes);
+    char* const p_room = (char*)ctx->ws + p.x_bytes;
+    uint16_t* const lb_room = (uint16_t*)(p_room + p.p_bytes + p.la_bytes);
     if (!p.many) {
         if (r > 0) {
-            g.P = (float*)ctx->ws;
+            g.P = (float*)p_room;
             if (!lb_vec) {
                 g.lb_ld = align_up(w->n, 8);
                 ASER_TRY(pad_rows(ctx, L_B, (int64_t)w->count * r, w->n, g.lb_ld, lb_room));
@@ -755,9 +782,18 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
         }
         return run_few(ctx, g, p.nt, w->count < groups.positions ? w->count : groups.positions, swiglu, f32);
     }
+    if (groups.order) {
+        uint8_t* const codes = (uint8_t*)ctx->ws;
+        uint32_t* const scales = (uint32_t*)(codes + mx4_size(groups.positions, g.words) * 64);
+        mx4_gather_kernel<<<(unsigned)ceil_div64(groups.positions, 16), 256, 0, ctx->stream>>>(groups, g.xc, g.xs, g.words, codes, scales);
+        ASER_TRY(aser_check_launch(ctx, "mx4_gather_kernel"));
+        g.xc = codes;
+        g.xs = scales;
+        g.groups.order = nullptr;
+    }
     if (r > 0) {
         const int terms = f32 ? 3 : 2, width = (int)align_up(r, 32);
-        g.planes = (uint16_t*)ctx->ws;
+        g.planes = (uint16_t*)p_room;
         g.lr_steps = width / 32 * terms;
         g.lb_frags = width / 16;
         const int64_t units = (int64_t)w->count * g.words * g.lb_frags * 256, grid = ceil_div64(units, 256);
@@ -770,7 +806,7 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
 #endif
         ASER_TRY(f32 ? (launch_down<DOWN, 3>(ctx, g)) : (launch_down<DOWN, 2>(ctx, g)));
         if (r != width || ((uintptr_t)L_A & 15)) {
-            uint16_t* const padded = (uint16_t*)((char*)ctx->ws + p.p_bytes);
+            uint16_t* const padded = (uint16_t*)(p_room + p.p_bytes);
             ASER_TRY(pad_rows(ctx, L_A, w->rows * w->count, r, width, padded));
             g.la = padded;
             g.la_ld = width;

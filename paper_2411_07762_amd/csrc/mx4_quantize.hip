@@ -90,9 +90,9 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(QuantArgs g) {
     uint32_t w = byte << (8 * (li >> 2));
     w |= __shfl_xor(w, 4);
     w |= __shfl_xor(w, 8);
-    const int64_t e = row / g.rows, at0 = e * mx4_size(g.rows, g.words) + mx4_at(row - e * g.rows, g.words) + word * kMxNext;
-    ((uint32_t*)g.codes)[at0 * 16 + li] = codes;
-    if (li == 0) g.scales[at0] = w;
+    const int64_t e = row / g.rows, in = row - e * g.rows, matrix = e * mx4_size(g.rows, g.words);
+    ((uint32_t*)g.codes)[(matrix * 4 + mx4_code(in, g.words) + word * 64 + 16 * (li >> 2)) * 4 + (li & 3)] = codes;
+    if (li == 0) g.scales[matrix + mx4_at(in, g.words) + word * kMxNext] = w;
     if (!VALUES || here == 0) return;
     pair_t v2[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 1),
                     __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 3)};

@@ -58,9 +58,10 @@ def quantized(ctx, x, mdiag=None, values=None, count=None):
 
 
 def rows_of(t, rows):
-    """panels x words x 16 x k as rows x words x k."""
+    """Panels of scales (panels x words x 16 x 4) or of codes (panels x words x 4 x 16 x 16) as rows x words x bytes."""
     t = t.cpu().numpy()
-    return t.transpose(0, 2, 1, 3).reshape(-1, t.shape[1], t.shape[3])[:rows]
+    t = t.transpose(0, 3, 1, 2, 4) if t.ndim == 5 else t.transpose(0, 2, 1, 3)
+    return t.reshape(t.shape[0] * 16, t.shape[2], -1)[:rows]
 
 
 def check_quantized(x, out, values, mdiag=None):
