@@ -31,6 +31,7 @@ struct MxArgs {
     uint16_t* planes; int lr_steps;                         // many rows: [term][position][32 lr_steps / terms] bf16; steps of 32 ranks and one term
     void* Y; int64_t ldy; int64_t outs;                     // columns of Y
     bool vec;                                               // 16 bytes (few rows: four columns) of Y at a time
+    bool la_four;                                           // four ranks of L_A in a load
 };
 
 // Four-bit operands are the first four registers of the instruction's eight.
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(256) void mx4_pad_kernel(const uint16_t* __restrict
 constexpr int kMostParts = 4;                                // of the channels, for P of few rows
 
 template <int FA, int NT, int W, int U, bool GATED, bool F32>
-__global__ __launch_bounds__(64 * W, NT == 1 ? (U > 2 ? 5 : 6) : NT == 2 ? 4 : 3) void mx4_few_kernel(MxArgs g) {
+__global__ __launch_bounds__(64 * W, NT <= 2 ? 4 : 3) void mx4_few_kernel(MxArgs g) {
     extern __shared__ __align__(16) float part[];            // [wavefront][fragment][lane][4]
     constexpr int OF = GATED ? FA / 2 : FA;                  // fragments of outputs
     const int lane = threadIdx.x & 63, li = lane & 15, q = lane >> 4;
@@ -281,17 +282,25 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (U > 2 ? 5 : 6) : NT == 2 ? 4 : 3
     if (g.P) {
         const uint16_t* const la = g.la + (int64_t)e * g.m * g.r;
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c)
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int k = 16 * (wave + c * W) + 4 * q;
+            if (16 * (wave + c * W) >= g.rp) break;
 #pragma unroll
             for (int a = 0; a < FA; ++a) {
-                const int k = 16 * (wave + c * W) + 4 * q;
                 const uint16_t* const src = la + arow[a] * g.r + k;
+                if (g.la_four) {
+                    const uint2 v = *(const uint2*)(k < g.r ? src : la);
+                    lv[c][a][0] = k < g.r ? v.x : 0u;
+                    lv[c][a][1] = k < g.r ? v.y : 0u;
+                    continue;
+                }
                 uint32_t h[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) h[i] = k + i < g.r ? src[i] : 0u;
                 lv[c][a][0] = h[0] | h[1] << 16;
                 lv[c][a][1] = h[2] | h[3] << 16;
             }
+        }
         const int four = g.rp / 4;
         const int64_t next = g.groups.positions * g.rp;
         for (int i = threadIdx.x; i < 16 * NT * four; i += 64 * W) {
@@ -677,7 +686,7 @@ int run_few(aser_ctx* ctx, const MxArgs& g, int nt, int64_t matrices, bool gated
     if (nt == 3) return launch_few<2, 3, 4, 2>(ctx, g, gated, f32);
     if (nt == 4) return launch_few<2, 4, 4, 2>(ctx, g, gated, f32);
     const int64_t panels = matrices * ceil_div64(g.m, 16);
-    if (panels >= 1024) return launch_few<2, 1, 4, 2>(ctx, g, gated, f32);
+    if (panels >= 1024) return launch_few<2, 1, 4, 4>(ctx, g, gated, f32);
     if (gated) return launch_few<2, 1, 8, 2>(ctx, g, gated, f32);
     return launch_few_one<1, 1, 8, 4, false>(ctx, g, f32);
 }
@@ -766,6 +775,7 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
     g.Y = Y; g.ldy = ldy; g.outs = outs;
     const int64_t unit = p.many || f32 ? 16 : 8, size = f32 ? 4 : 2;
     g.vec = !((uintptr_t)Y & (unit - 1)) && !(ldy * size & (unit - 1));
+    g.la_four = !((uintptr_t)L_A & 7) && !(r & 3);
     ASER_TRY(aser_prepare_device(ctx));
     const bool lb_vec = !((uintptr_t)L_B & 15) && !(w->n & 7);
     char* const p_room = (char*)ctx->ws + p.x_bytes;
