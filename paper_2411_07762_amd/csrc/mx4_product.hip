@@ -230,7 +230,7 @@ __global__ __launch_bounds__(256) void mx4_pad_kernel(const uint16_t* __restrict
 constexpr int kMostParts = 4;                                // of the channels, for P of few rows
 
 template <int FA, int NT, int W, int U, bool GATED, bool F32>
-__global__ __launch_bounds__(64 * W, NT <= 2 ? 4 : 3) void mx4_few_kernel(MxArgs g) {
+__global__ __launch_bounds__(64 * W, FA * NT <= 4 ? 4 : FA * NT <= 8 ? 3 : 2) void mx4_few_kernel(MxArgs g) {
     extern __shared__ __align__(16) float part[];            // [wavefront][fragment][lane][4]
     constexpr int OF = GATED ? FA / 2 : FA;                  // fragments of outputs
     const int lane = threadIdx.x & 63, li = lane & 15, q = lane >> 4;
@@ -682,10 +682,10 @@ int run_few(aser_ctx* ctx, const MxArgs& g, int nt, int64_t matrices, bool gated
 #ifdef FEW
     return launch_few<FEW>(ctx, g, gated, f32);
 #endif
-    if (nt == 2) return launch_few<2, 2, 4, 2>(ctx, g, gated, f32);
-    if (nt == 3) return launch_few<2, 3, 4, 2>(ctx, g, gated, f32);
-    if (nt == 4) return launch_few<2, 4, 4, 2>(ctx, g, gated, f32);
     const int64_t panels = matrices * ceil_div64(g.m, 16);
+    if (nt == 2) return panels >= 4096 ? launch_few<4, 2, 4, 2>(ctx, g, gated, f32) : launch_few<2, 2, 4, 2>(ctx, g, gated, f32);
+    if (nt == 3) return panels >= 4096 ? launch_few<4, 3, 4, 2>(ctx, g, gated, f32) : launch_few<2, 3, 4, 2>(ctx, g, gated, f32);
+    if (nt == 4) return panels >= 4096 ? launch_few<4, 4, 4, 2>(ctx, g, gated, f32) : launch_few<2, 4, 4, 2>(ctx, g, gated, f32);
     if (panels >= 1024) return launch_few<2, 1, 4, 4>(ctx, g, gated, f32);
     if (gated) return launch_few<2, 1, 8, 2>(ctx, g, gated, f32);
     return launch_few_one<1, 1, 8, 4, false>(ctx, g, f32);
