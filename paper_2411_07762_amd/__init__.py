@@ -8,6 +8,7 @@ the HIP library has not been built, importing the entry points raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -745,43 +746,51 @@ class ExpertPlan:
 
 def aser_mx4_quantize(ctx: Context, X, out: Mx4, *, mdiag=None, values=None) -> int:
     """X: (matrices x) rows x n, bfloat16 or float32; mdiag: n float32; values: like X (may be X)."""
-    device, f32 = ctx.device, (_TYPES or _types())[1]
+    device, dtype = ctx.device, X.dtype
+    f32 = (_TYPES or _types())[1]
+    dt = ASER_DTYPE_F32 if dtype is f32 else _dtype_code(X)
     if X.dim() == 3:
         X = X.view(-1, X.shape[-1])
         values = None if values is None else values.view(-1, values.shape[-1])
+    rows, n, mp = X.shape[0], out.n, None
     if out.device != device:
         raise ValueError(_ELSEWHERE)
-    rows, dt = out.rows * out.count, _dtype_code(X)
-    xp, ldx, n = _rows(X, rows, X.dtype, device)
-    if n != out.n or X.shape[0] != rows or (mdiag is not None and mdiag.numel() != n):
-        raise ValueError("X must have the rows and channels of the result, mdiag a float32 for each channel")
-    vp, ldv, width = (None, n, n) if values is None else _rows(values, rows, X.dtype, device)
+    xp, ldx, cols = _rows(X, rows, dtype, device)
+    if cols != n or rows != out.rows * out.count:
+        raise ValueError("X must have the rows and channels of the result")
+    if mdiag is not None:
+        if mdiag.numel() != n:
+            raise ValueError("mdiag must have a float32 for each channel")
+        mp = _floats((mdiag,), f32, device)[0]
+    vp, ldv, width = (None, n, n) if values is None else _rows(values, rows, dtype, device)
     if width < n:
         raise ValueError("values must be as wide as X")
-    return ctx._lib.aser_mx4_quantize(ctx.handle, xp, dt, ldx, _floats((mdiag,), f32, device)[0], out.ref, vp, ldv)
+    return ctx._lib.aser_mx4_quantize(ctx.handle, xp, dt, ldx, mp, out.ref, vp, ldv)
 
 
 def _product(ctx: Context, x: Mx4, w: Mx4, Y, rows: int, L_A, L_B, swiglu: bool):
     """(address of L_A, of L_B, rank, swiglu, address of Y, its type, its leading dimension) after the checks that the library cannot make."""
-    device, bf16 = ctx.device, (_TYPES or _types())[0]
+    device = ctx.device
     if x.device != device or w.device != device:
         raise ValueError(_ELSEWHERE)
-    r, la, lb = 0, None, None
-    if (L_A is None) != (L_B is None):
-        raise ValueError("L_A and L_B go together")
-    if L_A is not None:
+    r, la, lb, outs, dtype = 0, None, None, w.rows, Y.dtype
+    bf16, f32, _ = _TYPES or _types()
+    if L_A is not None and L_B is not None:
         r = L_A.shape[-1]
-        if tuple(L_A.shape) != w.front + (w.rows, r) or tuple(L_B.shape) != w.front + (r, w.n) or not (L_A.is_contiguous() and L_B.is_contiguous()):
+        if L_A.shape != w.front + (outs, r) or L_B.shape != w.front + (r, w.n) or not (L_A.is_contiguous() and L_B.is_contiguous()):
             raise ValueError("L_A must be (matrices x) outputs x r and L_B (matrices x) r x channels, contiguous")
-        if L_A.dtype != bf16 or L_B.dtype != bf16:
+        if L_A.dtype is not bf16 or L_B.dtype is not bf16:
             raise TypeError("L_A and L_B must be bfloat16")
         if L_A.get_device() != device or L_B.get_device() != device:
             raise ValueError(_ELSEWHERE)
-        la, lb = (L_A.data_ptr(), L_B.data_ptr()) if r else (None, None)
-    yp, ldy, width = _rows(Y, rows, Y.dtype, device)
-    if width < (w.rows // 2 if swiglu else w.rows):
+        if r:
+            la, lb = L_A.data_ptr(), L_B.data_ptr()
+    elif L_A is not None or L_B is not None:
+        raise ValueError("L_A and L_B go together")
+    yp, ldy, width = _rows(Y, rows, dtype, device)
+    if width < (outs // 2 if swiglu else outs):
         raise ValueError("Y must have a column for each output")
-    return la, lb, r, 1 if swiglu else 0, yp, _dtype_code(Y), ldy
+    return la, lb, r, 1 if swiglu else 0, yp, ASER_DTYPE_F32 if dtype is f32 else _dtype_code(Y), ldy
 
 
 def aser_mx4_forward_workspace_bytes(rows: int, n: int, m: int, r: int) -> int:
@@ -797,6 +806,11 @@ def aser_route_workspace_bytes(rows: int, n_experts: int, top_k: int) -> int:
     return int(load_library().aser_route_workspace_bytes(rows, n_experts, top_k))
 
 
+@functools.lru_cache(maxsize=64)
+def _route_opts(sigmoid, groups, top_groups, group_top, renormalize, scale):
+    return ctypes.byref(aser_route_opts(1 if sigmoid else 0, groups, top_groups, group_top, 1 if renormalize else 0, scale))
+
+
 def aser_route_experts(ctx: Context, logits, plan: ExpertPlan, *, bias=None, sigmoid: bool = False, groups: int = 1, top_groups: int = 1, group_top: int = 1,
                        renormalize: bool = True, scale: float = 1.0) -> int:
     """logits: rows x experts, bfloat16 or float32; bias: experts float32.  Fills the plan."""
@@ -806,8 +820,8 @@ def aser_route_experts(ctx: Context, logits, plan: ExpertPlan, *, bias=None, sig
     lp, ldl, experts = _rows(logits, plan.rows, logits.dtype, device)
     if experts != plan.n_experts or (bias is not None and bias.numel() != experts):
         raise ValueError("logits and bias must have a column for each expert")
-    opts = aser_route_opts(1 if sigmoid else 0, groups, top_groups, group_top, 1 if renormalize else 0, scale)
-    return ctx._lib.aser_route_experts(ctx.handle, lp, _dtype_code(logits), ldl, _floats((bias,), f32, device)[0], ctypes.byref(opts), plan.ref)
+    opts = _route_opts(bool(sigmoid), groups, top_groups, group_top, bool(renormalize), scale)
+    return ctx._lib.aser_route_experts(ctx.handle, lp, _dtype_code(logits), ldl, None if bias is None else _floats((bias,), f32, device)[0], opts, plan.ref)
 
 
 def aser_expert_forward_workspace_bytes(positions: int, n: int, m: int, n_experts: int, r: int) -> int:
