@@ -10,7 +10,7 @@
 
 namespace {
 
-constexpr int kTok = 32, kWaves = 16;
+constexpr int kTok = 32, kWaves = 16;         // rows of a workgroup, its wavefronts
 constexpr double kMinus = -__builtin_huge_val();
 
 struct RouteArgs {
@@ -24,6 +24,7 @@ struct RouteArgs {
     int32_t* totals;      // [expert]
     int groups;           // workgroups
     int per_bits;         // 2^per_bits lanes look at a group of experts
+    float per_expert;     // 1 / experts of a group
 };
 
 // Steps of a reduction over a wavefront by the data-parallel moves: after the six of them lane 63 has the result of all.  Lanes that a move does not reach get `idle`.
@@ -67,27 +68,26 @@ __device__ __forceinline__ uint64_t key_of(double v) {
     return b >> 63 ? ~b : b | (uint64_t)1 << 63;
 }
 
-// exp(x) in 64 bits for x <= 709, or any x whose exponential is to be capped there: x = k ln 2 + r, |r| <= ln 2 / 2, and the Taylor series of exp(r) to r^13 / 13!, whose rest
-// is below 2^-57 of it.  Half the instructions of the library's function, which a third of the routing's time went into.
-__device__ __forceinline__ double exp64(double x) {
-    x = fmin(fmax(x, -746.0), 709.0);
-    const double k = rint(x * 1.4426950408889634);
-    const double r = fma(-k, 2.3190468138462996e-17, fma(-k, 0.6931471805599453, x));      // ln 2 as the nearest number of 64 bits and what it leaves
-    double p = 1.0 / 6227020800.0;
-    p = fma(p, r, 1.0 / 479001600.0);
-    p = fma(p, r, 1.0 / 39916800.0);
-    p = fma(p, r, 1.0 / 3628800.0);
-    p = fma(p, r, 1.0 / 362880.0);
-    p = fma(p, r, 1.0 / 40320.0);
-    p = fma(p, r, 1.0 / 5040.0);
-    p = fma(p, r, 1.0 / 720.0);
-    p = fma(p, r, 1.0 / 120.0);
-    p = fma(p, r, 1.0 / 24.0);
-    p = fma(p, r, 1.0 / 6.0);
-    p = fma(p, r, 0.5);
-    p = fma(p, r, 1.0);
-    p = fma(p, r, 1.0);
-    return __builtin_amdgcn_ldexp(p, (int)k);
+// x[j] to exp(x[j]) in 64 bits, 709 and more as 709: x = k ln 2 + r, |r| <= ln 2 / 2, and the Taylor series of exp(r) to r^13 / 13!, whose rest is below 2^-57 of it.  All
+// numbers of a lane at once, so that the constants are there once; half the instructions of the library's function, which a third of the routing's time went into.
+template <int V>
+__device__ __forceinline__ void exp64(double* x) {
+    constexpr double kOver[12] = {1.0 / 479001600.0, 1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0,
+                                  1.0 / 720.0,       1.0 / 120.0,      1.0 / 24.0,      1.0 / 6.0,      0.5,           1.0};
+    double k[V], r[V], p[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const double v = fmin(fmax(x[j], -746.0), 709.0);
+        k[j] = rint(v * 1.4426950408889634);
+        r[j] = fma(-k[j], 2.3190468138462996e-17, fma(-k[j], 0.6931471805599453, v));      // ln 2 as the nearest number of 64 bits and what it leaves
+        p[j] = 1.0 / 6227020800.0;
+    }
+#pragma unroll
+    for (int i = 0; i < 12; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) p[j] = fma(p[j], r[j], kOver[i]);
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = __builtin_amdgcn_ldexp(fma(p[j], r[j], 1.0), (int)k[j]);
 }
 // 1 / x for x in [1, 2^1023]: the instruction's approximation and two steps of Newton's method.
 __device__ __forceinline__ double reciprocal64(double x) {
@@ -141,6 +141,9 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(RouteArgs g) {
     int32_t* const first = (int32_t*)(marks + g.experts);                   // experts + 1
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t row0 = (int64_t)blockIdx.x * kTok;
+    float bias[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) bias[j] = g.bias && lane + 64 * j < g.experts ? g.bias[lane + 64 * j] : 0.f;
     for (int e = threadIdx.x; e < g.experts; e += kWaves * 64) marks[e] = 0;
     __syncthreads();
     const bool by_logit = !g.bias && (g.o.n_groups == 1 || g.o.group_top == 1);
@@ -157,32 +160,33 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(RouteArgs g) {
             if (l[j] > 3.402823466e38f) l[j] = 3.402823466e38f;
             top = fmaxf(top, l[j]);
         }
+        // the largest logit, by the keys of 32 bits that order floats
+        double l_top = 0.0;
+        if (!g.o.sigmoid) {
+            const uint32_t tb = __float_as_uint(top + 0.f), most = wave_max(tb >> 31 ? ~tb : tb | 0x80000000u);
+            l_top = __uint_as_float(most >> 31 ? most & 0x7FFFFFFFu : ~most);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[j] = g.o.sigmoid ? -(double)l[j] : (double)l[j] - l_top;
+        exp64<V>(s);
         if (g.o.sigmoid) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) s[j] = l[j] == -__builtin_huge_valf() ? 0.0 : reciprocal64(1.0 + exp64(-(double)l[j]));
+            for (int j = 0; j < V; ++j) s[j] = l[j] == -__builtin_huge_valf() ? 0.0 : reciprocal64(1.0 + s[j]);
         } else {
-            // the largest logit, by the keys of 32 bits that order floats
-            const uint32_t tb = __float_as_uint(top + 0.f), most = wave_max(tb >> 31 ? ~tb : tb | 0x80000000u);
-            const double l_top = __uint_as_float(most >> 31 ? most & 0x7FFFFFFFu : ~most);
             double sum = 0.0;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                s[j] = l[j] == -__builtin_huge_valf() ? 0.0 : exp64((double)l[j] - l_top);
+                if (l[j] == -__builtin_huge_valf()) s[j] = 0.0;
                 sum += s[j];
             }
             sum = wave_sum(sum);
-            const double by = sum > 0.0 ? sum : 1.0;
+            const double by = reciprocal64(sum > 0.0 ? sum : 1.0);       // the largest of the terms is 1
 #pragma unroll
-            for (int j = 0; j < V; ++j) s[j] = s[j] / by;
+            for (int j = 0; j < V; ++j) s[j] *= by;
         }
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const int e = lane + 64 * j;
-            double v = l[j];
-            if (!by_logit) {
-                v = s[j];
-                if (g.bias && e < g.experts) v += (double)g.bias[e];
-            }
+            const double v = by_logit ? (double)l[j] : s[j] + (double)bias[j];
             c[j] = l[j] == -__builtin_huge_valf() || !(v == v) ? kMinus : v;
         }
         if (g.o.n_groups > 1) {
@@ -216,7 +220,8 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(RouteArgs g) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const int e = lane + 64 * j;
-                if (e < g.experts && !((open >> ((e / size) << g.per_bits)) & 1)) c[j] = kMinus;
+                const int of = (int)(((float)e + 0.5f) * g.per_expert);          // e / size: far from a whole number for what e < 1024 can be
+                if (e < g.experts && !((open >> (of << g.per_bits)) & 1)) c[j] = kMinus;
             }
         }
         uint64_t key[V];
@@ -442,6 +447,7 @@ extern "C" int aser_route_experts(aser_ctx* ctx, const void* logits, int32_t x_d
     RouteArgs g{logits, ldl, bias, *opts, plan->ids, plan->weights, plan->offsets, plan->order, plan->place, plan->rows, plan->top_k, experts, nullptr, nullptr,
                 (int)ceil_div64(plan->rows, kTok)};
     while ((opts->n_groups << (g.per_bits + 1)) <= 64) ++g.per_bits;
+    g.per_expert = (float)opts->n_groups / (float)experts;
     if (g.groups > 1) {
         if (!ctx->ws || ctx->ws_bytes < need) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "route_experts: workspace too small");
         g.counts = (int32_t*)ctx->ws;
