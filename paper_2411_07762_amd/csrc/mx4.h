@@ -44,13 +44,13 @@ __device__ __forceinline__ uint32_t mx4_tiles(const MxGroups& g, int bm) {
 // Tiles of bm positions, `across` of them beside each other for other outputs, numbered matrix by matrix: the matrix that number id belongs to, its first position, the
 // number of its positions, and id's place among its tiles.  False: there is no such tile.  Every wavefront looks for itself: a lane has a matrix, and the
 // running sum of their tiles says whose the number is.
-__device__ __forceinline__ bool mx4_find(const MxGroups& g, uint32_t id, int bm, uint32_t across, int* e, int64_t* first, int* count, uint32_t* place) {
+__device__ __forceinline__ bool mx4_find(const MxGroups& g, uint64_t id, int bm, uint32_t across, int* e, int64_t* first, int* count, uint32_t* place) {
     if (!g.offsets) {
         *e = 0;
         *first = 0;
         *count = (int)g.positions;
-        *place = id;
-        return (int64_t)(id / across) * bm < g.positions;
+        *place = (uint32_t)id;
+        return (int64_t)((uint32_t)id / across) * bm < g.positions;
     }
     const int lane = threadIdx.x & 63;
     const int32_t most = (int32_t)g.positions;
@@ -70,13 +70,13 @@ __device__ __forceinline__ bool mx4_find(const MxGroups& g, uint32_t id, int bm,
             const uint32_t v = __shfl_up(upto, d);
             if (lane >= d) upto += v;
         }
-        const uint64_t over = __ballot((before + upto) * across > id);
+        const uint64_t over = __ballot((uint64_t)(before + upto) * across > id);      // offsets that make no sense can name more tiles than 32 bits count
         if (over) {
             const int at = __builtin_ctzll(over);
             *e = e0 + at;
             *first = __builtin_amdgcn_readlane(s, at);
             *count = __builtin_amdgcn_readlane(n, at);
-            *place = id - (before + (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), at)) * across;
+            *place = (uint32_t)(id - (uint64_t)(before + (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), at)) * across);
             return true;
         }
         before += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);

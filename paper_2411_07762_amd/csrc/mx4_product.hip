@@ -401,13 +401,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wa = wave >> 1, wb = wave & 1;
 
-    const uint32_t total = mx4_tiles(g.groups, BN) * out_tiles, per_xcd = (total + 7) / 8;
-    const uint32_t id = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    const uint64_t total = (uint64_t)mx4_tiles(g.groups, BN) * out_tiles, per_xcd = (total + 7) / 8;
+    const uint64_t id = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= per_xcd || id >= total) return;
     int e, count;
     int64_t first_p;
     uint32_t in;
-    mx4_find(g.groups, id, BN, out_tiles, &e, &first_p, &count, &in);
+    if (!mx4_find(g.groups, id, BN, out_tiles, &e, &first_p, &count, &in)) return;
     const uint32_t tiles = (uint32_t)(count + BN - 1) / BN, panel = in / (kPanel * out_tiles), in_panel = in - panel * kPanel * out_tiles;
     const uint32_t high = tiles - panel * kPanel < kPanel ? tiles - panel * kPanel : kPanel, across = in_panel / high;
     const int before = (int)(panel * kPanel + in_panel - across * high) * BN, rows = count - before < BN ? count - before : BN;
@@ -677,28 +677,29 @@ int launch_tile(aser_ctx* ctx, const MxArgs& g, bool gated, bool f32) {
     return f32 ? launch_tile_one<MF, NF, ST, WG, false, true>(ctx, g) : launch_tile_one<MF, NF, ST, WG, false, false>(ctx, g);
 }
 
-// Rows of the weights of a workgroup, wavefronts, words ahead.  TODO
+// Rows of the weights and of x of a workgroup, its wavefronts and words ahead, by how many workgroups there are: `tiles` of 16 nt rows, and 32 weight rows each.  Many of them fill
+// the device by themselves and read x less often with 64 weight rows; few of them have to have more in flight.  Weights not in any cache, us (the other side):
+//   one row or up to 16: 1 x 4096 x 14336 twice, gated, rank 32 (1792 workgroups) <2, 1, 4, 4> 32.0 (<2, 1, 8, 2> 33.7, <4, 1, 4, 2> 36.5); 48 rows on 64 experts, 1408 x 2048 (4096)
+//   40 (47, 44); one row, 14336 x 4096 (128) <1, 1, 8, 4> 9.4 (<2, 1, 8, 2> 9.6, <2, 1, 4, 4> 11.3)
+//   24 rows, 4096 x 14336 (448) <2, 2, ..> 8.4 (<4, 2, ..> 9.2); 256 rows on 64 experts, 2048 x 2816 (5632) <4, 2, ..> 58 (77)
+//   64 rows, 4096 x 14336 (448) <4, 4, ..> 14.4 (<2, 4, ..> 15.7); 128 rows, 4096 x 4096 (256) <2, 4, ..> 8.6 (9.5)
 int run_few(aser_ctx* ctx, const MxArgs& g, int nt, int64_t matrices, bool gated, bool f32) {
-#ifdef FEW
-    return launch_few<FEW>(ctx, g, gated, f32);
-#endif
-    const int64_t panels = matrices * ceil_div64(g.m, 16);
-    if (nt == 2) return panels >= 4096 ? launch_few<4, 2, 4, 2>(ctx, g, gated, f32) : launch_few<2, 2, 4, 2>(ctx, g, gated, f32);
-    if (nt == 3) return panels >= 4096 ? launch_few<4, 3, 4, 2>(ctx, g, gated, f32) : launch_few<2, 3, 4, 2>(ctx, g, gated, f32);
-    if (nt == 4) return panels >= 4096 ? launch_few<4, 4, 4, 2>(ctx, g, gated, f32) : launch_few<2, 4, 4, 2>(ctx, g, gated, f32);
-    if (panels >= 1024) return launch_few<2, 1, 4, 4>(ctx, g, gated, f32);
-    if (gated) return launch_few<2, 1, 8, 2>(ctx, g, gated, f32);
-    return launch_few_one<1, 1, 8, 4, false>(ctx, g, f32);
+    const int64_t tiles = ceil_div64(g.groups.positions, 16 * nt), workgroups = (matrices > tiles ? matrices : tiles) * ceil_div64(g.m, 32);
+    if (nt == 1) {
+        if (workgroups >= 512) return launch_few<2, 1, 4, 4>(ctx, g, gated, f32);
+        return gated ? launch_few_one<2, 1, 8, 2, true>(ctx, g, f32) : launch_few_one<1, 1, 8, 4, false>(ctx, g, f32);
+    }
+    if (nt == 2) return workgroups >= 2048 ? launch_few<4, 2, 4, 2>(ctx, g, gated, f32) : launch_few<2, 2, 4, 2>(ctx, g, gated, f32);
+    if (nt == 3) return workgroups >= 2048 ? launch_few<4, 3, 4, 2>(ctx, g, gated, f32) : launch_few<2, 3, 4, 2>(ctx, g, gated, f32);
+    return workgroups >= 400 ? launch_few<4, 4, 4, 2>(ctx, g, gated, f32) : launch_few<2, 4, 4, 2>(ctx, g, gated, f32);
 }
 
+// The larger tiles unless they leave a part of the device idle.  Rows x channels x outputs, us: 1024 x 4096 x 14336 (448 of them) 256 x 128 43.5, 128 x 128 47.6; 2048 x 4096 x 4096
+// (256) 29.8, 25.6; 512 x 4096 x 14336 (224) 31.2, 25.0.  256 x 256, one workgroup a compute unit, is as fast where there are many (its loop moves less, its beginning and end are not covered
+// by another workgroup) and slower where there are few; 128 x 64 is faster only where the kernel for few rows is faster still.
 int run_many(aser_ctx* ctx, const MxArgs& g, bool gated, bool f32) {
-#ifdef CFG
-    return launch_tile<CFG>(ctx, g, gated, f32);
-#endif
-    auto tiles = [&](int mf, int nf) { return g.groups.most_tiles(64 * nf) * ceil_div64(g.m, 64 * mf); };
-    if (tiles(4, 2) >= 512) return launch_tile<4, 2, 3, 2>(ctx, g, gated, f32);
-    if (tiles(2, 2) >= 256) return launch_tile<2, 2, 4, 2>(ctx, g, gated, f32);
-    return launch_tile<2, 1, 4, 2>(ctx, g, gated, f32);
+    if (g.groups.most_tiles(128) * ceil_div64(g.m, 256) >= 384) return launch_tile<4, 2, 3, 2>(ctx, g, gated, f32);
+    return launch_tile<2, 2, 4, 2>(ctx, g, gated, f32);
 }
 
 struct Plan {
@@ -714,7 +715,9 @@ Plan plan_product(int64_t positions, int64_t n, int64_t m, int32_t count, int32_
     Plan p{};
     const int64_t each = ceil_div64(positions, count < positions ? count : positions);
     p.nt = (int)(each <= 64 ? ceil_div64(each, 16) : 4);
-    p.many = each > 64 && ceil_div64(positions, 64) * ceil_div64(m, 32) > 512;
+    // Tiles begin to pay where 64 rows by 64 outputs, which is what the other kernel takes at a time, make more workgroups than the device holds at once.  us, tiles (the other
+    // kernel): 128 x 4096 x 14336 15.3 (14.1), 192: 17.3 (19.2); 512 x 4096 x 4096 12.9 (12.2), 1024: 16.6 (20.9); 256 x 14336 x 4096 40 (22)
+    p.many = each > 64 && ceil_div64(positions, 64) * ceil_div64(m, 64) > 512;
     const int64_t words = mx4_words(n), tiles = ceil_div64(positions, 16);
     int64_t parts = p.many || tiles >= 256 ? 1 : ceil_div64(256, tiles);
     if (parts > ceil_div64(words, 8)) parts = ceil_div64(words, 8);
@@ -811,10 +814,7 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
         mx4_arrange_kernel<<<(unsigned)grid, 256, 0, ctx->stream>>>(L_B, units, g.words, g.lb_frags, r, w->n, lb_vec, (uint4*)lb_room);
         ASER_TRY(aser_check_launch(ctx, "mx4_arrange_kernel"));
         g.lb = lb_room;
-#ifndef DOWN
-#define DOWN 2, 2, 4, 4
-#endif
-        ASER_TRY(f32 ? (launch_down<DOWN, 3>(ctx, g)) : (launch_down<DOWN, 2>(ctx, g)));
+        ASER_TRY(f32 ? (launch_down<2, 2, 4, 4, 3>(ctx, g)) : (launch_down<2, 2, 4, 4, 2>(ctx, g)));
         if (r != width || ((uintptr_t)L_A & 15)) {
             uint16_t* const padded = (uint16_t*)(p_room + p.p_bytes);
             ASER_TRY(pad_rows(ctx, L_A, w->rows * w->count, r, width, padded));

@@ -179,7 +179,9 @@ def expected(x, w, a, b, swiglu, dtype, r):
 
 
 SHAPES = [(1, 1, 1, 0), (1, 31, 3, 1), (1, 4096, 48, 64), (2, 33, 16, 8), (5, 128, 17, 0), (16, 160, 33, 13), (17, 512, 100, 0), (31, 640, 64, 16), (33, 1408, 130, 32),
-          (64, 500, 257, 0), (65, 2056, 40, 128), (130, 256, 300, 0), (257, 384, 512, 64), (300, 4128, 258, 24), (515, 130, 770, 100), (700, 1000, 1030, 0)]
+          (64, 500, 257, 0), (65, 2056, 40, 128), (130, 256, 300, 0), (257, 384, 512, 64), (300, 4128, 258, 24), (515, 130, 770, 100), (700, 1000, 1030, 0),
+          # by the numbers of workgroups: other fragments for few rows, both kinds of tiles
+          (2, 160, 16390, 20), (61, 130, 12850, 8), (700, 260, 4200, 33), (1000, 130, 16500, 64)]
 
 
 @pytest.mark.parametrize("swiglu", [False, True], ids=["plain", "gated"])
@@ -199,11 +201,11 @@ def test_forward(ctx, rows, n, m, r, dtype, swiglu):
         assert (full[rows:] == 7).all() and (full[:, outs:] == 7).all()
 
 
-@pytest.mark.parametrize("rows", [1, 20, 40, 300])
-def test_forward_extreme_scales_and_nan(ctx, rows):
+@pytest.mark.parametrize("rows,m", [(1, 300), (20, 300), (40, 300), (300, 300), (700, 4200)])
+def test_forward_extreme_scales_and_nan(ctx, rows, m):
     """Blocks of the smallest and largest scales; NaN blocks stay in their rows and outputs."""
     rng = np.random.default_rng(rows)
-    n, m = 256, 300
+    n = 256
     xc, wc = rng.integers(0, 16, (rows, n)).astype(np.uint8), rng.integers(0, 16, (m, n)).astype(np.uint8)
     xs, ws = rng.integers(125, 130, (rows, n // 32)).astype(np.uint8), rng.integers(125, 130, (m, n // 32)).astype(np.uint8)
     xs[0, :4], xs[0, 4:] = 0, 1                                    # tokens of 2^-127, weights of 2^100 to 2^125
@@ -319,7 +321,10 @@ def given_plan(rng, rows, k, experts, drop=0.0, skew=0.0):
 
 
 EXPERTS = [(1, 8, 2, 256, 48, 0, 0, 0), (1, 4, 4, 40, 17, 5, 0, 0), (3, 100, 6, 128, 16, 0, 0, 0), (16, 64, 6, 256, 40, 16, 0.1, 0), (40, 5, 3, 1408, 36, 0, 0, 1.0),
-           (100, 8, 2, 384, 130, 32, 0.3, 0), (300, 3, 1, 200, 260, 0, 0, 2.0), (260, 4, 2, 512, 258, 64, 0, 0), (1000, 16, 4, 128, 64, 8, 0.5, 0.3), (200, 130, 2, 160, 33, 0, 0, 0)]
+           (100, 8, 2, 384, 130, 32, 0.3, 0), (300, 3, 1, 200, 260, 0, 0, 2.0), (260, 4, 2, 512, 258, 64, 0, 0), (1000, 16, 4, 128, 64, 8, 0.5, 0.3), (200, 130, 2, 160, 33, 0, 0, 0),
+           # by the numbers of workgroups: other fragments for few rows, both kinds of tiles
+           (640, 256, 8, 128, 264, 8, 0, 0), (1280, 256, 8, 100, 264, 0, 0, 0), (1700, 256, 8, 96, 40, 16, 0, 0), (1500, 4, 2, 256, 1100, 64, 0.1, 0.5),
+           (1200, 5, 2, 130, 6200, 5, 0, 0.3)]
 
 
 @pytest.mark.parametrize("gather,swiglu", [(True, True), (False, False), (True, False)], ids=["up", "down", "gather"])
@@ -382,3 +387,132 @@ def test_combine(ctx, rows, k, m, y_type, out_type, pad, base):
     ctx.check(aser.aser_expert_combine(ctx, y, plan, out, Y0=y0))
     off = (k + 1) * 2.0 ** -24 * size
     close(out, want, off + rounding(np.abs(want) + off, out_type))
+
+
+# ------------------------------------------------------------------------------------------------ together
+class Layer:
+    """A layer of experts on fixed buffers: what a decoding server replays."""
+
+    def __init__(self, ctx, rng, rows, experts, k, n, m, r):
+        self.ctx, self.rows, self.n = ctx, rows, n
+        self.up, self.up_v = matrix(rng, 2 * m, n, count=experts)
+        self.down, self.down_v = matrix(rng, n, m, count=experts)
+        self.a, self.b, self.av, self.bv = factors(rng, 2 * m, n, r, experts)
+        self.router = dev(rng.standard_normal((n, experts)) * 0.05, torch.float32)
+        self.x = torch.zeros(rows, n, dtype=torch.bfloat16, device=DEV)
+        self.logits = torch.zeros(rows, experts, device=DEV)
+        self.plan = aser.ExpertPlan.empty(rows, k, experts)
+        self.xq, self.hq = aser.Mx4.empty(rows, n), aser.Mx4.empty(rows * k, m)
+        self.h = torch.zeros(rows * k, m, dtype=torch.bfloat16, device=DEV)
+        self.y = torch.zeros(rows * k, n, dtype=torch.bfloat16, device=DEV)
+        self.out = torch.zeros(rows, n, dtype=torch.bfloat16, device=DEV)
+        for need in (aser.aser_route_workspace_bytes(rows, experts, k), aser.aser_expert_forward_workspace_bytes(rows * k, n, 2 * m, experts, r),
+                     aser.aser_expert_forward_workspace_bytes(rows * k, m, n, experts, 0)):
+            ctx.ensure_workspace(need)
+
+    def step(self):
+        c = self.ctx
+        c.check(aser.aser_route_experts(c, self.logits, self.plan, sigmoid=True))
+        c.check(aser.aser_mx4_quantize(c, self.x, self.xq))
+        c.check(aser.aser_expert_forward(c, self.xq, self.up, self.plan, self.h, gather=True, swiglu=True, L_A=self.a, L_B=self.b))
+        c.check(aser.aser_mx4_quantize(c, self.h, self.hq))
+        c.check(aser.aser_expert_forward(c, self.hq, self.down, self.plan, self.y, gather=False))
+        c.check(aser.aser_expert_combine(c, self.y, self.plan, self.out))
+
+    def give(self, rng):
+        x = dev(rng.standard_normal((self.rows, self.n)), torch.bfloat16)
+        self.x.copy_(x)
+        self.logits.copy_(x.float() @ self.router)
+        self.logits[self.rows // 2, 1:] = float("-inf")                          # one row has one expert only
+        return x
+
+
+@pytest.mark.parametrize("rows,experts,k,n,m,r", [(3, 8, 2, 256, 96, 16), (40, 6, 3, 384, 200, 32), (900, 4, 2, 256, 2100, 32)])
+def test_layer_replayed_on_another_stream(rows, experts, k, n, m, r):
+    """A captured layer gives the eager results' bits on every replay, with other inputs, eager work and other streams' work between them."""
+    rng = np.random.default_rng(rows)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        layer = Layer(aser.Context(0, side.cuda_stream), rng, rows, experts, k, n, m, r)
+        eager = Layer(aser.Context(0, side.cuda_stream), np.random.default_rng(rows), rows, experts, k, n, m, r)
+        layer.give(rng)
+        layer.step()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            layer.step()
+        other = aser.Context(0, torch.cuda.current_stream().cuda_stream)
+        for rep in range(4):
+            seed = 100 * rows + rep
+            layer.give(np.random.default_rng(seed))
+            eager.give(np.random.default_rng(seed))
+            graph.replay()
+            eager.step()
+            side.synchronize()
+            assert torch.equal(layer.out, eager.out) and torch.equal(layer.plan.order, eager.plan.order)
+            used = int(layer.plan.offsets[-1])
+            assert torch.equal(layer.h[:used], eager.h[:used]) and used == rows * k - (k - 1)
+            quantized(other, layer.x)
+    assert layer.out.isfinite().all() and layer.out.abs().max() > 0
+
+
+def test_two_contexts_at_once():
+    """Two layers on streams of their own, enqueued without a wait between them, have the results that each has alone."""
+    sizes = [(33, 8, 2, 256, 128, 16), (700, 4, 2, 128, 1500, 8)]
+    streams = [torch.cuda.Stream() for _ in sizes]
+    layers = []
+    for i, (s, size) in enumerate(zip(streams, sizes)):
+        with torch.cuda.stream(s):
+            layers.append(Layer(aser.Context(0, s.cuda_stream), np.random.default_rng(i), *size))
+            layers[-1].give(np.random.default_rng(i + 10))
+    alone = []
+    for layer in layers:
+        torch.cuda.synchronize()
+        layer.step()
+        torch.cuda.synchronize()
+        alone.append(layer.out.clone())
+    for layer in layers:
+        layer.out.zero_()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for layer in layers:
+            layer.step()
+    torch.cuda.synchronize()
+    for layer, want in zip(layers, alone):
+        assert torch.equal(layer.out, want)
+
+
+def test_calibrated_layer_in_four_bits():
+    """The quantizer between aser_smoothed_weight and aser_quant_target, then the compensated layer on its codes: with the factors the layer's outputs are nearer to
+    the weight's own than without, and as near as the oracle's product of the same codes and factors is."""
+    from gpu_util import new_ctx
+    ctx, rng = new_ctx(), np.random.default_rng(7)
+    m, n, r, f, tokens = 320, 512, 32, 8, 2048
+    W = dev(rng.standard_normal((m, n)) * 0.02, torch.float32)
+    x = rng.standard_normal((tokens, n))
+    x[:, rng.permutation(n)[:8]] *= 30.0
+    X = dev(x, torch.bfloat16)
+    buf = aser.LayerBuffers(m, n, r, f, 4, False)
+    ctx.ensure_workspace(aser.aser_workspace_bytes(m, n, r))
+    ctx.check(aser.aser_gram_accumulate(ctx, X, buf.G, buf.abs_sum, buf.count))
+    ctx.check(aser.aser_smooth_outliers(ctx, W, buf.abs_sum, buf.count, f, buf.idx, buf.mdiag))
+    Wq, w = torch.empty_like(W), aser.Mx4.empty(m, n)
+    ctx.check(aser.aser_smoothed_weight(ctx, W, buf.idx, f, Wq))
+    ctx.check(aser.aser_mx4_quantize(ctx, Wq, w, values=Wq))
+    ctx.check(aser.aser_quant_target(ctx, W, buf.mdiag, Wq, buf.T))
+    st, info = aser.aser_whiten(ctx, buf.G, buf.mdiag, 0.0, buf.S)
+    ctx.check(st)
+    st, err, _ = aser.aser_error_reconstruct(ctx, buf.T, buf.S, r, buf.L_A, buf.L_B, buf.sigma, idx=buf.idx, f=f)
+    ctx.check(st)
+    assert info == 0
+    L_A, L_B = buf.L_A.to(torch.bfloat16), buf.L_B.to(torch.bfloat16)
+    ctx.ensure_workspace(aser.aser_mx4_forward_workspace_bytes(200, n, m, r))
+    xq, values, y, bare = aser.Mx4.empty(200, n), torch.empty(200, n, dtype=torch.bfloat16, device=DEV), torch.empty(200, m, device=DEV), torch.empty(200, m, device=DEV)
+    ctx.check(aser.aser_mx4_quantize(ctx, X[:200], xq, mdiag=buf.mdiag, values=values))
+    ctx.check(aser.aser_mx4_forward(ctx, xq, w, y, L_A=L_A, L_B=L_B))
+    ctx.check(aser.aser_mx4_forward(ctx, xq, w, bare))
+    f64 = lambda t: t.double().cpu().numpy()                                     # noqa: E731
+    close(y, *expected(f64(values), f64(Wq), f64(L_A), f64(L_B), False, torch.float32, r))
+    # the same tokens through the weight: smoothing moves the outlier channels' share from the codes to the factors
+    want = f64(values) * f64(buf.mdiag) @ f64(W).T
+    assert np.linalg.norm(f64(y) - want) < 0.5 * np.linalg.norm(f64(bare) - want)
