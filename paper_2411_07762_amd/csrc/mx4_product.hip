@@ -694,12 +694,17 @@ int run_few(aser_ctx* ctx, const MxArgs& g, int nt, int64_t matrices, bool gated
     return workgroups >= 400 ? launch_few<4, 4, 4, 2>(ctx, g, gated, f32) : launch_few<2, 4, 4, 2>(ctx, g, gated, f32);
 }
 
-// The larger tiles unless they leave a part of the device idle.  Rows x channels x outputs, us: 1024 x 4096 x 14336 (448 of them) 256 x 128 43.5, 128 x 128 47.6; 2048 x 4096 x 4096
-// (256) 29.8, 25.6; 512 x 4096 x 14336 (224) 31.2, 25.0.  256 x 256, one workgroup a compute unit, is as fast where there are many (its loop moves less, its beginning and end are not covered
-// by another workgroup) and slower where there are few; 128 x 64 is faster only where the kernel for few rows is faster still.
+// Tiles of 128 x 128 where there are not enough larger ones.  Rows x channels x outputs, us: 2048 x 4096 x 4096 (256 of 256 x 128) 25.6, larger 29.8; 512 x 4096 x 14336 (224) 25.0, 31.2;
+// 1024 x 4096 x 14336 (448) 47.6, 43.5.  128 x 64 is faster only where the kernel for few rows is faster still.
+// 256 outputs x 256 positions, one workgroup a compute unit, move less for each product than 256 x 128, two of them, whose beginnings and ends cover each other: a word of the channels takes a
+// round of 256 of them 0.88 us, beside 8.5 at its ends, and a round of 512 of the others 1.05 and 6 (4096 rows and 16384 outputs of 1024 to 8192 channels: 60.5 to 256 us against
+// 55.9 to 286).  Which takes fewer such rounds' time decides: 4099 x 4096 x 14336 149 against 160, 1501 rows on 8 experts (375 each) 326 against 301.
 int run_many(aser_ctx* ctx, const MxArgs& g, bool gated, bool f32) {
-    if (g.groups.most_tiles(128) * ceil_div64(g.m, 256) >= 384) return launch_tile<4, 2, 3, 2>(ctx, g, gated, f32);
-    return launch_tile<2, 2, 4, 2>(ctx, g, gated, f32);
+    const int64_t across = ceil_div64(g.m, 256), tiles = g.groups.most_tiles(128) * across;
+    if (tiles < 384) return launch_tile<2, 2, 4, 2>(ctx, g, gated, f32);
+    const int steps = g.words + g.lr_steps;
+    const double large = (double)ceil_div64(g.groups.most_tiles(256) * across, 256) * (0.88 * steps + 8.5), small = (double)ceil_div64(tiles, 512) * (1.05 * steps + 6.0);
+    return large < small ? launch_tile<4, 4, 3, 1>(ctx, g, gated, f32) : launch_tile<4, 2, 3, 2>(ctx, g, gated, f32);
 }
 
 struct Plan {

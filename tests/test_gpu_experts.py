@@ -201,6 +201,37 @@ def test_forward(ctx, rows, n, m, r, dtype, swiglu):
         assert (full[rows:] == 7).all() and (full[:, outs:] == 7).all()
 
 
+@pytest.mark.parametrize("swiglu", [False, True], ids=["plain", "gated"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows,n,m,r", [(2050, 2100, 6210, 0), (1930, 2176, 6660, 40)])
+def test_forward_largest_tiles(ctx, rows, n, m, r, dtype, swiglu):
+    """Sizes that take tiles of 256 x 256; random codes, the products of the reference on the device, in 64 bits."""
+    rng = np.random.default_rng(rows)
+    outs, m = m, 2 * m if swiglu else m
+    made = []
+    for count in (rows, m):
+        codes, scales = rng.integers(0, 16, (count, orc.width(n))).astype(np.uint8), rng.integers(124, 128, (count, orc.width(n) // 32)).astype(np.uint8)
+        codes[:, n:] = 0
+        made.append((aser.Mx4(*(dev(a) for a in orc.pack(codes, scales)), n), dev(orc.values(codes, scales)[:, :n])))
+    (x, xv), (w, wv) = made
+    a, b, *_ = factors(rng, m, n, r) if r else (None, None)
+    z, size = xv @ wv.t(), xv.abs() @ wv.abs().t()
+    if r:
+        z += (xv @ b.double().t()) @ a.double().t()
+        size += (xv.abs() @ b.double().abs().t()) @ a.double().abs().t()
+    off = sums_off(n, r) * size
+    if swiglu:
+        g, u = z[:, :outs], z[:, outs:]
+        silu = g * torch.sigmoid(g)
+        off = 1.1 * off[:, :outs] * (u.abs() + off[:, outs:]) + silu.abs() * off[:, outs:] + (silu * u).abs() * 16 * 2.0 ** -24
+        z = silu * u
+    off += (z.abs() + off) * (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24)
+    ctx.ensure_workspace(aser.aser_mx4_forward_workspace_bytes(rows, n, m, r))
+    y = torch.full((rows, outs), 7.0, dtype=dtype, device=DEV)
+    ctx.check(aser.aser_mx4_forward(ctx, x, w, y, L_A=a, L_B=b, swiglu=swiglu))
+    assert ((y.double() - z).abs() <= off).all()
+
+
 @pytest.mark.parametrize("rows,m", [(1, 300), (20, 300), (40, 300), (300, 300), (700, 4200)])
 def test_forward_extreme_scales_and_nan(ctx, rows, m):
     """Blocks of the smallest and largest scales; NaN blocks stay in their rows and outputs."""
