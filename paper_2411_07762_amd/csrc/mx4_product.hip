@@ -26,7 +26,6 @@ struct MxArgs {
     int words;
     const uint16_t* la; const uint16_t* lb; int r;
     int64_t la_ld, lb_ld;                                   // their rows: r and n, or what they are padded to
-    int lb_frags;                                           // many rows: L_B is arranged, with so many times 16 ranks
     float* P; int parts, part_words, rp;                    // few rows: [part][position][rp] fp32, rp: r rounded up to 16
     uint16_t* planes; int lr_steps;                         // many rows: [term][position][32 lr_steps / terms] bf16; steps of 32 ranks and one term
     void* Y; int64_t ldy; int64_t outs;                     // columns of Y
@@ -67,14 +66,14 @@ __device__ __forceinline__ void store4(const MxArgs& g, int64_t p, int64_t o, co
 // ---------------------------------------------------------------------------------------------------------------- P = x L_B^T
 // 16 NT positions and 16 RF ranks a workgroup; W wavefronts share a part of the channels, a word at a time with the loads of U words in flight.  Ranks are in the
 // rows of the accumulator; tokens become bf16 on the way, exactly.
-// TERMS = 0, few rows: fp32 sums of the part.  L_B is read as it is: of each of a word's four blocks lane group q = lane / 16 has channels 8 q .. + 7.
-// Otherwise the sum (of one part) as so many bf16 terms, each what the ones before leave, rounded; and lane group q has block q, of L_B in the order
-// of the lanes (mx4_arrange_kernel).  Lanes next to each other have different rows, and a load of 16 bytes from 64 places occupies a compute unit's address unit
-// for 64 cycles where one from a kilobyte in a row takes 16: with L_B as it is 4099 tokens of 4096 channels, 64 ranks take 25 us.
+// TERMS = 0, few rows: fp32 sums of the part.  L_B goes into the registers as it is: of each of a word's four blocks lane group q = lane / 16 has channels 8 q .. + 7.
+// Otherwise the sum (of one part) as so many bf16 terms, each what the ones before leave, rounded; lane group q has block q, and L_B is turned through LDS: lanes next to each
+// other in the matrix instruction have different rows, and a load of 16 bytes from 64 places occupies a compute unit's address unit for 64 cycles where one of four rows'
+// 256 bytes takes 16.  Without that 4099 tokens of 4096 channels and 64 ranks take 25 us; with L_B put in order by a launch of its own 10 and 4.7.
 template <int RF, int NT, int W, int U, int TERMS>
 __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_tiles) {
-    extern __shared__ __align__(16) float part[];            // [wavefront][fragment][lane][4]
-    constexpr bool ARRANGED = TERMS > 0;
+    extern __shared__ __align__(16) float part[];            // the wavefronts' rows of L_B, then the sums, [wavefront][fragment][lane][4]
+    constexpr bool TURNED = TERMS > 0;
     const int lane = threadIdx.x & 63, li = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rt = blockIdx.x % rank_tiles, rest = blockIdx.x / rank_tiles, pt = rest % g.parts;
@@ -88,16 +87,19 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
         xat[t] = mx4_at(row, g.words);
         xcode[t] = mx4_code(row, g.words) * 16;
     }
-    const uint16_t* lrow[RF];
-    const uint4* const arranged = (const uint4*)g.lb + ((int64_t)e * g.words * g.lb_frags + rt * RF) * 256 + lane;
+    const uint16_t* lrow[TURNED ? 4 * RF : RF];              // ranks that are not there: the last one again, and what becomes of them is not kept
     f32x4_t acc[RF][NT];
 #pragma unroll
     for (int f = 0; f < RF; ++f) {
-        const int k = 16 * (rt * RF + f) + li;
-        lrow[f] = g.lb + ((int64_t)e * g.r + (k < g.r ? k : g.r - 1)) * g.lb_ld;
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[f][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < (TURNED ? 4 : 1); ++j) {         // turned: load 4 f + j has four rows, a lane a sixteenth of one's word
+            const int k = 16 * (rt * RF + f) + (TURNED ? 4 * j + q : li);
+            lrow[TURNED ? 4 * f + j : f] = g.lb + ((int64_t)e * g.r + (k < g.r ? k : g.r - 1)) * g.lb_ld;
+        }
     }
+    char* const turn = (char*)part + wave * (RF * 16 * 256);
     const int first = pt * g.part_words, last = first + g.part_words < g.words ? first + g.part_words : g.words;
     v4i_t codes[U][NT];
     uint32_t scale[U][NT];
@@ -106,27 +108,39 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const uint8_t* const code = g.xc + xcode[t] + (int64_t)w * 1024;
-            if (ARRANGED) codes[u][t] = *(const v4i_t*)(code + 256 * q);
+            if (TURNED) codes[u][t] = *(const v4i_t*)(code + 256 * q);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (!ARRANGED) codes[u][t][j] = *(const int*)(code + 256 * j + 4 * q);
+                if (!TURNED) codes[u][t][j] = *(const int*)(code + 256 * j + 4 * q);
             scale[u][t] = g.xs[xat[t] + (int64_t)w * kMxNext];
         }
-        const int64_t c0 = (int64_t)w * kMxWord + 8 * q;
-        // Behind the last channel the last ones are read again, against zeros of x; ranks that are not there read the last row, and what becomes of them is not kept.
+        // behind the last channel the last ones are read again, against zeros of x
+        const int64_t c0 = (int64_t)w * kMxWord + 8 * (TURNED ? li : q);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int64_t c = c0 + 32 * j < g.lb_ld ? c0 + 32 * j : g.lb_ld - 8;
+            const int64_t at = c0 + (TURNED ? 0 : 32 * j), c = at < g.lb_ld ? at : g.lb_ld - 8;
 #pragma unroll
-            for (int f = 0; f < RF; ++f) a[u][f][j] = ARRANGED ? arranged[(int64_t)w * g.lb_frags * 256 + (f * 4 + j) * 64] : *(const uint4*)(lrow[f] + c);
+            for (int f = 0; f < RF; ++f) a[u][f][j] = *(const uint4*)(lrow[TURNED ? 4 * f + j : f] + c);
         }
     };
     auto multiply = [&](int u) {
+        if (TURNED) {                                        // the sixteenths of a row change places by the row: neither writes nor reads meet on a bank
+#pragma unroll
+            for (int f = 0; f < RF; ++f)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) *(uint4*)(turn + (16 * f + 4 * j + q) * 256 + ((li ^ (4 * j + q)) << 4)) = a[u][f][j];
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int f = 0; f < RF; ++f)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) a[u][f][j] = *(const uint4*)(turn + (16 * f + li) * 256 + (((4 * q + j) ^ li) << 4));
+            __builtin_amdgcn_wave_barrier();
+        }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float by = __uint_as_float(((scale[u][t] >> (8 * (ARRANGED ? q : j))) & 255u) << 23);      // the conversion takes the exponent field for a scale byte
+                const float by = __uint_as_float(((scale[u][t] >> (8 * (TURNED ? q : j))) & 255u) << 23);      // the conversion takes the exponent field for a scale byte
                 const uint32_t w4 = (uint32_t)codes[u][t][j];
                 const bf16x2_t v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 1),
                                v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 3);
@@ -148,6 +162,7 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
         }
     }
     f32x4_t* const mine = (f32x4_t*)part + lane;
+    if (TURNED) __syncthreads();
 #pragma unroll
     for (int f = 0; f < RF; ++f)
 #pragma unroll
@@ -178,37 +193,18 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
     }
 }
 
-// L_B in the order in which a wavefront with ARRANGED above takes it: [matrix][word][16 ranks][eighths of a block][lane][8 channels], zeros where there is no rank or no channel.
-__global__ __launch_bounds__(256) void mx4_arrange_kernel(const uint16_t* __restrict__ lb, int64_t units, int words, int frags, int r, int64_t n, bool vec, uint4* __restrict__ out) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= units) return;
-    const int lane = (int)(i & 63), j = (int)(i >> 6) & 3;
-    const int64_t piece = i >> 8, ew = piece / frags, e = ew / words;
-    const int k = (int)(piece - ew * frags) * 16 + (lane & 15);
-    const int64_t c = (ew - e * words) * kMxWord + 32 * (lane >> 4) + 8 * j;
-    const uint16_t* const src = lb + (e * r + k) * n + c;
-    uint32_t v[8];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) v[u] = 0u;
-    if (k < r && vec && c < n) {                             // rows on 16-byte boundaries, n a multiple of 8
-        out[i] = *(const uint4*)src;
-        return;
-    }
-#pragma unroll
-    for (int u = 0; u < 8; ++u)
-        if (k < r && c + u < n) v[u] = src[u];
-    out[i] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
-}
-
 // The tokens of the positions in their order, so that tiles read them as they read any matrix: on their own, 16 bytes of a row here and there would take
-// the address unit four times as long.  A workgroup has a panel, its threads the rows' blocks and words of scales.
+// the address unit four times as long.  A workgroup has a part of a panel, its threads the rows' blocks and words of scales.
+constexpr int kGatherWords = 8;
 __global__ __launch_bounds__(256) void mx4_gather_kernel(MxGroups groups, const uint8_t* __restrict__ xc, const uint32_t* __restrict__ xs, int words, uint8_t* __restrict__ oc, uint32_t* __restrict__ os) {
     const int li = threadIdx.x & 15;
     const int64_t p = (int64_t)blockIdx.x * 16 + li, row = mx4_row(groups, p < groups.positions ? p : groups.positions - 1);
     const uint4* const from = (const uint4*)xc + mx4_code(row, words);
     uint4* const to = (uint4*)oc + (int64_t)blockIdx.x * words * 64 + li;
-    for (int i = threadIdx.x >> 4; i < 4 * words; i += 16) to[16 * i] = from[16 * i];
-    for (int i = threadIdx.x >> 4; i < words; i += 16) os[((int64_t)blockIdx.x * words + i) * 16 + li] = xs[mx4_at(row, words) + (int64_t)i * kMxNext];
+    const int first = blockIdx.y * kGatherWords, last = first + kGatherWords < words ? first + kGatherWords : words;
+    for (int i = 4 * first + (threadIdx.x >> 4); i < 4 * last; i += 16) to[16 * i] = from[16 * i];
+    const int w = first + (threadIdx.x >> 4);
+    if (w < last) os[((int64_t)blockIdx.x * words + w) * 16 + li] = xs[mx4_at(row, words) + (int64_t)w * kMxNext];
 }
 
 // A factor with its rows of r padded with zeros, where it cannot be read in pieces of 16 bytes as it is (L_B), or not in pieces of 64 (L_A of many rows).
@@ -712,11 +708,11 @@ struct Plan {
     bool many;               // tiles through LDS instead
     int parts, part_words;   // few rows: of the channels, for P
     size_t x_bytes;                          // many rows of experts: their codes and scales in order
-    size_t p_bytes, la_bytes, lb_bytes;      // P, and the factors as the kernels want them
+    size_t p_bytes, la_bytes, lb_bytes;      // P, and the factors should they have to be padded
     size_t all() const { return x_bytes + p_bytes + la_bytes + lb_bytes; }
 };
 
-Plan plan_product(int64_t positions, int64_t n, int64_t m, int32_t count, int32_t r) {
+Plan plan_product(int64_t positions, int64_t n, int64_t m, int32_t count, int32_t r, bool experts) {
     Plan p{};
     const int64_t each = ceil_div64(positions, count < positions ? count : positions);
     p.nt = (int)(each <= 64 ? ceil_div64(each, 16) : 4);
@@ -729,15 +725,14 @@ Plan plan_product(int64_t positions, int64_t n, int64_t m, int32_t count, int32_
     if (parts > kMostParts) parts = kMostParts;
     p.part_words = (int)ceil_div64(words, parts);
     p.parts = (int)ceil_div64(words, p.part_words);
-    if (p.many && count > 1) p.x_bytes = align_up((size_t)mx4_size(positions, words) * 68, 256);
+    if (p.many && experts) p.x_bytes = align_up((size_t)mx4_size(positions, words) * 68, 256);
     if (r <= 0) return p;
+    p.lb_bytes = align_up((size_t)count * r * align_up(n, 8) * 2, 256);
     if (p.many) {
         p.p_bytes = align_up((size_t)positions * align_up(r, 32) * 2 * 3, 256);
         p.la_bytes = align_up((size_t)count * m * align_up(r, 32) * 2, 256);
-        p.lb_bytes = align_up((size_t)count * words * kMxWord * align_up(r, 32) * 2, 256);
     } else {
         p.p_bytes = align_up((size_t)p.parts * positions * align_up(r, 16) * 4, 256);
-        p.lb_bytes = align_up((size_t)count * r * align_up(n, 8) * 2, 256);
     }
     return p;
 }
@@ -754,7 +749,7 @@ int launch_down(aser_ctx* ctx, const MxArgs& g) {
     const int rank_tiles = (int)ceil_div64(TERMS ? g.lr_steps / (TERMS ? TERMS : 1) * 32 : g.rp, 16 * RF);
     const int64_t grid = g.groups.most_tiles(16 * NT) * g.parts * rank_tiles;
     if (grid > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: too many rows");
-    mx4_down_kernel<RF, NT, W, U, TERMS><<<(unsigned)grid, 64 * W, (size_t)W * RF * NT * 1024, ctx->stream>>>(g, rank_tiles);
+    mx4_down_kernel<RF, NT, W, U, TERMS><<<(unsigned)grid, 64 * W, (size_t)W * RF * 1024 * (TERMS && NT < 4 ? 4 : NT), ctx->stream>>>(g, rank_tiles);
     return aser_check_launch(ctx, "mx4_down_kernel");
 }
 
@@ -771,7 +766,7 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
     if (((uintptr_t)Y & (f32 ? 3 : 1)) || (((uintptr_t)L_A | (uintptr_t)L_B) & 1)) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "%s: misaligned pointer", who);
     if (groups.positions == 0) return ASER_OK;
     if (!Y) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "%s: null pointer", who);
-    const Plan p = plan_product(groups.positions, w->n, w->rows, w->count, r);
+    const Plan p = plan_product(groups.positions, w->n, w->rows, w->count, r, groups.offsets != nullptr);
     if (p.all() > 0 && (!ctx->ws || ctx->ws_bytes < p.all() + kAserWsTail)) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "%s: workspace too small", who);
     MxArgs g{};
     g.groups = groups;
@@ -785,17 +780,16 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
     g.vec = !((uintptr_t)Y & (unit - 1)) && !(ldy * size & (unit - 1));
     g.la_four = !((uintptr_t)L_A & 7) && !(r & 3);
     ASER_TRY(aser_prepare_device(ctx));
-    const bool lb_vec = !((uintptr_t)L_B & 15) && !(w->n & 7);
     char* const p_room = (char*)ctx->ws + p.x_bytes;
-    uint16_t* const lb_room = (uint16_t*)(p_room + p.p_bytes + p.la_bytes);
+    if (r > 0 && (((uintptr_t)L_B & 15) || (w->n & 7))) {
+        uint16_t* const padded = (uint16_t*)(p_room + p.p_bytes + p.la_bytes);
+        g.lb_ld = align_up(w->n, 8);
+        ASER_TRY(pad_rows(ctx, L_B, (int64_t)w->count * r, w->n, g.lb_ld, padded));
+        g.lb = padded;
+    }
     if (!p.many) {
         if (r > 0) {
             g.P = (float*)p_room;
-            if (!lb_vec) {
-                g.lb_ld = align_up(w->n, 8);
-                ASER_TRY(pad_rows(ctx, L_B, (int64_t)w->count * r, w->n, g.lb_ld, lb_room));
-                g.lb = lb_room;
-            }
             ASER_TRY((launch_down<1, 1, 4, 2, 0>(ctx, g)));
         }
         return run_few(ctx, g, p.nt, w->count < groups.positions ? w->count : groups.positions, swiglu, f32);
@@ -803,7 +797,7 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
     if (groups.order) {
         uint8_t* const codes = (uint8_t*)ctx->ws;
         uint32_t* const scales = (uint32_t*)(codes + mx4_size(groups.positions, g.words) * 64);
-        mx4_gather_kernel<<<(unsigned)ceil_div64(groups.positions, 16), 256, 0, ctx->stream>>>(groups, g.xc, g.xs, g.words, codes, scales);
+        mx4_gather_kernel<<<dim3((unsigned)ceil_div64(groups.positions, 16), (unsigned)ceil_div64(g.words, kGatherWords)), 256, 0, ctx->stream>>>(groups, g.xc, g.xs, g.words, codes, scales);
         ASER_TRY(aser_check_launch(ctx, "mx4_gather_kernel"));
         g.xc = codes;
         g.xs = scales;
@@ -813,12 +807,6 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
         const int terms = f32 ? 3 : 2, width = (int)align_up(r, 32);
         g.planes = (uint16_t*)p_room;
         g.lr_steps = width / 32 * terms;
-        g.lb_frags = width / 16;
-        const int64_t units = (int64_t)w->count * g.words * g.lb_frags * 256, grid = ceil_div64(units, 256);
-        if (grid > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "%s: the factors are too large", who);
-        mx4_arrange_kernel<<<(unsigned)grid, 256, 0, ctx->stream>>>(L_B, units, g.words, g.lb_frags, r, w->n, lb_vec, (uint4*)lb_room);
-        ASER_TRY(aser_check_launch(ctx, "mx4_arrange_kernel"));
-        g.lb = lb_room;
         ASER_TRY(f32 ? (launch_down<2, 2, 4, 4, 3>(ctx, g)) : (launch_down<2, 2, 4, 4, 2>(ctx, g)));
         if (r != width || ((uintptr_t)L_A & 15)) {
             uint16_t* const padded = (uint16_t*)(p_room + p.p_bytes);
@@ -833,7 +821,8 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
 }  // namespace
 
 extern "C" size_t aser_mx4_forward_workspace_bytes(int64_t rows, int64_t n, int64_t m, int32_t r) {
-    return aser_expert_forward_workspace_bytes(rows, n, m, 1, r);
+    if (rows <= 0 || n <= 0 || m <= 0) return kAserWsTail;
+    return plan_product(rows, n, m, 1, r, false).all() + kAserWsTail;
 }
 
 extern "C" int aser_mx4_forward(aser_ctx* ctx, const aser_mx4* x, const aser_mx4* w, const uint16_t* L_A, const uint16_t* L_B, int32_t r, int32_t swiglu, void* Y,
@@ -847,8 +836,7 @@ extern "C" int aser_mx4_forward(aser_ctx* ctx, const aser_mx4* x, const aser_mx4
 
 extern "C" size_t aser_expert_forward_workspace_bytes(int64_t positions, int64_t n, int64_t m, int32_t n_experts, int32_t r) {
     if (positions <= 0 || n <= 0 || m <= 0 || n_experts <= 0) return kAserWsTail;
-    const Plan p = plan_product(positions, n, m, n_experts, r);
-    return p.all() + kAserWsTail;
+    return plan_product(positions, n, m, n_experts, r, true).all() + kAserWsTail;
 }
 
 extern "C" int aser_expert_forward(aser_ctx* ctx, const aser_mx4* x, const aser_mx4* w, const aser_expert_plan* plan, int32_t gather, const uint16_t* L_A,

@@ -127,7 +127,9 @@ def test_workspace_sizes():
     assert tail == 256 and lib.aser_route_workspace_bytes(32, 64, 4) == tail and lib.aser_expert_forward_workspace_bytes(0, 256, 64, 4, 8) == tail
     assert lib.aser_mx4_forward_workspace_bytes(100, 256, 64, 8) > tail and lib.aser_route_workspace_bytes(33, 64, 4) >= tail + 2 * 64 * 4
     # many rows of experts are put in order: a place for each position
-    assert lib.aser_expert_forward_workspace_bytes(100000, 256, 4096, 8, 0) >= tail + 100000 * 2 * 68
+    for experts in (8, 1):
+        assert lib.aser_expert_forward_workspace_bytes(100000, 256, 4096, experts, 0) >= tail + 100000 * 2 * 68
+    assert lib.aser_mx4_forward_workspace_bytes(100000, 256, 4096, 0) == tail
 
 
 # ------------------------------------------------------------------------------------------------ what the binding refuses

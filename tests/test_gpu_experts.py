@@ -355,7 +355,7 @@ EXPERTS = [(1, 8, 2, 256, 48, 0, 0, 0), (1, 4, 4, 40, 17, 5, 0, 0), (3, 100, 6, 
            (100, 8, 2, 384, 130, 32, 0.3, 0), (300, 3, 1, 200, 260, 0, 0, 2.0), (260, 4, 2, 512, 258, 64, 0, 0), (1000, 16, 4, 128, 64, 8, 0.5, 0.3), (200, 130, 2, 160, 33, 0, 0, 0),
            # by the numbers of workgroups: other fragments for few rows, both kinds of tiles
            (640, 256, 8, 128, 264, 8, 0, 0), (1280, 256, 8, 100, 264, 0, 0, 0), (1700, 256, 8, 96, 40, 16, 0, 0), (1500, 4, 2, 256, 1100, 64, 0.1, 0.5),
-           (1200, 5, 2, 130, 6200, 5, 0, 0.3)]
+           (1200, 5, 2, 130, 6200, 5, 0, 0.3), (700, 1, 1, 256, 4200, 32, 0.2, 0), (30, 1, 1, 130, 50, 0, 0, 0)]
 
 
 @pytest.mark.parametrize("gather,swiglu", [(True, True), (False, False), (True, False)], ids=["up", "down", "gather"])
