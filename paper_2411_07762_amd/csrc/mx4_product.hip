@@ -59,7 +59,7 @@ __device__ __forceinline__ void store4(const MxArgs& g, int64_t p, int64_t o, co
     for (int i = 0; i < 4; ++i) {
         if (o + i >= g.outs) continue;
         if (F32) ((float*)g.Y)[at + i] = y[i];
-        else ((uint16_t*)g.Y)[at + i] = (uint16_t)bf16_rne(y[i]);
+        else ((uint16_t*)g.Y)[at + i] = (uint16_t)bf16_pair(y[i], y[i]);
     }
 }
 

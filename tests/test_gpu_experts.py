@@ -260,6 +260,10 @@ def test_forward_extreme_scales_and_nan(ctx, rows, m):
         got = y.double().cpu().numpy()
         assert (np.isnan(got) == np.isnan(z))[top | np.isnan(z)].all()
         tiny = 2.0 ** -126                                         # sums below the normal numbers may be flushed
+        for pad in (0, 3):                                         # the same places are NaN in 16 bits, whatever the rows' alignment
+            half = strided(torch.zeros(rows, m, dtype=torch.bfloat16, device=DEV), pad)
+            ctx.check(aser.aser_mx4_forward(ctx, x, w, half, L_A=fa, L_B=None if fa is None else b))
+            assert torch.equal(half.isnan(), y.isnan())
         ok = np.abs(got - z) <= (sums_off(n, r) + 2.0 ** -24) * size + tiny * (1 + (np.abs(av).sum(1) if fa is not None else 0))
         assert (ok | np.isnan(z) | ~top).all(), np.argwhere(~(ok | np.isnan(z) | ~top))[:5]
 
