@@ -13,7 +13,6 @@ namespace {
 
 typedef int v4i_t __attribute__((ext_vector_type(4)));
 typedef int v8i_t __attribute__((ext_vector_type(8)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -226,7 +225,7 @@ __global__ __launch_bounds__(256) void mx4_pad_kernel(const uint16_t* __restrict
 constexpr int kMostParts = 4;                                // of the channels, for P of few rows
 
 template <int FA, int NT, int W, int U, bool GATED, bool F32>
-__global__ __launch_bounds__(64 * W, FA * NT <= 4 ? 4 : FA * NT <= 8 ? 3 : 2) void mx4_few_kernel(MxArgs g) {
+__global__ __launch_bounds__(64 * W, FA * NT <= 2 ? 5 : FA * NT <= 4 ? 4 : FA * NT <= 8 ? 3 : 2) void mx4_few_kernel(MxArgs g) {
     extern __shared__ __align__(16) float part[];            // [wavefront][fragment][lane][4]
     constexpr int OF = GATED ? FA / 2 : FA;                  // fragments of outputs
     const int lane = threadIdx.x & 63, li = lane & 15, q = lane >> 4;
@@ -273,30 +272,28 @@ __global__ __launch_bounds__(64 * W, FA * NT <= 4 ? 4 : FA * NT <= 8 ? 3 : 2) vo
         if (wave + u * W < g.words) load(u, wave + u * W);
     // the low-rank branch: 16 ranks at a time, each such chunk by one wavefront, four ranks an instruction, in fp32.  P's parts are summed into LDS; lane group q has
     // ranks 4 q .. + 3 of a chunk, of its four outputs' rows of L_A here and of P later
-    constexpr int CHUNKS = 8 / W;
-    uint32_t lv[CHUNKS][FA][2];
-    if (g.P) {
+    uint32_t lv[FA][2];
+    auto ranks_of = [&](int k0) {
         const uint16_t* const la = g.la + (int64_t)e * g.m * g.r;
+        const int k = k0 + 4 * q;
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            const int k = 16 * (wave + c * W) + 4 * q;
-            if (16 * (wave + c * W) >= g.rp) break;
-#pragma unroll
-            for (int a = 0; a < FA; ++a) {
-                const uint16_t* const src = la + arow[a] * g.r + k;
-                if (g.la_four) {
-                    const uint2 v = *(const uint2*)(k < g.r ? src : la);
-                    lv[c][a][0] = k < g.r ? v.x : 0u;
-                    lv[c][a][1] = k < g.r ? v.y : 0u;
-                    continue;
-                }
-                uint32_t h[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) h[i] = k + i < g.r ? src[i] : 0u;
-                lv[c][a][0] = h[0] | h[1] << 16;
-                lv[c][a][1] = h[2] | h[3] << 16;
+        for (int a = 0; a < FA; ++a) {
+            const uint16_t* const src = la + arow[a] * g.r + k;
+            if (g.la_four) {
+                const uint2 v = *(const uint2*)(k < g.r ? src : la);
+                lv[a][0] = k < g.r ? v.x : 0u;
+                lv[a][1] = k < g.r ? v.y : 0u;
+                continue;
             }
+            uint32_t h[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h[i] = k + i < g.r ? src[i] : 0u;
+            lv[a][0] = h[0] | h[1] << 16;
+            lv[a][1] = h[2] | h[3] << 16;
         }
+    };
+    if (g.P) {
+        if (16 * wave < g.rp) ranks_of(16 * wave);
         const int four = g.rp / 4;
         const int64_t next = g.groups.positions * g.rp;
         for (int i = threadIdx.x; i < 16 * NT * four; i += 64 * W) {
@@ -325,10 +322,8 @@ __global__ __launch_bounds__(64 * W, FA * NT <= 4 ? 4 : FA * NT <= 8 ? 3 : 2) vo
     }
     if (g.P) {
         __syncthreads();
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            const int k0 = 16 * (wave + c * W);
-            if (k0 >= g.rp) break;
+        for (int k0 = 16 * wave; k0 < g.rp; k0 += 16 * W) {
+            if (k0 >= 16 * W) ranks_of(k0);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const f32x4_t pv = *(const f32x4_t*)(part + (16 * t + li) * (g.rp + 4) + k0 + 4 * q);
@@ -336,7 +331,7 @@ __global__ __launch_bounds__(64 * W, FA * NT <= 4 ? 4 : FA * NT <= 8 ? 3 : 2) vo
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int a = 0; a < FA; ++a)
-                        acc[a][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(i & 1 ? lv[c][a][i >> 1] & 0xFFFF0000u : lv[c][a][i >> 1] << 16), pv[i], acc[a][t], 0, 0, 0);
+                        acc[a][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(i & 1 ? lv[a][i >> 1] & 0xFFFF0000u : lv[a][i >> 1] << 16), pv[i], acc[a][t], 0, 0, 0);
             }
         }
         __syncthreads();
@@ -675,14 +670,15 @@ int launch_tile(aser_ctx* ctx, const MxArgs& g, bool gated, bool f32) {
 
 // Rows of the weights and of x of a workgroup, its wavefronts and words ahead, by how many workgroups there are: `tiles` of 16 nt rows, and 32 weight rows each.  Many of them fill
 // the device by themselves and read x less often with 64 weight rows; few of them have to have more in flight.  Weights not in any cache, us (the other side):
-//   one row or up to 16: 1 x 4096 x 14336 twice, gated, rank 32 (1792 workgroups) <2, 1, 4, 4> 32.0 (<2, 1, 8, 2> 33.7, <4, 1, 4, 2> 36.5); 48 rows on 64 experts, 1408 x 2048 (4096)
-//   40 (47, 44); one row, 14336 x 4096 (128) <1, 1, 8, 4> 9.4 (<2, 1, 8, 2> 9.6, <2, 1, 4, 4> 11.3)
+//   one row or up to 16: <2, 1, 4, 3>, three words ahead and five wavefronts a SIMD, 1 x 4096 x 14336 twice, gated, rank 32 (1792 workgroups) 30.0, 48 rows on 64 experts,
+//   1408 x 2048, with the weighted sum (4096) 33.6; four words ahead and four wavefronts 30.2, 36.7; <2, 1, 8, 2> and <4, 1, 4, 2> 1.7 to 7 more than these; one row, 14336 x 4096
+//   (128) <1, 1, 8, 4> 9.4 (<2, 1, 8, 2> 9.6, <2, 1, 4, 4> 11.3)
 //   24 rows, 4096 x 14336 (448) <2, 2, ..> 8.4 (<4, 2, ..> 9.2); 256 rows on 64 experts, 2048 x 2816 (5632) <4, 2, ..> 58 (77)
 //   64 rows, 4096 x 14336 (448) <4, 4, ..> 14.4 (<2, 4, ..> 15.7); 128 rows, 4096 x 4096 (256) <2, 4, ..> 8.6 (9.5)
 int run_few(aser_ctx* ctx, const MxArgs& g, int nt, int64_t matrices, bool gated, bool f32) {
     const int64_t tiles = ceil_div64(g.groups.positions, 16 * nt), workgroups = (matrices > tiles ? matrices : tiles) * ceil_div64(g.m, 32);
     if (nt == 1) {
-        if (workgroups >= 512) return launch_few<2, 1, 4, 4>(ctx, g, gated, f32);
+        if (workgroups >= 512) return launch_few<2, 1, 4, 3>(ctx, g, gated, f32);
         return gated ? launch_few_one<2, 1, 8, 2, true>(ctx, g, f32) : launch_few_one<1, 1, 8, 4, false>(ctx, g, f32);
     }
     if (nt == 2) return workgroups >= 2048 ? launch_few<4, 2, 4, 2>(ctx, g, gated, f32) : launch_few<2, 2, 4, 2>(ctx, g, gated, f32);
