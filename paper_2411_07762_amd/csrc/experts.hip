@@ -41,7 +41,6 @@ __device__ __forceinline__ uint32_t wave_reduce(uint32_t v, uint32_t idle, F joi
     return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) { return wave_reduce(v, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; }); }
-__device__ __forceinline__ uint32_t wave_min(uint32_t v) { return wave_reduce(v, 0xFFFFFFFFu, [](uint32_t a, uint32_t b) { return a < b ? a : b; }); }
 template <int CTRL, int ROWS>
 __device__ __forceinline__ double moved(double v) {                 // 0 where no lane is reached
     const uint64_t b = __builtin_bit_cast(uint64_t, v);
@@ -224,36 +223,54 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(RouteArgs g) {
                 if (e < g.experts && !((open >> (of << g.per_bits)) & 1)) c[j] = kMinus;
             }
         }
-        uint64_t key[V];
+        uint32_t high[V], low[V];                            // halves of the keys, 0: not to be chosen, or chosen
 #pragma unroll
-        for (int j = 0; j < V; ++j) key[j] = c[j] > kMinus ? key_of(c[j]) : 0;
-        int my_id = -1;
-        double my_s = 0.0, total = 0.0;
-        for (int k = 0; k < g.top_k; ++k) {
-            uint64_t best = 0;
-            int at = 0;
-            double score = 0.0;
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (key[j] > best) { best = key[j]; at = j; score = s[j]; }
-            const uint32_t high = wave_max((uint32_t)(best >> 32));
-            if (high == 0) break;                            // nothing is left: keys of numbers are above 2^32
-            uint64_t who = __ballot((uint32_t)(best >> 32) == high);
-            if (__popcll(who) > 1) {                         // several lanes agree in the upper half: the lower one, then the lowest expert
-                const bool mine = (uint32_t)(best >> 32) == high;
-                const uint32_t low = wave_max(mine ? (uint32_t)best : 0u);
-                const bool same = mine && (uint32_t)best == low;
-                const uint32_t e = wave_min(same ? (uint32_t)(lane + 64 * at) : 0xFFFFFFFFu);
-                who = (uint64_t)1 << (e & 63);
-            }
-            const int owner = __builtin_ctzll(who), j_of = __builtin_amdgcn_readlane(at, owner);
-            score = lane_value(score, owner);
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (lane == owner && j == j_of) key[j] = 0;
-            if (lane == k) { my_id = owner + 64 * j_of; my_s = score; }
-            total += score;
+        for (int j = 0; j < V; ++j) {
+            const uint64_t key = c[j] > kMinus ? key_of(c[j]) : 0;
+            high[j] = (uint32_t)(key >> 32);
+            low[j] = (uint32_t)key;
         }
+        int my_id = -1;
+        for (int k = 0; k < g.top_k; ++k) {
+            uint32_t best = high[0];
+#pragma unroll
+            for (int j = 1; j < V; ++j) best = high[j] > best ? high[j] : best;
+            best = wave_max(best);
+            if (best == 0) break;                            // nothing is left: keys of numbers are above 2^32
+            uint64_t who[V];
+            int agree = 0, e = 0;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                who[j] = __ballot(high[j] == best);
+                agree += __popcll(who[j]);
+                if (who[j]) e = 64 * j + __builtin_ctzll(who[j]);
+            }
+            if (agree > 1) {                                 // several agree in the upper half: the lower one, then the lowest expert
+                uint32_t below = 0;
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (high[j] == best && low[j] > below) below = low[j];
+                below = wave_max(below);
+#pragma unroll
+                for (int j = V - 1; j >= 0; --j) {
+                    const uint64_t same = __ballot(high[j] == best && low[j] == below);
+                    if (same) e = 64 * j + __builtin_ctzll(same);
+                }
+#pragma unroll
+                for (int j = 0; j < V; ++j) who[j] = e >> 6 == j ? (uint64_t)1 << (e & 63) : 0;
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if ((who[j] >> lane) & 1) high[j] = 0;
+            if (lane == k) my_id = e;
+        }
+        double my_s = 0.0;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const double v = __shfl(s[j], my_id & 63);
+            if (my_id >> 6 == j) my_s = v;                   // none: -1 is nobody's
+        }
+        const double total = wave_sum(my_s);
         if (g.o.renormalize && total > 0.0) my_s /= total;
         if (lane < g.top_k) {
             g.ids[row * g.top_k + lane] = my_id;
