@@ -1,6 +1,6 @@
 // Routing of rows to experts, and the weighted sum of what the experts made of them.
 //
-// Routing: a wavefront has a row, its lanes the experts lane, lane + 64, ...  Scores are computed in 64 bits, so that experts are told apart where fp32 would
+// Routing: a wavefront or 16 of its lanes have a row, lane i the experts i, i + 64 (16), ...  Scores are computed in 64 bits, so that experts are told apart where fp32 would
 // round their scores to one number.  The top_k largest are found one after the other, by the upper halves of keys of 64 bits that order as the numbers do; only where lanes
 // agree in them the lower halves are looked at.  A workgroup has 32 rows: bit t of an expert's word says that row t chose it,
 // so the number of a pair among its expert's pairs is a count of bits, and the order by expert is the same whatever the timing.  Up
@@ -289,6 +289,176 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(RouteArgs g) {
     place_pairs(g, row0, marks, first, first[g.experts]);
 }
 
+// More than 32 rows, up to 256 experts: 16 lanes have a row, a lane the experts lane, lane + 16, ...  With a wavefront for a row the steps of its reductions, most of its
+// instructions, serve that row alone.  us a call (a wavefront for a row): 8191 rows of 256 experts, top 8 of 4 of 8 groups, sigmoid 25.7 (28.5), 64 rows 21.5 (24.0); 32000 rows of
+// 64 experts without groups 29.1 (44.4), 100 rows, softmax 10.1 (12.3).
+constexpr int kManyWaves = kTok / 4;
+template <int CTRL>
+__device__ __forceinline__ uint32_t turned(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 15, 15, true); }
+template <int CTRL>
+__device__ __forceinline__ double turned(double v) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint64_t lo = turned<CTRL>((uint32_t)b), hi = turned<CTRL>((uint32_t)(b >> 32));
+    return __builtin_bit_cast(double, lo | hi << 32);
+}
+// Every lane of 16 gets what all of them make: pairs, pairs of pairs, then halves and rows in the mirror.  Both sides of each step join the same two, so a rounded sum is the same
+// in all lanes (turns by 1, 2, 4 and 8 lanes would add in another order in each).
+template <class T, class F>
+__device__ __forceinline__ T row_reduce(T v, F join) {
+    v = join(v, turned<0xB1>(v));
+    v = join(v, turned<0x4E>(v));
+    v = join(v, turned<0x141>(v));
+    return join(v, turned<0x140>(v));
+}
+__device__ __forceinline__ uint32_t row_max(uint32_t v) { return row_reduce(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; }); }
+__device__ __forceinline__ uint32_t row_min(uint32_t v) { return row_reduce(v, [](uint32_t a, uint32_t b) { return a < b ? a : b; }); }
+__device__ __forceinline__ double row_sum(double v) { return row_reduce(v, [](double a, double b) { return a + b; }); }
+
+template <int V, bool F32>
+__global__ __launch_bounds__(kManyWaves * 64) void route_many_kernel(RouteArgs g) {
+    extern __shared__ __align__(16) char smem[];
+    const int room = g.experts + 16;                                        // of a row: neighbouring ones begin on other banks
+    double* const cbuf = (double*)smem;                                     // [row][expert]
+    uint32_t* const marks = (uint32_t*)(cbuf + (size_t)kTok * room);
+    const int lane = threadIdx.x & 63, sub = lane & 15, t = threadIdx.x >> 4;
+    const int64_t row0 = (int64_t)blockIdx.x * kTok;
+    const bool there = row0 + t < g.rows;
+    const int64_t row = there ? row0 + t : g.rows - 1;                      // behind the last row: that one again, not stored
+    float l[V], top = -__builtin_huge_valf();
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int e = sub + 16 * j;
+        l[j] = -__builtin_huge_valf();
+        if (e < g.experts) l[j] = F32 ? ((const float*)g.logits)[row * g.ldl + e] : __uint_as_float((uint32_t)((const uint16_t*)g.logits)[row * g.ldl + e] << 16);
+    }
+    for (int e = threadIdx.x; e < g.experts; e += kManyWaves * 64) marks[e] = 0;
+    __syncthreads();
+    const bool by_logit = !g.bias && (g.o.n_groups == 1 || g.o.group_top == 1);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        if (!(l[j] == l[j])) l[j] = -__builtin_huge_valf();
+        if (l[j] > 3.402823466e38f) l[j] = 3.402823466e38f;
+        top = fmaxf(top, l[j]);
+    }
+    double s[V], c[V], l_top = 0.0;
+    if (!g.o.sigmoid) {
+        const uint32_t tb = __float_as_uint(top + 0.f), most = row_max(tb >> 31 ? ~tb : tb | 0x80000000u);
+        l_top = __uint_as_float(most >> 31 ? most & 0x7FFFFFFFu : ~most);
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[j] = g.o.sigmoid ? -(double)l[j] : (double)l[j] - l_top;
+#pragma unroll
+    for (int j = 0; j < V; j += 4) exp64<4>(s + j);
+    if (g.o.sigmoid) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[j] = l[j] == -__builtin_huge_valf() ? 0.0 : reciprocal64(1.0 + s[j]);
+    } else {
+        double sum = 0.0;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if (l[j] == -__builtin_huge_valf()) s[j] = 0.0;
+            sum += s[j];
+        }
+        sum = row_sum(sum);
+        const double by = reciprocal64(sum > 0.0 ? sum : 1.0);
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[j] *= by;
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const double v = by_logit ? (double)l[j] : s[j] + (double)(g.bias && sub + 16 * j < g.experts ? g.bias[sub + 16 * j] : 0.f);
+        c[j] = l[j] == -__builtin_huge_valf() || !(v == v) ? kMinus : v;
+    }
+    double* const mine = cbuf + (size_t)t * room;
+    if (g.o.n_groups > 1) {
+        const int size = g.experts / g.o.n_groups;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (sub + 16 * j < g.experts) mine[sub + 16 * j] = c[j];
+        __builtin_amdgcn_wave_barrier();
+        // `per` lanes look at a group's members in turn, and join what they found
+        const int per = 1 << g.per_bits, group = sub >> g.per_bits;
+        double worth = kMinus, second = kMinus;
+        if (group < g.o.n_groups)
+            for (int i = sub & (per - 1); i < size; i += per) {
+                const double v = mine[group * size + i];
+                second = fmax(second, fmin(worth, v));
+                worth = fmax(worth, v);
+            }
+        for (int d = 1; d < per; d *= 2) {
+            const double w2 = __shfl_xor(worth, d), s2 = __shfl_xor(second, d);
+            second = fmax(fmax(second, s2), fmin(worth, w2));
+            worth = fmax(worth, w2);
+        }
+        if (g.o.group_top == 2 && second > kMinus) worth += second;
+        int ahead = 0;
+        for (int i = 0; i < g.o.n_groups; ++i) {
+            const double v = __shfl(worth, (lane & 48) + (i << g.per_bits));
+            ahead += v > worth || (v == worth && i < group);
+        }
+        const uint32_t open = (uint32_t)(__ballot(group < g.o.n_groups && ahead < g.o.top_groups) >> (lane & 48));
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int e = sub + 16 * j;
+            const int of = (int)(((float)e + 0.5f) * g.per_expert);              // e / size: far from a whole number for what e < 1024 can be
+            if (e < g.experts && !((open >> (of << g.per_bits)) & 1)) c[j] = kMinus;
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    uint32_t high[V], low[V];                                    // halves of the keys, 0: not to be chosen, or chosen
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const uint64_t key = c[j] > kMinus ? key_of(c[j]) : 0;
+        high[j] = (uint32_t)(key >> 32);
+        low[j] = (uint32_t)key;
+        if (sub + 16 * j < g.experts) mine[sub + 16 * j] = s[j];
+    }
+    int my_id = -1;
+    for (int k = 0; k < g.top_k; ++k) {
+        uint32_t best = high[0];
+#pragma unroll
+        for (int j = 1; j < V; ++j) best = high[j] > best ? high[j] : best;
+        best = row_max(best);
+        const uint64_t open = __ballot(best != 0);
+        if (!open) break;                                        // nothing is left: keys of numbers are above 2^32
+        const uint32_t want = best ? best : 0xFFFFFFFFu;         // nobody's key
+        uint32_t e = 0xFFFFFFFFu;
+        int agree = 0;
+#pragma unroll
+        for (int j = V - 1; j >= 0; --j) {
+            agree += __popcll(__ballot(high[j] == want));
+            if (high[j] == want) e = sub + 16 * j;
+        }
+        if (16 * agree > __popcll(open)) {                       // in some row several agree in the upper half: the lower one, then the lowest expert
+            uint32_t below = 0;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (high[j] == want && low[j] > below) below = low[j];
+            below = row_max(below);
+            e = 0xFFFFFFFFu;
+#pragma unroll
+            for (int j = V - 1; j >= 0; --j)
+                if (high[j] == want && low[j] == below) e = sub + 16 * j;
+        }
+        e = row_min(e);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (e == (uint32_t)(sub + 16 * j)) high[j] = 0;
+        if (sub == k) my_id = (int)e;
+    }
+    __builtin_amdgcn_wave_barrier();
+    double my_s = my_id >= 0 ? mine[my_id] : 0.0;
+    const double total = row_sum(my_s);
+    if (g.o.renormalize && total > 0.0) my_s /= total;
+    if (there && sub < g.top_k) {
+        g.ids[row * g.top_k + sub] = my_id;
+        g.weights[row * g.top_k + sub] = (float)(my_s * (double)g.o.scale);
+        if (my_id >= 0) atomicOr(&marks[my_id], 1u << t);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < g.experts; e += kManyWaves * 64) g.counts[(int64_t)e * g.groups + blockIdx.x] = __popc(marks[e]);
+}
+
 // counts[e][*] to the numbers of pairs in the workgroups before, totals[e] their sum.  A wavefront has an expert.
 __global__ __launch_bounds__(64) void route_sum_kernel(RouteArgs g) {
     const int lane = threadIdx.x;
@@ -343,6 +513,15 @@ int launch_route(aser_ctx* ctx, const RouteArgs& g, bool f32) {
     if (lds > 65536) ASER_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
     kernel<<<(unsigned)g.groups, kWaves * 64, lds, ctx->stream>>>(g);
     return aser_check_launch(ctx, "route_kernel");
+}
+
+template <int V>
+int launch_route_many(aser_ctx* ctx, const RouteArgs& g, bool f32) {
+    const size_t lds = (size_t)kTok * (g.experts + 16) * 8 + (size_t)g.experts * 4;
+    auto kernel = f32 ? route_many_kernel<V, true> : route_many_kernel<V, false>;
+    if (lds > 65536) ASER_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    kernel<<<(unsigned)g.groups, kManyWaves * 64, lds, ctx->stream>>>(g);
+    return aser_check_launch(ctx, "route_many_kernel");
 }
 
 // ---------------------------------------------------------------------------------------------------------------- the weighted sum
@@ -463,7 +642,8 @@ extern "C" int aser_route_experts(aser_ctx* ctx, const void* logits, int32_t x_d
     const size_t need = aser_route_workspace_bytes(plan->rows, experts, plan->top_k);
     RouteArgs g{logits, ldl, bias, *opts, plan->ids, plan->weights, plan->offsets, plan->order, plan->place, plan->rows, plan->top_k, experts, nullptr, nullptr,
                 (int)ceil_div64(plan->rows, kTok)};
-    while ((opts->n_groups << (g.per_bits + 1)) <= 64) ++g.per_bits;
+    const bool sixteen = g.groups > 1 && experts <= 256 && opts->n_groups <= 16 && plan->top_k <= 16;
+    while ((opts->n_groups << (g.per_bits + 1)) <= (sixteen ? 16 : 64)) ++g.per_bits;
     g.per_expert = (float)opts->n_groups / (float)experts;
     if (g.groups > 1) {
         if (!ctx->ws || ctx->ws_bytes < need) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "route_experts: workspace too small");
@@ -471,7 +651,8 @@ extern "C" int aser_route_experts(aser_ctx* ctx, const void* logits, int32_t x_d
         g.totals = g.counts + (int64_t)g.groups * experts;
     }
     ASER_TRY(aser_prepare_device(ctx));
-    if (experts <= 64) ASER_TRY(launch_route<1>(ctx, g, f32));
+    if (sixteen) ASER_TRY(experts <= 64 ? launch_route_many<4>(ctx, g, f32) : experts <= 128 ? launch_route_many<8>(ctx, g, f32) : launch_route_many<16>(ctx, g, f32));
+    else if (experts <= 64) ASER_TRY(launch_route<1>(ctx, g, f32));
     else if (experts <= 128) ASER_TRY(launch_route<2>(ctx, g, f32));
     else if (experts <= 256) ASER_TRY(launch_route<4>(ctx, g, f32));
     else if (experts <= 512) ASER_TRY(launch_route<8>(ctx, g, f32));

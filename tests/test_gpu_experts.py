@@ -337,6 +337,26 @@ def test_route_ties_masks_and_values_that_are_none(ctx, rows, bias, sigmoid):
         check_routed(logits, routed(ctx, logits, 6, **opts), 6, **opts)
 
 
+# 33 rows and more, around the widths, choices and groups up to which 16 lanes have a row; few different logits, so that experts tie within and across lanes
+@pytest.mark.parametrize("rows", [33, 97])
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("experts,k,opts", [
+    (16, 16, dict()), (17, 3, dict(renormalize=False)), (64, 16, dict(groups=16, top_groups=7, group_top=2)), (65, 17, dict()), (66, 4, dict(groups=33, top_groups=8)),
+    (128, 8, dict(groups=4, top_groups=2, group_top=2)), (129, 5, dict(groups=3, top_groups=2)), (255, 15, dict(groups=15, top_groups=4, group_top=2, bias=True)),
+    (256, 16, dict(bias=True)), (256, 32, dict()), (256, 8, dict(groups=2, top_groups=1)), (257, 6, dict(bias=True))])
+def test_route_many_rows_with_ties(ctx, rows, sigmoid, experts, k, opts):
+    g = torch.Generator().manual_seed(rows + experts + k)
+    logits = torch.randint(-3, 4, (rows, experts), generator=g).float()
+    logits[rows // 2] = -float("inf")
+    logits[rows - 1, k // 2:] = -float("inf")
+    logits[:, experts - 1] = float("nan")
+    opts = dict(opts, sigmoid=sigmoid)
+    if opts.get("bias"):
+        opts["bias"] = (torch.randint(-1, 2, (experts,), generator=g).float() * 0.25).to(DEV)
+    logits = logits.to(DEV)
+    check_routed(logits, routed(ctx, logits, k, **opts), k, **opts)
+
+
 def test_route_no_rows(ctx):
     plan = aser.ExpertPlan.empty(0, 2, 300)
     plan.offsets.fill_(9)
