@@ -289,9 +289,9 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(RouteArgs g) {
     place_pairs(g, row0, marks, first, first[g.experts]);
 }
 
-// More than 32 rows, up to 256 experts: 16 lanes have a row, a lane the experts lane, lane + 16, ...  With a wavefront for a row the steps of its reductions, most of its
+// More than 32 rows, up to 384 experts: 16 lanes have a row, a lane the experts lane, lane + 16, ...  With a wavefront for a row the steps of its reductions, most of its
 // instructions, serve that row alone.  us a call (a wavefront for a row): 8191 rows of 256 experts, top 8 of 4 of 8 groups, sigmoid 25.7 (28.5), 64 rows 21.5 (24.0); 32000 rows of
-// 64 experts without groups 29.1 (44.4), 100 rows, softmax 10.1 (12.3).
+// 64 experts without groups 29.1 (44.4), 100 rows, softmax 10.1 (12.3); 3627 rows of 384 experts 30.1 (36.8), 4000 of 512 no less (39.0).
 constexpr int kManyWaves = kTok / 4;
 template <int CTRL>
 __device__ __forceinline__ uint32_t turned(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 15, 15, true); }
@@ -642,7 +642,7 @@ extern "C" int aser_route_experts(aser_ctx* ctx, const void* logits, int32_t x_d
     const size_t need = aser_route_workspace_bytes(plan->rows, experts, plan->top_k);
     RouteArgs g{logits, ldl, bias, *opts, plan->ids, plan->weights, plan->offsets, plan->order, plan->place, plan->rows, plan->top_k, experts, nullptr, nullptr,
                 (int)ceil_div64(plan->rows, kTok)};
-    const bool sixteen = g.groups > 1 && experts <= 256 && opts->n_groups <= 16 && plan->top_k <= 16;
+    const bool sixteen = g.groups > 1 && experts <= 384 && opts->n_groups <= 16 && plan->top_k <= 16;
     while ((opts->n_groups << (g.per_bits + 1)) <= (sixteen ? 16 : 64)) ++g.per_bits;
     g.per_expert = (float)opts->n_groups / (float)experts;
     if (g.groups > 1) {
@@ -651,7 +651,7 @@ extern "C" int aser_route_experts(aser_ctx* ctx, const void* logits, int32_t x_d
         g.totals = g.counts + (int64_t)g.groups * experts;
     }
     ASER_TRY(aser_prepare_device(ctx));
-    if (sixteen) ASER_TRY(experts <= 64 ? launch_route_many<4>(ctx, g, f32) : experts <= 128 ? launch_route_many<8>(ctx, g, f32) : launch_route_many<16>(ctx, g, f32));
+    if (sixteen) ASER_TRY(experts <= 64 ? launch_route_many<4>(ctx, g, f32) : experts <= 128 ? launch_route_many<8>(ctx, g, f32) : experts <= 256 ? launch_route_many<16>(ctx, g, f32) : launch_route_many<24>(ctx, g, f32));
     else if (experts <= 64) ASER_TRY(launch_route<1>(ctx, g, f32));
     else if (experts <= 128) ASER_TRY(launch_route<2>(ctx, g, f32));
     else if (experts <= 256) ASER_TRY(launch_route<4>(ctx, g, f32));

@@ -343,7 +343,8 @@ def test_route_ties_masks_and_values_that_are_none(ctx, rows, bias, sigmoid):
 @pytest.mark.parametrize("experts,k,opts", [
     (16, 16, dict()), (17, 3, dict(renormalize=False)), (64, 16, dict(groups=16, top_groups=7, group_top=2)), (65, 17, dict()), (66, 4, dict(groups=33, top_groups=8)),
     (128, 8, dict(groups=4, top_groups=2, group_top=2)), (129, 5, dict(groups=3, top_groups=2)), (255, 15, dict(groups=15, top_groups=4, group_top=2, bias=True)),
-    (256, 16, dict(bias=True)), (256, 32, dict()), (256, 8, dict(groups=2, top_groups=1)), (257, 6, dict(bias=True))])
+    (256, 16, dict(bias=True)), (256, 32, dict()), (256, 8, dict(groups=2, top_groups=1)), (257, 6, dict(bias=True)),
+    (384, 8, dict(groups=8, top_groups=4, group_top=2, bias=True)), (385, 4, dict())])
 def test_route_many_rows_with_ties(ctx, rows, sigmoid, experts, k, opts):
     g = torch.Generator().manual_seed(rows + experts + k)
     logits = torch.randint(-3, 4, (rows, experts), generator=g).float()
