@@ -68,7 +68,8 @@ __device__ __forceinline__ void store4(const MxArgs& g, int64_t p, int64_t o, co
 // TERMS = 0, few rows: fp32 sums of the part.  L_B goes into the registers as it is: of each of a word's four blocks lane group q = lane / 16 has channels 8 q .. + 7.
 // Otherwise the sum (of one part) as so many bf16 terms, each what the ones before leave, rounded; lane group q has block q, and L_B is turned through LDS: lanes next to each
 // other in the matrix instruction have different rows, and a load of 16 bytes from 64 places occupies a compute unit's address unit for 64 cycles where one of four rows'
-// 256 bytes takes 16.  Without that 4099 tokens of 4096 channels and 64 ranks take 25 us; with L_B put in order by a launch of its own 10 and 4.7.
+// 256 bytes takes 16.  Without that 4099 tokens of 4096 channels and 64 ranks take 25 us; with L_B put in order by a launch of its own 10 and 4.7.  Latency bounds it: 16 ranks of 32
+// tokens and two words ahead, two workgroups a compute unit, take 10.8; 32 ranks and four words, one workgroup, 12.8; eight wavefronts 13 to 15; 64 tokens 11.6 to 12.5.
 template <int RF, int NT, int W, int U, int TERMS>
 __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_tiles) {
     extern __shared__ __align__(16) float part[];            // the wavefronts' rows of L_B, then the sums, [wavefront][fragment][lane][4]
@@ -803,7 +804,7 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
         const int terms = f32 ? 3 : 2, width = (int)align_up(r, 32);
         g.planes = (uint16_t*)p_room;
         g.lr_steps = width / 32 * terms;
-        ASER_TRY(f32 ? (launch_down<2, 2, 4, 4, 3>(ctx, g)) : (launch_down<2, 2, 4, 4, 2>(ctx, g)));
+        ASER_TRY(f32 ? (launch_down<1, 2, 4, 2, 3>(ctx, g)) : (launch_down<1, 2, 4, 2, 2>(ctx, g)));
         if (r != width || ((uintptr_t)L_A & 15)) {
             uint16_t* const padded = (uint16_t*)(p_room + p.p_bytes);
             ASER_TRY(pad_rows(ctx, L_A, w->rows * w->count, r, width, padded));
