@@ -820,7 +820,7 @@ def aser_route_experts(ctx: Context, logits, plan: ExpertPlan, *, bias=None, sig
     lp, ldl, experts = _rows(logits, plan.rows, logits.dtype, device)
     if experts != plan.n_experts or (bias is not None and bias.numel() != experts):
         raise ValueError("logits and bias must have a column for each expert")
-    opts = _route_opts(bool(sigmoid), groups, top_groups, group_top, bool(renormalize), scale)
+    opts = _route_opts(bool(sigmoid), int(groups), int(top_groups), int(group_top), bool(renormalize), float(scale))      # kept by their values
     return ctx._lib.aser_route_experts(ctx.handle, lp, _dtype_code(logits), ldl, None if bias is None else _floats((bias,), f32, device)[0], opts, plan.ref)
 
 

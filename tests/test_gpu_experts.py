@@ -358,6 +358,14 @@ def test_route_many_rows_with_ties(ctx, rows, sigmoid, experts, k, opts):
     check_routed(logits, routed(ctx, logits, k, **opts), k, **opts)
 
 
+def test_route_scale_that_is_changed_in_place(ctx):
+    logits, scale = torch.randn(5, 8, generator=torch.Generator().manual_seed(2)).to(DEV), torch.tensor(2.0)
+    for value in (2.0, 3.0):
+        scale.fill_(value)
+        plan = routed(ctx, logits, 2, scale=scale)
+        check_routed(logits, plan, 2, scale=value)
+
+
 def test_route_no_rows(ctx):
     plan = aser.ExpertPlan.empty(0, 2, 300)
     plan.offsets.fill_(9)
