@@ -102,12 +102,7 @@ __device__ __forceinline__ void sum_experts(int experts, int32_t* offs, COUNT co
     int32_t before = 0;
     for (int e0 = 0; e0 < experts; e0 += 64) {
         const int32_t mine = e0 + lane < experts ? count(e0 + lane) : 0;
-        int32_t upto = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int32_t v = __shfl_up(upto, d);
-            if (lane >= d) upto += v;
-        }
+        const int32_t upto = (int32_t)mx4_sums_upto((uint32_t)mine);
         if (e0 + lane < experts) offs[e0 + lane] = before + upto - mine;
         before += __builtin_amdgcn_readlane(upto, 63);
     }
@@ -290,7 +285,7 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(RouteArgs g) {
 }
 
 // More than 32 rows, up to 384 experts: 16 lanes have a row, a lane the experts lane, lane + 16, ...  With a wavefront for a row the steps of its reductions, most of its
-// instructions, serve that row alone.  us a call (a wavefront for a row): 8191 rows of 256 experts, top 8 of 4 of 8 groups, sigmoid 25.7 (28.5), 64 rows 21.5 (24.0); 32000 rows of
+// instructions, serve that row alone.  us a call (a wavefront for a row): 8191 rows of 256 experts, top 8 of 4 of 8 groups, sigmoid 25.7 (28.5; both 1.4 less since the running sums need no LDS), 64 rows 21.5 (24.0); 32000 rows of
 // 64 experts without groups 29.1 (44.4), 100 rows, softmax 10.1 (12.3); 3627 rows of 384 experts 30.1 (36.8), 4000 of 512 no less (39.0).
 constexpr int kManyWaves = kTok / 4;
 template <int CTRL>
@@ -466,12 +461,7 @@ __global__ __launch_bounds__(64) void route_sum_kernel(RouteArgs g) {
     int32_t before = 0;
     for (int i0 = 0; i0 < g.groups; i0 += 64) {
         const int32_t v = i0 + lane < g.groups ? mine[i0 + lane] : 0;
-        int32_t upto = v;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int32_t u = __shfl_up(upto, d);
-            if (lane >= d) upto += u;
-        }
+        const int32_t upto = (int32_t)mx4_sums_upto((uint32_t)v);
         if (i0 + lane < g.groups) mine[i0 + lane] = before + upto - v;
         before += __builtin_amdgcn_readlane(upto, 63);
     }

@@ -26,6 +26,18 @@ struct MxGroups {
     }
 };
 
+// The sum over the lanes up to this one, by moves within rows of 16 lanes and from the last of a row to the following rows.  Every workgroup begins with this: with shuffles through
+// LDS 48 rows on 64 experts, 1408 x 2048, take 33.1 us instead of 32.0.
+__device__ __forceinline__ uint32_t mx4_sums_upto(uint32_t v) {
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false);       // row_shr by 1, 2, 4, 8
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false);       // row_bcast of lane 15 to rows 1 and 3, of lane 31 to rows 2 and 3
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false);
+    return v;
+}
+
 // Tiles of bm positions that there are.
 __device__ __forceinline__ uint32_t mx4_tiles(const MxGroups& g, int bm) {
     if (!g.offsets) return (uint32_t)((g.positions + bm - 1) / bm);
@@ -37,20 +49,7 @@ __device__ __forceinline__ uint32_t mx4_tiles(const MxGroups& g, int bm) {
         const int32_t s = a < 0 ? 0 : a > most ? most : a, t = b > most ? most : b;
         sum += t > s ? (t - s + bm - 1) / bm : 0;
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    return __builtin_amdgcn_readfirstlane(sum);
-}
-// The sum over the lanes up to this one, by moves within rows of 16 lanes and from the last of a row to the following rows.  Every workgroup begins with this: with shuffles through
-// LDS 48 rows on 64 experts, 1408 x 2048, take 33.1 us instead of 32.0.
-__device__ __forceinline__ uint32_t mx4_sums_upto(uint32_t v) {
-    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false);       // row_shr by 1, 2, 4, 8
-    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false);
-    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false);
-    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false);
-    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false);       // row_bcast of lane 15 to rows 1 and 3, of lane 31 to rows 2 and 3
-    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false);
-    return v;
+    return (uint32_t)__builtin_amdgcn_readlane((int)mx4_sums_upto((uint32_t)sum), 63);
 }
 // Tiles of bm positions, `across` of them beside each other for other outputs, numbered matrix by matrix: the matrix that number id belongs to, its first position, the
 // number of its positions, and id's place among its tiles.  False: there is no such tile.  Every wavefront looks for itself: a lane has a matrix, and the
