@@ -563,7 +563,7 @@ typedef struct aser_route_opts {
     float scale;           /* and multiplied by this at last                                                                       */
 } aser_route_opts;
 
-/* Scores s of logits (rows x n_experts, bf16 or fp32, ldl) are computed in 64 bits.  Chosen are the top_k experts of the largest c = s + bias (fp32,
+/* Scores s of logits (rows x n_experts, bf16 or fp32, ldl) are computed in 64 bits; a sigmoid 1 / (1 + exp(-l)) is 0 where exp(-l) is above their range, l < -709.78.  Chosen are the top_k experts of the largest c = s + bias (fp32,
  * n_experts; NULL: none; without a bias the scores are ordered as the logits are, and unless groups are summed c is the
  * logit), of equal ones the lower number; groups likewise.  Weights are made of s, not of c.
  * An expert whose logit is -inf or NaN, or whose c is NaN or -inf, is never chosen, and such logits do not count in the softmax; a logit of

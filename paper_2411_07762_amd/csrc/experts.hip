@@ -67,7 +67,7 @@ __device__ __forceinline__ uint64_t key_of(double v) {
     return b >> 63 ? ~b : b | (uint64_t)1 << 63;
 }
 
-// x[j] to exp(x[j]) in 64 bits, 709 and more as 709: x = k ln 2 + r, |r| <= ln 2 / 2, and the Taylor series of exp(r) to r^13 / 13!, whose rest is below 2^-57 of it.  All
+// x[j] <= 0 to exp(x[j]) in 64 bits, -746 and less (and NaN) to 0: x = k ln 2 + r, |r| <= ln 2 / 2, and the Taylor series of exp(r) to r^13 / 13!, whose rest is below 2^-57 of it.  All
 // numbers of a lane at once, so that the constants are there once; half the instructions of the library's function, which a third of the routing's time went into.
 template <int V>
 __device__ __forceinline__ void exp64(double* x) {
@@ -76,7 +76,7 @@ __device__ __forceinline__ void exp64(double* x) {
     double k[V], r[V], p[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const double v = fmin(fmax(x[j], -746.0), 709.0);
+        const double v = fmax(x[j], -746.0);
         k[j] = rint(v * 1.4426950408889634);
         r[j] = fma(-k[j], 2.3190468138462996e-17, fma(-k[j], 0.6931471805599453, v));      // ln 2 as the nearest number of 64 bits and what it leaves
         p[j] = 1.0 / 6227020800.0;
@@ -88,11 +88,17 @@ __device__ __forceinline__ void exp64(double* x) {
 #pragma unroll
     for (int j = 0; j < V; ++j) x[j] = __builtin_amdgcn_ldexp(fma(p[j], r[j], 1.0), (int)k[j]);
 }
-// 1 / x for x in [1, 2^1023]: the instruction's approximation and two steps of Newton's method.
+// 1 / x for x in [1, 1024]: the instruction's approximation and two steps of Newton's method.
 __device__ __forceinline__ double reciprocal64(double x) {
     double y = __builtin_amdgcn_rcp(x);
     y = fma(fma(-x, y, 1.0), y, y);
     return fma(fma(-x, y, 1.0), y, y);
+}
+// The sigmoid 1 / (1 + exp(-l)) from t = exp(-|l|): 1 / (1 + t), below zero t / (1 + t), which has its own value down to the smallest numbers.  0 where exp(-l) is
+// above the largest number of 64 bits, exp(709.7827...), as the definition evaluated in 64 bits is.
+__device__ __forceinline__ double sigmoid64(float l, double t) {
+    const double s = (l < 0.f ? t : 1.0) * reciprocal64(1.0 + t);
+    return (double)l < -709.782712893384 ? 0.0 : s;
 }
 
 // Running sum over the experts: offs[e] = sum of count(e') for e' < e, offs[experts] the total.  One wavefront.
@@ -161,11 +167,11 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(RouteArgs g) {
             l_top = __uint_as_float(most >> 31 ? most & 0x7FFFFFFFu : ~most);
         }
 #pragma unroll
-        for (int j = 0; j < V; ++j) s[j] = g.o.sigmoid ? -(double)l[j] : (double)l[j] - l_top;
+        for (int j = 0; j < V; ++j) s[j] = g.o.sigmoid ? -fabs((double)l[j]) : (double)l[j] - l_top;
         exp64<V>(s);
         if (g.o.sigmoid) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) s[j] = l[j] == -__builtin_huge_valf() ? 0.0 : reciprocal64(1.0 + s[j]);
+            for (int j = 0; j < V; ++j) s[j] = sigmoid64(l[j], s[j]);
         } else {
             double sum = 0.0;
 #pragma unroll
@@ -341,12 +347,12 @@ __global__ __launch_bounds__(kManyWaves * 64) void route_many_kernel(RouteArgs g
         l_top = __uint_as_float(most >> 31 ? most & 0x7FFFFFFFu : ~most);
     }
 #pragma unroll
-    for (int j = 0; j < V; ++j) s[j] = g.o.sigmoid ? -(double)l[j] : (double)l[j] - l_top;
+    for (int j = 0; j < V; ++j) s[j] = g.o.sigmoid ? -fabs((double)l[j]) : (double)l[j] - l_top;
 #pragma unroll
     for (int j = 0; j < V; j += 4) exp64<4>(s + j);
     if (g.o.sigmoid) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) s[j] = l[j] == -__builtin_huge_valf() ? 0.0 : reciprocal64(1.0 + s[j]);
+        for (int j = 0; j < V; ++j) s[j] = sigmoid64(l[j], s[j]);
     } else {
         double sum = 0.0;
 #pragma unroll

@@ -358,6 +358,39 @@ def test_route_many_rows_with_ties(ctx, rows, sigmoid, experts, k, opts):
     check_routed(logits, routed(ctx, logits, k, **opts), k, **opts)
 
 
+# rows whose logits all lie where 64 bits end: exp(-l) is finite down to -709.78265380859375 in 32 bits, infinite from the next number on
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("rows", [19, 80])
+def test_route_far_below_zero(ctx, rows, sigmoid, dtype):
+    lowest = float(torch.finfo(dtype).min)
+    far = [-700.0, -705.0, -708.0, -709.5, -709.78265380859375, -709.78271484375, -710.0, -712.0, -715.0, -720.0, -725.0, -730.0, -736.0, -740.0, -744.0, -745.0, -746.0, -750.0,
+           -760.0, -1e3, -1e4, -1e9, -3e38, lowest]
+    experts = len(far)
+    logits = torch.full((rows, experts), lowest)
+    g = torch.Generator().manual_seed(rows)
+    logits[0] = torch.tensor(far)
+    logits[1] = torch.tensor(far)[torch.randperm(experts, generator=g)]
+    logits[2, 4:12] = torch.tensor([-720.0, -730.0, -740.0, -715.0, -716.0, -717.0, -718.0, -719.0])
+    logits[3] = torch.arange(experts) * -2.0 - 690.0
+    logits[4] = -1e9
+    logits[5] = torch.arange(experts) * -1e4 - 1e4
+    logits[6] = torch.tensor(far)
+    logits[6, 3::5] = torch.arange(5) * 1.5 - 2.0                                # ordinary ones among them
+    logits[7] = -709.0
+    logits[8] = -float("inf")
+    logits[8, :4] = torch.tensor([-705.0, -715.0, -1000.0, lowest])
+    logits[9, :2] = 3.0                                                          # the rest is masked with the lowest number, and some of it has to be chosen
+    for t in range(11, rows):
+        logits[t] = torch.tensor(far)[torch.randint(0, experts, (experts,), generator=g)]        # row 10 is masked altogether
+    logits = logits.to(dtype).to(DEV)
+    b = (torch.randint(-1, 2, (experts,), generator=g).float() * 0.25).to(DEV)
+    for bias in (None, b):
+        for opts in (dict(), dict(renormalize=False), dict(groups=4, top_groups=2, group_top=2), dict(groups=6, top_groups=3)):
+            opts = dict(opts, bias=bias, sigmoid=sigmoid, scale=2.5)
+            check_routed(logits, routed(ctx, logits, 6, **opts), 6, **opts)
+
+
 def test_route_scale_that_is_changed_in_place(ctx):
     logits, scale = torch.randn(5, 8, generator=torch.Generator().manual_seed(2)).to(DEV), torch.tensor(2.0)
     for value in (2.0, 3.0):
