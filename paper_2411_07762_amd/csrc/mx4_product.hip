@@ -27,6 +27,7 @@ struct MxArgs {
     int64_t la_ld, lb_ld;                                   // their rows: r and n, or what they are padded to
     float* P; int parts, part_words, rp;                    // few rows: [part][position][rp] fp32, rp: r rounded up to 16
     uint16_t* planes; int lr_steps;                         // many rows: [term][position][32 lr_steps / terms] bf16; steps of 32 ranks and one term
+    float* exact; uint8_t* marks;                           // and P itself, fp32, [position][32 lr_steps / terms], where terms do not hold it: [position][8], a byte for 16 ranks
     void* Y; int64_t ldy; int64_t outs;                     // columns of Y
     bool vec;                                               // 16 bytes (few rows: four columns) of Y at a time
     bool la_four;                                           // four ranks of L_A in a load
@@ -66,7 +67,9 @@ __device__ __forceinline__ void store4(const MxArgs& g, int64_t p, int64_t o, co
 // 16 NT positions and 16 RF ranks a workgroup; W wavefronts share a part of the channels, a word at a time with the loads of U words in flight.  Ranks are in the
 // rows of the accumulator; tokens become bf16 on the way, exactly.
 // TERMS = 0, few rows: fp32 sums of the part.  L_B goes into the registers as it is: of each of a word's four blocks lane group q = lane / 16 has channels 8 q .. + 7.
-// Otherwise the sum (of one part) as so many bf16 terms, each what the ones before leave, rounded; lane group q has block q, and L_B is turned through LDS: lanes next to each
+// Otherwise the sum (of one part) as so many bf16 terms, each what the ones before leave, rounded: three hold its 24 bits, two (for bf16 outputs) leave 2^-17 of it.  Where they do
+// not (below 1e-33 or so bits fall under the smallest bf16 value, the largest numbers round to an infinity) a token's 16 sums are marked and kept in fp32, and their terms are zeros.
+// Lane group q has block q, and L_B is turned through LDS: lanes next to each
 // other in the matrix instruction have different rows, and a load of 16 bytes from 64 places occupies a compute unit's address unit for 64 cycles where one of four rows'
 // 256 bytes takes 16.  Without that 4099 tokens of 4096 channels and 64 ranks take 25 us; with L_B put in order by a launch of its own 10 and 4.7.  Latency bounds it: 16 ranks of 32
 // tokens and two words ahead, two workgroups a compute unit, take 10.8; 32 ranks and four words, one workgroup, 12.8; eight wavefronts 13 to 15; 64 tokens 11.6 to 12.5.
@@ -172,24 +175,34 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
         f32x4_t sum = mine[i * 64];
 #pragma unroll
         for (int w = 1; w < W; ++w) sum += mine[(w * RF * NT + i) * 64];
-        const int k = 16 * (rt * RF + i / NT) + 4 * q, at = 16 * (i % NT) + li;
-        if (at >= rows) continue;
+        const int tile = rt * RF + i / NT, k = 16 * tile + 4 * q, at = 16 * (i % NT) + li;
 #pragma unroll
         for (int u = 0; u < 4; ++u)
             if (k + u >= g.r) sum[u] = 0.f;
         if (TERMS == 0) {
-            if (k < g.rp) *(f32x4_t*)(g.P + ((int64_t)pt * g.groups.positions + p0 + at) * g.rp + k) = sum;
+            if (at < rows && k < g.rp) *(f32x4_t*)(g.P + ((int64_t)pt * g.groups.positions + p0 + at) * g.rp + k) = sum;
             continue;
         }
         const int64_t width = g.lr_steps / (TERMS ? TERMS : 1) * 32;
-        if (k >= width) continue;
+        if (16 * tile >= width) continue;
+        const f32x4_t whole = sum;
+        uint2 term[TERMS ? TERMS : 1];
+#pragma unroll
+        for (int u = 0; u < TERMS; ++u) {
+            term[u] = make_uint2(bf16_pair(sum[0], sum[1]), bf16_pair(sum[2], sum[3]));
+            sum -= f32x4_t{__uint_as_float(term[u].x << 16), __uint_as_float(term[u].x & 0xFFFF0000u), __uint_as_float(term[u].y << 16), __uint_as_float(term[u].y & 0xFFFF0000u)};
+        }
+        bool held = true;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) held = held && fabsf(sum[u]) <= (TERMS == 3 ? 0.f : 0x1p-17f * fabsf(whole[u]));      // not so for infinities and NaN
+        const uint64_t lost = __ballot(!held);
+        if (at >= rows) continue;
+        const bool mark = (lost >> li) & 0x0001000100010001u;        // by the token's 16 sums, so that the other tokens of the tile do not matter
         uint16_t* dst = g.planes + (p0 + at) * width + k;
 #pragma unroll
-        for (int u = 0; u < TERMS; ++u, dst += g.groups.positions * width) {
-            const uint32_t w0 = bf16_pair(sum[0], sum[1]), w1 = bf16_pair(sum[2], sum[3]);
-            *(uint2*)dst = make_uint2(w0, w1);
-            sum -= f32x4_t{__uint_as_float(w0 << 16), __uint_as_float(w0 & 0xFFFF0000u), __uint_as_float(w1 << 16), __uint_as_float(w1 & 0xFFFF0000u)};
-        }
+        for (int u = 0; u < TERMS; ++u, dst += g.groups.positions * width) *(uint2*)dst = mark ? make_uint2(0u, 0u) : term[u];
+        if (mark) *(f32x4_t*)(g.exact + (p0 + at) * width + k) = whole;
+        if (q == 0) g.marks[(p0 + at) * 8 + tile] = mark;
     }
 }
 
@@ -574,7 +587,45 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
     int s = 0;
     for (; s + ST - 1 < words; ++s) step(s, std::true_type{}, std::false_type{});
     for (; s < words; ++s) step(s, std::false_type{}, std::false_type{});
-    for (; s < steps; ++s) step(s, std::false_type{}, std::true_type{});
+    if (g.lr_steps) {
+        // sums of P that terms do not hold: the marks of this lane's positions, looked at when the steps of ranks are through
+        uint64_t marked[NF], some = 0;
+#pragma unroll
+        for (int j = 0; j < NF; ++j) marked[j] = ((const uint64_t*)g.marks)[token_row(wb * 32 * NF + 32 * j + li)];
+        for (; s < steps; ++s) step(s, std::false_type{}, std::true_type{});
+#pragma unroll
+        for (int j = 0; j < NF; ++j) {
+            marked[j] = wb * 32 * NF + 32 * j + li < rows ? marked[j] & (~(uint64_t)0 >> (64 - 16 * (g.lr_steps / TERMS))) : 0;      // the bytes that were written
+            some |= marked[j];
+        }
+        if (__ballot(some != 0)) {
+            // rare: these by the fp32 instruction, half h of the lanes the second of two ranks; other positions get zeros.  A whole call of such rows takes twice as long (4099 x 4096 x
+            // 14336, rank 64: 189 us to 352); the look whether there are any 0.2 % where the marks are on their way during the steps of ranks (loaded behind them 2 %)
+            const int64_t width = 32 * (int64_t)(g.lr_steps / TERMS);
+#pragma unroll 1
+            for (int k0 = 0; k0 < g.r; k0 += 2) {
+                const int k = k0 + h;
+                float a[MF], b[NF];
+                bool has = false;
+#pragma unroll
+                for (int j = 0; j < NF; ++j) {
+                    const bool mine = k < g.r && (marked[j] >> (8 * (k >> 4)) & 1);
+                    b[j] = mine ? g.exact[(p0 + wb * 32 * NF + 32 * j + li) * width + k] : 0.f;
+                    has = has || mine;
+                }
+                if (!__ballot(has)) continue;
+#pragma unroll
+                for (int i = 0; i < MF; ++i) {
+                    const uint16_t* const row = g.la + ((int64_t)e * g.m + weight_row(wa * 32 * MF + 32 * i + li)) * g.la_ld;
+                    a[i] = k < g.r ? __uint_as_float((uint32_t)row[k] << 16) : 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < MF; ++i)
+#pragma unroll
+                    for (int j = 0; j < NF; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[j], acc[i][j], 0, 0, 0);
+            }
+        }
+    }
 
     // acc[i][j][k]: output 32 i + 8 (k / 4) + 4 h + k % 4, position 32 j + li of the wavefront's.  They are turned through the wavefront's part of the ring, as many
     // positions at a time as it holds, so that rows of Y are written in whole lines; the 16-byte chunks of a row change places by the row, which keeps both the writes
@@ -726,7 +777,7 @@ Plan plan_product(int64_t positions, int64_t n, int64_t m, int32_t count, int32_
     if (r <= 0) return p;
     p.lb_bytes = align_up((size_t)count * r * align_up(n, 8) * 2, 256);
     if (p.many) {
-        p.p_bytes = align_up((size_t)positions * align_up(r, 32) * 2 * 3, 256);
+        p.p_bytes = align_up((size_t)positions * align_up(r, 32) * (3 * 2 + 4) + (size_t)positions * 8, 256);      // terms, sums, marks
         p.la_bytes = align_up((size_t)count * m * align_up(r, 32) * 2, 256);
     } else {
         p.p_bytes = align_up((size_t)p.parts * positions * align_up(r, 16) * 4, 256);
@@ -804,6 +855,8 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
         const int terms = f32 ? 3 : 2, width = (int)align_up(r, 32);
         g.planes = (uint16_t*)p_room;
         g.lr_steps = width / 32 * terms;
+        g.exact = (float*)(g.planes + groups.positions * width * 3);
+        g.marks = (uint8_t*)(g.exact + groups.positions * width);
         ASER_TRY(f32 ? (launch_down<1, 2, 4, 2, 3>(ctx, g)) : (launch_down<1, 2, 4, 2, 2>(ctx, g)));
         if (r != width || ((uintptr_t)L_A & 15)) {
             uint16_t* const padded = (uint16_t*)(p_room + p.p_bytes);
