@@ -67,7 +67,8 @@ __device__ __forceinline__ void store4(const MxArgs& g, int64_t p, int64_t o, co
 // 16 NT positions and 16 RF ranks a workgroup; W wavefronts share a part of the channels, a word at a time with the loads of U words in flight.  Ranks are in the
 // rows of the accumulator; tokens become bf16 on the way, exactly.
 // TERMS = 0, few rows: fp32 sums of the part.  L_B goes into the registers as it is: of each of a word's four blocks lane group q = lane / 16 has channels 8 q .. + 7.
-// Otherwise the sum (of one part) as so many bf16 terms, each what the ones before leave, rounded: three hold its 24 bits, two (for bf16 outputs) leave 2^-17 of it.  Where they do
+// Otherwise the sum (of one part) as so many bf16 terms, each what the ones before leave, rounded: three hold its 24 bits, two leave 2^-17 of it, and are taken for
+// bf16 outputs, whose own rounding is 2^-8 (a third would be half as many steps of ranks again).  Where they do
 // not (below 1e-33 or so bits fall under the smallest bf16 value, the largest numbers round to an infinity) a token's 16 sums are marked and kept in fp32, and their terms are zeros.
 // Lane group q has block q, and L_B is turned through LDS: lanes next to each
 // other in the matrix instruction have different rows, and a load of 16 bytes from 64 places occupies a compute unit's address unit for 64 cycles where one of four rows'

@@ -7,7 +7,7 @@ import numpy as np
 
 from oracle import mx4_oracle as orc
 
-ENDS = {"small": ((0, -60, -100, -112, -118, -122), 20), "large": ((0, 60, 118, 126, 127), -14)}
+ENDS = {"middle": ((0, -20, 30), -2), "small": ((0, -60, -100, -112, -118, -122), 20), "large": ((0, 60, 118, 126, 127), -14)}
 
 
 def ranks_alone(rng, rows, n, m, r, end, swiglu=False, tokens=None):
