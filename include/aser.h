@@ -533,7 +533,7 @@ int aser_mx4_quantize(aser_ctx* ctx, const void* X, int x_dtype, int64_t ldx, co
  * tokens whose scale bytes are at most 252, as the quantizer's are.  What multiplies L_A is P with all its 24 bits, but for bf16 Y and many rows (more than 64 for each matrix, and
  * enough outputs): there it is P to within 2^-17 of it, as two bf16 terms, at both ends of the range as well.  A NaN
  * block of a token is its row's, one of a weight its output's.  Deterministic.  Asynchronous.  rows == 0 is a no-op.
- * Needs aser_mx4_forward_workspace_bytes(T, n, m, r) bytes of workspace. */
+ * Needs aser_mx4_forward_workspace_bytes(T, n, m, r) bytes of workspace, which no smaller T needs more of. */
 size_t aser_mx4_forward_workspace_bytes(int64_t rows, int64_t n, int64_t m, int32_t r);
 int aser_mx4_forward(aser_ctx* ctx, const aser_mx4* x, const aser_mx4* w, const uint16_t* L_A, const uint16_t* L_B, int32_t r,
                      int32_t swiglu, void* Y, int32_t y_dtype, int64_t ldy);
@@ -579,7 +579,7 @@ int aser_route_experts(aser_ctx* ctx, const void* logits, int32_t x_dtype, int64
 /* aser_mx4_forward of every position with its expert: w has n_experts matrices, L_A (n_experts x m x r) and L_B (n_experts x r x n)
  * as many.  Row p of Y is position p (rows * top_k rows).  gather != 0: position p reads row order[p] / top_k of x, which has a row for each
  * token; 0: row p of x, which has rows * top_k.  Rows of Y behind offsets[n_experts] are left as they are.
- * Needs aser_expert_forward_workspace_bytes(rows * top_k, n, m, n_experts, r) bytes of workspace. */
+ * Needs aser_expert_forward_workspace_bytes(rows * top_k, n, m, n_experts, r) bytes of workspace, which no smaller rows * top_k needs more of. */
 size_t aser_expert_forward_workspace_bytes(int64_t positions, int64_t n, int64_t m, int32_t n_experts, int32_t r);
 int aser_expert_forward(aser_ctx* ctx, const aser_mx4* x, const aser_mx4* w, const aser_expert_plan* plan, int32_t gather,
                         const uint16_t* L_A, const uint16_t* L_B, int32_t r, int32_t swiglu, void* Y, int32_t y_dtype, int64_t ldy);

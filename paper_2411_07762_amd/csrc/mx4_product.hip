@@ -777,11 +777,15 @@ Plan plan_product(int64_t positions, int64_t n, int64_t m, int32_t count, int32_
     if (p.many && experts) p.x_bytes = align_up((size_t)mx4_size(positions, words) * 68, 256);
     if (r <= 0) return p;
     p.lb_bytes = align_up((size_t)count * r * align_up(n, 8) * 2, 256);
+    // Few rows, P: parts x positions, but what any fewer positions need as well, so that who asks for the largest batch has room for all: parts are at most 256 / tiles rounded up,
+    // (255 + tiles) / tiles, of tiles of 16 positions
+    const int64_t most_parts = words > 8 * kMostParts ? kMostParts : ceil_div64(words, 8);
+    const int64_t sums = most_parts * positions < positions + 255 * 16 ? most_parts * positions : positions + 255 * 16;
+    p.p_bytes = align_up((size_t)sums * align_up(r, 16) * 4, 256);
     if (p.many) {
-        p.p_bytes = align_up((size_t)positions * align_up(r, 32) * (3 * 2 + 4) + (size_t)positions * 8, 256);      // terms, sums, marks
+        const size_t bytes = align_up((size_t)positions * align_up(r, 32) * (3 * 2 + 4) + (size_t)positions * 8, 256);      // terms, sums, marks
+        if (p.p_bytes < bytes) p.p_bytes = bytes;
         p.la_bytes = align_up((size_t)count * m * align_up(r, 32) * 2, 256);
-    } else {
-        p.p_bytes = align_up((size_t)p.parts * positions * align_up(r, 16) * 4, 256);
     }
     return p;
 }

@@ -251,3 +251,14 @@ def test_inputs_for_ranks_tell_terms_apart(end):
             with np.errstate(all="ignore"):
                 held = np.abs(mx4_ranks.terms(P, count) @ L_A.T - Z) <= mx4_ranks.off(S, Z, bf16, True, False)
             assert held[there].all() == (count >= enough and end == "middle"), (bf16, count)
+
+
+@pytest.mark.parametrize("n,m,r,experts", [(4096, 512, 64, 1), (4096, 1024, 64, 64), (4096, 14336, 32, 8), (1000, 48, 128, 1), (300, 6000, 1, 3), (128, 64, 16, 1024), (8192, 2048, 0, 16)])
+def test_workspace_for_the_largest_batch_is_enough_for_the_others(n, m, r, experts):
+    """A caller who asks for the largest number of rows has what every smaller one needs."""
+    lib = aser.load_library()
+    rows = list(range(1, 5000)) + [5000 + 37 * i for i in range(1500)]
+    for need in ([lib.aser_mx4_forward_workspace_bytes(t, n, m, r) for t in rows], [lib.aser_expert_forward_workspace_bytes(t, n, m, experts, r) for t in rows],
+                 [lib.aser_route_workspace_bytes(t, experts, 1) for t in rows]):
+        falls = [(t, b - a) for t, a, b in zip(rows[1:], need, need[1:]) if b < a]
+        assert not falls, falls[:3]
