@@ -524,7 +524,7 @@ int launch_route_many(aser_ctx* ctx, const RouteArgs& g, bool f32) {
 struct CombineArgs {
     const void* Y; int64_t ldy, m;
     const int32_t* place; const float* weights;
-    int64_t positions;
+    int64_t rows, positions;
     int top_k;
     const void* Y0; int64_t ldy0;
     void* out; int64_t ldo;
@@ -559,8 +559,8 @@ __device__ __forceinline__ void eight(const void* p, int64_t at, int here, bool 
 // A workgroup has 2048 columns of a token, a thread eight.
 template <bool YF32, bool OF32>
 __global__ __launch_bounds__(256) void combine_kernel(CombineArgs g) {
-    const int64_t t = blockIdx.x, c = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 8;
-    if (c >= g.m) return;
+    const int64_t t = blockIdx.z * kMxAcross + blockIdx.x, c = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 8;
+    if (t >= g.rows || c >= g.m) return;
     const int here = (int)(g.m - c < 8 ? g.m - c : 8);
     float sum[8];
     if (g.Y0) eight<OF32>(g.Y0, t * g.ldy0 + c, here, g.vec, sum);
@@ -671,9 +671,9 @@ extern "C" int aser_expert_combine(aser_ctx* ctx, const void* Y, int32_t y_dtype
     const bool yf = y_dtype == ASER_DTYPE_F32, of = out_dtype == ASER_DTYPE_F32;
     if (((uintptr_t)Y & (yf ? 3 : 1)) || (((uintptr_t)Y0 | (uintptr_t)out) & (of ? 3 : 1))) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "expert_combine: misaligned pointer");
     if (plan->rows == 0) return ASER_OK;
-    CombineArgs g{Y, ldy, m, plan->place, plan->weights, plan->rows * plan->top_k, plan->top_k, Y0, ldy0, out, ldo, false};
+    CombineArgs g{Y, ldy, m, plan->place, plan->weights, plan->rows, plan->rows * plan->top_k, plan->top_k, Y0, ldy0, out, ldo, false};
     g.vec = row16(Y, ldy, yf ? 4 : 2) && row16(out, ldo, of ? 4 : 2) && (!Y0 || row16(Y0, ldy0, of ? 4 : 2));
-    const dim3 grid((unsigned)plan->rows, (unsigned)ceil_div64(m, 2048));
+    const dim3 grid((unsigned)(plan->rows < kMxAcross ? plan->rows : kMxAcross), (unsigned)ceil_div64(m, 2048), (unsigned)ceil_div64(plan->rows, kMxAcross));
     ASER_TRY(aser_prepare_device(ctx));
     if (yf) of ? combine_kernel<true, true><<<grid, 256, 0, ctx->stream>>>(g) : combine_kernel<true, false><<<grid, 256, 0, ctx->stream>>>(g);
     else of ? combine_kernel<false, true><<<grid, 256, 0, ctx->stream>>>(g) : combine_kernel<false, false><<<grid, 256, 0, ctx->stream>>>(g);

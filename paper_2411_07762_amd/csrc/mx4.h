@@ -4,6 +4,10 @@
 
 static const int64_t kMxWord = 128;         // channels of a scale word: four blocks of 32, 64 bytes of codes
 
+// A dimension of a launch has fewer than 2^32 threads.  Where more are wanted, workgroups are numbered over two dimensions, kMxAcross of them in the first.
+static const int64_t kMxAcross = (int64_t)1 << 23;
+static inline bool mx4_fits(int64_t workgroups, int64_t threads) { return workgroups <= (int64_t)UINT32_MAX / threads; }
+
 static inline int64_t mx4_words(int64_t n) { return ceil_div64(n, kMxWord); }
 // Rows are in panels of 16: the word of scales of a row is at mx4_at, in words, the following one kMxNext further; the 16 bytes of codes of block q are at
 // 16 mx4_code + 256 q bytes, those of the following word 64 kMxNext bytes further.  Matrix e begins e mx4_size words and 64 times as many bytes behind the first.

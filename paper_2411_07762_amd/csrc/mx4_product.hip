@@ -711,7 +711,7 @@ int launch_tile_one(aser_ctx* ctx, const MxArgs& g) {
     const auto kernel = mx4_tile_kernel<MF, NF, ST, WG, GATED, F32>;
     ASER_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds));
     const int64_t out_tiles = ceil_div64(g.outs, GATED ? 32 * MF : 64 * MF), grid = ceil_div64(g.groups.most_tiles(64 * NF) * out_tiles, 8) * 8;
-    if (grid > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: too many rows times outputs");
+    if (!mx4_fits(grid, 256)) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: too many rows times outputs");
     kernel<<<(unsigned)grid, 256, kLds, ctx->stream>>>(g, (uint32_t)out_tiles);
     return aser_check_launch(ctx, "mx4_tile_kernel");
 }
@@ -792,7 +792,7 @@ Plan plan_product(int64_t positions, int64_t n, int64_t m, int32_t count, int32_
 
 int pad_rows(aser_ctx* ctx, const uint16_t* f, int64_t rows, int64_t r, int64_t width, uint16_t* out) {
     const int64_t grid = ceil_div64(rows * width, 2048);
-    if (grid > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: the factors are too large");
+    if (!mx4_fits(grid, 256)) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: the factors are too large");
     mx4_pad_kernel<<<(unsigned)grid, 256, 0, ctx->stream>>>(f, rows, r, width, out);
     return aser_check_launch(ctx, "mx4_pad_kernel");
 }
@@ -801,7 +801,7 @@ template <int RF, int NT, int W, int U, int TERMS>
 int launch_down(aser_ctx* ctx, const MxArgs& g) {
     const int rank_tiles = (int)ceil_div64(TERMS ? g.lr_steps / (TERMS ? TERMS : 1) * 32 : g.rp, 16 * RF);
     const int64_t grid = g.groups.most_tiles(16 * NT) * g.parts * rank_tiles;
-    if (grid > INT32_MAX) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: too many rows");
+    if (!mx4_fits(grid, 64 * W)) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: too many rows");
     mx4_down_kernel<RF, NT, W, U, TERMS><<<(unsigned)grid, 64 * W, (size_t)W * RF * 1024 * (TERMS && NT < 4 ? 4 : NT), ctx->stream>>>(g, rank_tiles);
     return aser_check_launch(ctx, "mx4_down_kernel");
 }
@@ -820,6 +820,7 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
     if (groups.positions == 0) return ASER_OK;
     if (!Y) ASER_FAIL(ctx, ASER_ERR_INVALID_ARG, "%s: null pointer", who);
     const Plan p = plan_product(groups.positions, w->n, w->rows, w->count, r, groups.offsets != nullptr);
+    if (r > 0 && p.many && !mx4_fits(groups.most_tiles(32) * (align_up(r, 32) / 16), 256)) ASER_FAIL(ctx, ASER_ERR_SHAPE, "%s: too many rows for this rank", who);
     if (p.all() > 0 && (!ctx->ws || ctx->ws_bytes < p.all() + kAserWsTail)) ASER_FAIL(ctx, ASER_ERR_WORKSPACE, "%s: workspace too small", who);
     MxArgs g{};
     g.groups = groups;

@@ -46,7 +46,7 @@ __device__ __forceinline__ float load1(const void* X, int64_t at) {
 
 template <bool F32, bool M, bool VALUES>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(QuantArgs g) {
-    const uint32_t words = (uint32_t)g.words, tile = blockIdx.x / words, word = blockIdx.x - tile * words, row = tile * 16 + (threadIdx.x >> 4);
+    const uint32_t words = (uint32_t)g.words, id = blockIdx.y * (uint32_t)kMxAcross + blockIdx.x, tile = id / words, word = id - tile * words, row = tile * 16 + (threadIdx.x >> 4);
     if (row >= (uint32_t)g.all_rows) return;                 // the same for all lanes of a group
     const int li = threadIdx.x & 15;
     const int64_t c = (int64_t)word * kMxWord + 8 * li;
@@ -121,7 +121,8 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(QuantArgs g) {
 
 template <bool F32, bool M>
 void launch(const QuantArgs& g, hipStream_t s) {
-    const unsigned grid = (unsigned)(ceil_div64(g.all_rows, 16) * g.words);
+    const int64_t workgroups = ceil_div64(g.all_rows, 16) * g.words;        // below 2^31
+    const dim3 grid((unsigned)(workgroups < kMxAcross ? workgroups : kMxAcross), (unsigned)ceil_div64(workgroups, kMxAcross));
     if (g.values) mx4_quantize_kernel<F32, M, true><<<grid, 256, 0, s>>>(g);
     else mx4_quantize_kernel<F32, M, false><<<grid, 256, 0, s>>>(g);
 }

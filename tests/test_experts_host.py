@@ -262,3 +262,9 @@ def test_workspace_for_the_largest_batch_is_enough_for_the_others(n, m, r, exper
                  [lib.aser_route_workspace_bytes(t, experts, 1) for t in rows]):
         falls = [(t, b - a) for t, a, b in zip(rows[1:], need, need[1:]) if b < a]
         assert not falls, falls[:3]
+
+
+def test_forward_refuses_more_threads_than_a_launch_takes(ctx):
+    most = (1 << 26) - 1                                                         # 2^21 tiles of 32 rows
+    assert forward(ctx, x=mx(most), r=128, a=P, b=P) == SHAPE and "too many rows" in ctx.last_error()
+    assert forward(ctx, x=mx(most), r=96, a=P, b=P) == ROOM

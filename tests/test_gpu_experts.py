@@ -613,3 +613,27 @@ def test_calibrated_layer_in_four_bits():
     # the same tokens through the weight: smoothing moves the outlier channels' share from the codes to the factors
     want = f64(values) * f64(buf.mdiag) @ f64(W).T
     assert np.linalg.norm(f64(y) - want) < 0.5 * np.linalg.norm(f64(bare) - want)
+
+
+# ------------------------------------------------------------------------------------------------ more workgroups than a dimension of a launch takes threads for
+def test_combine_more_than_2_to_the_24_rows(ctx):
+    rows, m = 2 ** 24 + 5, 8
+    y = torch.randint(-100, 100, (rows, m), device=DEV, dtype=torch.int32).to(torch.bfloat16)
+    place = torch.arange(rows - 1, -1, -1, device=DEV, dtype=torch.int32)
+    weights = torch.randint(1, 3, (rows, 1), device=DEV, dtype=torch.int32).float()
+    plan = aser.ExpertPlan(torch.zeros(rows, 1, device=DEV, dtype=torch.int32), weights, torch.tensor([0, rows], device=DEV, dtype=torch.int32), place, place)
+    out = torch.full((rows, m), 7.0, device=DEV)
+    ctx.check(aser.aser_expert_combine(ctx, y, plan, out))
+    assert torch.equal(out, y.flip(0).float() * weights)
+
+
+def test_quantize_more_than_2_to_the_24_panels(ctx):
+    rows, count = 2 ** 27 - 11, 3
+    x = torch.randint(-4, 5, (count, rows, 1), device=DEV, dtype=torch.int8).to(torch.bfloat16)
+    out, values = aser.Mx4.empty(rows, 1, count), torch.full((count, rows, 1), 7.0, device=DEV, dtype=torch.bfloat16)
+    ctx.check(aser.aser_mx4_quantize(ctx, x, out, values=values))
+    assert torch.equal(values, x)                                  # one number alone in its block is kept
+    for e in range(count):
+        for at, here in ((0, 16), (2 ** 22, 16), (rows // 16, rows % 16)):
+            want, _ = orc.quantize(x[e, 16 * at:16 * at + here].float().cpu().numpy())
+            assert np.array_equal(out.codes[e, at, 0, 0, :here, 0].cpu().numpy() & 15, want[:, 0])
