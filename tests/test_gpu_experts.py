@@ -461,6 +461,29 @@ def test_experts_plan_is_not_trusted(ctx):
         assert (full[:10] == 7).all() and (full[50:] == 7).all()
 
 
+@pytest.mark.parametrize("gather", [True, False])
+@pytest.mark.parametrize("rows,experts,m,r", [(900, 3, 2400, 0), (900, 3, 2400, 40), (1500, 20, 4200, 0), (1500, 20, 4200, 24)])
+def test_experts_plan_is_not_trusted_with_many_rows(ctx, rows, experts, m, r, gather):
+    """The same for tiles: their numbering, the rows put in order, P and its terms."""
+    rng = np.random.default_rng(rows + r)
+    k, n = 2, 256
+    pairs = rows * k
+    plan, *_ = given_plan(rng, rows, k, experts)
+    x, w = aser.Mx4.empty(rows if gather else pairs, n), aser.Mx4.empty(m, n, experts)
+    for t in (x, w):
+        t.codes.random_(0, 256)
+        t.scales.random_(120, 130)
+    a, b, *_ = factors(rng, m, n, r, experts) if r else (None,) * 4
+    ctx.ensure_workspace(aser.aser_expert_forward_workspace_bytes(pairs, n, m, experts, r))
+    full = torch.full((pairs + 600, m), 7.0, device=DEV, dtype=torch.bfloat16)
+    ends = [2 ** 31 - 1, -2 ** 31, 0, pairs, pairs - 1, 7, -1, pairs + 1, pairs // 2]
+    for offsets in (rng.integers(-2 ** 31, 2 ** 31, experts + 1), rng.choice(ends, experts + 1), np.sort(rng.integers(0, pairs + 1, experts + 1))[::-1], np.resize([0, 2 ** 31 - 1], experts + 1)):
+        plan.offsets.copy_(dev(offsets.astype(np.int32)))
+        plan.order.copy_(dev(rng.integers(-2 ** 31, 2 ** 31, pairs).astype(np.int32)))
+        ctx.check(aser.aser_expert_forward(ctx, x, w, plan, full[300:300 + pairs], gather=gather, L_A=a, L_B=b))
+        assert (full[:300] == 7).all() and (full[300 + pairs:] == 7).all()
+
+
 # ------------------------------------------------------------------------------------------------ the weighted sum
 @pytest.mark.parametrize("rows,k,m,y_type,out_type,pad,base", [
     (1, 1, 1, torch.float32, torch.float32, 0, "none"), (1, 6, 2048, torch.bfloat16, torch.bfloat16, 0, "none"), (7, 2, 100, torch.bfloat16, torch.float32, 3, "other"),
@@ -551,6 +574,37 @@ def test_layer_replayed_on_another_stream(rows, experts, k, n, m, r):
             assert torch.equal(layer.h[:used], eager.h[:used]) and used == rows * k - (k - 1)
             quantized(other, layer.x)
     assert layer.out.isfinite().all() and layer.out.abs().max() > 0
+
+
+@pytest.mark.parametrize("rows,experts,k,n,m,r", [(40, 6, 3, 384, 200, 32), (900, 4, 2, 256, 2100, 32)])
+def test_layer_replayed_beside_another_streams_work(rows, experts, k, n, m, r):
+    """Replays while another stream runs an eager layer of its own, with no wait between the two: both have the bits of quiet runs."""
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    layers = []
+    for stream, seed in ((side, rows), (other, rows + 1)):
+        with torch.cuda.stream(stream):
+            layers.append(Layer(aser.Context(0, stream.cuda_stream), np.random.default_rng(seed), rows, experts, k, n, m, r))
+            layers[-1].give(np.random.default_rng(seed + 50))
+            layers[-1].step()
+    torch.cuda.synchronize()
+    want = [layer.out.clone() for layer in layers]
+    captured, eager = layers
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        captured.step()
+    for rep in range(6):
+        torch.cuda.synchronize()
+        for layer in layers:
+            layer.out.zero_()
+        torch.cuda.synchronize()
+        for _ in range(3):
+            with torch.cuda.stream(side):
+                graph.replay()
+            with torch.cuda.stream(other):
+                eager.step()
+        torch.cuda.synchronize()
+        for layer, out in zip(layers, want):
+            assert torch.equal(layer.out, out), rep
 
 
 def test_two_contexts_at_once():
