@@ -195,7 +195,7 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(RouteArgs g) {
 #pragma unroll
             for (int j = 0; j < V; ++j)
                 if (lane + 64 * j < g.experts) mine[lane + 64 * j] = c[j];
-            __builtin_amdgcn_wave_barrier();
+            mx4_lanes_meet();
             // `per` lanes look at a group's members in turn, and join what they found
             const int per = 1 << g.per_bits, group = lane >> g.per_bits;
             double worth = kMinus, second = kMinus;
@@ -376,7 +376,7 @@ __global__ __launch_bounds__(kManyWaves * 64) void route_many_kernel(RouteArgs g
 #pragma unroll
         for (int j = 0; j < V; ++j)
             if (sub + 16 * j < g.experts) mine[sub + 16 * j] = c[j];
-        __builtin_amdgcn_wave_barrier();
+        mx4_lanes_meet();
         // `per` lanes look at a group's members in turn, and join what they found
         const int per = 1 << g.per_bits, group = sub >> g.per_bits;
         double worth = kMinus, second = kMinus;
@@ -404,7 +404,7 @@ __global__ __launch_bounds__(kManyWaves * 64) void route_many_kernel(RouteArgs g
             const int of = (int)(((float)e + 0.5f) * g.per_expert);              // e / size: far from a whole number for what e < 1024 can be
             if (e < g.experts && !((open >> (of << g.per_bits)) & 1)) c[j] = kMinus;
         }
-        __builtin_amdgcn_wave_barrier();
+        mx4_lanes_meet();
     }
     uint32_t high[V], low[V];                                    // halves of the keys, 0: not to be chosen, or chosen
 #pragma unroll
@@ -447,7 +447,7 @@ __global__ __launch_bounds__(kManyWaves * 64) void route_many_kernel(RouteArgs g
             if (e == (uint32_t)(sub + 16 * j)) high[j] = 0;
         if (sub == k) my_id = (int)e;
     }
-    __builtin_amdgcn_wave_barrier();
+    mx4_lanes_meet();
     double my_s = my_id >= 0 ? mine[my_id] : 0.0;
     const double total = row_sum(my_s);
     if (g.o.renormalize && total > 0.0) my_s /= total;

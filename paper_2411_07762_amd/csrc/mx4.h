@@ -30,6 +30,12 @@ struct MxGroups {
     }
 };
 
+// Between a wavefront's writes to LDS and other lanes' reads of them, and back: LDS serves a wavefront's accesses in order, so that the compiler has to keep it is all that is wanted.
+__device__ __forceinline__ void mx4_lanes_meet() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // The sum over the lanes up to this one, by moves within rows of 16 lanes and from the last of a row to the following rows.  Every workgroup begins with this: with shuffles through
 // LDS 48 rows on 64 experts, 1408 x 2048, take 33.1 us instead of 32.0.
 __device__ __forceinline__ uint32_t mx4_sums_upto(uint32_t v) {

@@ -133,12 +133,12 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
             for (int f = 0; f < RF; ++f)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) *(uint4*)(turn + (16 * f + 4 * j + q) * 256 + ((li ^ (4 * j + q)) << 4)) = a[u][f][j];
-            __builtin_amdgcn_wave_barrier();
+            mx4_lanes_meet();
 #pragma unroll
             for (int f = 0; f < RF; ++f)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) a[u][f][j] = *(const uint4*)(turn + (16 * f + li) * 256 + (((4 * q + j) ^ li) << 4));
-            __builtin_amdgcn_wave_barrier();
+            mx4_lanes_meet();
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -657,7 +657,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
                     else *(uint2*)(row + 16 * chunk_of(li, o / 8) + 8 * h) = make_uint2(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]));
                 }
         }
-        __builtin_amdgcn_wave_barrier();
+        mx4_lanes_meet();
         constexpr int EACH = 16 / SIZE, ROWS = 64 / CHUNKS;  // outputs of a lane, rows an instruction
         const int c = lane % CHUNKS, o = c * EACH, r0 = lane / CHUNKS, base = wb * 32 * NF + 32 * j0;
         char* dst = (char*)g.Y + ((p0 + base + r0) * g.ldy + ow + o) * SIZE;
@@ -682,7 +682,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WG, WG))) v
                 }
             }
         }
-        __builtin_amdgcn_wave_barrier();
+        mx4_lanes_meet();
     }
 }
 
