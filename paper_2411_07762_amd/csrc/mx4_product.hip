@@ -64,7 +64,7 @@ __device__ __forceinline__ void store4(const MxArgs& g, int64_t p, int64_t o, co
 }
 
 // ---------------------------------------------------------------------------------------------------------------- P = x L_B^T
-// 16 NT positions and 16 RF ranks a workgroup; W wavefronts share a part of the channels, a word at a time with the loads of U words in flight.  Ranks are in the
+// 16 NT positions and 16 ranks a workgroup; W wavefronts share a part of the channels, a word at a time with the loads of U words in flight.  Ranks are in the
 // rows of the accumulator; tokens become bf16 on the way, exactly.
 // TERMS = 0, few rows: fp32 sums of the part.  L_B goes into the registers as it is: of each of a word's four blocks lane group q = lane / 16 has channels 8 q .. + 7.
 // Otherwise the sum (of one part) as so many bf16 terms, each what the ones before leave, rounded: three hold its 24 bits, two leave 2^-17 of it, and are taken for
@@ -74,9 +74,9 @@ __device__ __forceinline__ void store4(const MxArgs& g, int64_t p, int64_t o, co
 // other in the matrix instruction have different rows, and a load of 16 bytes from 64 places occupies a compute unit's address unit for 64 cycles where one of four rows'
 // 256 bytes takes 16.  Without that 4099 tokens of 4096 channels and 64 ranks take 25 us; with L_B put in order by a launch of its own 10 and 4.7.  Latency bounds it: 16 ranks of 32
 // tokens and two words ahead, two workgroups a compute unit, take 10.8; 32 ranks and four words, one workgroup, 12.8; eight wavefronts 13 to 15; 64 tokens 11.6 to 12.5.
-template <int RF, int NT, int W, int U, int TERMS>
+template <int NT, int W, int U, int TERMS>
 __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_tiles) {
-    extern __shared__ __align__(16) float part[];            // the wavefronts' rows of L_B, then the sums, [wavefront][fragment][lane][4]
+    extern __shared__ __align__(16) float part[];            // the wavefronts' rows of L_B, then the sums, [wavefront][tokens][lane][4]
     constexpr bool TURNED = TERMS > 0;
     const int lane = threadIdx.x & 63, li = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -91,23 +91,20 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
         xat[t] = mx4_at(row, g.words);
         xcode[t] = mx4_code(row, g.words) * 16;
     }
-    const uint16_t* lrow[TURNED ? 4 * RF : RF];              // ranks that are not there: the last one again, and what becomes of them is not kept
-    f32x4_t acc[RF][NT];
+    const uint16_t* lrow[TURNED ? 4 : 1];                    // ranks that are not there: the last one again, and what becomes of them is not kept
+    f32x4_t acc[NT];
 #pragma unroll
-    for (int f = 0; f < RF; ++f) {
+    for (int t = 0; t < NT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int t = 0; t < NT; ++t) acc[f][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < (TURNED ? 4 : 1); ++j) {         // turned: load 4 f + j has four rows, a lane a sixteenth of one's word
-            const int k = 16 * (rt * RF + f) + (TURNED ? 4 * j + q : li);
-            lrow[TURNED ? 4 * f + j : f] = g.lb + ((int64_t)e * g.r + (k < g.r ? k : g.r - 1)) * g.lb_ld;
-        }
+    for (int j = 0; j < (TURNED ? 4 : 1); ++j) {             // turned: load j has four rows, a lane a sixteenth of one's word
+        const int k = 16 * rt + (TURNED ? 4 * j + q : li);
+        lrow[j] = g.lb + ((int64_t)e * g.r + (k < g.r ? k : g.r - 1)) * g.lb_ld;
     }
-    char* const turn = (char*)part + wave * (RF * 16 * 256);
+    char* const turn = (char*)part + wave * (16 * 256);
     const int first = pt * g.part_words, last = first + g.part_words < g.words ? first + g.part_words : g.words;
     v4i_t codes[U][NT];
     uint32_t scale[U][NT];
-    uint4 a[U][RF][4];
+    uint4 a[U][4];
     auto load = [&](int u, int w) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -123,21 +120,16 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int64_t at = c0 + (TURNED ? 0 : 32 * j), c = at < g.lb_ld ? at : g.lb_ld - 8;
-#pragma unroll
-            for (int f = 0; f < RF; ++f) a[u][f][j] = *(const uint4*)(lrow[TURNED ? 4 * f + j : f] + c);
+            a[u][j] = *(const uint4*)(lrow[TURNED ? j : 0] + c);
         }
     };
     auto multiply = [&](int u) {
         if (TURNED) {                                        // the sixteenths of a row change places by the row: neither writes nor reads meet on a bank
 #pragma unroll
-            for (int f = 0; f < RF; ++f)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) *(uint4*)(turn + (16 * f + 4 * j + q) * 256 + ((li ^ (4 * j + q)) << 4)) = a[u][f][j];
+            for (int j = 0; j < 4; ++j) *(uint4*)(turn + (4 * j + q) * 256 + ((li ^ (4 * j + q)) << 4)) = a[u][j];
             mx4_lanes_meet();
 #pragma unroll
-            for (int f = 0; f < RF; ++f)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) a[u][f][j] = *(const uint4*)(turn + (16 * f + li) * 256 + (((4 * q + j) ^ li) << 4));
+            for (int j = 0; j < 4; ++j) a[u][j] = *(const uint4*)(turn + li * 256 + (((4 * q + j) ^ li) << 4));
             mx4_lanes_meet();
         }
 #pragma unroll
@@ -149,8 +141,7 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
                 const bf16x2_t v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 1),
                                v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w4, by, 3);
                 const bf16x8_t b = {v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
-#pragma unroll
-                for (int f = 0; f < RF; ++f) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a[u][f][j]), b, acc[f][t], 0, 0, 0);
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a[u][j]), b, acc[t], 0, 0, 0);
             }
     };
     const int count = first + wave < last ? (last - first - wave + W - 1) / W : 0;
@@ -168,24 +159,21 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
     f32x4_t* const mine = (f32x4_t*)part + lane;
     if (TURNED) __syncthreads();
 #pragma unroll
-    for (int f = 0; f < RF; ++f)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) mine[(wave * RF * NT + f * NT + t) * 64] = acc[f][t];
+    for (int t = 0; t < NT; ++t) mine[(wave * NT + t) * 64] = acc[t];
     __syncthreads();
-    for (int i = wave; i < RF * NT; i += W) {                // ranks 16 f + 4 q .. + 3 of token li
+    for (int i = wave; i < NT; i += W) {                     // ranks 4 q .. + 3 of token li
         f32x4_t sum = mine[i * 64];
 #pragma unroll
-        for (int w = 1; w < W; ++w) sum += mine[(w * RF * NT + i) * 64];
-        const int tile = rt * RF + i / NT, k = 16 * tile + 4 * q, at = 16 * (i % NT) + li;
+        for (int w = 1; w < W; ++w) sum += mine[(w * NT + i) * 64];
+        const int k = 16 * rt + 4 * q, at = 16 * i + li;
 #pragma unroll
         for (int u = 0; u < 4; ++u)
             if (k + u >= g.r) sum[u] = 0.f;
         if (TERMS == 0) {
-            if (at < rows && k < g.rp) *(f32x4_t*)(g.P + ((int64_t)pt * g.groups.positions + p0 + at) * g.rp + k) = sum;
+            if (at < rows) *(f32x4_t*)(g.P + ((int64_t)pt * g.groups.positions + p0 + at) * g.rp + k) = sum;
             continue;
         }
         const int64_t width = g.lr_steps / (TERMS ? TERMS : 1) * 32;
-        if (16 * tile >= width) continue;
         const f32x4_t whole = sum;
         uint2 term[TERMS ? TERMS : 1];
 #pragma unroll
@@ -203,7 +191,7 @@ __global__ __launch_bounds__(64 * W) void mx4_down_kernel(MxArgs g, int rank_til
 #pragma unroll
         for (int u = 0; u < TERMS; ++u, dst += g.groups.positions * width) *(uint2*)dst = mark ? make_uint2(0u, 0u) : term[u];
         if (mark) *(f32x4_t*)(g.exact + (p0 + at) * width + k) = whole;
-        if (q == 0) g.marks[(p0 + at) * 8 + tile] = mark;
+        if (q == 0) g.marks[(p0 + at) * 8 + rt] = mark;
     }
 }
 
@@ -797,12 +785,12 @@ int pad_rows(aser_ctx* ctx, const uint16_t* f, int64_t rows, int64_t r, int64_t 
     return aser_check_launch(ctx, "mx4_pad_kernel");
 }
 
-template <int RF, int NT, int W, int U, int TERMS>
+template <int NT, int W, int U, int TERMS>
 int launch_down(aser_ctx* ctx, const MxArgs& g) {
-    const int rank_tiles = (int)ceil_div64(TERMS ? g.lr_steps / (TERMS ? TERMS : 1) * 32 : g.rp, 16 * RF);
+    const int rank_tiles = (int)ceil_div64(TERMS ? g.lr_steps / (TERMS ? TERMS : 1) * 32 : g.rp, 16);
     const int64_t grid = g.groups.most_tiles(16 * NT) * g.parts * rank_tiles;
     if (!mx4_fits(grid, 64 * W)) ASER_FAIL(ctx, ASER_ERR_SHAPE, "mx4: too many rows");
-    mx4_down_kernel<RF, NT, W, U, TERMS><<<(unsigned)grid, 64 * W, (size_t)W * RF * 1024 * (TERMS && NT < 4 ? 4 : NT), ctx->stream>>>(g, rank_tiles);
+    mx4_down_kernel<NT, W, U, TERMS><<<(unsigned)grid, 64 * W, (size_t)W * 1024 * (TERMS && NT < 4 ? 4 : NT), ctx->stream>>>(g, rank_tiles);
     return aser_check_launch(ctx, "mx4_down_kernel");
 }
 
@@ -844,7 +832,7 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
     if (!p.many) {
         if (r > 0) {
             g.P = (float*)p_room;
-            ASER_TRY((launch_down<1, 1, 4, 2, 0>(ctx, g)));
+            ASER_TRY((launch_down<1, 4, 2, 0>(ctx, g)));
         }
         return run_few(ctx, g, p.nt, w->count < groups.positions ? w->count : groups.positions, swiglu, f32);
     }
@@ -863,7 +851,7 @@ int run_product(aser_ctx* ctx, const char* who, const aser_mx4* x, const aser_mx
         g.lr_steps = width / 32 * terms;
         g.exact = (float*)(g.planes + groups.positions * width * 3);
         g.marks = (uint8_t*)(g.exact + groups.positions * width);
-        ASER_TRY(f32 ? (launch_down<1, 2, 4, 2, 3>(ctx, g)) : (launch_down<1, 2, 4, 2, 2>(ctx, g)));
+        ASER_TRY(f32 ? (launch_down<2, 4, 2, 3>(ctx, g)) : (launch_down<2, 4, 2, 2>(ctx, g)));
         if (r != width || ((uintptr_t)L_A & 15)) {
             uint16_t* const padded = (uint16_t*)(p_room + p.p_bytes);
             ASER_TRY(pad_rows(ctx, L_A, w->rows * w->count, r, width, padded));
