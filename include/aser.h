@@ -529,7 +529,7 @@ int aser_mx4_quantize(aser_ctx* ctx, const void* X, int x_dtype, int64_t ldx, co
  *     Y[t][o] = sum_i x[t][i] w[o][i] + sum_k P[t][k] L_A[o][k],   P[t][k] = sum_i x[t][i] L_B[k][i]
  * L_A: m x r, L_B: r x n, bf16, dense, finite; r == 0: no compensation (both may be NULL); r <= 128.
  * swiglu != 0: the first half of the outputs are gates (m even), and Y[t][o] = z / (1 + exp(-z)) Z[t][m / 2 + o], z = Z[t][o], Z the
- * sums above; Y then has m / 2 columns.  Y: bf16 or fp32 (y_dtype, ldy), rounded once.  Sums are fp32, P too, of
+ * sums above; Y then has m / 2 columns (bf16 Y: gates below -87 count as 0).  Y: bf16 or fp32 (y_dtype, ldy), rounded once.  Sums are fp32, P too, of
  * tokens whose scale bytes are at most 252, as the quantizer's are.  What multiplies L_A is P with all its 24 bits, but for bf16 Y and many rows (more than 64 for each matrix, and
  * enough outputs): there it is P to within 2^-17 of it, as two bf16 terms, at both ends of the range as well.  A NaN
  * block of a token is its row's, one of a weight its output's.  Deterministic.  Asynchronous.  rows == 0 is a no-op.
